@@ -300,6 +300,132 @@ int pag_searcher_search(pag_searcher* s, const float* Q, uint64_t nq, uint32_t K
 int pag_searcher_get_counters(const pag_searcher* s, pag_counters* out);
 int pag_searcher_free(pag_searcher* s);
 
+/*
+ * A memory that is searched: the keys and values of a language model's tokens in 8 bits, in pages, and attention over all of
+ * them or over the tokens that a search returned (pag_search on an index over the keys; its ids, -1 where there is none, go
+ * into pag_kv_attend_selected as they are).
+ *
+ * These calls belong into a decoding loop, many to a step, so they differ from the ones above in two points: they enqueue
+ * their work on the stream that they are given and return without waiting for it, and they allocate nothing, so that a loop
+ * can be captured into a HIP graph.  The stream belongs to the current GPU; its device pointers are that GPU's.  Arguments
+ * that the host can see are checked before anything is launched; what only the GPU sees (lengths, page numbers, slots, ids)
+ * is checked by the kernels: what is out of range counts as absent.
+ *
+ * A cache has a row of keys and a row of values side by side for every page, head and token, W = head_dim rounded up to a
+ * multiple of 64 bytes each (zeros behind head_dim), and an exponent per block of 16 tokens, head and kind:
+ *     data      uint8 [num_pages][kv_heads][page_tokens][2][W]
+ *     exponents int8  [num_pages][kv_heads][page_tokens / 16][2]            number = code * 2^exponent
+ * Codes are signed integers (largest 127) or floats of 4 exponent and 3 mantissa bits without infinities (largest 448).
+ * A power of two as scale means that a product with it never rounds and that a block which outgrows its exponent is rounded
+ * again at most once per doubling.  slot = page * page_tokens + place in the page; a request's token p is in page table[p / page_tokens].
+ */
+typedef enum { PAG_KV_INT8 = 0, PAG_KV_FP8 = 1 } pag_kv_format;
+typedef enum { PAG_F32 = 0, PAG_F16 = 1, PAG_BF16 = 2 } pag_dtype;
+
+typedef struct {
+    uint32_t struct_size;
+    uint32_t format;       /* pag_kv_format */
+    uint32_t kv_heads;
+    uint32_t head_dim;     /* a multiple of 8, at most 256 */
+    uint32_t page_tokens;  /* a multiple of 16 */
+    uint32_t reserved;     /* 0 */
+    uint64_t num_pages;    /* num_pages * kv_heads * page_tokens < 2^32 */
+    uint8_t* data;         /* dev, 16-byte aligned */
+    int8_t*  exponents;    /* dev, 2-byte aligned */
+} pag_kv_cache;
+
+/* The block tables of `requests` requests and the pages that nobody holds (a stack: the last one is taken first).  All dev. */
+typedef struct {
+    uint32_t struct_size;
+    uint32_t requests;
+    uint32_t max_pages;    /* columns of table in use */
+    uint32_t page_tokens;
+    uint64_t table_stride; /* entries from row to row */
+    uint64_t num_pages;    /* entries of free_pages */
+    int32_t* table;        /* [requests * table_stride] */
+    int32_t* lengths;      /* [requests] tokens held */
+    int32_t* free_pages;   /* [num_pages] */
+    int32_t* free_count;   /* [1] */
+} pag_kv_tables;
+
+/* One step of a batch: its new tokens, request after request.  Written by pag_kv_extend; the attention calls read it.  All dev. */
+typedef struct {
+    uint32_t struct_size;
+    uint32_t requests;
+    uint32_t max_pages;        /* as in pag_kv_tables */
+    uint32_t max_new;          /* no request has more new tokens than this (0: not known); a hint, results never depend on it */
+    uint64_t table_stride;
+    uint64_t tokens;           /* rows of the step's arrays, padding behind the last request included */
+    const int32_t* table;
+    int32_t* offsets;          /* [requests + 1] first new token of each request */
+    int32_t* context;          /* [requests] tokens that it holds once the new ones are written; 0 if it was refused */
+    int32_t* request;          /* [tokens] request of a token, -1 for padding (pag_kv_attend_selected reads it, pag_kv_attend does not) */
+    int32_t* positions;        /* [tokens] position in the request, -1 for padding and for refused requests (likewise) */
+    int64_t* slots;            /* [tokens] where its key and value go, -1 likewise (only pag_kv_extend uses the fields from here on) */
+    int32_t* granted;          /* [requests] 1, or 0 if there were not enough pages */
+    int32_t* lengths;          /* [requests] lengths after the step; may be pag_kv_tables.lengths itself */
+    int32_t* free_count;       /* [1] likewise */
+    int32_t* scratch;          /* [requests + 1] */
+} pag_kv_step;
+
+typedef struct {
+    uint32_t struct_size;
+    uint32_t dtype;            /* of q and out: PAG_F16 or PAG_BF16 */
+    uint32_t heads;            /* query heads, a multiple of kv_heads: head h reads key/value head h * kv_heads / heads */
+    uint32_t window;           /* a token reads the last `window` tokens, itself among them; 0: all (pag_kv_attend) or none (pag_kv_attend_selected) */
+    float    scale;            /* scores are scale * <q, k> */
+    float    softcap;          /* > 0: then softcap * tanh(score / softcap) */
+    const float* slopes;       /* dev [heads] or null: then minus slopes[h] * (position of the query - position of the key) */
+    const void* q;             /* dev [tokens][heads][head_dim], strides in elements; last dimension dense */
+    int64_t  q_token_stride, q_head_stride;     /* multiples of 8; q 16-byte aligned */
+    void*    out;              /* dev, like q */
+    int64_t  out_token_stride, out_head_stride;
+    float*   lse;              /* dev [tokens * heads]: log of the sum of exp(score); or null */
+    void*    workspace;        /* dev, 16-byte aligned, pag_kv_workspace_bytes() bytes; calls that may overlap in time need one each */
+    uint64_t workspace_bytes;
+} pag_kv_attention;
+
+/*
+ * pag_kv_extend: request r gets add[r] (dev int32 [requests], negative counts as 0) new tokens.  Requests are served in order; one
+ * that needs more pages than its row of the table or the stack has left is refused as a whole (granted 0, slots -1), and so
+ * is every later one that needs a page once the stack could not serve one before it.  Writes the new entries of the tables
+ * and all arrays of `step`; the rest of `tables` changes only where step->lengths and step->free_count are its own arrays, so
+ * a step can be looked at before it is taken over.
+ * pag_kv_release: the requests with done[r] != 0 (dev int32 [requests]) give back their pages, first page first, in order of
+ * their numbers, and hold nothing then.
+ */
+int pag_kv_extend(const pag_kv_tables* tables, const int32_t* add, const pag_kv_step* step, void* stream);
+int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* stream);
+
+/*
+ * pag_kv_append: writes the keys and values of `tokens` tokens (dev, dtype PAG_F32 / F16 / BF16, [tokens][kv_heads][head_dim], strides in
+ * elements, multiples of 16 bytes) into their slots (dev int64 [tokens]; -1 or out of range: left out).  The tokens of one block have to
+ * follow each other in the call, in ascending order, as pag_kv_extend numbers them.  A block that begins with the call (its
+ * first token is among the new ones) is cleared first; its exponent is the smallest e >= -64 at which the largest code reaches the
+ * largest finite magnitude.  Another block keeps its exponent unless the new tokens need a larger one; then what it held is
+ * rounded again.  Rounding is to nearest even; infinities are held as the largest code, NaN as 0.
+ * pag_kv_read: rows of the cache as numbers, [tokens][kv_heads][head_dim] with strides in elements (multiples of 8 bytes); k or v may be
+ * null.  Slots -1 or out of range give zeros.  PAG_F32 and PAG_BF16 hold every number of the cache exactly.
+ */
+int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                  const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, uint64_t tokens, void* stream);
+int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens, uint32_t dtype, void* k, int64_t k_token_stride,
+                int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride, void* stream);
+
+/*
+ * pag_kv_attend: every token of the step attends to the tokens of its request up to itself: out = sum softmax(score) v.
+ * pag_kv_attend_selected: it attends to the last `window` tokens and to the tokens whose positions ids lists (dev int64
+ * [tokens][id_heads][k], strides in elements, last dimension dense): id_heads is kv_heads (the heads of a group share a list), heads, or a
+ * multiple of kv_heads that divides heads.  Ids below 0, in the window or beyond the token itself are passed over (the window's tokens count
+ * once); an id listed twice counts twice.
+ * A token that finds nothing to attend to gets zeros and an lse of -inf; so does padding.
+ * Sums, maxima and scores are held in 32 bits; softmax weights are rounded to 16-bit floats for their product with the values.
+ */
+uint64_t pag_kv_workspace_bytes(const pag_kv_cache* cache, uint64_t tokens, uint32_t heads);
+int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, void* stream);
+int pag_kv_attend_selected(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, const int64_t* ids,
+                           int64_t ids_token_stride, int64_t ids_head_stride, uint32_t id_heads, uint32_t k, void* stream);
+
 const char* pag_last_error(void);
 
 #ifdef __cplusplus

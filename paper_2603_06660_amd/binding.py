@@ -25,6 +25,7 @@ EXPORTED_SYMBOLS = (
     "pag_prepare_queries", "pag_exact_distances", "pag_screen", "pag_edge_info", "pag_insertion_candidates",
     "pag_search_layout", "pag_measure_row_reads",
     "pag_searcher_create", "pag_searcher_search", "pag_searcher_get_counters", "pag_searcher_free",
+    "pag_kv_extend", "pag_kv_release", "pag_kv_append", "pag_kv_read", "pag_kv_workspace_bytes", "pag_kv_attend", "pag_kv_attend_selected",
     "pag_last_error",
 )
 
@@ -73,6 +74,7 @@ def load_library():
                            "(or __graft_entry__.build())")
         lib = C.CDLL(_LIB_PATH)
         lib.pag_last_error.restype = C.c_char_p
+        lib.pag_kv_workspace_bytes.restype = C.c_uint64
         for name in EXPORTED_SYMBOLS:
             getattr(lib, name)
         _lib = lib

@@ -18,11 +18,6 @@ static thread_local std::string g_last_error;
 void pag_set_error(const std::string& msg) { g_last_error = msg; }
 extern "C" const char* pag_last_error(void) { return g_last_error.c_str(); }
 
-#define PAG_CHECK(cond, code, msg)                 \
-    do {                                           \
-        if (!(cond)) { pag_set_error(msg); return (code); } \
-    } while (0)
-
 namespace {
 
 using pag_random::Rng;
@@ -108,20 +103,6 @@ int check_params(const pag_params* p) {
     // the reverse-edge pairs of one batch (2 * max_degree per vector) are counted in 32 bits
     PAG_CHECK(p->insert_subbatch <= (1u << 20), PAG_EUNSUPPORTED, "insert_subbatch above 2^20 is not built");
     return PAG_OK;
-}
-
-// Runs the body of an entry point; no exception leaves the library (host allocations can throw).
-template <typename F>
-int guarded(const char* what, F&& body) {
-    try {
-        return body();
-    } catch (const std::bad_alloc&) {
-        pag_set_error(std::string(what) + ": host allocation failed");
-        return PAG_ENOMEM;
-    } catch (const std::exception& e) {
-        pag_set_error(std::string(what) + ": " + e.what());
-        return PAG_EINVAL;
-    }
 }
 
 template <typename T>

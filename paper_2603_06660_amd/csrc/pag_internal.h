@@ -5,6 +5,8 @@
 #include <hip/hip_fp16.h>
 #include <stdint.h>
 
+#include <exception>
+#include <new>
 #include <string>
 
 #include "pag.h"
@@ -31,6 +33,11 @@ constexpr int pag_team_max(int nw) { return nw <= 8 ? 12 : 8; }
 
 void pag_set_error(const std::string& msg);
 
+#define PAG_CHECK(cond, code, msg)                 \
+    do {                                           \
+        if (!(cond)) { pag_set_error(msg); return (code); } \
+    } while (0)
+
 #define PAG_HIP(call)                                                                        \
     do {                                                                                     \
         hipError_t e__ = (call);                                                             \
@@ -39,6 +46,20 @@ void pag_set_error(const std::string& msg);
             return PAG_EHIP;                                                                 \
         }                                                                                    \
     } while (0)
+
+// Runs the body of an entry point; no exception leaves the library (host allocations can throw).
+template <typename F>
+int guarded(const char* what, F&& body) {
+    try {
+        return body();
+    } catch (const std::bad_alloc&) {
+        pag_set_error(std::string(what) + ": host allocation failed");
+        return PAG_ENOMEM;
+    } catch (const std::exception& e) {
+        pag_set_error(std::string(what) + ": " + e.what());
+        return PAG_EINVAL;
+    }
+}
 
 // Device-side statistics, summed with atomics by every wave when it retires.  They are kept PAG_CTR_COPIES times, a 128-byte line
 // each, and a workgroup adds to the copy of its number: atomics on one address are done one after the other, 14 ns each across the

@@ -1,0 +1,334 @@
+// Block tables and slots of a step, and what goes into the 8-bit cache and comes out of it.
+#include "pag_kv.h"
+
+namespace pagkv {
+namespace {
+
+constexpr u32 PLAN_THREADS = 1024;
+
+// inclusive sum over the workgroup; sh: an entry a wave
+__device__ __forceinline__ u64 scan1024(u64 x, u64* sh) {
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (u32 o = 1; o < 64; o <<= 1) {
+        const u64 y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 63) sh[wave] = x;
+    __syncthreads();
+    u64 before = 0;
+    for (u32 w = 0; w < wave; ++w) before += sh[w];
+    __syncthreads();
+    return x + before;
+}
+
+struct Extend {
+    const int32_t *add, *lengths, *free_pages, *free_count;
+    int32_t* table;
+    u64 table_stride, tokens;
+    u32 requests, max_pages, page_tokens, num_pages;
+    int32_t *offsets, *context, *granted, *out_lengths, *out_free_count, *scratch, *request, *positions;
+    int64_t* slots;
+};
+
+struct Want { u64 have, need, add, length; bool fits; };
+
+__device__ __forceinline__ Want want_of(const Extend& e, u32 r) {
+    Want w;
+    const int32_t n = e.lengths[r], a = e.add[r];
+    w.length = n < 0 ? 0 : (u64)n;
+    w.add = a < 0 ? 0 : (u64)a;
+    w.have = (w.length + e.page_tokens - 1) / e.page_tokens;
+    w.need = (w.length + w.add + e.page_tokens - 1) / e.page_tokens - w.have;
+    w.fits = w.have + w.need <= e.max_pages;
+    return w;
+}
+
+// Slot of new token t, and the entry of the table if the token is the first of a page.  offsets, granted, out_lengths and scratch
+// (pages that were taken before the request's; behind the requests the count of free pages before the step) are written.
+__device__ __forceinline__ void fill_token(const Extend& e, u64 t, u64 free_before) {
+    int32_t request = -1, position = -1;
+    int64_t slot = -1;
+    if (t < (u64)(u32)e.offsets[e.requests]) {
+        u32 lo = 0, hi = e.requests;               // the last request whose tokens begin at t or before, with tokens of its own
+        while (hi - lo > 1) {
+            const u32 mid = (lo + hi) / 2;
+            if ((u64)(u32)e.offsets[mid] <= t) lo = mid; else hi = mid;
+        }
+        request = (int32_t)lo;
+        if (e.granted[lo]) {
+            const u64 i = t - (u32)e.offsets[lo], add = (u32)(e.offsets[lo + 1] - e.offsets[lo]);
+            const u64 length = (u32)e.out_lengths[lo] - add, p = length + i;
+            const u64 have = (length + e.page_tokens - 1) / e.page_tokens, at = p / e.page_tokens, place = p % e.page_tokens;
+            int32_t page;
+            int32_t* entry = e.table + lo * e.table_stride + at;
+            if (at >= have) {
+                page = e.free_pages[free_before - 1 - (u32)e.scratch[lo] - (at - have)];
+                if (place == 0) *entry = page;
+            } else {
+                page = *entry;
+            }
+            position = (int32_t)p;
+            if (page >= 0 && (u32)page < e.num_pages) slot = (int64_t)page * e.page_tokens + (int64_t)place;
+        }
+    }
+    e.request[t] = request;
+    e.positions[t] = position;
+    e.slots[t] = slot;
+}
+
+// One workgroup: who gets pages, and from where.  A thread has a run of consecutive requests; the sums over all of them come from one scan
+// of the threads' sums.  Up to `fill` tokens get their slots here as well.
+__global__ void __launch_bounds__(PLAN_THREADS) k_extend(Extend e, u64 fill) {
+    __shared__ u64 sh[PLAN_THREADS / 64];
+    __shared__ u64 sh_taken;
+    const u32 per = (e.requests + PLAN_THREADS - 1) / PLAN_THREADS, r0 = min(threadIdx.x * per, e.requests), r1 = min(r0 + per, e.requests);
+    int32_t count = *e.free_count;
+    const u64 avail = count < 0 ? 0 : min((u32)count, e.num_pages);
+    if (threadIdx.x == 0) sh_taken = 0;
+    u64 need = 0, add = 0;
+    for (u32 r = r0; r < r1; ++r) {
+        const Want w = want_of(e, r);
+        if (w.fits) need += w.need;
+        add += w.add;
+    }
+    u64 upto = scan1024(need, sh) - need, first = scan1024(add, sh) - add, taken = 0;
+    for (u32 r = r0; r < r1; ++r) {
+        const Want w = want_of(e, r);
+        const u64 before = upto;
+        if (w.fits) upto += w.need;
+        const bool granted = w.fits && (w.need == 0 || upto <= avail);
+        if (granted && w.need) taken = upto;
+        e.offsets[r] = (int32_t)min(first, (u64)0x7FFFFFFF);
+        first += w.add;
+        e.granted[r] = granted ? 1 : 0;
+        e.scratch[r] = (int32_t)min(before, (u64)0x7FFFFFFF);
+        const int32_t length = (int32_t)(granted ? w.length + w.add : w.length);
+        e.context[r] = granted ? length : 0;
+        e.out_lengths[r] = length;
+        if (r + 1 == e.requests) e.offsets[e.requests] = (int32_t)min(first, (u64)0x7FFFFFFF);
+    }
+    if (taken) atomicMax((unsigned long long*)&sh_taken, (unsigned long long)taken);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        *e.out_free_count = (int32_t)(avail - sh_taken);
+        e.scratch[e.requests] = (int32_t)avail;
+    }
+    // what this workgroup has written, its threads read
+    __threadfence_block();
+    __syncthreads();
+    for (u64 t = threadIdx.x; t < fill; t += PLAN_THREADS) fill_token(e, t, avail);
+}
+
+__global__ void __launch_bounds__(256) k_extend_tokens(Extend e) {
+    const u64 t = (u64)blockIdx.x * 256 + threadIdx.x;
+    if (t < e.tokens) fill_token(e, t, (u64)(u32)e.scratch[e.requests]);
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) k_release(pag_kv_tables t, const int32_t* __restrict__ done) {
+    __shared__ u64 sh[PLAN_THREADS / 64];
+    __shared__ u64 sh_end;
+    const u32 per = (t.requests + PLAN_THREADS - 1) / PLAN_THREADS, r0 = min(threadIdx.x * per, t.requests), r1 = min(r0 + per, t.requests);
+    const int32_t count = *t.free_count;
+    const u64 have = count < 0 ? 0 : min((u64)count, t.num_pages);
+    const auto pages_of = [&](u32 r) -> u64 {
+        const int32_t n = t.lengths[r];
+        return done[r] && n > 0 ? min(((u64)n + t.page_tokens - 1) / t.page_tokens, (u64)t.max_pages) : 0;
+    };
+    u64 back = 0;
+    for (u32 r = r0; r < r1; ++r) back += pages_of(r);
+    u64 upto = scan1024(back, sh);
+    if (threadIdx.x == PLAN_THREADS - 1) sh_end = min(have + upto, t.num_pages);
+    u64 at = have + upto - back;
+    for (u32 r = r0; r < r1; ++r) {
+        const u64 n = pages_of(r);
+        for (u64 i = 0; i < n; ++i, ++at)
+            if (at < t.num_pages) t.free_pages[at] = t.table[r * t.table_stride + i];
+        if (done[r]) t.lengths[r] = 0;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *t.free_count = (int32_t)sh_end;
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+    return x;
+}
+
+struct Store {
+    Cache c;
+    const void* x[2];
+    int64_t ts[2], hs[2];
+    const int64_t* slots;
+    u64 tokens;
+    u32 dtype;
+};
+
+// One wave writes the new tokens of one block, for one head and kind: the wave of the first of them, the others' waves have
+// nothing to do.  8 numbers of a row are a lane's; a block of 16 rows is 2 C of these pieces a lane.
+template <int FMT, int C>
+__global__ void __launch_bounds__(256) k_append(Store a) {
+    const u32 lane = threadIdx.x & 63, kinds = 2 * a.c.kv_heads;
+    const u64 wave = (u64)blockIdx.x * 4 + (threadIdx.x >> 6), t = wave / kinds;
+    if (t >= a.tokens) return;
+    const u32 head = (u32)(wave % kinds) >> 1, kind = (u32)(wave % kinds) & 1;
+    // lane 0: the token before, lanes 1 .. 16: this one and the next 15
+    int64_t slot = -1;
+    if (lane <= BLOCK && t + lane >= 1 && t + lane - 1 < a.tokens) slot = a.slots[t + lane - 1];
+    if (slot >= (int64_t)a.c.num_pages * a.c.page_tokens || slot < 0) slot = -1;
+    const int block = slot < 0 ? -1 : (int)(slot / BLOCK), place = (int)(slot & (BLOCK - 1));
+    const int mine = __builtin_amdgcn_readlane(block, 1);
+    if (mine < 0 || __builtin_amdgcn_readlane(block, 0) == mine) return;
+    const u64 same = __ballot(block == mine && lane >= 1 && lane <= BLOCK) >> 1;
+    const u32 run = (u32)__builtin_ctzll(~same);
+    u32 present = 0;
+    for (u32 i = 0; i < run; ++i) present |= 1u << __builtin_amdgcn_readlane(place, i + 1);
+    const bool begins = present & 1u;
+    const u32 page = (u32)mine / a.c.page_blocks, first = (u32)mine % a.c.page_blocks * BLOCK;
+    uint8_t* rows = a.c.data + (u64)row_of(a.c, page, head, first) * (2 * a.c.width) + kind * a.c.width;
+    int8_t* exponent = a.c.exponents + ((u64)(page * a.c.kv_heads + head) * a.c.page_blocks + first / BLOCK) * 2 + kind;
+    const int held = *exponent;
+
+    float x[2 * C][8];
+    float most = 0.f;
+#pragma unroll
+    for (int n = 0; n < 2 * C; ++n) {
+        const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[n][j] = 0.f;
+        if (row < run && at < a.c.dim) load8(a.x[kind], (t + row) * (u64)a.ts[kind] + head * (u64)a.hs[kind] + at, a.dtype, x[n]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float y = fabsf(x[n][j]);
+            if (y <= 3.402823466e38f) most = fmaxf(most, y);
+        }
+    }
+    const int least = least_exponent<FMT>(wave_max(most));
+    const int e = begins ? least : max(least, held);
+    const float down = power(-e);
+#pragma unroll
+    for (int n = 0; n < 2 * C; ++n) {
+        const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
+        const int to = __shfl(place, (int)(row + 1));
+        if (row < run) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[n][j] *= down;
+            *(uint2*)(rows + (u64)to * (2 * a.c.width) + at) = make_uint2(encode4<FMT>(x[n]), encode4<FMT>(x[n] + 4));
+        }
+    }
+    if (begins || e > held) {
+        const float again = begins ? 0.f : power(max(held - e, -126));
+#pragma unroll
+        for (int n = 0; n < 2 * C; ++n) {
+            const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
+            if (!(present >> row & 1u)) {
+                uint2* p = (uint2*)(rows + (u64)row * (2 * a.c.width) + at);
+                uint2 w = make_uint2(0, 0);
+                if (!begins) {
+                    w = *p;
+                    float y[8];
+                    decode4<FMT>(w.x, y);
+                    decode4<FMT>(w.y, y + 4);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] *= again;
+                    w = make_uint2(encode4<FMT>(y), encode4<FMT>(y + 4));
+                }
+                *p = w;
+            }
+        }
+    }
+    if (lane == 0) *exponent = (int8_t)e;
+}
+
+struct Load {
+    Cache c;
+    void* x[2];
+    int64_t ts[2], hs[2];
+    const int64_t* slots;
+    u64 pieces;                // tokens * kv_heads * 2 * width / 8
+    u32 dtype;
+};
+
+// Eight numbers a thread.
+template <int FMT, int C>
+__global__ void __launch_bounds__(256) k_read(Load a) {
+    const u64 i = (u64)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.pieces) return;
+    const u32 piece = (u32)(i % (16 * C)), kind = piece / (8 * C), at = piece % (8 * C) * 8, head = (u32)(i / (16 * C) % a.c.kv_heads);
+    const u64 t = i / (16 * C) / a.c.kv_heads;
+    if (!a.x[kind] || at >= a.c.dim) return;
+    const int64_t slot = a.slots[t];
+    float x[8] = { 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f };
+    if (slot >= 0 && slot < (int64_t)a.c.num_pages * a.c.page_tokens) {
+        const u32 page = (u32)((u64)slot / a.c.page_tokens), place = (u32)((u64)slot % a.c.page_tokens);
+        const uint2 w = *(const uint2*)(a.c.data + (u64)row_of(a.c, page, head, place) * (2 * a.c.width) + kind * a.c.width + at);
+        const float up = power(a.c.exponents[((u64)(page * a.c.kv_heads + head) * a.c.page_blocks + place / BLOCK) * 2 + kind]);
+        decode4<FMT>(w.x, x);
+        decode4<FMT>(w.y, x + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= up;
+    }
+    store8(a.x[kind], t * (u64)a.ts[kind] + head * (u64)a.hs[kind] + at, a.dtype, x);
+}
+
+// f<FMT, C>() for the cache's format and row width
+template <template <int, int> class F, typename... A>
+void for_cache(const Cache& c, A&&... args) {
+    const u32 n = c.width / 64;
+    if (c.fmt == PAG_KV_INT8) {
+        if (n == 1) F<PAG_KV_INT8, 1>::run(args...);
+        else if (n == 2) F<PAG_KV_INT8, 2>::run(args...);
+        else if (n == 3) F<PAG_KV_INT8, 3>::run(args...);
+        else F<PAG_KV_INT8, 4>::run(args...);
+    } else {
+        if (n == 1) F<PAG_KV_FP8, 1>::run(args...);
+        else if (n == 2) F<PAG_KV_FP8, 2>::run(args...);
+        else if (n == 3) F<PAG_KV_FP8, 3>::run(args...);
+        else F<PAG_KV_FP8, 4>::run(args...);
+    }
+}
+
+template <int FMT, int C>
+struct RunAppend { static void run(hipStream_t st, u32 grid, const Store& a) { k_append<FMT, C><<<grid, 256, 0, st>>>(a); } };
+template <int FMT, int C>
+struct RunRead { static void run(hipStream_t st, u32 grid, const Load& a) { k_read<FMT, C><<<grid, 256, 0, st>>>(a); } };
+
+int launched(const char* what) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { pag_set_error(std::string(what) + ": " + hipGetErrorString(e)); return PAG_EHIP; }
+    return PAG_OK;
+}
+
+}  // namespace
+
+int launch_extend(hipStream_t st, const pag_kv_tables& t, const int32_t* add, const pag_kv_step& s) {
+    const Extend e{ add, t.lengths, t.free_pages, t.free_count, t.table, t.table_stride, s.tokens, t.requests, t.max_pages, t.page_tokens,
+                    (u32)t.num_pages, s.offsets, s.context, s.granted, s.lengths, s.free_count, s.scratch, s.request, s.positions, s.slots };
+    const bool alone = s.tokens <= 4 * PLAN_THREADS;
+    k_extend<<<1, PLAN_THREADS, 0, st>>>(e, alone ? s.tokens : 0);
+    if (!alone) k_extend_tokens<<<(u32)((s.tokens + 255) / 256), 256, 0, st>>>(e);
+    return launched("pag_kv_extend");
+}
+
+int launch_release(hipStream_t st, const pag_kv_tables& t, const int32_t* done) {
+    k_release<<<1, PLAN_THREADS, 0, st>>>(t, done);
+    return launched("pag_kv_release");
+}
+
+int launch_append(hipStream_t st, const Cache& c, u32 dtype, const void* k, int64_t k_ts, int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs,
+                  const int64_t* slots, u64 tokens) {
+    const Store a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, tokens, dtype };
+    for_cache<RunAppend>(c, st, (u32)((tokens * 2 * c.kv_heads + 3) / 4), a);
+    return launched("pag_kv_append");
+}
+
+int launch_read(hipStream_t st, const Cache& c, const int64_t* slots, u64 tokens, u32 dtype, void* k, int64_t k_ts, int64_t k_hs, void* v,
+                int64_t v_ts, int64_t v_hs) {
+    const u64 pieces = tokens * c.kv_heads * 2 * (c.width / 8);
+    const Load a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, pieces, dtype };
+    for_cache<RunRead>(c, st, (u32)((pieces + 255) / 256), a);
+    return launched("pag_kv_read");
+}
+
+}  // namespace pagkv

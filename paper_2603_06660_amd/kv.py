@@ -1,0 +1,346 @@
+"""The 8-bit key/value cache of include/pag.h: argument marshalling only.
+
+A decoding step, in order (every call goes onto the current stream and returns without waiting):
+
+    tables = KvTables(requests, max_pages, num_pages, page_tokens)      # who holds which pages
+    cache = KvCache(num_pages, kv_heads, head_dim, page_tokens)         # one for each layer, with the same tables
+    step = tables.extend(add, total)                                    # add: new tokens of each request
+    cache.append(k, v, step.slots)
+    out, lse = cache.attend(q, step)                                    # reads everything
+    out, lse = cache.attend_selected(q, ids, step, window=64)           # reads what a search found, and the last 64 tokens
+    tables.commit(step)
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from .binding import PagError, _check, load_library
+
+_FORMATS = {"int8": 0, "fp8": 1}
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+class _Cache(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("format", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32),
+                ("page_tokens", C.c_uint32), ("reserved", C.c_uint32), ("num_pages", C.c_uint64), ("data", C.c_void_p),
+                ("exponents", C.c_void_p)]
+
+
+class _Tables(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("requests", C.c_uint32), ("max_pages", C.c_uint32), ("page_tokens", C.c_uint32),
+                ("table_stride", C.c_uint64), ("num_pages", C.c_uint64), ("table", C.c_void_p), ("lengths", C.c_void_p),
+                ("free_pages", C.c_void_p), ("free_count", C.c_void_p)]
+
+
+class _Step(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("requests", C.c_uint32), ("max_pages", C.c_uint32), ("max_new", C.c_uint32),
+                ("table_stride", C.c_uint64), ("tokens", C.c_uint64), ("table", C.c_void_p), ("offsets", C.c_void_p),
+                ("context", C.c_void_p), ("request", C.c_void_p), ("positions", C.c_void_p), ("slots", C.c_void_p),
+                ("granted", C.c_void_p), ("lengths", C.c_void_p), ("free_count", C.c_void_p), ("scratch", C.c_void_p)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("heads", C.c_uint32), ("window", C.c_uint32),
+                ("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p),
+                ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
+                ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+def _gpu(device):
+    device = torch.device("cuda" if device is None else device)
+    if device.type != "cuda":
+        raise PagError("the cache lives on a GPU, not on %s" % device)
+    return device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
+
+
+def _array(t, dtype, shape, device, what):
+    """The address of a dense tensor of this type, shape and device."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise PagError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
+    return t.data_ptr()
+
+
+def _rows(t, shape, device, what, dtypes=_DTYPES):
+    """Checks a [tokens, heads, dim] tensor whose last dimension is dense; the other strides are free."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or t.device != device:
+        raise PagError("%s must be a tensor of shape %s on %s, of type %s" %
+                       (what, tuple(shape), device, ", ".join(str(x) for x in dtypes)))
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise PagError("%s: the last dimension must be dense" % what)
+
+
+class _On:
+    """Makes a GPU current if another one is, and gives its current stream."""
+
+    __slots__ = ("device", "before")
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.device)
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *_):
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.before)
+
+
+class KvStep:
+    """One step of a batch (pag_kv_step): its new tokens, request after request, padding at the end.
+
+    table [requests, max_pages], offsets [requests + 1], context [requests], request and positions [tokens], all int32; slots int64
+    [tokens].  KvTables.extend makes them; a program with tables of its own passes them in.  attend needs offsets and context,
+    attend_selected request and positions.
+    """
+
+    def __init__(self, table, offsets=None, context=None, requests=None, positions=None, slots=None, max_new=0, granted=None,
+                 lengths=None, free_count=None, scratch=None, tokens=None):
+        self.table, self.offsets, self.context = table, offsets, context
+        self.requests, self.positions, self.slots = requests, positions, slots
+        self.granted, self.lengths, self.free_count, self.scratch = granted, lengths, free_count, scratch
+        self.max_new = int(max_new)
+        for t in (positions, requests, slots):
+            if tokens is None and t is not None:
+                tokens = t.shape[0]
+        self._s = _Step(struct_size=C.sizeof(_Step), max_new=self.max_new)
+        self.tokens = tokens
+        if table is not None:
+            self._bind(table)
+
+    @classmethod
+    def empty(cls, requests, total, device=None):
+        """Room for a step of `requests` requests and `total` tokens, for KvTables.extend(out=...)."""
+        device = _gpu(device)
+        ints = torch.empty(5 * requests + 3 + 2 * total, dtype=torch.int32, device=device)
+        offsets, context, granted, lengths, scratch, free_count, request, positions = ints.split(
+            [requests + 1, requests, requests, requests, requests + 1, 1, total, total])
+        return cls(None, offsets, context, request, positions, torch.empty(total, dtype=torch.int64, device=device), 0, granted,
+                   lengths, free_count, scratch, total)
+
+    def _bind(self, table):
+        """Takes over a table and looks the arrays over."""
+        if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.dim() != 2 or not table.is_cuda or \
+                (table.stride(1) != 1 and table.shape[1] > 1) or table.shape[0] == 0 or table.shape[1] == 0:
+            raise PagError("table must be an int32 CUDA tensor [requests, max_pages] with dense rows")
+        device, n, s = table.device, table.shape[0], self._s
+        self.table, self.device = table, device
+        s.requests, s.max_pages = n, table.shape[1]
+        s.table_stride = table.stride(0) if n > 1 else max(table.stride(0), table.shape[1])
+        s.table = table.data_ptr()
+        for name, shape, field in (("offsets", (n + 1,), "offsets"), ("context", (n,), "context"), ("granted", (n,), "granted"),
+                                   ("lengths", (n,), "lengths"), ("free_count", (1,), "free_count"), ("scratch", (n + 1,), "scratch"),
+                                   ("requests", (self.tokens,), "request"), ("positions", (self.tokens,), "positions")):
+            t = getattr(self, name)
+            if t is not None:
+                setattr(s, field, _array(t, torch.int32, shape, device, name))
+        if self.slots is not None:
+            s.slots = _array(self.slots, torch.int64, (self.tokens,), device, "slots")
+
+    def _with(self, tokens):
+        if self.table is None:
+            raise PagError("the step has no table: it comes from KvStep.empty and KvTables.extend has not filled it")
+        if self.tokens is not None and tokens != self.tokens:
+            raise PagError("the step has %d tokens, q has %d" % (self.tokens, tokens))
+        self._s.tokens = tokens
+        return self._s
+
+
+class KvTables:
+    """The block tables of `requests` requests over a pool of pages, on the GPU (pag_kv_tables)."""
+
+    def __init__(self, requests, max_pages, num_pages, page_tokens=64, device=None):
+        device = _gpu(device)
+        self._set(torch.zeros(requests, dtype=torch.int32, device=device),
+                  torch.full((requests, max_pages), -1, dtype=torch.int32, device=device),
+                  torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device),
+                  torch.full((1,), num_pages, dtype=torch.int32, device=device), page_tokens)
+
+    @classmethod
+    def from_tensors(cls, lengths, table, free_pages, free_count, page_tokens):
+        """Tables over the caller's own int32 tensors: [requests], [requests, max_pages], [num_pages], [1]."""
+        self = cls.__new__(cls)
+        self._set(lengths, table, free_pages, free_count, page_tokens)
+        return self
+
+    def _set(self, lengths, table, free_pages, free_count, page_tokens):
+        if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.dim() != 2 or not table.is_cuda or \
+                (table.stride(1) != 1 and table.shape[1] > 1):
+            raise PagError("table must be an int32 CUDA tensor [requests, max_pages] with dense rows")
+        self.device, self.page_tokens = table.device, int(page_tokens)
+        n = table.shape[0]
+        self.table, self.free_pages = table, free_pages
+        self._t = _Tables(C.sizeof(_Tables), n, table.shape[1], self.page_tokens, table.stride(0) if n > 1 else max(table.stride(0), table.shape[1]),
+                          free_pages.numel(), table.data_ptr())
+        self._t.free_pages = _array(free_pages, torch.int32, (free_pages.numel(),), self.device, "free_pages")
+        self._take(lengths, free_count)
+
+    def _take(self, lengths, free_count):
+        self._t.lengths = _array(lengths, torch.int32, (self._t.requests,), self.device, "lengths")
+        self._t.free_count = _array(free_count, torch.int32, (1,), self.device, "free_count")
+        self.lengths, self.free_count = lengths, free_count
+
+    def extend(self, add, total, max_new=0, out=None, commit=False):
+        """-> KvStep for add[r] (int32 [requests]) new tokens of each request, `total` rows in all (more than the sum: padding).
+        max_new: no request gets more tokens (0: not known).  out: a step whose arrays are written again.  The tables keep their
+        lengths and free pages until commit(step); commit=True writes them in place, as a captured loop needs it."""
+        if out is None:
+            out = KvStep.empty(self._t.requests, total, self.device)
+        elif out.tokens != total:
+            raise PagError("the step has %s tokens, not %d" % (out.tokens, total))
+        if out.slots is None or out.granted is None or out.scratch is None:
+            raise PagError("out has no room for slots: use KvStep.empty")
+        if out.table is not self.table:
+            out._bind(self.table)
+        s = out._s
+        out.max_new = s.max_new = int(max_new)
+        s.tokens = total
+        if commit:
+            out.lengths, out.free_count = self.lengths, self.free_count
+            s.lengths, s.free_count = self._t.lengths, self._t.free_count
+        elif out.lengths is self.lengths or out.free_count is self.free_count:
+            out.lengths, out.free_count = torch.empty_like(self.lengths), torch.empty_like(self.free_count)
+            s.lengths, s.free_count = out.lengths.data_ptr(), out.free_count.data_ptr()
+        with _On(self.device) as stream:
+            _check(load_library().pag_kv_extend(C.byref(self._t), C.c_void_p(_array(add, torch.int32, (self._t.requests,), self.device, "add")),
+                                                C.byref(s), C.c_void_p(stream)), "pag_kv_extend")
+        return out
+
+    def commit(self, step):
+        """Takes over the lengths and the free pages of a step that extend() made for these tables."""
+        if step.table is not self.table or step.lengths is None or step.free_count is None:
+            raise PagError("the step belongs to other tables")
+        self._take(step.lengths, step.free_count)
+
+    def release(self, done):
+        """The requests with done[r] != 0 (int32 [requests]) give their pages back."""
+        with _On(self.device) as stream:
+            _check(load_library().pag_kv_release(C.byref(self._t), C.c_void_p(_array(done, torch.int32, (self._t.requests,), self.device, "done")),
+                                                 C.c_void_p(stream)), "pag_kv_release")
+
+
+class KvCache:
+    """Keys and values in 8 bits, in pages (pag_kv_cache).  format: "int8" or "fp8" (4 exponent and 3 mantissa bits)."""
+
+    def __init__(self, num_pages, kv_heads, head_dim, page_tokens=64, format="int8", device=None):
+        device = _gpu(device)
+        width = -(-head_dim // 64) * 64
+        self._set(torch.zeros((num_pages, kv_heads, page_tokens, 2, width), dtype=torch.uint8, device=device),
+                  torch.zeros((num_pages, kv_heads, page_tokens // 16, 2), dtype=torch.int8, device=device), head_dim, format)
+
+    @classmethod
+    def from_tensors(cls, data, exponents, head_dim, format="int8"):
+        """A cache over the caller's tensors: uint8 [num_pages, kv_heads, page_tokens, 2, width], int8 [num_pages, kv_heads, page_tokens / 16, 2];
+        width is head_dim rounded up to a multiple of 64, with zeros behind head_dim."""
+        self = cls.__new__(cls)
+        self._set(data, exponents, head_dim, format)
+        return self
+
+    def _set(self, data, exponents, head_dim, format):
+        if format not in _FORMATS:
+            raise PagError("format must be one of %s" % ", ".join(sorted(_FORMATS)))
+        if not isinstance(data, torch.Tensor) or data.dim() != 5 or not data.is_cuda:
+            raise PagError("data must be a uint8 CUDA tensor [num_pages, kv_heads, page_tokens, 2, width]")
+        pages, heads, tokens = data.shape[:3]
+        self.device = data.device
+        self.num_pages, self.kv_heads, self.page_tokens, self.head_dim, self.format = pages, heads, tokens, int(head_dim), format
+        self._c = _Cache(C.sizeof(_Cache), _FORMATS[format], heads, self.head_dim, tokens, 0, pages,
+                         _array(data, torch.uint8, (pages, heads, tokens, 2, -(-self.head_dim // 64) * 64), self.device, "data"),
+                         _array(exponents, torch.int8, (pages, heads, tokens // 16, 2), self.device, "exponents"))
+        self.data, self.exponents = data, exponents
+        lib = load_library()
+        nothing = [C.c_void_p(None), C.c_int64(0), C.c_int64(0)]
+        _check(lib.pag_kv_read(C.byref(self._c), C.c_void_p(None), C.c_uint64(0), C.c_uint32(0), *nothing, *nothing, C.c_void_p(None)), "KvCache")
+        with _On(self.device):
+            self._partial = lib.pag_kv_workspace_bytes(C.byref(self._c), C.c_uint64(0), C.c_uint32(0))
+
+    def append(self, k, v, slots):
+        """Writes k and v [tokens, kv_heads, head_dim] (float32, float16 or bfloat16) into slots (int64 [tokens], -1: left out)."""
+        tokens = slots.shape[0]
+        shape = (tokens, self.kv_heads, self.head_dim)
+        _rows(k, shape, self.device, "k")
+        _rows(v, shape, self.device, "v", (k.dtype,))
+        with _On(self.device) as stream:
+            _check(load_library().pag_kv_append(
+                C.byref(self._c), C.c_uint32(_DTYPES[k.dtype]), C.c_void_p(k.data_ptr()), C.c_int64(k.stride(0)), C.c_int64(k.stride(1)),
+                C.c_void_p(v.data_ptr()), C.c_int64(v.stride(0)), C.c_int64(v.stride(1)),
+                C.c_void_p(_array(slots, torch.int64, (tokens,), self.device, "slots")), C.c_uint64(tokens), C.c_void_p(stream)), "pag_kv_append")
+
+    def read(self, slots, dtype=torch.float32, out=None):
+        """-> (k, v) [tokens, kv_heads, head_dim]: the rows in these slots as numbers; zeros for -1.  out: (k, v) to write into, of any
+        token and head strides; one of them may be None."""
+        tokens = slots.shape[0]
+        shape = (tokens, self.kv_heads, self.head_dim)
+        if out is None:
+            out = (torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device))
+        k, v = out
+        some = k if k is not None else v
+        if some is None:
+            raise PagError("read: both outputs are None")
+        dtype = some.dtype
+        if dtype not in _DTYPES:
+            raise PagError("read gives float32, float16 or bfloat16, not %s" % dtype)
+        args = []
+        for t, what in ((k, "k"), (v, "v")):
+            if t is None:
+                args += [C.c_void_p(None), C.c_int64(0), C.c_int64(0)]
+            else:
+                _rows(t, shape, self.device, what, (dtype,))
+                args += [C.c_void_p(t.data_ptr()), C.c_int64(t.stride(0)), C.c_int64(t.stride(1))]
+        with _On(self.device) as stream:
+            _check(load_library().pag_kv_read(C.byref(self._c), C.c_void_p(_array(slots, torch.int64, (tokens,), self.device, "slots")),
+                                              C.c_uint64(tokens), C.c_uint32(_DTYPES[dtype]), *args, C.c_void_p(stream)), "pag_kv_read")
+        return k, v
+
+    def _attention(self, q, step, scale, window, softcap, slopes, out):
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise PagError("q must be a tensor [tokens, heads, head_dim]")
+        tokens, heads = q.shape[0], q.shape[1]
+        shape = (tokens, heads, self.head_dim)
+        _rows(q, shape, self.device, "q", (torch.float16, torch.bfloat16))
+        if step.table is not None and step.device != self.device:
+            raise PagError("the step is on %s, the cache on %s" % (step.device, self.device))
+        if not 0 <= window < 1 << 31:
+            raise PagError("window must be between 0 and 2^31 - 1")
+        if out is None:
+            out = (torch.empty(shape, dtype=q.dtype, device=self.device), torch.empty((tokens, heads), dtype=torch.float32, device=self.device))
+        o, lse = out
+        _rows(o, shape, self.device, "out", (q.dtype,))
+        room = torch.empty(self._partial + 8 * tokens * heads, dtype=torch.uint8, device=self.device)
+        a = _Attention(C.sizeof(_Attention), _DTYPES[q.dtype], heads, window, self.head_dim ** -0.5 if scale is None else scale, softcap,
+                       None if slopes is None else _array(slopes, torch.float32, (heads,), self.device, "slopes"),
+                       q.data_ptr(), q.stride(0), q.stride(1), o.data_ptr(), o.stride(0), o.stride(1),
+                       None if lse is None else _array(lse, torch.float32, (tokens, heads), self.device, "lse"), room.data_ptr(), room.numel())
+        return out, step._with(tokens), a, room
+
+    def attend(self, q, step, scale=None, window=0, softcap=0.0, slopes=None, out=None):
+        """-> (out like q, lse float32 [tokens, heads]): every token of q [tokens, heads, head_dim] (float16 or bfloat16) attends to its request's
+        tokens up to itself.  window > 0: to the last `window` of them.  softcap > 0: scores become softcap * tanh(score / softcap).
+        slopes (float32 [heads]): minus slope * distance.  scale: head_dim ** -0.5.  out: (out, lse) to write into; lse may be None."""
+        if step.offsets is None or step.context is None:
+            raise PagError("attend needs the step's offsets and context")
+        out, s, a, room = self._attention(q, step, scale, window, softcap, slopes, out)
+        with _On(self.device) as stream:
+            _check(load_library().pag_kv_attend(C.byref(self._c), C.byref(s), C.byref(a), C.c_void_p(stream)), "pag_kv_attend")
+        return out
+
+    def attend_selected(self, q, ids, step, scale=None, window=0, softcap=0.0, slopes=None, out=None):
+        """attend(), but a token reads the positions that ids (int64 [tokens, id_heads, k], -1: none; what a search of the request's keys
+        returned) lists for its head, and the last `window` tokens.  id_heads: kv_heads, heads, or a multiple of the one that
+        divides the other."""
+        if step.requests is None or step.positions is None:
+            raise PagError("attend_selected needs the step's requests and positions")
+        if not isinstance(ids, torch.Tensor) or ids.dtype != torch.int64 or ids.dim() != 3 or ids.device != self.device or ids.shape[0] != q.shape[0] or \
+                (ids.shape[2] > 1 and ids.stride(2) != 1):
+            raise PagError("ids must be an int64 tensor [tokens, id_heads, k] on %s whose last dimension is dense" % self.device)
+        out, s, a, room = self._attention(q, step, scale, window, softcap, slopes, out)
+        with _On(self.device) as stream:
+            _check(load_library().pag_kv_attend_selected(C.byref(self._c), C.byref(s), C.byref(a), C.c_void_p(ids.data_ptr()), C.c_int64(ids.stride(0)),
+                                                         C.c_int64(ids.stride(1)), C.c_uint32(ids.shape[1]), C.c_uint32(ids.shape[2]),
+                                                         C.c_void_p(stream)), "pag_kv_attend_selected")
+        return out
