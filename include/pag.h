@@ -421,7 +421,7 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
  * A token that finds nothing to attend to gets zeros and an lse of -inf; so does padding.
  * Sums, maxima and scores are held in 32 bits; softmax weights are rounded to 16-bit floats for their product with the values.
  */
-uint64_t pag_kv_workspace_bytes(const pag_kv_cache* cache, uint64_t tokens, uint32_t heads);
+uint64_t pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, uint32_t heads);   /* 0: wrong arguments, or no GPU */
 int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, void* stream);
 int pag_kv_attend_selected(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, const int64_t* ids,
                            int64_t ids_token_stride, int64_t ids_head_stride, uint32_t id_heads, uint32_t k, void* stream);

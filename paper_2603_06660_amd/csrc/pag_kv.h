@@ -124,8 +124,8 @@ struct Attend {
     int64_t q_ts, q_hs, o_ts, o_hs, ids_ts, ids_hs;
     u32 heads, group, dtype, window, id_heads, k, listed;      // listed: attention over ids and a window
     float scale, softcap;
-    float* partial;                       // two of a workgroup: of the piece that another one began, of the piece that it began and another one ends
-    int2* joined;                         // [tokens * heads] first and last workgroup of the row's pieces; first < 0: written whole
+    float* partial;                       // the workspace: two parts a workgroup, of the piece that another one began, and of the piece that it began and another one ends
+    int2* joined;                         // narrow kernels: [tokens * heads] first and last workgroup of the row's pieces; first < 0: written whole
 };
 
 int launch_extend(hipStream_t st, const pag_kv_tables& t, const int32_t* add, const pag_kv_step& s);
@@ -136,7 +136,10 @@ int launch_read(hipStream_t st, const Cache& c, const int64_t* slots, u64 tokens
                 int64_t v_ts, int64_t v_hs);
 int launch_attend(hipStream_t st, const Attend& a, int num_cu);
 
-u64 partial_floats(u32 width, int num_cu);      // of a workspace
+int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu);
+
+u64 narrow_workspace(u32 width, u64 rows, int num_cu);      // bytes
+u64 wide_workspace(u32 width, int num_cu);
 int num_cu_of_current();                        // < 0: no GPU
 
 }  // namespace pagkv

@@ -1,4 +1,5 @@
 // C ABI of the 8-bit key/value cache: argument checking; everything that computes runs in the kernels.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 
@@ -60,6 +61,12 @@ int check_tables(const pag_kv_tables* t) {
     return PAG_OK;
 }
 
+// Whether a request has more query rows to a key/value head than a tile of the narrow kernel.
+bool many_rows(const pag_kv_step* s, u32 group) {
+    const u64 tokens = s->max_new ? s->max_new : (s->tokens + s->requests - 1) / s->requests;
+    return tokens * group > 16;
+}
+
 int check_rows(const void* p, int64_t token_stride, int64_t head_stride, u32 bytes, u32 to, const char* message) {
     PAG_CHECK(aligned(p, to) && token_stride * (int64_t)bytes % (int64_t)to == 0 && head_stride * (int64_t)bytes % (int64_t)to == 0, PAG_EINVAL, message);
     return PAG_OK;
@@ -81,7 +88,7 @@ int attend_common(const pag_kv_cache* cache, const pag_kv_step* step, const pag_
     if ((rc = check_rows(args->out, args->out_token_stride, args->out_head_stride, 2, 16, "out must be 16-byte aligned, its strides multiples of 8 elements"))) return rc;
     PAG_CHECK((args->slopes == nullptr || aligned(args->slopes, 4)) && (args->lse == nullptr || aligned(args->lse, 4)), PAG_EINVAL, "slopes and lse must be 4-byte aligned");
     PAG_CHECK(args->workspace != nullptr && aligned(args->workspace, 16), PAG_EINVAL, "workspace is null or not 16-byte aligned");
-    PAG_CHECK(args->workspace_bytes >= pag_kv_workspace_bytes(cache, step->tokens, args->heads), PAG_EINVAL, "workspace is smaller than pag_kv_workspace_bytes");
+    PAG_CHECK(args->workspace_bytes >= pag_kv_workspace_bytes(cache, step, args->heads), PAG_EINVAL, "workspace is smaller than pag_kv_workspace_bytes");
     *num_cu = num_cu_of_current();
     PAG_CHECK(*num_cu > 0, PAG_EHIP, "no current GPU");
     a->s = Step{ step->table, step->offsets, step->context, step->request, step->positions, step->table_stride, step->requests, step->max_pages, (u32)step->tokens };
@@ -95,7 +102,6 @@ int attend_common(const pag_kv_cache* cache, const pag_kv_step* step, const pag_
     a->scale = args->scale;
     a->softcap = args->softcap;
     a->partial = (float*)args->workspace;
-    a->joined = (int2*)(a->partial + partial_floats(a->c.width, *num_cu));
     return PAG_OK;
 }
 
@@ -160,11 +166,13 @@ extern "C" int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint
     });
 }
 
-extern "C" uint64_t pag_kv_workspace_bytes(const pag_kv_cache* cache, uint64_t tokens, uint32_t heads) {
-    if (!cache || cache->head_dim == 0 || cache->head_dim > 256) return 0;
+extern "C" uint64_t pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, uint32_t heads) {
+    if (!cache || !step || cache->head_dim == 0 || cache->head_dim > 256 || cache->kv_heads == 0 || step->requests == 0) return 0;
     const int num_cu = num_cu_of_current();
     if (num_cu <= 0) return 0;
-    return 4 * partial_floats((cache->head_dim + 63) / 64 * 64, num_cu) + 8 * tokens * heads;
+    const u32 width = (cache->head_dim + 63) / 64 * 64;
+    const u64 narrow = narrow_workspace(width, step->tokens * heads, num_cu);
+    return many_rows(step, heads / cache->kv_heads) ? std::max(narrow, wide_workspace(width, num_cu)) : narrow;
 }
 
 extern "C" int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, void* stream) {
@@ -175,7 +183,7 @@ extern "C" int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step,
         if (rc || step->tokens == 0) return rc;
         PAG_CHECK(step->offsets && step->context, PAG_EINVAL, "step: offsets or context is null");
         a.group = a.heads / a.c.kv_heads;
-        return launch_attend((hipStream_t)stream, a, num_cu);
+        return many_rows(step, a.group) ? launch_attend_wide((hipStream_t)stream, a, num_cu) : launch_attend((hipStream_t)stream, a, num_cu);
     });
 }
 

@@ -1,0 +1,110 @@
+// What the attention kernels share: widening of codes, shares of the work, rows that have nothing to read.
+#pragma once
+
+#include "pag_kv.h"
+
+namespace pagkv {
+
+constexpr float LOWEST = -3.0e38f;        // M before the first key
+constexpr float HEADROOM = 15.f;          // weights stay below 2^15
+constexpr float START = 7.f;              // and are 2^7 at most when M moves: 16-bit floats then hold 2^-31 of the largest
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LN2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ u32 perm(u32 hi, u32 lo, u32 sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
+
+// two codes, bytes 0 and 2 of a word whose other bytes are zero, as 16-bit floats: 1024 + (code + 128) has the code's bits, with the
+// sign turned, as its lowest
+__device__ __forceinline__ half2_t widen_int8(u32 w) {
+    const half2_t bias = { (_Float16)1152.f, (_Float16)1152.f };
+    return __builtin_bit_cast(half2_t, w ^ 0x64806480u) - bias;
+}
+
+// eight codes in their order
+template <int FMT>
+__device__ __forceinline__ half8_t widen8(u32 lo, u32 hi) {
+    half2_t h[4];
+    if constexpr (FMT == PAG_KV_INT8) {
+        h[0] = widen_int8(perm(0, lo, 0x0c010c00));
+        h[1] = widen_int8(perm(0, lo, 0x0c030c02));
+        h[2] = widen_int8(perm(0, hi, 0x0c010c00));
+        h[3] = widen_int8(perm(0, hi, 0x0c030c02));
+    } else {
+        h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false);
+        h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
+        h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false);
+        h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+    }
+    return half8_t{ h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y };
+}
+
+// byte c of eight words, c = 0 .. 3: a column of eight tokens for each of four numbers of a row
+template <int FMT>
+__device__ __forceinline__ void columns(const u32* w, half8_t* out) {
+    if constexpr (FMT == PAG_KV_INT8) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            half2_t h[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) h[p] = widen_int8(perm(w[2 * p + 1], w[2 * p], 0x0c040c00u + 0x00010001u * c));
+            out[c] = half8_t{ h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y };
+        }
+    } else {
+        u32 lo[2][2], t[2][4];                       // pairs of bytes of two words, then four bytes of four words
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            lo[0][0] = perm(w[4 * q + 1], w[4 * q], 0x05010400);
+            lo[0][1] = perm(w[4 * q + 1], w[4 * q], 0x07030602);
+            lo[1][0] = perm(w[4 * q + 3], w[4 * q + 2], 0x05010400);
+            lo[1][1] = perm(w[4 * q + 3], w[4 * q + 2], 0x07030602);
+            t[q][0] = perm(lo[1][0], lo[0][0], 0x05040100);
+            t[q][1] = perm(lo[1][0], lo[0][0], 0x07060302);
+            t[q][2] = perm(lo[1][1], lo[0][1], 0x05040100);
+            t[q][3] = perm(lo[1][1], lo[0][1], 0x07060302);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) out[c] = widen8<FMT>(t[0][c], t[1][c]);
+    }
+}
+
+__device__ __forceinline__ u64 share(u64 total, u32 parts, u32 i) { return total * i / parts; }
+
+// zeros for the heads of tokens [t0, t1)
+__device__ __forceinline__ void write_empty(const Attend& a, u32 t0, u32 t1) {
+    const u32 pieces = a.c.dim / 8;
+    const u64 n = (u64)(t1 - t0) * a.heads * pieces;
+    for (u64 i = threadIdx.x; i < n; i += blockDim.x) {
+        const u32 at = (u32)(i % pieces) * 8, head = (u32)(i / pieces % a.heads), t = t0 + (u32)(i / pieces / a.heads);
+        *(uint4*)((uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + at) = make_uint4(0, 0, 0, 0);
+        if (at == 0) {
+            if (a.lse) a.lse[(u64)t * a.heads + head] = -INFINITY;
+            if (a.joined) a.joined[(u64)t * a.heads + head] = make_int2(-1, -1);
+        }
+    }
+}
+
+
+// tokens of a request, tokens that it holds (no more than its row of the table), and where its first new token stands
+struct Span {
+    u32 t0, tokens;
+    int context, first;
+};
+
+__device__ __forceinline__ Span span_of(const Attend& a, u32 b) {
+    Span s;
+    const int32_t from = a.s.offsets[b], to = a.s.offsets[b + 1];
+    s.t0 = min((u32)max(from, 0), a.s.tokens);
+    s.tokens = max(min((u32)max(to, 0), a.s.tokens), s.t0) - s.t0;
+    s.context = (int)min((u64)(u32)max(a.s.context[b], 0), (u64)a.s.max_pages * a.c.page_tokens);
+    s.first = s.context - (int)s.tokens;
+    return s;
+}
+
+// zeros for tokens behind the last request; this workgroup's part of them
+__device__ __forceinline__ void write_padding(const Attend& a) {
+    const u32 last = min((u32)max(a.s.offsets[a.s.requests], 0), a.s.tokens), pad = a.s.tokens - last;
+    const u32 from = last + (u32)((u64)pad * blockIdx.x / gridDim.x), to = last + (u32)((u64)pad * (blockIdx.x + 1) / gridDim.x);
+    if (from < to) write_empty(a, from, to);
+}
+
+}  // namespace pagkv

@@ -13,7 +13,7 @@
 // A workgroup's four waves take every fourth tile of its piece, and add up their sums in LDS.
 // Work is split evenly over a fixed number of workgroups, in units of 128 keys, across requests of any lengths: each finds its share by
 // one sum over the requests' lengths.  A row block whose keys went to several workgroups is joined by a second kernel.
-#include "pag_kv.h"
+#include "pag_kv_attend.h"
 
 namespace pagkv {
 namespace {
@@ -22,67 +22,6 @@ constexpr u32 ROWS = 16;                  // query rows of a tile
 constexpr u32 TILE = 32;                  // keys of a tile
 constexpr u32 WAVES = 4;
 constexpr u32 UNIT = WAVES * TILE;        // keys of the smallest share
-constexpr float LOWEST = -3.0e38f;        // M before the first key
-constexpr float HEADROOM = 15.f;          // weights stay below 2^15
-constexpr float START = 7.f;              // and are 2^7 at most when M moves: 16-bit floats then hold 2^-31 of the largest
-constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LN2 = 0.69314718055994530942f;
-
-__device__ __forceinline__ u32 perm(u32 hi, u32 lo, u32 sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
-
-// two codes, bytes 0 and 2 of a word whose other bytes are zero, as 16-bit floats: 1024 + (code + 128) has the code's bits, with the
-// sign turned, as its lowest
-__device__ __forceinline__ half2_t widen_int8(u32 w) {
-    const half2_t bias = { (_Float16)1152.f, (_Float16)1152.f };
-    return __builtin_bit_cast(half2_t, w ^ 0x64806480u) - bias;
-}
-
-// eight codes in their order
-template <int FMT>
-__device__ __forceinline__ half8_t widen8(u32 lo, u32 hi) {
-    half2_t h[4];
-    if constexpr (FMT == PAG_KV_INT8) {
-        h[0] = widen_int8(perm(0, lo, 0x0c010c00));
-        h[1] = widen_int8(perm(0, lo, 0x0c030c02));
-        h[2] = widen_int8(perm(0, hi, 0x0c010c00));
-        h[3] = widen_int8(perm(0, hi, 0x0c030c02));
-    } else {
-        h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false);
-        h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
-        h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false);
-        h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
-    }
-    return half8_t{ h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y };
-}
-
-// byte c of eight words, c = 0 .. 3: a column of eight tokens for each of four numbers of a row
-template <int FMT>
-__device__ __forceinline__ void columns(const u32* w, half8_t* out) {
-    if constexpr (FMT == PAG_KV_INT8) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            half2_t h[4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) h[p] = widen_int8(perm(w[2 * p + 1], w[2 * p], 0x0c040c00u + 0x00010001u * c));
-            out[c] = half8_t{ h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y };
-        }
-    } else {
-        u32 lo[2][2], t[2][4];                       // pairs of bytes of two words, then four bytes of four words
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            lo[0][0] = perm(w[4 * q + 1], w[4 * q], 0x05010400);
-            lo[0][1] = perm(w[4 * q + 1], w[4 * q], 0x07030602);
-            lo[1][0] = perm(w[4 * q + 3], w[4 * q + 2], 0x05010400);
-            lo[1][1] = perm(w[4 * q + 3], w[4 * q + 2], 0x07030602);
-            t[q][0] = perm(lo[1][0], lo[0][0], 0x05040100);
-            t[q][1] = perm(lo[1][0], lo[0][0], 0x07060302);
-            t[q][2] = perm(lo[1][1], lo[0][1], 0x05040100);
-            t[q][3] = perm(lo[1][1], lo[0][1], 0x07060302);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) out[c] = widen8<FMT>(t[0][c], t[1][c]);
-    }
-}
 
 // a lane's part of 32 keys: of row lane % 16 of both halves the 16-byte pieces lane / 16 + 4 h, and of tokens 4 (lane / 16) + 0 .. 3
 // of both halves the values' numbers 4 C (lane % 16) + 0 .. 4 C - 1
@@ -299,40 +238,21 @@ __device__ __forceinline__ void finish(const Attend& a, const Where& w, Rows<C>&
 // ---- attention over all tokens --------------------------------------------------------------------------------------
 
 struct Request {
-    u32 t0, tokens, tiles, units;      // units of one row tile
-    int context;
+    Span s;
+    u32 tiles, units;      // units of one row tile
 };
 
 __device__ __forceinline__ Request request_of(const Attend& a, u32 b) {
     Request r;
-    const int32_t from = a.s.offsets[b], to = a.s.offsets[b + 1];
-    r.t0 = min((u32)max(from, 0), a.s.tokens);
-    r.tokens = max(min((u32)max(to, 0), a.s.tokens), r.t0) - r.t0;
-    r.context = (int)min((u64)(u32)max(a.s.context[b], 0), (u64)a.s.max_pages * a.c.page_tokens);
-    r.tiles = (r.tokens * a.group + ROWS - 1) / ROWS;
+    r.s = span_of(a, b);
+    r.tiles = (r.s.tokens * a.group + ROWS - 1) / ROWS;
     // with a window a tile's first token begins `window` before itself, at the edge of a block
-    const u32 span = a.window ? (u32)min((u64)r.context, (u64)a.window + (ROWS - 1) / a.group + 1 + BLOCK - 1) : (u32)r.context;
-    r.units = r.tokens ? (span + UNIT - 1) / UNIT : 0;
+    const u32 span = a.window ? (u32)min((u64)r.s.context, (u64)a.window + (ROWS - 1) / a.group + 1 + BLOCK - 1) : (u32)r.s.context;
+    r.units = r.s.tokens ? (span + UNIT - 1) / UNIT : 0;
     return r;
 }
 
 __device__ __forceinline__ u64 units_of(const Attend& a, const Request& r) { return (u64)r.tiles * r.units * a.c.kv_heads; }
-
-__device__ __forceinline__ u64 share(u64 total, u32 parts, u32 i) { return total * i / parts; }
-
-// zeros for the heads of tokens [t0, t1)
-__device__ __forceinline__ void write_empty(const Attend& a, u32 t0, u32 t1) {
-    const u32 pieces = a.c.dim / 8;
-    const u64 n = (u64)(t1 - t0) * a.heads * pieces;
-    for (u64 i = threadIdx.x; i < n; i += blockDim.x) {
-        const u32 at = (u32)(i % pieces) * 8, head = (u32)(i / pieces % a.heads), t = t0 + (u32)(i / pieces / a.heads);
-        *(uint4*)((uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + at) = make_uint4(0, 0, 0, 0);
-        if (at == 0) {
-            if (a.lse) a.lse[(u64)t * a.heads + head] = -INFINITY;
-            a.joined[(u64)t * a.heads + head] = make_int2(-1, -1);
-        }
-    }
-}
 
 __device__ __forceinline__ void write_joined(const Attend& a, const Where& w, int2 j) {
     if (threadIdx.x < ROWS && w.row0 + threadIdx.x < w.rows) {
@@ -385,13 +305,9 @@ __global__ void __launch_bounds__(256) k_attend(Attend a) {
     // tokens that have nothing to read, and padding
     for (u32 b = blockIdx.x; b < a.s.requests; b += gridDim.x) {
         const Request r = request_of(a, b);
-        if (r.tokens && !r.units) write_empty(a, r.t0, r.t0 + r.tokens);
+        if (r.s.tokens && !r.units) write_empty(a, r.s.t0, r.s.t0 + r.s.tokens);
     }
-    {
-        const u32 last = min((u32)max(a.s.offsets[a.s.requests], 0), a.s.tokens), pad = a.s.tokens - last;
-        const u32 from = last + (u32)((u64)pad * blockIdx.x / gridDim.x), to = last + (u32)((u64)pad * (blockIdx.x + 1) / gridDim.x);
-        if (from < to) write_empty(a, from, to);
-    }
+    write_padding(a);
     if (begin >= end) return;
     __syncthreads();
     u32 b = sh_b;
@@ -409,18 +325,17 @@ __global__ void __launch_bounds__(256) k_attend(Attend a) {
         const u64 in = at - before;
         const u32 u0 = (u32)(in % q.units), u1 = (u32)min((u64)q.units, u0 + (end - at));
         Where w;
-        w.t0 = q.t0;
-        w.rows = q.tokens * a.group;
+        w.t0 = q.s.t0;
+        w.rows = q.s.tokens * a.group;
         w.row0 = (u32)(in / q.units % q.tiles) * ROWS;
         w.kv_head = (u32)(in / q.units / q.tiles);
         w.head0 = w.kv_head * a.group;
-        const int first_position = q.context - (int)q.tokens;
-        const int p0 = first_position + (int)(w.row0 / a.group), p1 = first_position + (int)(min(w.row0 + ROWS - 1, w.rows - 1) / a.group);
+        const int p0 = q.s.first + (int)(w.row0 / a.group), p1 = q.s.first + (int)(min(w.row0 + ROWS - 1, w.rows - 1) / a.group);
         const int low = a.window ? max(0, p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
         const int start = (low & ~(int)(BLOCK - 1)) + (int)(u0 * UNIT), stop = min(p1 + 1, start + (int)((u1 - u0) * UNIT));
 
         Rows<C> rows;
-        load_rows<C>(a, w, first_position, rows);
+        load_rows<C>(a, w, q.s.first, rows);
         const u32 col = lane & 15, g = lane >> 4;
         const int32_t* table = a.s.table + b * a.s.table_stride;
         // 64 blocks of this wave's tiles at a time: lane 2 i + s has block s of tile i
@@ -658,6 +573,7 @@ __global__ void __launch_bounds__(256) k_join(Attend a, bool listed, int groups)
 }
 
 constexpr u32 groups_per_cu(u32 width) { return width <= 128 ? 3 : 2; }
+u64 partial_floats(u32 width, int num_cu) { return 2ull * (u32)num_cu * groups_per_cu(width) * ROWS * (width + 2); }
 
 template <int FMT, int C>
 void run_attend(hipStream_t st, const Attend& a, int num_cu) {
@@ -673,9 +589,11 @@ void run_attend(hipStream_t st, const Attend& a, int num_cu) {
 
 }  // namespace
 
-u64 partial_floats(u32 width, int num_cu) { return 2ull * (u32)num_cu * groups_per_cu(width) * ROWS * (width + 2); }
+u64 narrow_workspace(u32 width, u64 rows, int num_cu) { return 4 * partial_floats(width, num_cu) + 8 * rows; }
 
-int launch_attend(hipStream_t st, const Attend& a, int num_cu) {
+int launch_attend(hipStream_t st, const Attend& args, int num_cu) {
+    Attend a = args;
+    a.joined = (int2*)(a.partial + partial_floats(a.c.width, num_cu));
     const u32 n = a.c.width / 64;
     if (a.c.fmt == PAG_KV_INT8) {
         if (n == 1) run_attend<PAG_KV_INT8, 1>(st, a, num_cu);

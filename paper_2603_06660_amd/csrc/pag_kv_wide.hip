@@ -1,0 +1,503 @@
+// Attention of many query rows over the same keys: pag_kv_attend for chunks of prompts and wide groups.
+//
+// The mathematics is that of pag_kv_attend.hip; what bounds it is different.  With 16 rows a tile a key is widened to 16-bit floats
+// once for each of them, and the vector units are what a long chunk waits for.  Here four waves have 32 rows each, and 64 keys are
+// widened once for all 128, into LDS: keys row by row, values transposed, in the order in which the scores leave the matrix unit,
+// so that weights go back in from their registers as in the narrow kernel.  The next 64 keys are on their way from memory
+// meanwhile.  Shares are counted in steps of 64 keys of the tiles' own causal lengths: tile j and the j-th from the end make a pair,
+// and all pairs of a request are equally long, so that a share is found without adding up tiles.
+#include "pag_kv_attend.h"
+
+namespace pagkv {
+namespace {
+
+constexpr u32 WROWS = 32;                   // query rows of a wave
+constexpr u32 ROWS = 4 * WROWS;             // of a workgroup
+constexpr u32 STEP = 64;                    // keys of a step, one block of 16 a wave to fetch
+
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+struct Tiles {
+    Span s;
+    u32 rows, count, pairs, pair_units, mid_units;
+    u64 units;                              // of one key/value head
+};
+
+struct Range { int start, stop, p0, p1; u32 units; };
+
+__device__ __forceinline__ Range range_of(const Attend& a, const Span& s, u32 rows, u32 tile) {
+    Range r;
+    r.p0 = s.first + (int)(tile * ROWS / a.group);
+    r.p1 = s.first + (int)(min(tile * ROWS + ROWS - 1, rows - 1) / a.group);
+    r.start = a.window ? max(0, r.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) & ~(int)(BLOCK - 1) : 0;
+    r.stop = max(r.p1 + 1, r.start);
+    r.units = max(((u32)(r.stop - r.start) + STEP - 1) / STEP, 1u);
+    return r;
+}
+
+__device__ __forceinline__ Tiles tiles_of(const Attend& a, u32 b) {
+    Tiles t;
+    t.s = span_of(a, b);
+    t.rows = t.s.tokens * a.group;
+    t.count = t.s.context ? (t.rows + ROWS - 1) / ROWS : 0;
+    t.pairs = t.count / 2;
+    t.mid_units = t.count & 1 ? range_of(a, t.s, t.rows, t.pairs).units : 0;
+    // no pair is longer: two ends of tiles that lie opposite add up to the same, and each is rounded up once
+    u64 most = (2 * (u64)max(t.s.first + 1, 0) + ((u64)ROWS * (t.count ? t.count - 1 : 0) + 2 * (ROWS - 1)) / a.group + 1) / STEP + 2;
+    if (a.window) most = min(most, 2 * (((u64)a.window + (ROWS - 1) / a.group + 1 + BLOCK - 1 + STEP - 1) / STEP));
+    t.pair_units = (u32)max(most, (u64)2);
+    t.units = (u64)t.pairs * t.pair_units + t.mid_units;
+    return t;
+}
+
+struct Head {                               // of a piece that another workgroup goes on with
+    u32 t0, rows, row0, head0;
+    int last;                               // workgroup that ends it; -1: none
+};
+
+// halves of a row of keys, in pieces of 8; of a row of values (64 tokens of a number), likewise.  Rows that a wave reads together lie in
+// different banks.
+template <int C>
+__device__ __forceinline__ u32 key_at(u32 token, u32 piece) {
+    const u32 turn = C % 2 ? token >> 1 & 7u : token & (C == 2 ? 15u : 7u);
+    return token * (64 * C) + (piece ^ turn) * 8;
+}
+
+__device__ __forceinline__ u32 value_at(u32 d, u32 piece) { return d * STEP + (piece ^ (d >> 2 & 7u) ^ (d & 2u)) * 8; }
+
+// what a thread fetches of the next 64 keys: 16 C bytes of a key, and 8 tokens' words of the values
+template <int C>
+struct Fetch {
+    static constexpr int N = (32 * C + 63) / 64;         // words of values a lane has at most
+    uint4 k[C];
+    u32 v[N][8];
+};
+
+template <int FMT, int C>
+__global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, Head* heads) {
+    constexpr u32 W = 64 * C, KEYS = STEP * W, VALUES = W * STEP;
+    extern __shared__ __align__(16) _Float16 lds[];       // two buffers of keys and values
+    __shared__ float sh_scale[2][4][2];                   // 2^e of the keys' block, e of the values'
+    __shared__ u32 sh_there[2][4];
+    __shared__ u64 sh_sum[4];
+    __shared__ u64 sh_begin;
+    __shared__ u32 sh_b;
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, hi = lane >> 5;
+
+    // this workgroup's share
+    const u32 per = (a.s.requests + 255) / 256, b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
+    u64 mine = 0;
+    for (u32 b = b0; b < b1; ++b) mine += tiles_of(a, b).units * a.c.kv_heads;
+    u64 upto = mine;
+#pragma unroll
+    for (u32 o = 1; o < 64; o <<= 1) {
+        const u64 y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+    }
+    if (lane == 63) sh_sum[wave] = upto;
+    __syncthreads();
+    u64 total = 0;
+    for (u32 x = 0; x < 4; ++x) {
+        if (x < wave) upto += sh_sum[x];
+        total += sh_sum[x];
+    }
+    const u32 parts = (u32)min((u64)gridDim.x, total);
+    const u64 begin = blockIdx.x < parts ? share(total, parts, blockIdx.x) : total, end = blockIdx.x < parts ? share(total, parts, blockIdx.x + 1) : total;
+    if (begin < end && begin >= upto - mine && begin < upto) {
+        u64 before = upto - mine;
+        u32 b = b0;
+        for (;; ++b) {
+            const u64 n = tiles_of(a, b).units * a.c.kv_heads;
+            if (begin < before + n) break;
+            before += n;
+        }
+        sh_b = b;
+        sh_begin = before;
+    }
+    for (u32 b = blockIdx.x; b < a.s.requests; b += gridDim.x) {
+        const Span s = span_of(a, b);
+        if (s.tokens && !s.context) write_empty(a, s.t0, s.t0 + s.tokens);
+    }
+    write_padding(a);
+    if (threadIdx.x == 0) heads[blockIdx.x].last = -1;
+    if (begin >= end) return;
+    __syncthreads();
+    u32 b = sh_b;
+    u64 before = sh_begin, at = begin;
+    Tiles q = tiles_of(a, b);
+
+    while (at < end) {
+        while (at >= before + q.units * a.c.kv_heads) {
+            before += q.units * a.c.kv_heads;
+            ++b;
+            q = tiles_of(a, b);
+        }
+        const u32 kv_head = (u32)((at - before) / q.units);
+        const u64 in = (at - before) % q.units;
+        u32 tile, u0, skip = 0;
+        Range r;
+        if (in >= (u64)q.pairs * q.pair_units) {
+            tile = q.pairs;
+            u0 = (u32)(in - (u64)q.pairs * q.pair_units);
+            r = range_of(a, q.s, q.rows, tile);
+        } else {
+            const u32 pair = (u32)(in / q.pair_units);
+            u0 = (u32)(in % q.pair_units);
+            tile = q.count - 1 - pair;                      // the longer one first
+            r = range_of(a, q.s, q.rows, tile);
+            if (u0 >= r.units) {
+                u0 -= r.units;
+                tile = pair;
+                r = range_of(a, q.s, q.rows, tile);
+                if (u0 >= r.units) skip = (u32)(q.pair_units - in % q.pair_units);
+            }
+        }
+        if (skip) {                                         // what the pair was rounded up by
+            at += skip;
+            continue;
+        }
+        const u32 u1 = (u32)min((u64)r.units, u0 + (end - at));
+        const int start = r.start + (int)(u0 * STEP), stop = min(r.stop, start + (int)((u1 - u0) * STEP));
+
+        // this wave's rows
+        const u32 row = tile * ROWS + wave * WROWS + col, token = row / a.group, head = kv_head * a.group + row % a.group;
+        const bool real = row < q.rows;
+        const int position = real ? q.s.first + (int)token : -1;
+        const u32 w_row = tile * ROWS + wave * WROWS;
+        const bool busy = w_row < q.rows;                   // the wave has rows
+        const int w_p0 = q.s.first + (int)(min(w_row, q.rows - 1) / a.group), w_p1 = q.s.first + (int)(min(w_row + WROWS - 1, q.rows - 1) / a.group);
+        const int oldest = a.window ? max(0, position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
+        const int w_first = a.window ? max(0, w_p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
+        const int w_full = a.window ? w_p1 - (int)min(a.window - 1, 0x7FFFFFFEu) : 0;      // keys from here on are in the window of all rows
+        const float slope = real && a.slopes ? a.slopes[head] * LOG2E : 0.f;
+
+        half8_t Q[4 * C];                                   // numbers 16 n + 8 hi + 0 .. 7 in Q[n]
+        float factor;
+        {
+            // scaled by a power of two, so that 16-bit floats hold it; two sweeps over the row rather than all of it in 32 bits
+            float most = 0.f;
+            const u64 from = (u64)(q.s.t0 + token) * (u64)a.q_ts + head * (u64)a.q_hs;
+#pragma unroll
+            for (int n = 0; n < 4 * C; ++n) {
+                const u32 d = n * 16 + hi * 8;
+                float x[8] = { 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f };
+                if (real && d < a.c.dim) load8(a.q, from + d, a.dtype, x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
+            }
+            most = fmaxf(most, __shfl_xor(most, 32));
+            int e = (int)(__float_as_uint(most) >> 23) - 127 - 7;
+            e = min(max(e, -100), 100);
+            const float down = power(-e);
+#pragma unroll
+            for (int n = 0; n < 4 * C; ++n) {
+                const u32 d = n * 16 + hi * 8;
+                float x[8] = { 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f };
+                if (real && d < a.c.dim) load8(a.q, from + d, a.dtype, x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) Q[n][j] = (_Float16)(x[j] * down);
+            }
+            factor = a.scale * power(e);
+        }
+        float M = LOWEST, sum = 0.f;
+        float16_t acc[2 * C];
+#pragma unroll
+        for (int n = 0; n < 2 * C; ++n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
+        }
+
+        const int32_t* table = a.s.table + b * a.s.table_stride;
+        // this wave's blocks of the next 64 steps, a lane each
+        u32 block_row = 0;
+        int ek_mine = 0, ev_mine = 0;
+        u64 there = 0;
+        const auto look_up = [&](int from) {
+            const int at_key = from + (int)(lane * STEP + wave * BLOCK);
+            bool ok = false;
+            block_row = 0;
+            ek_mine = ev_mine = 0;
+            if (at_key < stop) {
+                const u32 blk = (u32)at_key / BLOCK, page = (u32)table[blk / a.c.page_blocks];
+                if (page < a.c.num_pages) {
+                    ok = true;
+                    block_row = row_of(a.c, page, kv_head, blk % a.c.page_blocks * BLOCK);
+                    const int8_t* e = a.c.exponents + (u64)(block_row / BLOCK) * 2;
+                    ek_mine = e[0];
+                    ev_mine = e[1];
+                }
+            }
+            there = __ballot(ok);
+        };
+        Fetch<C> f;
+        const auto fetch = [&](u32 n) {
+            const uint8_t* rows = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, (int)(n & 63)) * (2 * W);
+            const uint8_t* k = rows + (lane >> 2) * (2 * W) + (lane & 3) * (16 * C);
+#pragma unroll
+            for (int i = 0; i < C; ++i) f.k[i] = *(const uint4*)(k + 16 * i);
+#pragma unroll
+            for (int i = 0; i < Fetch<C>::N; ++i) {
+                const u32 item = lane + 64 * i, word = item % (16 * C), half = item / (16 * C);
+                if (half < 2) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f.v[i][j] = *(const u32*)(rows + (8 * (j >> 2) + 4 * half + (j & 3)) * (2 * W) + W + word * 4);
+                }
+            }
+        };
+        const auto stage = [&](u32 n, int from, u32 buffer) {
+            _Float16* keys = lds + buffer * (KEYS + VALUES);
+            _Float16* values = keys + KEYS;
+            const u32 token = wave * BLOCK + (lane >> 2), piece = (lane & 3) * (2 * C);
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                *(half8_t*)(keys + key_at<C>(token, piece + 2 * i)) = widen8<FMT>(f.k[i].x, f.k[i].y);
+                *(half8_t*)(keys + key_at<C>(token, piece + 2 * i + 1)) = widen8<FMT>(f.k[i].z, f.k[i].w);
+            }
+            const bool ok = there >> (n & 63) & 1;
+            const int base = from + (int)(wave * BLOCK);
+#pragma unroll
+            for (int i = 0; i < Fetch<C>::N; ++i) {
+                const u32 item = lane + 64 * i, word = item % (16 * C), half = item / (16 * C);
+                if (half < 2) {
+                    if (!ok || base + (int)BLOCK > stop) {      // the memory behind the last token may hold anything
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (!ok || base + (int)(8 * (j >> 2) + 4 * half + (j & 3)) >= stop) f.v[i][j] = 0;
+                    }
+                    half8_t v[4];
+                    columns<FMT>(f.v[i], v);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) *(half8_t*)(values + value_at(word * 4 + c, wave * 2 + half)) = v[c];
+                }
+            }
+            if (lane == 0) {
+                sh_scale[buffer][wave][0] = power(__builtin_amdgcn_readlane(ek_mine, (int)(n & 63)));
+                sh_scale[buffer][wave][1] = (float)__builtin_amdgcn_readlane(ev_mine, (int)(n & 63));
+                sh_there[buffer][wave] = ok && base < stop ? 1u : 0u;
+            }
+        };
+
+        const u32 steps = (u32)(max(stop - start, 0) + (int)STEP - 1) / STEP;
+        __syncthreads();                                        // the piece before has been read
+        if (steps) {
+            look_up(start);
+            fetch(0);
+            stage(0, start, 0);
+        }
+        __syncthreads();
+        for (u32 n = 0; n < steps; ++n) {
+            const int from = start + (int)(n * STEP);
+            const u32 buffer = n & 1;
+            if (n + 1 < steps) {
+                if (((n + 1) & 63) == 0) look_up(from + (int)STEP);
+                fetch(n + 1);
+            }
+            if (busy && from <= w_p1 && from + (int)STEP > w_first) {
+                const _Float16* keys = lds + buffer * (KEYS + VALUES);
+                const _Float16* values = keys + KEYS;
+                float16_t S[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) S[h][i] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4 * C; ++i)
+                        S[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(keys + key_at<C>(h * 32 + col, 2 * i + hi)), Q[i], S[h], 0, 0, 0);
+                }
+                float ev[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) ev[x] = sh_scale[buffer][x][1];
+                // key 32 h + 8 (i / 4) + 4 hi + i % 4 in S[h][i]; i / 8 is its block's half
+                if (a.softcap > 0.f) {
+                    const float in = 2.f * LOG2E * factor / a.softcap, cap = a.softcap * LOG2E;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const float by = in * sh_scale[buffer][x][0], top = cap + ev[x];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float s = S[x >> 1][8 * (x & 1) + i];
+                            S[x >> 1][8 * (x & 1) + i] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * by)), top);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const float by = factor * LOG2E * sh_scale[buffer][x][0];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            S[x >> 1][8 * (x & 1) + i] = __builtin_fmaf(S[x >> 1][8 * (x & 1) + i], by, ev[x]);
+                        }
+                    }
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) S[h][i] -= slope * (float)(position - (from + h * 32 + 8 * (i >> 2) + 4 * (int)hi + (i & 3)));
+                    }
+                }
+                const bool all = sh_there[buffer][0] & sh_there[buffer][1] & sh_there[buffer][2] & sh_there[buffer][3];
+                if (!all || from + (int)STEP > w_p0 + 1 || from < w_full) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const bool ok = sh_there[buffer][x];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int p = from + 16 * x + 8 * (i >> 2) + 4 * (int)hi + (i & 3);
+                            if (!ok || p > position || p < oldest) S[x >> 1][8 * (x & 1) + i] = -INFINITY;
+                        }
+                    }
+                }
+                float most = fmaxf(S[0][0], S[1][0]);
+#pragma unroll
+                for (int i = 1; i < 16; ++i) most = fmaxf(most, fmaxf(S[0][i], S[1][i]));
+                if (__ballot(most > M + HEADROOM)) {
+                    most = fmaxf(most, __shfl_xor(most, 32));
+                    const float to = most > M + HEADROOM ? most - START : M, alpha = __builtin_amdgcn_exp2f(M - to);
+                    sum *= alpha;
+#pragma unroll
+                    for (int n = 0; n < 2 * C; ++n) acc[n] *= alpha;
+                    M = to;
+                }
+                half8_t P[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    float part = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float y = __builtin_amdgcn_exp2f(S[x >> 1][8 * (x & 1) + i] - M);
+                        part += y;
+                        P[x][i] = (_Float16)y;
+                    }
+                    sum = __builtin_fmaf(part, power(-(int)ev[x]), sum);
+                }
+#pragma unroll
+                for (int n = 0; n < 2 * C; ++n) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(values + value_at(n * 32 + col, 2 * x + hi)), P[x], acc[n], 0, 0, 0);
+                }
+            }
+            if (n + 1 < steps) stage(n + 1, from + (int)STEP, buffer ^ 1);
+            __syncthreads();
+        }
+
+        sum += __shfl_xor(sum, 32);
+        const bool begun = u0 == 0, ended = u1 == r.units;
+        if (begun && ended) {
+            if (real) {
+                const float by = sum != 0.f ? 1.f / sum : 0.f;
+                uint16_t* out = (uint16_t*)a.out + (int64_t)(q.s.t0 + token) * a.o_ts + (int64_t)head * a.o_hs;
+#pragma unroll
+                for (int n = 0; n < 2 * C; ++n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const u32 d = n * 32 + 8 * i + 4 * hi;
+                        if (d < a.c.dim)
+                            *(uint2*)(out + d) = make_uint2(pack2(acc[n][4 * i] * by, acc[n][4 * i + 1] * by, a.dtype), pack2(acc[n][4 * i + 2] * by, acc[n][4 * i + 3] * by, a.dtype));
+                    }
+                }
+                if (a.lse && hi == 0) a.lse[(u64)(q.s.t0 + token) * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
+            }
+        } else {
+            float* partial = a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (W + 2));
+            const u32 r_here = wave * WROWS + col;
+            if (hi == 0) { partial[r_here] = M; partial[ROWS + r_here] = sum; }
+#pragma unroll
+            for (int n = 0; n < 2 * C; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *(float4*)(partial + 2 * ROWS + r_here * W + n * 32 + 8 * i + 4 * hi) = make_float4(acc[n][4 * i], acc[n][4 * i + 1], acc[n][4 * i + 2], acc[n][4 * i + 3]);
+            }
+            if (begun && threadIdx.x == 0) {
+                Head h;
+                h.t0 = q.s.t0; h.rows = q.rows; h.row0 = tile * ROWS; h.head0 = kv_head * a.group;
+                h.last = (int)(((at + r.units) * parts - 1) / total);       // the workgroup of the tile's last unit
+                heads[blockIdx.x] = h;
+            }
+        }
+        at += u1 - u0;
+    }
+}
+
+// Adds up the pieces of a tile that several workgroups had: workgroup (g, y) rows 16 y to 16 y + 15 of the tile that g began
+template <int C>
+__global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) {
+    constexpr u32 W = 64 * C, SLOT = ROWS * (W + 2);
+    const Head h = heads[blockIdx.x];
+    if (h.last <= (int)blockIdx.x || h.last >= (int)gridDim.x) return;
+    const u32 r = blockIdx.y * 16 + (threadIdx.x >> 4), first = (threadIdx.x & 15) * 4 * C, row = h.row0 + r;
+    if (row >= h.rows) return;
+    float M = LOWEST, sum = 0.f, acc[4 * C];
+#pragma unroll
+    for (int c = 0; c < 4 * C; ++c) acc[c] = 0.f;
+    for (int g = (int)blockIdx.x; g <= h.last; ++g) {
+        const float* p = a.partial + (2 * (u64)g + (g == (int)blockIdx.x ? 1 : 0)) * SLOT;
+        const float m = p[r], s = p[ROWS + r], top = fmaxf(M, m);
+        const float was = __builtin_amdgcn_exp2f(M - top), is = __builtin_amdgcn_exp2f(m - top);
+        sum = sum * was + s * is;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const float4 y = *(const float4*)(p + 2 * ROWS + r * W + first + 4 * c);
+            acc[4 * c] = acc[4 * c] * was + y.x * is;
+            acc[4 * c + 1] = acc[4 * c + 1] * was + y.y * is;
+            acc[4 * c + 2] = acc[4 * c + 2] * was + y.z * is;
+            acc[4 * c + 3] = acc[4 * c + 3] * was + y.w * is;
+        }
+        M = top;
+    }
+    const u32 t = h.t0 + row / a.group, head = h.head0 + row % a.group;
+    const float by = sum != 0.f ? 1.f / sum : 0.f;
+    uint16_t* out = (uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + first;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (first + 4 * c < a.c.dim)
+            *(uint2*)(out + 4 * c) = make_uint2(pack2(acc[4 * c] * by, acc[4 * c + 1] * by, a.dtype), pack2(acc[4 * c + 2] * by, acc[4 * c + 3] * by, a.dtype));
+    }
+    if (a.lse && first == 0) a.lse[(u64)t * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
+}
+
+constexpr u32 groups_per_cu(u32 width) { return width <= 128 ? 2 : 1; }
+constexpr u32 lds_bytes(u32 width) { return 2 * 2 * STEP * width * 2; }
+
+template <int FMT, int C>
+int run(hipStream_t st, const Attend& a, int num_cu) {
+    const u32 grid = (u32)num_cu * groups_per_cu(64 * C);
+    Head* heads = (Head*)(a.partial + 2ull * grid * ROWS * (64 * C + 2));
+    if (lds_bytes(64 * C) >= 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void*)k_attend_wide<FMT, C>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes(64 * C));
+        if (e != hipSuccess) { pag_set_error(std::string("hipFuncSetAttribute: ") + hipGetErrorString(e)); return PAG_EHIP; }
+    }
+    k_attend_wide<FMT, C><<<grid, 256, lds_bytes(64 * C), st>>>(a, heads);
+    k_join_wide<C><<<dim3(grid, ROWS / 16), 256, 0, st>>>(a, heads);
+    return PAG_OK;
+}
+
+}  // namespace
+
+u64 wide_workspace(u32 width, int num_cu) {
+    const u64 grid = (u64)num_cu * groups_per_cu(width);
+    return 4 * 2 * grid * ROWS * (width + 2) + (grid * sizeof(Head) + 15) / 16 * 16;
+}
+
+int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu) {
+    const u32 n = a.c.width / 64;
+    int rc;
+    if (a.c.fmt == PAG_KV_INT8) {
+        if (n == 1) rc = run<PAG_KV_INT8, 1>(st, a, num_cu);
+        else if (n == 2) rc = run<PAG_KV_INT8, 2>(st, a, num_cu);
+        else if (n == 3) rc = run<PAG_KV_INT8, 3>(st, a, num_cu);
+        else rc = run<PAG_KV_INT8, 4>(st, a, num_cu);
+    } else {
+        if (n == 1) rc = run<PAG_KV_FP8, 1>(st, a, num_cu);
+        else if (n == 2) rc = run<PAG_KV_FP8, 2>(st, a, num_cu);
+        else if (n == 3) rc = run<PAG_KV_FP8, 3>(st, a, num_cu);
+        else rc = run<PAG_KV_FP8, 4>(st, a, num_cu);
+    }
+    if (rc) return rc;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { pag_set_error(std::string("pag_kv_attend: ") + hipGetErrorString(e)); return PAG_EHIP; }
+    return PAG_OK;
+}
+
+}  // namespace pagkv

@@ -256,8 +256,7 @@ class KvCache:
         lib = load_library()
         nothing = [C.c_void_p(None), C.c_int64(0), C.c_int64(0)]
         _check(lib.pag_kv_read(C.byref(self._c), C.c_void_p(None), C.c_uint64(0), C.c_uint32(0), *nothing, *nothing, C.c_void_p(None)), "KvCache")
-        with _On(self.device):
-            self._partial = lib.pag_kv_workspace_bytes(C.byref(self._c), C.c_uint64(0), C.c_uint32(0))
+        self._rooms = {}        # sizes of workspaces
 
     def append(self, k, v, slots):
         """Writes k and v [tokens, kv_heads, head_dim] (float32, float16 or bfloat16) into slots (int64 [tokens], -1: left out)."""
@@ -311,12 +310,20 @@ class KvCache:
             out = (torch.empty(shape, dtype=q.dtype, device=self.device), torch.empty((tokens, heads), dtype=torch.float32, device=self.device))
         o, lse = out
         _rows(o, shape, self.device, "out", (q.dtype,))
-        room = torch.empty(self._partial + 8 * tokens * heads, dtype=torch.uint8, device=self.device)
+        s = step._with(tokens)
+        size = self._rooms.get((tokens, heads, s.requests, s.max_new))
+        if size is None:
+            with _On(self.device):
+                size = load_library().pag_kv_workspace_bytes(C.byref(self._c), C.byref(s), C.c_uint32(heads))
+            if len(self._rooms) > 4096:
+                self._rooms.clear()
+            self._rooms[tokens, heads, s.requests, s.max_new] = size
+        room = torch.empty(size, dtype=torch.uint8, device=self.device)
         a = _Attention(C.sizeof(_Attention), _DTYPES[q.dtype], heads, window, self.head_dim ** -0.5 if scale is None else scale, softcap,
                        None if slopes is None else _array(slopes, torch.float32, (heads,), self.device, "slopes"),
                        q.data_ptr(), q.stride(0), q.stride(1), o.data_ptr(), o.stride(0), o.stride(1),
                        None if lse is None else _array(lse, torch.float32, (tokens, heads), self.device, "lse"), room.data_ptr(), room.numel())
-        return out, step._with(tokens), a, room
+        return out, s, a, room
 
     def attend(self, q, step, scale=None, window=0, softcap=0.0, slopes=None, out=None):
         """-> (out like q, lse float32 [tokens, heads]): every token of q [tokens, heads, head_dim] (float16 or bfloat16) attends to its request's
