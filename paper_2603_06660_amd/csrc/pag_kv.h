@@ -75,14 +75,7 @@ __device__ __forceinline__ int least_exponent(float most) {
     return e < LOWEST_EXPONENT ? LOWEST_EXPONENT : e;
 }
 
-// eight numbers of an input row in 32 bits
-__device__ __forceinline__ void load8(const void* p, u64 at, u32 dtype, float* x) {
-    if (dtype == PAG_F32) {
-        const float4 a = *(const float4*)((const float*)p + at), b = *(const float4*)((const float*)p + at + 4);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-        return;
-    }
-    const uint4 r = *(const uint4*)((const uint16_t*)p + at);
+__device__ __forceinline__ void widen_row8(const uint4& r, u32 dtype, float* x) {      // PAG_F16 or PAG_BF16
     const u32 w[4] = { r.x, r.y, r.z, r.w };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -95,6 +88,16 @@ __device__ __forceinline__ void load8(const void* p, u64 at, u32 dtype, float* x
             x[2 * i + 1] = (float)h.y;
         }
     }
+}
+
+// eight numbers of an input row in 32 bits
+__device__ __forceinline__ void load8(const void* p, u64 at, u32 dtype, float* x) {
+    if (dtype == PAG_F32) {
+        const float4 a = *(const float4*)((const float*)p + at), b = *(const float4*)((const float*)p + at + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        return;
+    }
+    widen_row8(*(const uint4*)((const uint16_t*)p + at), dtype, x);
 }
 
 __device__ __forceinline__ u32 pack2(float a, float b, u32 dtype) {       // to nearest even

@@ -23,6 +23,10 @@ constexpr u32 TILE = 32;                  // keys of a tile
 constexpr u32 WAVES = 4;
 constexpr u32 UNIT = WAVES * TILE;        // keys of the smallest share
 
+constexpr u32 PIECE = 4;                  // what beginning and ending a piece costs, in units
+
+constexpr u32 groups_per_cu(u32 width) { return width <= 128 ? 2 : 1; }
+
 // a lane's part of 32 keys: of row lane % 16 of both halves the 16-byte pieces lane / 16 + 4 h, and of tokens 4 (lane / 16) + 0 .. 3
 // of both halves the values' numbers 4 C (lane % 16) + 0 .. 4 C - 1
 template <int C>
@@ -63,23 +67,35 @@ struct Where {
     u32 t0, rows, row0, head0, kv_head;      // first token, rows of the block's request and group, first row of this tile, first query head, its keys' head
 };
 
+// the numbers of row lane % 16 as they come
 template <int C>
-__device__ __forceinline__ void load_rows(const Attend& a, const Where& w, int first_position, Rows<C>& r) {
+struct RawRows { uint4 x[2 * C]; };
+
+template <int C>
+__device__ __forceinline__ void fetch_rows(const Attend& a, const Where& w, RawRows<C>& raw) {
     const u32 lane = threadIdx.x & 63, row = w.row0 + (lane & 15), g = lane >> 4;
-    const u32 i = row / a.group, head = w.head0 + row % a.group;
-    const bool real = row < w.rows;
-    r.position = real ? first_position + (int)i : -1;
-    r.slope = real && a.slopes ? a.slopes[head] * LOG2E : 0.f;
-    float x[2 * C][8];
-    float most = 0.f;
+    const u64 from = (u64)(w.t0 + row / a.group) * (u64)a.q_ts + (w.head0 + row % a.group) * (u64)a.q_hs;
 #pragma unroll
     for (int n = 0; n < 2 * C; ++n) {
         const u32 at = (n >> 1) * 64 + g * 16 + (n & 1) * 8;
+        raw.x[n] = make_uint4(0, 0, 0, 0);
+        if (row < w.rows && at < a.c.dim) raw.x[n] = *(const uint4*)((const uint16_t*)a.q + from + at);
+    }
+}
+
+template <int C>
+__device__ __forceinline__ void start_rows(const Attend& a, const Where& w, int first_position, const RawRows<C>& raw, Rows<C>& r) {
+    const u32 lane = threadIdx.x & 63, row = w.row0 + (lane & 15);
+    const bool real = row < w.rows;
+    r.position = real ? first_position + (int)(row / a.group) : -1;
+    r.slope = real && a.slopes ? a.slopes[w.head0 + row % a.group] * LOG2E : 0.f;
+    float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[n][j] = 0.f;
-        if (real && at < a.c.dim) load8(a.q, (u64)(w.t0 + i) * (u64)a.q_ts + head * (u64)a.q_hs + at, a.dtype, x[n]);
+    for (int n = 0; n < 2 * C; ++n) {
+        float x[8];
+        widen_row8(raw.x[n], a.dtype, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[n][j]));
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
     }
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
@@ -89,8 +105,10 @@ __device__ __forceinline__ void load_rows(const Attend& a, const Where& w, int f
     const float down = power(-e);
 #pragma unroll
     for (int n = 0; n < 2 * C; ++n) {
+        float x[8];
+        widen_row8(raw.x[n], a.dtype, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r.q[n][j] = (_Float16)(x[n][j] * down);
+        for (int j = 0; j < 8; ++j) r.q[n][j] = (_Float16)(x[j] * down);
     }
     r.factor = a.scale * power(e);
     r.M = LOWEST;
@@ -99,10 +117,18 @@ __device__ __forceinline__ void load_rows(const Attend& a, const Where& w, int f
     for (int c = 0; c < 4 * C; ++c) r.acc[c] = float4_t{ 0.f, 0.f, 0.f, 0.f };
 }
 
-// ek, ev: this lane's 8 keys' scales as 2^e (keys) and e (values); position of its key j; keep: bit j set if the row may read key j.
-// LISTED: the keys have their own exponents and positions; otherwise keys 0 .. 3 and 4 .. 7 share theirs, and have position at, at + 1, ..
+// What this lane's 8 keys are scaled by: 2^e of the keys, e of the values and 2^-e of the values.
+// LISTED: every key has its own and its position; otherwise keys 0 .. 3 and 4 .. 7 share theirs, and at holds the first one's position
+template <bool LISTED>
+struct Scales {
+    static constexpr int N = LISTED ? 8 : 2;
+    float ek[N], ev[N], down[N];
+    int at[N];
+};
+
+// keep: bit j set if the row may read key j; looked at only if `masked`
 template <int FMT, int C, bool LISTED>
-__device__ __forceinline__ void add_tile(const Attend& a, Tile<C>& tile, Rows<C>& r, const float* ek, const float* ev, const int* at, bool masked, u32 keep) {
+__device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, Rows<C>& r, const Scales<LISTED>& x, bool masked, u32 keep) {
     float4_t s[2] = { { 0.f, 0.f, 0.f, 0.f }, { 0.f, 0.f, 0.f, 0.f } };
 #pragma unroll
     for (int h = 0; h < C; ++h) {
@@ -112,32 +138,41 @@ __device__ __forceinline__ void add_tile(const Attend& a, Tile<C>& tile, Rows<C>
             s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<FMT>(tile.k[b][h].z, tile.k[b][h].w), r.q[2 * h + 1], s[b], 0, 0, 0);
         }
     }
+    // t = score * log2 e + e of the values - offset, and the largest of them
     float t[8];
-    if (a.softcap > 0.f) {
-        // tanh(y) = 1 - 2 / (1 + e^(2 y))
-        const float in = 2.f * LOG2E * r.factor / a.softcap, cap = a.softcap * LOG2E;
+    const auto exponents = [&](float offset) {
+        if (a.softcap > 0.f) {
+            // tanh(y) = 1 - 2 / (1 + e^(2 y))
+            const float in = 2.f * LOG2E * r.factor / a.softcap, cap = a.softcap * LOG2E;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float z = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] * (in * ek[LISTED ? j : j >> 2]));
-            t[j] = cap - 2.f * cap * __builtin_amdgcn_rcpf(1.f + z);
+            for (int j = 0; j < 8; ++j) {
+                const int n = LISTED ? j : j >> 2;
+                const float z = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] * (in * x.ek[n]));
+                t[j] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + z), cap + (x.ev[n] - offset));
+            }
+        } else {
+            const float f = r.factor * LOG2E;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int n = LISTED ? j : j >> 2;
+                t[j] = __builtin_fmaf(s[j >> 2][j & 3], f * x.ek[n], x.ev[n] - offset);
+            }
         }
-    } else {
-        const float f = r.factor * LOG2E;
+        if (a.slopes) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = s[j >> 2][j & 3] * (f * ek[LISTED ? j : j >> 2]);
-    }
-    if (a.slopes) {
+            for (int j = 0; j < 8; ++j) t[j] -= r.slope * (float)(r.position - (LISTED ? x.at[LISTED ? j : 0] : x.at[j >> 2] + (j & 3)));
+        }
+        if (masked) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] -= r.slope * (float)(r.position - (LISTED ? at[j] : at[j >> 2] + (j & 3)));
-    }
-    float most = -INFINITY;
+            for (int j = 0; j < 8; ++j) t[j] = keep >> j & 1u ? t[j] : -INFINITY;
+        }
+        float most = fmaxf(t[0], t[1]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        t[j] += ev[LISTED ? j : j >> 2];
-        if (masked && !(keep >> j & 1u)) t[j] = -INFINITY;
-        most = fmaxf(most, t[j]);
-    }
-    if (__ballot(most > r.M + HEADROOM)) {
+        for (int j = 2; j < 8; ++j) most = fmaxf(most, t[j]);
+        return most;
+    };
+    if (__ballot(exponents(r.M) > HEADROOM)) {
+        float most = exponents(0.f);
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
         // rows that need not move stay as they are: a row's result does not depend on its neighbours in the tile
@@ -146,13 +181,20 @@ __device__ __forceinline__ void add_tile(const Attend& a, Tile<C>& tile, Rows<C>
 #pragma unroll
         for (int c = 0; c < 4 * C; ++c) r.acc[c] *= alpha;
         r.M = M;
+        exponents(M);
     }
     half8_t p;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float x = __builtin_amdgcn_exp2f(t[j] - r.M);
-        r.sum = __builtin_fmaf(x, power(-(int)ev[LISTED ? j : j >> 2]), r.sum);
-        p[j] = (_Float16)x;
+    for (int n = 0; n < Scales<LISTED>::N; ++n) {
+        constexpr int EACH = 8 / Scales<LISTED>::N;
+        float part = 0.f;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const float y = __builtin_amdgcn_exp2f(t[n * EACH + i]);
+            part = i ? part + y : y;
+            p[n * EACH + i] = (_Float16)y;
+        }
+        r.sum = __builtin_fmaf(part, x.down[n], r.sum);
     }
 #pragma unroll
     for (int w = 0; w < C; ++w) {
@@ -166,54 +208,64 @@ __device__ __forceinline__ void add_tile(const Attend& a, Tile<C>& tile, Rows<C>
     }
 }
 
-// Adds up the four waves' sums and writes the rows' results, or the piece's sums for the second kernel.  partial: null, or
-// [16] offsets, [16] sums, [16][width]
+// LDS traffic only: loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 template <int C>
-__device__ __forceinline__ void finish(const Attend& a, const Where& w, Rows<C>& r, float* lds, float* partial) {
-    constexpr u32 W = 64 * C, STRIDE = W + 4;
+struct Exchange {
+    static constexpr u32 STRIDE = 64 * C + 4;
+    float m[WAVES][ROWS], sum[WAVES][ROWS];
+    float acc[WAVES][ROWS][STRIDE];
+};
+
+// The four waves' sums, into LDS.  All waves call it; the rows are free afterwards.
+template <int C>
+__device__ __forceinline__ void exchange(const Rows<C>& r, Exchange<C>& x) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-    float* sh_m = lds;                           // [waves][16]
-    float* sh_s = lds + WAVES * ROWS;
-    float* sh_acc = lds + 2 * WAVES * ROWS;      // [waves][16][STRIDE]
     float sum = r.sum;
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (g == 0) {
-        sh_m[wave * ROWS + col] = r.M;
-        sh_s[wave * ROWS + col] = sum;
+        x.m[wave][col] = r.M;
+        x.sum[wave][col] = sum;
     }
-    __syncthreads();
-    float M = sh_m[col];
-#pragma unroll
-    for (u32 x = 1; x < WAVES; ++x) M = fmaxf(M, sh_m[x * ROWS + col]);
-    const float alpha = __builtin_amdgcn_exp2f(r.M - M);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int q = 0; q < C; ++q) {
-            float4 x;
-            x.x = r.acc[4 * q][i] * alpha; x.y = r.acc[4 * q + 1][i] * alpha; x.z = r.acc[4 * q + 2][i] * alpha; x.w = r.acc[4 * q + 3][i] * alpha;
-            *(float4*)(sh_acc + (wave * ROWS + col) * STRIDE + (4 * g + i) * 4 * C + 4 * q) = x;
-        }
+        for (int q = 0; q < C; ++q)
+            *(float4*)&x.acc[wave][col][(4 * g + i) * 4 * C + 4 * q] = make_float4(r.acc[4 * q][i], r.acc[4 * q + 1][i], r.acc[4 * q + 2][i], r.acc[4 * q + 3][i]);
     }
-    __syncthreads();
+    lds_barrier();
+}
+
+// Adds them up and writes the rows' results, or the piece's sums for the second kernel.  partial: null, or
+// [16] offsets, [16] sums, [16][width]
+template <int C>
+__device__ __forceinline__ void finish(const Attend& a, const Where& w, const Exchange<C>& x, float* partial) {
+    constexpr u32 W = 64 * C;
     // 16 threads a row, 4 C numbers each
     const u32 row = threadIdx.x >> 4, first = (threadIdx.x & 15) * 4 * C;
-    M = sh_m[row];
+    float M = x.m[0][row];
 #pragma unroll
-    for (u32 x = 1; x < WAVES; ++x) M = fmaxf(M, sh_m[x * ROWS + row]);
-    sum = 0.f;
-#pragma unroll
-    for (u32 x = 0; x < WAVES; ++x) sum += sh_s[x * ROWS + row] * __builtin_amdgcn_exp2f(sh_m[x * ROWS + row] - M);
-    float o[4 * C];
+    for (u32 v = 1; v < WAVES; ++v) M = fmaxf(M, x.m[v][row]);
+    float sum = 0.f, o[4 * C];
 #pragma unroll
     for (int n = 0; n < 4 * C; ++n) o[n] = 0.f;
 #pragma unroll
-    for (u32 x = 0; x < WAVES; ++x) {
+    for (u32 v = 0; v < WAVES; ++v) {
+        const float by = __builtin_amdgcn_exp2f(x.m[v][row] - M);
+        sum = __builtin_fmaf(x.sum[v][row], by, sum);
 #pragma unroll
         for (int q = 0; q < C; ++q) {
-            const float4 y = *(const float4*)(sh_acc + (x * ROWS + row) * STRIDE + first + 4 * q);
-            o[4 * q] += y.x; o[4 * q + 1] += y.y; o[4 * q + 2] += y.z; o[4 * q + 3] += y.w;
+            const float4 y = *(const float4*)&x.acc[v][row][first + 4 * q];
+            o[4 * q] = __builtin_fmaf(y.x, by, o[4 * q]);
+            o[4 * q + 1] = __builtin_fmaf(y.y, by, o[4 * q + 1]);
+            o[4 * q + 2] = __builtin_fmaf(y.z, by, o[4 * q + 2]);
+            o[4 * q + 3] = __builtin_fmaf(y.w, by, o[4 * q + 3]);
         }
     }
     if (partial) {
@@ -232,7 +284,7 @@ __device__ __forceinline__ void finish(const Attend& a, const Where& w, Rows<C>&
         }
         if (a.lse && first == 0) a.lse[(u64)t * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
     }
-    __syncthreads();
+    lds_barrier();
 }
 
 // ---- attention over all tokens --------------------------------------------------------------------------------------
@@ -252,7 +304,7 @@ __device__ __forceinline__ Request request_of(const Attend& a, u32 b) {
     return r;
 }
 
-__device__ __forceinline__ u64 units_of(const Attend& a, const Request& r) { return (u64)r.tiles * r.units * a.c.kv_heads; }
+__device__ __forceinline__ u64 units_of(const Attend& a, const Request& r) { return r.units ? (u64)r.tiles * (r.units + PIECE) * a.c.kv_heads : 0; }
 
 __device__ __forceinline__ void write_joined(const Attend& a, const Where& w, int2 j) {
     if (threadIdx.x < ROWS && w.row0 + threadIdx.x < w.rows) {
@@ -261,16 +313,22 @@ __device__ __forceinline__ void write_joined(const Attend& a, const Where& w, in
     }
 }
 
-template <int C>
-constexpr u32 lds_floats() { return 2 * WAVES * ROWS + WAVES * ROWS * (64 * C + 4); }
+// A piece of a workgroup's share: rows of a tile, keys start .. stop - 1.
+struct Piece {
+    Where w;
+    Span s;
+    u32 b, units, u0, u1;
+    int p0, p1, start, stop;
+    int last;                  // the workgroup that ends the tile
+};
 
 template <int FMT, int C>
-__global__ void __launch_bounds__(256) k_attend(Attend a) {
-    __shared__ __align__(16) float lds[lds_floats<C>()];
-    __shared__ u64 sh_sum[256 / 64];
+__global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend(Attend a) {
+    __shared__ __align__(16) Exchange<C> sh;
+    __shared__ u64 sh_sum[WAVES];
     __shared__ u64 sh_begin;
     __shared__ u32 sh_b;
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
 
     // this workgroup's share of all units
     const u32 per = (a.s.requests + 255) / 256, b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
@@ -285,7 +343,7 @@ __global__ void __launch_bounds__(256) k_attend(Attend a) {
     if (lane == 63) sh_sum[wave] = upto;
     __syncthreads();
     u64 total = 0;
-    for (u32 x = 0; x < 256 / 64; ++x) {
+    for (u32 x = 0; x < WAVES; ++x) {
         if (x < wave) upto += sh_sum[x];
         total += sh_sum[x];
     }
@@ -310,221 +368,345 @@ __global__ void __launch_bounds__(256) k_attend(Attend a) {
     write_padding(a);
     if (begin >= end) return;
     __syncthreads();
+
     u32 b = sh_b;
     u64 before = sh_begin, at = begin;
-
-    while (at < end) {
-        Request q = request_of(a, b);
-        u64 n = units_of(a, q);
-        while (at >= before + n) {
-            before += n;
-            ++b;
-            q = request_of(a, b);
-            n = units_of(a, q);
+    Request q = request_of(a, b);
+    u64 n = units_of(a, q);
+    const auto next_piece = [&](Piece& p) -> bool {
+        while (at < end) {
+            while (at >= before + n) {
+                before += n;
+                ++b;
+                q = request_of(a, b);
+                n = units_of(a, q);
+            }
+            const u32 cost = q.units + PIECE;
+            const u64 in = at - before;
+            const u32 part = (u32)divide(in, cost), c0 = (u32)(in - (u64)part * cost), c1 = (u32)min((u64)cost, c0 + (end - at));
+            at += c1 - c0;
+            // the units of a row tile come after the cost of beginning it
+            p.u0 = max(c0, PIECE) - PIECE;
+            p.u1 = max(c1, PIECE) - PIECE;
+            if (p.u0 == p.u1) continue;
+            p.s = q.s;
+            p.b = b;
+            p.units = q.units;
+            p.last = p.u0 == 0 && p.u1 < p.units ? (int)divide((before + (u64)(part + 1) * cost) * parts - 1, total) : -1;
+            p.w.t0 = q.s.t0;
+            p.w.rows = q.s.tokens * a.group;
+            p.w.row0 = part % q.tiles * ROWS;
+            p.w.kv_head = part / q.tiles;
+            p.w.head0 = p.w.kv_head * a.group;
+            p.p0 = q.s.first + (int)(p.w.row0 / a.group);
+            p.p1 = q.s.first + (int)(min(p.w.row0 + ROWS - 1, p.w.rows - 1) / a.group);
+            const int low = a.window ? max(0, p.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
+            p.start = (low & ~(int)(BLOCK - 1)) + (int)(p.u0 * UNIT);
+            p.stop = min(p.p1 + 1, p.start + (int)((p.u1 - p.u0) * UNIT));
+            return true;
         }
-        const u64 in = at - before;
-        const u32 u0 = (u32)(in % q.units), u1 = (u32)min((u64)q.units, u0 + (end - at));
-        Where w;
-        w.t0 = q.s.t0;
-        w.rows = q.s.tokens * a.group;
-        w.row0 = (u32)(in / q.units % q.tiles) * ROWS;
-        w.kv_head = (u32)(in / q.units / q.tiles);
-        w.head0 = w.kv_head * a.group;
-        const int p0 = q.s.first + (int)(w.row0 / a.group), p1 = q.s.first + (int)(min(w.row0 + ROWS - 1, w.rows - 1) / a.group);
-        const int low = a.window ? max(0, p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
-        const int start = (low & ~(int)(BLOCK - 1)) + (int)(u0 * UNIT), stop = min(p1 + 1, start + (int)((u1 - u0) * UNIT));
+        return false;
+    };
 
-        Rows<C> rows;
-        load_rows<C>(a, w, q.s.first, rows);
-        const u32 col = lane & 15, g = lane >> 4;
-        const int32_t* table = a.s.table + b * a.s.table_stride;
-        // 64 blocks of this wave's tiles at a time: lane 2 i + s has block s of tile i
-        for (int from = start + (int)(wave * TILE); from < stop; from += 32 * (int)UNIT) {
-            const int mine_at = from + (int)(lane >> 1) * (int)UNIT + (int)(lane & 1) * (int)BLOCK;
-            u32 block_row = 0;
-            int ek_mine = 0, ev_mine = 0;
-            bool ok = false;
-            if (mine_at < stop) {
-                const u32 blk = (u32)mine_at / BLOCK, page = (u32)table[blk / a.c.page_blocks];
-                if (page < a.c.num_pages) {
-                    ok = true;
-                    block_row = row_of(a.c, page, w.kv_head, blk % a.c.page_blocks * BLOCK);
-                    const int8_t* e = a.c.exponents + (u64)(block_row / BLOCK) * 2;
-                    ek_mine = e[0];
-                    ev_mine = e[1];
+    Piece p;
+    Rows<C> rows;
+    RawRows<C> raw;
+    Tile<C> even, odd;
+    // 64 blocks of this wave's tiles at a time: lane 2 i + s has block s of tile i
+    const int mine_at = (int)(lane >> 1) * (int)UNIT + (int)(lane & 1) * (int)BLOCK;
+    int from = 0;
+    u32 page = 0, block_row = 0;
+    uint16_t exponents = 0;
+    u64 there = 0;
+    const auto page_of = [&](int at_key) -> u32 {
+        return at_key < p.stop ? (u32)a.s.table[p.b * a.s.table_stride + (u32)at_key / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
+    };
+    const auto ask = [&]() {                  // what does not depend on each other is asked for together: pages and rows,
+        from = p.start + (int)(wave * TILE);
+        page = page_of(from + mine_at);
+        fetch_rows<C>(a, p.w, raw);
+    };
+    const auto look_up = [&]() {              // then exponents and the first tile
+        const bool ok = page < a.c.num_pages;
+        block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)(from + mine_at) / BLOCK % a.c.page_blocks * BLOCK) : 0;
+        exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
+        there = __ballot(ok);
+        page = page_of(from + 32 * (int)UNIT + mine_at);
+    };
+    const u32 k_at = col * (128 * C) + g * 16, v_at = 4 * g * (128 * C) + 64 * C + col * (4 * C);
+    const auto load = [&](Tile<C>& tile, int i) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint8_t* rows_at = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s) * (128 * C);
+#pragma unroll
+            for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(rows_at + k_at + h * 64);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) load_words<C>(rows_at + v_at + j * (128 * C), tile.v[4 * s + j]);
+        }
+    };
+    const auto add = [&](Tile<C>& tile, int i) {
+        const int pos = from + i * (int)UNIT;
+        Scales<false> x;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int e = __builtin_amdgcn_readlane((int)exponents, 2 * i + s), ev = (int)(int8_t)(e >> 8);
+            x.ek[s] = power((int)(int8_t)e);
+            x.ev[s] = (float)ev;
+            x.down[s] = power(-ev);
+            x.at[s] = pos + s * (int)BLOCK + 4 * (int)g;
+        }
+        const u32 two = (u32)(there >> (2 * i)) & 3u;
+        const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos <= p.p1 - (int)min(a.window - 1, 0x7FFFFFFEu) - 1;
+        u32 keep = 0xFF;
+        if (masked) {
+            keep = 0;
+            const int oldest = a.window ? max(0, rows.position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = x.at[j >> 2] + (j & 3);
+                const bool exists = (two >> (j >> 2) & 1u) && k < p.stop;
+                if (exists && k <= rows.position && k >= oldest) keep |= 1u << j;
+                if (!exists) {
+#pragma unroll
+                    for (int y = 0; y < C; ++y) tile.v[j][y] = 0;      // the memory behind the last token may hold anything
                 }
             }
-            const u64 there = __ballot(ok);
-            const int count = min(32, (stop - from + (int)UNIT - 1) / (int)UNIT);
-            for (int i = 0; i < count; ++i) {
-                const int pos = from + i * (int)UNIT;
-                Tile<C> tile;
-                float ek[2], ev[2];
-                int where[2];
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const uint8_t* rows_at = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s) * (2 * a.c.width);
-                    ek[s] = power(__builtin_amdgcn_readlane(ek_mine, 2 * i + s));
-                    ev[s] = (float)__builtin_amdgcn_readlane(ev_mine, 2 * i + s);
-                    where[s] = pos + s * (int)BLOCK + 4 * (int)g;
-#pragma unroll
-                    for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(rows_at + col * (128 * C) + h * 64 + g * 16);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) load_words<C>(rows_at + (4 * g + j) * (128 * C) + 64 * C + col * (4 * C), tile.v[4 * s + j]);
+        }
+        add_tile<FMT, C, false>(a, tile, rows, x, masked, keep);
+    };
+
+    bool more = next_piece(p);
+    if (more) {
+        ask();
+        if (from < p.stop) {
+            look_up();
+            load(even, 0);
+        }
+    }
+    while (more) {
+        start_rows<C>(a, p.w, p.s.first, raw, rows);
+        while (from < p.stop) {
+            // a tile is on its way while the one before it is added; behind the last one the last is asked for again, which the cache has
+            const int count = min(32, (p.stop - from + (int)UNIT - 1) / (int)UNIT);
+            for (int i = 0; i < count; i += 2) {
+                load(odd, min(i + 1, count - 1));
+                add(even, i);
+                if (i + 1 < count) {
+                    load(even, min(i + 2, count - 1));
+                    add(odd, i + 1);
                 }
-                const u32 two = (u32)(there >> (2 * i)) & 3u;
-                const bool masked = two != 3u || pos + (int)TILE > p0 + 1 || pos <= p1 - (int)min(a.window - 1, 0x7FFFFFFEu) - 1;
-                u32 keep = 0xFF;
-                if (masked) {
-                    keep = 0;
-                    const int oldest = a.window ? max(0, rows.position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int p = where[j >> 2] + (j & 3);
-                        const bool exists = (two >> (j >> 2) & 1u) && p < stop;
-                        if (exists && p <= rows.position && p >= oldest) keep |= 1u << j;
-                        if (!exists) {
-#pragma unroll
-                            for (int x = 0; x < C; ++x) tile.v[j][x] = 0;      // the memory behind the last token may hold anything
-                        }
-                    }
-                }
-                add_tile<FMT, C, false>(a, tile, rows, ek, ev, where, masked, keep);
+            }
+            from += 32 * (int)UNIT;
+            if (from < p.stop) {
+                look_up();
+                load(even, 0);
             }
         }
-        const bool begun = u0 == 0, ended = u1 == q.units;
-        float* partial = nullptr;
-        if (!begun || !ended) partial = a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2));
-        if (begun) {
-            int2 j = make_int2(-1, -1);
-            if (!ended) j = make_int2((int)blockIdx.x, (int)(((at + q.units) * parts - 1) / total));     // the workgroup of unit at + q.units - 1
-            write_joined(a, w, j);
+        // the next piece's first tile is on its way while this one's waves are added up
+        const Where w = p.w;
+        const bool begun = p.u0 == 0, ended = p.u1 == p.units;
+        float* partial = !begun || !ended ? a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2)) : nullptr;
+        if (begun) write_joined(a, w, p.last >= 0 ? make_int2((int)blockIdx.x, p.last) : make_int2(-1, -1));
+        more = next_piece(p);
+        if (more) ask();
+        exchange<C>(rows, sh);
+        if (more && from < p.stop) {
+            look_up();
+            load(even, 0);
         }
-        finish<C>(a, w, rows, lds, partial);
-        at += u1 - u0;
+        finish<C>(a, w, sh, partial);
     }
 }
 
 // ---- attention over listed tokens -----------------------------------------------------------------------------------
 
+// what a wave knows of 64 keys that it will add or is adding
+struct Entries {
+    u32 row[64];
+    float ek[64], ev[64], down[64];
+    int at[64];
+};
+
 template <int FMT, int C>
-__global__ void __launch_bounds__(256) k_attend_selected(Attend a, u32 units, u32 tiles) {
-    __shared__ __align__(16) float lds[lds_floats<C>()];
-    __shared__ uint4 sh_entry[WAVES][64];        // row, exponents of key and value, position, found
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const u64 total = (u64)a.s.tokens * a.id_heads * tiles * units;
+__global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(Attend a, u32 units, u32 tiles) {
+    __shared__ __align__(16) Exchange<C> sh;
+    __shared__ __align__(16) Entries sh_entries[WAVES][2];
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const u32 cost = units + PIECE;
+    const u64 total = (u64)a.s.tokens * a.id_heads * tiles * cost;
     const u32 parts = (u32)min((u64)gridDim.x, total);
     if (blockIdx.x >= parts) return;
     u64 at = share(total, parts, blockIdx.x);
     const u64 end = share(total, parts, blockIdx.x + 1);
     const u32 entries = a.k + a.window;
 
-    while (at < end) {
-        const u32 u0 = (u32)(at % units), u1 = (u32)min((u64)units, u0 + (end - at));
-        const u64 list = at / units / tiles;
-        const u32 t = (u32)(list / a.id_heads), id_head = (u32)(list % a.id_heads);
-        Where w;
-        w.t0 = t;
-        w.rows = a.group;
-        w.row0 = (u32)(at / units % tiles) * ROWS;
-        w.head0 = id_head * a.group;
-        w.kv_head = (u32)((u64)id_head * a.c.kv_heads / a.id_heads);
-        const int request = a.s.request[t];
-        int position = a.s.positions[t];
+    Where w;
+    u32 t = 0, id_head = 0, u0 = 0, u1 = 0;
+    int last = -1;
+    const auto next_piece = [&]() -> bool {
+        while (at < end) {
+            const u64 part = divide(at, cost), list = divide(part, tiles);
+            const u32 c0 = (u32)(at - part * cost), c1 = (u32)min((u64)cost, c0 + (end - at));
+            at += c1 - c0;
+            u0 = max(c0, PIECE) - PIECE;
+            u1 = max(c1, PIECE) - PIECE;
+            if (u0 == u1) continue;
+            last = u0 == 0 && u1 < units ? (int)divide((part + 1) * cost * parts - 1, total) : -1;
+            t = (u32)divide(list, a.id_heads);
+            id_head = (u32)(list - (u64)t * a.id_heads);
+            w.t0 = t;
+            w.rows = a.group;
+            w.row0 = (u32)(part - list * tiles) * ROWS;
+            w.head0 = id_head * a.group;
+            w.kv_head = id_head / (a.id_heads / a.c.kv_heads);
+            return true;
+        }
+        return false;
+    };
+
+    Rows<C> rows;
+    RawRows<C> raw;
+    Tile<C> even, odd;
+    u32 from = 0, stop = 0;                      // this wave's next entries
+    int request = -1, position = -1;
+    int64_t id = -1;                             // of the entries two batches on,
+    int key = -1;                                // the positions and pages of the next one
+    u32 page = 0;
+    u64 there = 0;                               // which of this batch are keys
+    const u32 mine = (lane & 31) + (lane >> 5) * UNIT;
+    const auto id_of = [&](u32 n) -> int64_t { return n < a.k && n < stop ? a.ids[(int64_t)t * a.ids_ts + (int64_t)id_head * a.ids_hs + n] : -1; };
+    const auto key_of = [&](u32 n) {             // from id
+        int64_t k = id;
+        if (n >= a.k) k = (int64_t)position - (int64_t)(n - a.k);
+        else if (k > (int64_t)position - (int64_t)a.window) k = -1;
+        key = n < stop && position >= 0 && k >= 0 ? (int)k : -1;
+        page = key >= 0 ? (u32)a.s.table[(u64)(u32)request * a.s.table_stride + (u32)key / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
+    };
+    const auto ask = [&]() {
+        from = u0 * UNIT + wave * TILE;
+        stop = min(entries, u1 * UNIT);
+        id = id_of(from + mine);
+        request = a.s.request[t];
+        position = a.s.positions[t];
+        fetch_rows<C>(a, w, raw);
+    };
+    const auto check = [&]() {
         if (request < 0 || (u32)request >= a.s.requests || (u64)(u32)max(position, 0) >= (u64)a.s.max_pages * a.c.page_tokens) position = -1;
-        const int32_t* table = a.s.table + (u64)(u32)max(position < 0 ? 0 : request, 0) * a.s.table_stride;
-        const int64_t* ids = a.ids + (int64_t)t * a.ids_ts + (int64_t)id_head * a.ids_hs;
-        Rows<C> rows;
-        load_rows<C>(a, w, position, rows);
-        const u32 col = lane & 15, g = lane >> 4;
-        const u32 start = u0 * UNIT, stop = min(entries, u1 * UNIT);
-        for (u32 from = start + wave * TILE; from < stop; from += 2 * UNIT) {
-            // 64 entries, two tiles
-            const u32 n = from + (lane & 31) + (lane >> 5) * UNIT;
-            uint4 entry = make_uint4(0, 0, 0, 0);
-            if (n < stop && position >= 0) {
-                int64_t p = n < a.k ? ids[n] : (int64_t)position - (int64_t)(n - a.k);
-                if (n < a.k && p > (int64_t)position - (int64_t)a.window) p = -1;
-                if (p >= 0) {
-                    const u32 blk = (u32)p / BLOCK, page = (u32)table[blk / a.c.page_blocks];
-                    if (page < a.c.num_pages) {
-                        entry.x = row_of(a.c, page, w.kv_head, blk % a.c.page_blocks * BLOCK + ((u32)p & (BLOCK - 1)));
-                        const int8_t* e = a.c.exponents + (u64)(entry.x / BLOCK) * 2;
-                        entry.y = (u32)(uint8_t)e[0] | (u32)(uint8_t)e[1] << 8;
-                        entry.z = (u32)p;
-                        entry.w = 1;
-                    }
-                }
-            }
-            const u64 there = __ballot(entry.w != 0);
-            sh_entry[wave][lane] = entry;
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const u32 found = (u32)(there >> (32 * i));
-                if (!found) continue;
-                Tile<C> tile;
-                float ek[8], ev[8];
-                int where[8];
-                u32 keep = 0;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const u32 row = sh_entry[wave][32 * i + 16 * s + col].x;
-                    const uint8_t* p = a.c.data + (u64)row * (2 * a.c.width) + g * 16;
-#pragma unroll
-                    for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(p + h * 64);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint4 x = sh_entry[wave][32 * i + 16 * s + 4 * g + j];
-                        load_words<C>(a.c.data + (u64)x.x * (2 * a.c.width) + 64 * C + col * (4 * C), tile.v[4 * s + j]);
-                        ek[4 * s + j] = power((int8_t)x.y);
-                        ev[4 * s + j] = (float)(int8_t)(x.y >> 8);
-                        where[4 * s + j] = (int)x.z;
-                        keep |= x.w << (4 * s + j);
-                    }
-                }
-                const bool masked = found != 0xFFFFFFFFu;
-                if (masked) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        if (!(keep >> j & 1u)) {
-#pragma unroll
-                            for (int x = 0; x < C; ++x) tile.v[j][x] = 0;
-                        }
-                    }
-                }
-                add_tile<FMT, C, true>(a, tile, rows, ek, ev, where, masked, keep);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+    };
+    // the 64 entries whose pages have been asked for, into LDS; the pages of the next and the ids after those are asked for
+    const auto look_up = [&](u32 buffer) {
+        Entries& x = sh_entries[wave][buffer];
+        const bool ok = page < a.c.num_pages;
+        const u32 row = ok ? row_of(a.c, page, w.kv_head, (u32)key / BLOCK % a.c.page_blocks * BLOCK + ((u32)key & (BLOCK - 1))) : 0;
+        const u32 e = ok ? *(const uint16_t*)(a.c.exponents + (u64)(row / BLOCK) * 2) : 0;
+        there = __ballot(ok);
+        x.row[lane] = row;
+        x.at[lane] = key;
+        const u32 next = from + 2 * UNIT + mine;
+        if (from + 2 * UNIT < stop) {
+            key_of(next);
+            id = id_of(next + 2 * UNIT);
         }
+        const int ev = (int)(int8_t)(e >> 8);
+        x.ek[lane] = power((int)(int8_t)e);
+        x.ev[lane] = (float)ev;
+        x.down[lane] = power(-ev);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    const auto load = [&](Tile<C>& tile, u32 buffer, int i) {
+        const Entries& x = sh_entries[wave][buffer];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint8_t* k = a.c.data + (u64)x.row[32 * i + 16 * s + col] * (128 * C) + g * 16;
+            const uint4 r = *(const uint4*)&x.row[32 * i + 16 * s + 4 * g];
+            const u32 v[4] = { r.x, r.y, r.z, r.w };
+#pragma unroll
+            for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(k + h * 64);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) load_words<C>(a.c.data + (u64)v[j] * (128 * C) + 64 * C + col * (4 * C), tile.v[4 * s + j]);
+        }
+    };
+    const auto add = [&](Tile<C>& tile, u32 buffer, int i, u32 found) {
+        const Entries& x = sh_entries[wave][buffer];
+        Scales<true> scales;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const u32 at0 = 32 * i + 16 * s + 4 * g;
+            const float4 ek = *(const float4*)&x.ek[at0], ev = *(const float4*)&x.ev[at0], down = *(const float4*)&x.down[at0];
+            const int4 pos = *(const int4*)&x.at[at0];
+            scales.ek[4 * s] = ek.x; scales.ek[4 * s + 1] = ek.y; scales.ek[4 * s + 2] = ek.z; scales.ek[4 * s + 3] = ek.w;
+            scales.ev[4 * s] = ev.x; scales.ev[4 * s + 1] = ev.y; scales.ev[4 * s + 2] = ev.z; scales.ev[4 * s + 3] = ev.w;
+            scales.down[4 * s] = down.x; scales.down[4 * s + 1] = down.y; scales.down[4 * s + 2] = down.z; scales.down[4 * s + 3] = down.w;
+            scales.at[4 * s] = pos.x; scales.at[4 * s + 1] = pos.y; scales.at[4 * s + 2] = pos.z; scales.at[4 * s + 3] = pos.w;
+        }
+        const bool masked = found != 0xFFFFFFFFu;
+        const u32 keep = (found >> (4 * g) & 15u) | (found >> (16 + 4 * g) & 15u) << 4;
+        if (masked) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (!(keep >> j & 1u)) {
+#pragma unroll
+                    for (int y = 0; y < C; ++y) tile.v[j][y] = 0;
+                }
+            }
+        }
+        add_tile<FMT, C, true>(a, tile, rows, scales, masked, keep);
+    };
+    u32 buffer = 0;
+    const auto begin_piece = [&]() {
+        check();
+        key_of(from + mine);
+        id = id_of(from + 2 * UNIT + mine);
+        look_up(buffer);
+        load(even, buffer, 0);
+    };
+
+    bool more = next_piece();
+    if (more) {
+        ask();
+        if (from < stop) begin_piece();
+    }
+    while (more) {
+        start_rows<C>(a, w, position, raw, rows);
+        while (from < stop) {
+            const u32 lo = (u32)there, hi = (u32)(there >> 32), now = buffer;
+            load(odd, now, 1);
+            if (lo) add(even, now, 0, lo);
+            from += 2 * UNIT;
+            if (from < stop) {
+                buffer ^= 1;
+                look_up(buffer);
+                load(even, buffer, 0);
+            }
+            if (hi) add(odd, now, 1, hi);
+        }
+        const Where done = w;
         const bool begun = u0 == 0, ended = u1 == units;
-        float* partial = nullptr;
-        if (!begun || !ended) partial = a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2));
-        if (begun) {
-            int2 j = make_int2(-1, -1);
-            if (!ended) j = make_int2((int)blockIdx.x, (int)(((at + units) * parts - 1) / total));
-            write_joined(a, w, j);
-        }
-        finish<C>(a, w, rows, lds, partial);
-        at += u1 - u0;
+        float* partial = !begun || !ended ? a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2)) : nullptr;
+        if (begun) write_joined(a, done, last >= 0 ? make_int2((int)blockIdx.x, last) : make_int2(-1, -1));
+        more = next_piece();
+        if (more) ask();
+        exchange<C>(rows, sh);
+        if (more && from < stop) begin_piece();
+        finish<C>(a, done, sh, partial);
     }
 }
 
 // ---- joining --------------------------------------------------------------------------------------------------------
 
-// A workgroup for each token and head; if its keys went to several workgroups, its waves take every fourth of their pieces.
+// A workgroup for each token and head; if its keys went to several workgroups, its threads look at their pieces' offsets first, and then
+// each wave adds up every fourth piece, eight of them asked for at a time.
 template <int C>
-__global__ void __launch_bounds__(256) k_join(Attend a, bool listed, int groups) {
-    __shared__ float sh_m[4], sh_s[4];
+__global__ void __launch_bounds__(256) k_join(Attend a, int groups) {
+    __shared__ float sh_max[4], sh_by[256], sh_sum[4];
     __shared__ float sh_acc[4][64 * C];
     const u32 t = blockIdx.x / a.heads, head = blockIdx.x % a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int2 j = a.joined[(u64)t * a.heads + head];
     if (j.x < 0 || j.y < j.x || j.y >= groups) return;
     u32 row = head % a.group;
-    if (!listed) {
+    if (!a.listed) {
         // number of the token in its request
         u32 lo = 0, hi = a.s.requests;
         while (hi - lo > 1) {
@@ -535,44 +717,60 @@ __global__ void __launch_bounds__(256) k_join(Attend a, bool listed, int groups)
     }
     row %= ROWS;
     constexpr u32 SLOT = ROWS * (64 * C + 2);
-    float M = LOWEST, sum = 0.f, acc[C];
+    const int pieces = j.y - j.x + 1;
+    const auto piece = [&](int i) { return a.partial + (2 * (u64)(j.x + i) + (i == 0 ? 1 : 0)) * SLOT; };
+    float top = LOWEST;
+    for (int i = (int)threadIdx.x; i < pieces; i += 256) top = fmaxf(top, piece(i)[row]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) sh_max[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(sh_max[0], sh_max[1]), fmaxf(sh_max[2], sh_max[3]));
+    float sum = 0.f, acc[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) acc[c] = 0.f;
-    for (int wg = j.x + (int)wave; wg <= j.y; wg += 4) {
-        const float* p = a.partial + (2 * (u64)wg + (wg == j.x ? 1 : 0)) * SLOT;
-        const float m = p[row], s = p[ROWS + row], top = fmaxf(M, m);
-        const float was = __builtin_amdgcn_exp2f(M - top), is = __builtin_amdgcn_exp2f(m - top);
-        sum = sum * was + s * is;
+    for (int first = 0; first < pieces; first += 256) {
+        const int n = min(256, pieces - first);
+        __syncthreads();
+        if ((int)threadIdx.x < n) {
+            const float* p = piece(first + (int)threadIdx.x);
+            const float by = __builtin_amdgcn_exp2f(p[row] - top);
+            sh_by[threadIdx.x] = by;
+            sum = __builtin_fmaf(p[ROWS + row], by, sum);
+        }
+        __syncthreads();
+        for (int i = (int)wave; i < n; i += 32) {
+            float x[8][C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) acc[c] = acc[c] * was + p[2 * ROWS + row * (64 * C) + c * 64 + lane] * is;
-        M = top;
+            for (int u = 0; u < 8; ++u) {
+                const float* p = piece(first + min(i + 4 * u, n - 1)) + 2 * ROWS + row * (64 * C) + lane * C;
+#pragma unroll
+                for (int c = 0; c < C; ++c) x[u][c] = p[c];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float by = i + 4 * u < n ? sh_by[i + 4 * u] : 0.f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) acc[c] = i + 4 * u < n ? __builtin_fmaf(x[u][c], by, acc[c]) : acc[c];
+            }
+        }
     }
-    if (lane == 0) { sh_m[wave] = M; sh_s[wave] = sum; }
 #pragma unroll
-    for (int c = 0; c < C; ++c) sh_acc[wave][c * 64 + lane] = acc[c];
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) sh_sum[wave] = sum;
+#pragma unroll
+    for (int c = 0; c < C; ++c) sh_acc[wave][lane * C + c] = acc[c];
     __syncthreads();
-    const float top = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
-    float f[4], all = 0.f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        f[x] = __builtin_amdgcn_exp2f(sh_m[x] - top);
-        all += sh_s[x] * f[x];
-    }
+    const float all = sh_sum[0] + sh_sum[1] + sh_sum[2] + sh_sum[3];
     const u32 d = threadIdx.x * 2;
     if (d < a.c.dim) {
-        float o[2] = { 0.f, 0.f };
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            o[0] += sh_acc[x][d] * f[x];
-            o[1] += sh_acc[x][d + 1] * f[x];
-        }
         const float by = all != 0.f ? 1.f / all : 0.f;
-        *(u32*)((uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + d) = pack2(o[0] * by, o[1] * by, a.dtype);
+        const float x = sh_acc[0][d] + sh_acc[1][d] + sh_acc[2][d] + sh_acc[3][d], y = sh_acc[0][d + 1] + sh_acc[1][d + 1] + sh_acc[2][d + 1] + sh_acc[3][d + 1];
+        *(u32*)((uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + d) = pack2(x * by, y * by, a.dtype);
     }
     if (a.lse && threadIdx.x == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }
 
-constexpr u32 groups_per_cu(u32 width) { return width <= 128 ? 3 : 2; }
 u64 partial_floats(u32 width, int num_cu) { return 2ull * (u32)num_cu * groups_per_cu(width) * ROWS * (width + 2); }
 
 template <int FMT, int C>
@@ -584,7 +782,7 @@ void run_attend(hipStream_t st, const Attend& a, int num_cu) {
     } else {
         k_attend<FMT, C><<<grid, 256, 0, st>>>(a);
     }
-    k_join<C><<<a.s.tokens * a.heads, 256, 0, st>>>(a, a.listed != 0, (int)grid);
+    k_join<C><<<a.s.tokens * a.heads, 256, 0, st>>>(a, (int)grid);
 }
 
 }  // namespace
