@@ -413,6 +413,8 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
                 int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride, void* stream);
 
 /*
+ * pag_kv_workspace_bytes: the workspace of such a call of pag_kv_attend (selected = 0, id_heads and k are not looked at) or pag_kv_attend_selected;
+ * often 0, then args->workspace may be null.  Of args it reads dtype, heads and window.
  * pag_kv_attend: every token of the step attends to the tokens of its request up to itself: out = sum softmax(score) v.
  * pag_kv_attend_selected: it attends to the last `window` tokens and to the tokens whose positions ids lists (dev int64
  * [tokens][id_heads][k], strides in elements, last dimension dense): id_heads is kv_heads (the heads of a group share a list), heads, or a
@@ -421,7 +423,8 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
  * A token that finds nothing to attend to gets zeros and an lse of -inf; so does padding.
  * Sums, maxima and scores are held in 32 bits; softmax weights are rounded to 16-bit floats for their product with the values.
  */
-uint64_t pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, uint32_t heads);   /* 0: wrong arguments, or no GPU */
+int pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, int selected, uint32_t id_heads,
+                           uint32_t k, uint64_t* bytes);
 int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, void* stream);
 int pag_kv_attend_selected(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, const int64_t* ids,
                            int64_t ids_token_stride, int64_t ids_head_stride, uint32_t id_heads, uint32_t k, void* stream);

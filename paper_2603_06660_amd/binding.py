@@ -74,7 +74,6 @@ def load_library():
                            "(or __graft_entry__.build())")
         lib = C.CDLL(_LIB_PATH)
         lib.pag_last_error.restype = C.c_char_p
-        lib.pag_kv_workspace_bytes.restype = C.c_uint64
         for name in EXPORTED_SYMBOLS:
             getattr(lib, name)
         _lib = lib

@@ -141,7 +141,7 @@ int launch_attend(hipStream_t st, const Attend& a, int num_cu);
 
 int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu);
 
-u64 narrow_workspace(u32 width, u64 rows, int num_cu);      // bytes
+u64 narrow_workspace(const Attend& a, int num_cu);      // bytes
 u64 wide_workspace(u32 width, int num_cu);
 int num_cu_of_current();                        // < 0: no GPU
 

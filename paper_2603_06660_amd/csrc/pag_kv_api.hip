@@ -72,7 +72,8 @@ int check_rows(const void* p, int64_t token_stride, int64_t head_stride, u32 byt
     return PAG_OK;
 }
 
-int attend_common(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, Attend* a, int* num_cu) {
+// What decides how a call is laid out: everything but its arrays.
+int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, bool selected, uint32_t id_heads, uint32_t k, Attend* a) {
     int rc;
     if ((rc = cache_of(cache, &a->c)) || (rc = check_step(step))) return rc;
     PAG_CHECK(args != nullptr, PAG_EINVAL, "args is null");
@@ -80,25 +81,46 @@ int attend_common(const pag_kv_cache* cache, const pag_kv_step* step, const pag_
     PAG_CHECK(args->dtype == PAG_F16 || args->dtype == PAG_BF16, PAG_EUNSUPPORTED, "attention takes PAG_F16 or PAG_BF16");
     PAG_CHECK(args->heads > 0 && args->heads <= 65536 && args->heads % a->c.kv_heads == 0, PAG_EINVAL, "heads must be a multiple of kv_heads, at most 65536");
     PAG_CHECK((u64)step->max_pages * a->c.page_tokens <= 0x7FFF0000ull, PAG_EUNSUPPORTED, "requests of more than 2^31 - 2^16 tokens are not built");
-    PAG_CHECK(step->tokens * args->heads < (1ull << 31), PAG_EUNSUPPORTED, "tokens * heads must be below 2^31");
+    PAG_CHECK(step->tokens * args->heads < (1ull << 31) && (u64)step->requests * a->c.kv_heads < (1ull << 31), PAG_EUNSUPPORTED,
+              "tokens * heads and requests * kv_heads must be below 2^31");
+    a->s = Step{ step->table, step->offsets, step->context, step->request, step->positions, step->table_stride, step->requests, step->max_pages, (u32)step->tokens };
+    a->heads = args->heads;
+    a->dtype = args->dtype;
+    a->window = args->window;
+    a->group = a->heads / a->c.kv_heads;
+    if (selected) {
+        PAG_CHECK(id_heads > 0 && id_heads % a->c.kv_heads == 0 && args->heads % id_heads == 0, PAG_EINVAL, "id_heads must be a multiple of kv_heads that divides heads");
+        PAG_CHECK((u64)k + args->window < (1ull << 30), PAG_EUNSUPPORTED, "k + window must be below 2^30");
+        a->listed = 1;
+        a->id_heads = id_heads;
+        a->k = k;
+        a->group = a->heads / id_heads;
+    }
+    return PAG_OK;
+}
+
+u64 workspace_of(const Attend& a, const pag_kv_step* step, int num_cu) {
+    return !a.listed && many_rows(step, a.group) ? wide_workspace(a.c.width, num_cu) : narrow_workspace(a, num_cu);
+}
+
+int arrays_of(const pag_kv_step* step, const pag_kv_attention* args, Attend* a, int* num_cu) {
     PAG_CHECK(std::isfinite(args->scale) && std::isfinite(args->softcap) && args->softcap >= 0.f, PAG_EINVAL, "scale and softcap must be finite, softcap not negative");
     if (step->tokens == 0) return PAG_OK;
+    int rc;
     PAG_CHECK(args->q != nullptr && args->out != nullptr, PAG_EINVAL, "q or out is null");
     if ((rc = check_rows(args->q, args->q_token_stride, args->q_head_stride, 2, 16, "q must be 16-byte aligned, its strides multiples of 8 elements"))) return rc;
     if ((rc = check_rows(args->out, args->out_token_stride, args->out_head_stride, 2, 16, "out must be 16-byte aligned, its strides multiples of 8 elements"))) return rc;
     PAG_CHECK((args->slopes == nullptr || aligned(args->slopes, 4)) && (args->lse == nullptr || aligned(args->lse, 4)), PAG_EINVAL, "slopes and lse must be 4-byte aligned");
-    PAG_CHECK(args->workspace != nullptr && aligned(args->workspace, 16), PAG_EINVAL, "workspace is null or not 16-byte aligned");
-    PAG_CHECK(args->workspace_bytes >= pag_kv_workspace_bytes(cache, step, args->heads), PAG_EINVAL, "workspace is smaller than pag_kv_workspace_bytes");
+    PAG_CHECK(aligned(args->workspace, 16) && (args->workspace != nullptr || args->workspace_bytes == 0), PAG_EINVAL,
+              "workspace is null but has a size, or is not 16-byte aligned");
     *num_cu = num_cu_of_current();
     PAG_CHECK(*num_cu > 0, PAG_EHIP, "no current GPU");
-    a->s = Step{ step->table, step->offsets, step->context, step->request, step->positions, step->table_stride, step->requests, step->max_pages, (u32)step->tokens };
+    const u64 need = workspace_of(*a, step, *num_cu);
+    PAG_CHECK(need == 0 || (args->workspace != nullptr && args->workspace_bytes >= need), PAG_EINVAL, "workspace is null or smaller than pag_kv_workspace_bytes");
     a->q = args->q; a->q_ts = args->q_token_stride; a->q_hs = args->q_head_stride;
     a->out = args->out; a->o_ts = args->out_token_stride; a->o_hs = args->out_head_stride;
     a->lse = args->lse;
     a->slopes = args->slopes;
-    a->heads = args->heads;
-    a->dtype = args->dtype;
-    a->window = args->window;
     a->scale = args->scale;
     a->softcap = args->softcap;
     a->partial = (float*)args->workspace;
@@ -166,23 +188,26 @@ extern "C" int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint
     });
 }
 
-extern "C" uint64_t pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, uint32_t heads) {
-    if (!cache || !step || cache->head_dim == 0 || cache->head_dim > 256 || cache->kv_heads == 0 || step->requests == 0) return 0;
-    const int num_cu = num_cu_of_current();
-    if (num_cu <= 0) return 0;
-    const u32 width = (cache->head_dim + 63) / 64 * 64;
-    const u64 narrow = narrow_workspace(width, step->tokens * heads, num_cu);
-    return many_rows(step, heads / cache->kv_heads) ? std::max(narrow, wide_workspace(width, num_cu)) : narrow;
+extern "C" int pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, int selected, uint32_t id_heads, uint32_t k,
+                                      uint64_t* bytes) {
+    return guarded("pag_kv_workspace_bytes", [&]() -> int {
+        Attend a = {};
+        const int rc = layout_of(cache, step, args, selected != 0, id_heads, k, &a);
+        if (rc) return rc;
+        PAG_CHECK(bytes != nullptr, PAG_EINVAL, "bytes is null");
+        const int num_cu = num_cu_of_current();
+        PAG_CHECK(num_cu > 0, PAG_EHIP, "no current GPU");
+        *bytes = workspace_of(a, step, num_cu);
+        return PAG_OK;
+    });
 }
 
 extern "C" int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, void* stream) {
     return guarded("pag_kv_attend", [&]() -> int {
         Attend a = {};
-        int num_cu = 0;
-        const int rc = attend_common(cache, step, args, &a, &num_cu);
-        if (rc || step->tokens == 0) return rc;
+        int num_cu = 0, rc;
+        if ((rc = layout_of(cache, step, args, false, 0, 0, &a)) || (rc = arrays_of(step, args, &a, &num_cu)) || step->tokens == 0) return rc;
         PAG_CHECK(step->offsets && step->context, PAG_EINVAL, "step: offsets or context is null");
-        a.group = a.heads / a.c.kv_heads;
         return many_rows(step, a.group) ? launch_attend_wide((hipStream_t)stream, a, num_cu) : launch_attend((hipStream_t)stream, a, num_cu);
     });
 }
@@ -191,22 +216,13 @@ extern "C" int pag_kv_attend_selected(const pag_kv_cache* cache, const pag_kv_st
                                       int64_t ids_head_stride, uint32_t id_heads, uint32_t k, void* stream) {
     return guarded("pag_kv_attend_selected", [&]() -> int {
         Attend a = {};
-        int num_cu = 0;
-        const int rc = attend_common(cache, step, args, &a, &num_cu);
-        if (rc) return rc;
-        PAG_CHECK(id_heads > 0 && a.c.kv_heads > 0 && id_heads % a.c.kv_heads == 0 && args->heads % id_heads == 0, PAG_EINVAL,
-                  "id_heads must be a multiple of kv_heads that divides heads");
-        PAG_CHECK((u64)k + args->window < (1ull << 30), PAG_EUNSUPPORTED, "k + window must be below 2^30");
-        if (step->tokens == 0) return PAG_OK;
+        int num_cu = 0, rc;
+        if ((rc = layout_of(cache, step, args, true, id_heads, k, &a)) || (rc = arrays_of(step, args, &a, &num_cu)) || step->tokens == 0) return rc;
         PAG_CHECK(step->request && step->positions, PAG_EINVAL, "step: request or positions is null");
         PAG_CHECK(k == 0 || (ids != nullptr && aligned(ids, 8)), PAG_EINVAL, "ids is null or not 8-byte aligned");
-        a.listed = 1;
         a.ids = ids;
         a.ids_ts = ids_token_stride;
         a.ids_hs = ids_head_stride;
-        a.id_heads = id_heads;
-        a.k = k;
-        a.group = a.heads / id_heads;
         return launch_attend((hipStream_t)stream, a, num_cu);
     });
 }

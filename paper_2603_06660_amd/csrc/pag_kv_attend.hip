@@ -13,6 +13,8 @@
 // A workgroup's four waves take every fourth tile of its piece, and add up their sums in LDS.
 // Work is split evenly over a fixed number of workgroups, in units of 128 keys, across requests of any lengths: each finds its share by
 // one sum over the requests' lengths.  A row block whose keys went to several workgroups is joined by a second kernel.
+#include <algorithm>
+
 #include "pag_kv_attend.h"
 
 namespace pagkv {
@@ -20,8 +22,8 @@ namespace {
 
 constexpr u32 ROWS = 16;                  // query rows of a tile
 constexpr u32 TILE = 32;                  // keys of a tile
-constexpr u32 WAVES = 4;
-constexpr u32 UNIT = WAVES * TILE;        // keys of the smallest share
+constexpr u32 SPLIT_WAVES = 4;            // waves of a workgroup whose keys are a share of all,
+constexpr u32 UNIT = SPLIT_WAVES * TILE;  // and keys of the smallest share
 
 constexpr u32 PIECE = 4;                  // what beginning and ending a piece costs, in units
 
@@ -215,74 +217,73 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("" ::: "memory");
 }
 
-template <int C>
+template <int C, int NW>
 struct Exchange {
     static constexpr u32 STRIDE = 64 * C + 4;
-    float m[WAVES][ROWS], sum[WAVES][ROWS];
-    float acc[WAVES][ROWS][STRIDE];
+    float m[NW][ROWS], sum[NW][ROWS];
+    float acc[NW][ROWS][STRIDE];
 };
 
-// The four waves' sums, into LDS.  All waves call it; the rows are free afterwards.
-template <int C>
-__device__ __forceinline__ void exchange(const Rows<C>& r, Exchange<C>& x) {
+// The waves' sums, into LDS, of the rows that there are.  All waves call it; the rows are free afterwards.
+template <int C, int NW>
+__device__ __forceinline__ void exchange(const Rows<C>& r, const Where& w, Exchange<C, NW>& x) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
     float sum = r.sum;
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (g == 0) {
-        x.m[wave][col] = r.M;
-        x.sum[wave][col] = sum;
-    }
+    if (w.row0 + col < w.rows) {
+        if (g == 0) {
+            x.m[wave][col] = r.M;
+            x.sum[wave][col] = sum;
+        }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int q = 0; q < C; ++q)
-            *(float4*)&x.acc[wave][col][(4 * g + i) * 4 * C + 4 * q] = make_float4(r.acc[4 * q][i], r.acc[4 * q + 1][i], r.acc[4 * q + 2][i], r.acc[4 * q + 3][i]);
+            for (int q = 0; q < C; ++q)
+                *(float4*)&x.acc[wave][col][(4 * g + i) * 4 * C + 4 * q] = make_float4(r.acc[4 * q][i], r.acc[4 * q + 1][i], r.acc[4 * q + 2][i], r.acc[4 * q + 3][i]);
+        }
     }
     lds_barrier();
 }
 
 // Adds them up and writes the rows' results, or the piece's sums for the second kernel.  partial: null, or
 // [16] offsets, [16] sums, [16][width]
-template <int C>
-__device__ __forceinline__ void finish(const Attend& a, const Where& w, const Exchange<C>& x, float* partial) {
-    constexpr u32 W = 64 * C;
-    // 16 threads a row, 4 C numbers each
-    const u32 row = threadIdx.x >> 4, first = (threadIdx.x & 15) * 4 * C;
-    float M = x.m[0][row];
+template <int C, int NW>
+__device__ __forceinline__ void finish(const Attend& a, const Where& w, const Exchange<C, NW>& x, float* partial) {
+    constexpr u32 W = 64 * C, THREADS = 64 * NW / ROWS, N = W / THREADS;      // threads of a row, numbers of a thread
+    const u32 row = threadIdx.x / THREADS, first = threadIdx.x % THREADS * N;
+    if (w.row0 + row < w.rows) {
+        float M = x.m[0][row];
 #pragma unroll
-    for (u32 v = 1; v < WAVES; ++v) M = fmaxf(M, x.m[v][row]);
-    float sum = 0.f, o[4 * C];
+        for (u32 v = 1; v < NW; ++v) M = fmaxf(M, x.m[v][row]);
+        float sum = 0.f, o[N];
 #pragma unroll
-    for (int n = 0; n < 4 * C; ++n) o[n] = 0.f;
+        for (u32 n = 0; n < N; ++n) o[n] = 0.f;
 #pragma unroll
-    for (u32 v = 0; v < WAVES; ++v) {
-        const float by = __builtin_amdgcn_exp2f(x.m[v][row] - M);
-        sum = __builtin_fmaf(x.sum[v][row], by, sum);
+        for (u32 v = 0; v < NW; ++v) {
+            const float by = __builtin_amdgcn_exp2f(x.m[v][row] - M);
+            sum = __builtin_fmaf(x.sum[v][row], by, sum);
 #pragma unroll
-        for (int q = 0; q < C; ++q) {
-            const float4 y = *(const float4*)&x.acc[v][row][first + 4 * q];
-            o[4 * q] = __builtin_fmaf(y.x, by, o[4 * q]);
-            o[4 * q + 1] = __builtin_fmaf(y.y, by, o[4 * q + 1]);
-            o[4 * q + 2] = __builtin_fmaf(y.z, by, o[4 * q + 2]);
-            o[4 * q + 3] = __builtin_fmaf(y.w, by, o[4 * q + 3]);
+            for (u32 n = 0; n < N; n += 2) {
+                const float2 y = *(const float2*)&x.acc[v][row][first + n];
+                o[n] = __builtin_fmaf(y.x, by, o[n]);
+                o[n + 1] = __builtin_fmaf(y.y, by, o[n + 1]);
+            }
         }
-    }
-    if (partial) {
-        if (first == 0) { partial[row] = M; partial[ROWS + row] = sum; }
+        if (partial) {
+            if (first == 0) { partial[row] = M; partial[ROWS + row] = sum; }
 #pragma unroll
-        for (int q = 0; q < C; ++q)
-            *(float4*)(partial + 2 * ROWS + row * W + first + 4 * q) = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-    } else if (w.row0 + row < w.rows) {
-        const u32 t = w.t0 + (w.row0 + row) / a.group, head = w.head0 + (w.row0 + row) % a.group;
-        const float f = sum != 0.f ? 1.f / sum : 0.f;
-        uint16_t* out = (uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + first;
+            for (u32 n = 0; n < N; n += 2) *(float2*)(partial + 2 * ROWS + row * W + first + n) = make_float2(o[n], o[n + 1]);
+        } else {
+            const u32 t = w.t0 + (w.row0 + row) / a.group, head = w.head0 + (w.row0 + row) % a.group;
+            const float f = sum != 0.f ? 1.f / sum : 0.f;
+            uint16_t* out = (uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + first;
 #pragma unroll
-        for (int q = 0; q < C; ++q) {
-            if (first + 4 * q < a.c.dim)
-                *(uint2*)(out + 4 * q) = make_uint2(pack2(o[4 * q] * f, o[4 * q + 1] * f, a.dtype), pack2(o[4 * q + 2] * f, o[4 * q + 3] * f, a.dtype));
+            for (u32 n = 0; n < N; n += 2) {
+                if (first + n < a.c.dim) *(u32*)(out + n) = pack2(o[n] * f, o[n + 1] * f, a.dtype);
+            }
+            if (a.lse && first == 0) a.lse[(u64)t * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
         }
-        if (a.lse && first == 0) a.lse[(u64)t * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
     }
     lds_barrier();
 }
@@ -322,13 +323,162 @@ struct Piece {
     int last;                  // the workgroup that ends the tile
 };
 
+// rows, first and last key of the piece with units u0 to u1 - 1, of `unit` keys each, of row tile `tile`
+__device__ __forceinline__ void place_piece(const Attend& a, Piece& p, const Span& s, u32 tile, u32 kv_head, u32 unit) {
+    p.s = s;
+    p.w.t0 = s.t0;
+    p.w.rows = s.tokens * a.group;
+    p.w.row0 = tile * ROWS;
+    p.w.kv_head = kv_head;
+    p.w.head0 = kv_head * a.group;
+    p.p0 = s.first + (int)(p.w.row0 / a.group);
+    p.p1 = s.first + (int)(min(p.w.row0 + ROWS - 1, p.w.rows - 1) / a.group);
+    const int low = a.window ? max(0, p.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
+    p.start = (low & ~(int)(BLOCK - 1)) + (int)(p.u0 * unit);
+    p.stop = (int)min((int64_t)p.p1 + 1, (int64_t)p.start + (int64_t)(p.u1 - p.u0) * unit);
+}
+
+// The pieces that next(p) gives, one after the other.  WHOLE: they are whole row tiles.
+template <int FMT, int C, int NW, bool WHOLE, typename Next>
+__device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& sh, Next&& next) {
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    Piece p;
+    Rows<C> rows;
+    RawRows<C> raw;
+    // 64 blocks of this wave's tiles at a time: lane 2 i + s has block s of tile i
+    const int mine_at = (int)(lane >> 1) * (int)(NW * TILE) + (int)(lane & 1) * (int)BLOCK;
+    int from = 0;
+    u32 page = 0, block_row = 0;
+    uint16_t exponents = 0;
+    u64 there = 0;
+    const auto page_of = [&](int at_key) -> u32 {
+        return at_key < p.stop ? (u32)a.s.table[p.b * a.s.table_stride + (u32)at_key / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
+    };
+    const auto ask = [&]() {                  // what does not depend on each other is asked for together: pages and rows,
+        from = p.start + (int)(wave * TILE);
+        page = page_of(from + mine_at);
+        fetch_rows<C>(a, p.w, raw);
+    };
+    const auto look_up = [&]() {              // then exponents and the first tile
+        const bool ok = page < a.c.num_pages;
+        block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)(from + mine_at) / BLOCK % a.c.page_blocks * BLOCK) : 0;
+        exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
+        there = __ballot(ok);
+        page = page_of(from + 32 * (int)(NW * TILE) + mine_at);
+    };
+    const u32 k_at = col * (128 * C) + g * 16, v_at = 4 * g * (128 * C) + 64 * C + col * (4 * C);
+    const auto load = [&](Tile<C>& tile, int i) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint8_t* rows_at = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s) * (128 * C);
+#pragma unroll
+            for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(rows_at + k_at + h * 64);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) load_words<C>(rows_at + v_at + j * (128 * C), tile.v[4 * s + j]);
+        }
+    };
+    const auto add = [&](Tile<C>& tile, int i) {
+        const int pos = from + i * (int)(NW * TILE);
+        Scales<false> x;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int e = __builtin_amdgcn_readlane((int)exponents, 2 * i + s), ev = (int)(int8_t)(e >> 8);
+            x.ek[s] = power((int)(int8_t)e);
+            x.ev[s] = (float)ev;
+            x.down[s] = power(-ev);
+            x.at[s] = pos + s * (int)BLOCK + 4 * (int)g;
+        }
+        const u32 two = (u32)(there >> (2 * i)) & 3u;
+        const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos <= p.p1 - (int)min(a.window - 1, 0x7FFFFFFEu) - 1;
+        u32 keep = 0xFF;
+        if (masked) {
+            keep = 0;
+            const int oldest = a.window ? max(0, rows.position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = x.at[j >> 2] + (j & 3);
+                const bool exists = (two >> (j >> 2) & 1u) && k < p.stop;
+                if (exists && k <= rows.position && k >= oldest) keep |= 1u << j;
+                if (!exists) {
+#pragma unroll
+                    for (int y = 0; y < C; ++y) tile.v[j][y] = 0;      // the memory behind the last token may hold anything
+                }
+            }
+        }
+        add_tile<FMT, C, false>(a, tile, rows, x, masked, keep);
+    };
+
+    if constexpr (WHOLE) {
+        // Few tiles a wave: their latency is what counts, and a fetch of instructions that are used once costs more than a fetch of keys.
+        while (next(p)) {
+            ask();
+            start_rows<C>(a, p.w, p.s.first, raw, rows);
+            while (from < p.stop) {
+                look_up();
+                const int count = min(32, (p.stop - from + (int)(NW * TILE) - 1) / (int)(NW * TILE));
+                for (int i = 0; i < count; ++i) {
+                    Tile<C> tile;
+                    load(tile, i);
+                    add(tile, i);
+                }
+                from += 32 * (int)(NW * TILE);
+            }
+            exchange(rows, p.w, sh);
+            finish(a, p.w, sh, nullptr);
+        }
+        return;
+    }
+    Tile<C> even, odd;
+    bool more = next(p);
+    if (more) {
+        ask();
+        if (from < p.stop) {
+            look_up();
+            load(even, 0);
+        }
+    }
+    while (more) {
+        start_rows<C>(a, p.w, p.s.first, raw, rows);
+        while (from < p.stop) {
+            // a tile is on its way while the one before it is added; behind the last one the last is asked for again, which the cache has
+            const int count = min(32, (p.stop - from + (int)(NW * TILE) - 1) / (int)(NW * TILE));
+            for (int i = 0; i < count; i += 2) {
+                load(odd, min(i + 1, count - 1));
+                add(even, i);
+                if (i + 1 < count) {
+                    load(even, min(i + 2, count - 1));
+                    add(odd, i + 1);
+                }
+            }
+            from += 32 * (int)(NW * TILE);
+            if (from < p.stop) {
+                look_up();
+                load(even, 0);
+            }
+        }
+        // the next piece's first tile is on its way while this one's waves are added up
+        const Where w = p.w;
+        const bool begun = p.u0 == 0, ended = p.u1 == p.units;
+        float* partial = !begun || !ended ? a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2)) : nullptr;
+        if (begun) write_joined(a, w, p.last >= 0 ? make_int2((int)blockIdx.x, p.last) : make_int2(-1, -1));
+        more = next(p);
+        if (more) ask();
+        exchange(rows, w, sh);
+        if (more && from < p.stop) {
+            look_up();
+            load(even, 0);
+        }
+        finish(a, w, sh, partial);
+    }
+}
+
 template <int FMT, int C>
 __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend(Attend a) {
-    __shared__ __align__(16) Exchange<C> sh;
-    __shared__ u64 sh_sum[WAVES];
+    __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
+    __shared__ u64 sh_sum[SPLIT_WAVES];
     __shared__ u64 sh_begin;
     __shared__ u32 sh_b;
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
     // this workgroup's share of all units
     const u32 per = (a.s.requests + 255) / 256, b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
@@ -343,7 +493,7 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend(Attend a)
     if (lane == 63) sh_sum[wave] = upto;
     __syncthreads();
     u64 total = 0;
-    for (u32 x = 0; x < WAVES; ++x) {
+    for (u32 x = 0; x < SPLIT_WAVES; ++x) {
         if (x < wave) upto += sh_sum[x];
         total += sh_sum[x];
     }
@@ -389,133 +539,40 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend(Attend a)
             p.u0 = max(c0, PIECE) - PIECE;
             p.u1 = max(c1, PIECE) - PIECE;
             if (p.u0 == p.u1) continue;
-            p.s = q.s;
             p.b = b;
             p.units = q.units;
             p.last = p.u0 == 0 && p.u1 < p.units ? (int)divide((before + (u64)(part + 1) * cost) * parts - 1, total) : -1;
-            p.w.t0 = q.s.t0;
-            p.w.rows = q.s.tokens * a.group;
-            p.w.row0 = part % q.tiles * ROWS;
-            p.w.kv_head = part / q.tiles;
-            p.w.head0 = p.w.kv_head * a.group;
-            p.p0 = q.s.first + (int)(p.w.row0 / a.group);
-            p.p1 = q.s.first + (int)(min(p.w.row0 + ROWS - 1, p.w.rows - 1) / a.group);
-            const int low = a.window ? max(0, p.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
-            p.start = (low & ~(int)(BLOCK - 1)) + (int)(p.u0 * UNIT);
-            p.stop = min(p.p1 + 1, p.start + (int)((p.u1 - p.u0) * UNIT));
+            place_piece(a, p, q.s, part % q.tiles, part / q.tiles, UNIT);
             return true;
         }
         return false;
     };
+    attend_pieces<FMT, C, SPLIT_WAVES, false>(a, sh, next_piece);
+}
 
-    Piece p;
-    Rows<C> rows;
-    RawRows<C> raw;
-    Tile<C> even, odd;
-    // 64 blocks of this wave's tiles at a time: lane 2 i + s has block s of tile i
-    const int mine_at = (int)(lane >> 1) * (int)UNIT + (int)(lane & 1) * (int)BLOCK;
-    int from = 0;
-    u32 page = 0, block_row = 0;
-    uint16_t exponents = 0;
-    u64 there = 0;
-    const auto page_of = [&](int at_key) -> u32 {
-        return at_key < p.stop ? (u32)a.s.table[p.b * a.s.table_stride + (u32)at_key / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
-    };
-    const auto ask = [&]() {                  // what does not depend on each other is asked for together: pages and rows,
-        from = p.start + (int)(wave * TILE);
-        page = page_of(from + mine_at);
-        fetch_rows<C>(a, p.w, raw);
-    };
-    const auto look_up = [&]() {              // then exponents and the first tile
-        const bool ok = page < a.c.num_pages;
-        block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)(from + mine_at) / BLOCK % a.c.page_blocks * BLOCK) : 0;
-        exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
-        there = __ballot(ok);
-        page = page_of(from + 32 * (int)UNIT + mine_at);
-    };
-    const u32 k_at = col * (128 * C) + g * 16, v_at = 4 * g * (128 * C) + 64 * C + col * (4 * C);
-    const auto load = [&](Tile<C>& tile, int i) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint8_t* rows_at = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s) * (128 * C);
-#pragma unroll
-            for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(rows_at + k_at + h * 64);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) load_words<C>(rows_at + v_at + j * (128 * C), tile.v[4 * s + j]);
-        }
-    };
-    const auto add = [&](Tile<C>& tile, int i) {
-        const int pos = from + i * (int)UNIT;
-        Scales<false> x;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int e = __builtin_amdgcn_readlane((int)exponents, 2 * i + s), ev = (int)(int8_t)(e >> 8);
-            x.ek[s] = power((int)(int8_t)e);
-            x.ev[s] = (float)ev;
-            x.down[s] = power(-ev);
-            x.at[s] = pos + s * (int)BLOCK + 4 * (int)g;
-        }
-        const u32 two = (u32)(there >> (2 * i)) & 3u;
-        const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos <= p.p1 - (int)min(a.window - 1, 0x7FFFFFFEu) - 1;
-        u32 keep = 0xFF;
-        if (masked) {
-            keep = 0;
-            const int oldest = a.window ? max(0, rows.position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int k = x.at[j >> 2] + (j & 3);
-                const bool exists = (two >> (j >> 2) & 1u) && k < p.stop;
-                if (exists && k <= rows.position && k >= oldest) keep |= 1u << j;
-                if (!exists) {
-#pragma unroll
-                    for (int y = 0; y < C; ++y) tile.v[j][y] = 0;      // the memory behind the last token may hold anything
-                }
-            }
-        }
-        add_tile<FMT, C, false>(a, tile, rows, x, masked, keep);
-    };
-
-    bool more = next_piece(p);
-    if (more) {
-        ask();
-        if (from < p.stop) {
-            look_up();
-            load(even, 0);
-        }
+// A workgroup for each request and key/value head, which reads all of its keys: nothing to share out and nothing to join.
+template <int FMT, int C, int NW>
+__global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_whole(Attend a) {
+    __shared__ __align__(16) Exchange<C, NW> sh;
+    const u32 b = blockIdx.x / a.c.kv_heads, kv_head = blockIdx.x % a.c.kv_heads;
+    const Span s = span_of(a, b);
+    write_padding(a);
+    if (s.tokens == 0) return;
+    if (s.context == 0) {
+        if (kv_head == 0) write_empty(a, s.t0, s.t0 + s.tokens);
+        return;
     }
-    while (more) {
-        start_rows<C>(a, p.w, p.s.first, raw, rows);
-        while (from < p.stop) {
-            // a tile is on its way while the one before it is added; behind the last one the last is asked for again, which the cache has
-            const int count = min(32, (p.stop - from + (int)UNIT - 1) / (int)UNIT);
-            for (int i = 0; i < count; i += 2) {
-                load(odd, min(i + 1, count - 1));
-                add(even, i);
-                if (i + 1 < count) {
-                    load(even, min(i + 2, count - 1));
-                    add(odd, i + 1);
-                }
-            }
-            from += 32 * (int)UNIT;
-            if (from < p.stop) {
-                look_up();
-                load(even, 0);
-            }
-        }
-        // the next piece's first tile is on its way while this one's waves are added up
-        const Where w = p.w;
-        const bool begun = p.u0 == 0, ended = p.u1 == p.units;
-        float* partial = !begun || !ended ? a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2)) : nullptr;
-        if (begun) write_joined(a, w, p.last >= 0 ? make_int2((int)blockIdx.x, p.last) : make_int2(-1, -1));
-        more = next_piece(p);
-        if (more) ask();
-        exchange<C>(rows, sh);
-        if (more && from < p.stop) {
-            look_up();
-            load(even, 0);
-        }
-        finish<C>(a, w, sh, partial);
-    }
+    const u32 tiles = (s.tokens * a.group + ROWS - 1) / ROWS;
+    u32 tile = 0;
+    attend_pieces<FMT, C, NW, true>(a, sh, [&](Piece& p) -> bool {
+        if (tile == tiles) return false;
+        p.b = b;
+        p.units = p.u1 = 1;
+        p.u0 = 0;
+        p.last = -1;
+        place_piece(a, p, s, tile++, kv_head, 0x7FFFFFFFu);
+        return true;
+    });
 }
 
 // ---- attention over listed tokens -----------------------------------------------------------------------------------
@@ -527,54 +584,37 @@ struct Entries {
     int at[64];
 };
 
-template <int FMT, int C>
-__global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(Attend a, u32 units, u32 tiles) {
-    __shared__ __align__(16) Exchange<C> sh;
-    __shared__ __align__(16) Entries sh_entries[WAVES][2];
+// a token's list, or a part of it
+struct ListPiece : Where {
+    u32 id_head, u0, u1;
+    int last;
+};
+
+__device__ __forceinline__ void place_list(const Attend& a, ListPiece& p, u64 list, u32 tile) {
+    p.t0 = (u32)divide(list, a.id_heads);
+    p.id_head = (u32)(list - (u64)p.t0 * a.id_heads);
+    p.rows = a.group;
+    p.row0 = tile * ROWS;
+    p.head0 = p.id_head * a.group;
+    p.kv_head = p.id_head / (a.id_heads / a.c.kv_heads);
+}
+
+// The pieces that next(p) gives; a list has `units` units of 32 NW entries.
+template <int FMT, int C, int NW, bool WHOLE, typename Next>
+__device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& sh, Entries (&sh_entries)[NW][2], u32 units, Next&& next) {
     const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-    const u32 cost = units + PIECE;
-    const u64 total = (u64)a.s.tokens * a.id_heads * tiles * cost;
-    const u32 parts = (u32)min((u64)gridDim.x, total);
-    if (blockIdx.x >= parts) return;
-    u64 at = share(total, parts, blockIdx.x);
-    const u64 end = share(total, parts, blockIdx.x + 1);
     const u32 entries = a.k + a.window;
-
-    Where w;
-    u32 t = 0, id_head = 0, u0 = 0, u1 = 0;
-    int last = -1;
-    const auto next_piece = [&]() -> bool {
-        while (at < end) {
-            const u64 part = divide(at, cost), list = divide(part, tiles);
-            const u32 c0 = (u32)(at - part * cost), c1 = (u32)min((u64)cost, c0 + (end - at));
-            at += c1 - c0;
-            u0 = max(c0, PIECE) - PIECE;
-            u1 = max(c1, PIECE) - PIECE;
-            if (u0 == u1) continue;
-            last = u0 == 0 && u1 < units ? (int)divide((part + 1) * cost * parts - 1, total) : -1;
-            t = (u32)divide(list, a.id_heads);
-            id_head = (u32)(list - (u64)t * a.id_heads);
-            w.t0 = t;
-            w.rows = a.group;
-            w.row0 = (u32)(part - list * tiles) * ROWS;
-            w.head0 = id_head * a.group;
-            w.kv_head = id_head / (a.id_heads / a.c.kv_heads);
-            return true;
-        }
-        return false;
-    };
-
+    ListPiece w = {};
     Rows<C> rows;
     RawRows<C> raw;
-    Tile<C> even, odd;
     u32 from = 0, stop = 0;                      // this wave's next entries
     int request = -1, position = -1;
     int64_t id = -1;                             // of the entries two batches on,
     int key = -1;                                // the positions and pages of the next one
     u32 page = 0;
     u64 there = 0;                               // which of this batch are keys
-    const u32 mine = (lane & 31) + (lane >> 5) * UNIT;
-    const auto id_of = [&](u32 n) -> int64_t { return n < a.k && n < stop ? a.ids[(int64_t)t * a.ids_ts + (int64_t)id_head * a.ids_hs + n] : -1; };
+    const u32 mine = (lane & 31) + (lane >> 5) * (NW * TILE);
+    const auto id_of = [&](u32 n) -> int64_t { return n < a.k && n < stop ? a.ids[(int64_t)w.t0 * a.ids_ts + (int64_t)w.id_head * a.ids_hs + n] : -1; };
     const auto key_of = [&](u32 n) {             // from id
         int64_t k = id;
         if (n >= a.k) k = (int64_t)position - (int64_t)(n - a.k);
@@ -583,11 +623,11 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(
         page = key >= 0 ? (u32)a.s.table[(u64)(u32)request * a.s.table_stride + (u32)key / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
     };
     const auto ask = [&]() {
-        from = u0 * UNIT + wave * TILE;
-        stop = min(entries, u1 * UNIT);
+        from = w.u0 * (NW * TILE) + wave * TILE;
+        stop = min(entries, w.u1 * (NW * TILE));
         id = id_of(from + mine);
-        request = a.s.request[t];
-        position = a.s.positions[t];
+        request = a.s.request[w.t0];
+        position = a.s.positions[w.t0];
         fetch_rows<C>(a, w, raw);
     };
     const auto check = [&]() {
@@ -602,10 +642,10 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(
         there = __ballot(ok);
         x.row[lane] = row;
         x.at[lane] = key;
-        const u32 next = from + 2 * UNIT + mine;
-        if (from + 2 * UNIT < stop) {
+        const u32 next = from + 2 * (NW * TILE) + mine;
+        if (from + 2 * (NW * TILE) < stop) {
             key_of(next);
-            id = id_of(next + 2 * UNIT);
+            id = id_of(next + 2 * (NW * TILE));
         }
         const int ev = (int)(int8_t)(e >> 8);
         x.ek[lane] = power((int)(int8_t)e);
@@ -654,16 +694,17 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(
         }
         add_tile<FMT, C, true>(a, tile, rows, scales, masked, keep);
     };
+    Tile<C> even, odd;
     u32 buffer = 0;
     const auto begin_piece = [&]() {
         check();
         key_of(from + mine);
-        id = id_of(from + 2 * UNIT + mine);
+        id = id_of(from + 2 * (NW * TILE) + mine);
         look_up(buffer);
         load(even, buffer, 0);
     };
 
-    bool more = next_piece();
+    bool more = next(w);
     if (more) {
         ask();
         if (from < stop) begin_piece();
@@ -674,7 +715,7 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(
             const u32 lo = (u32)there, hi = (u32)(there >> 32), now = buffer;
             load(odd, now, 1);
             if (lo) add(even, now, 0, lo);
-            from += 2 * UNIT;
+            from += 2 * (NW * TILE);
             if (from < stop) {
                 buffer ^= 1;
                 look_up(buffer);
@@ -683,15 +724,61 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(
             if (hi) add(odd, now, 1, hi);
         }
         const Where done = w;
-        const bool begun = u0 == 0, ended = u1 == units;
-        float* partial = !begun || !ended ? a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2)) : nullptr;
-        if (begun) write_joined(a, done, last >= 0 ? make_int2((int)blockIdx.x, last) : make_int2(-1, -1));
-        more = next_piece();
+        float* partial = nullptr;
+        if (!WHOLE) {
+            const bool begun = w.u0 == 0, ended = w.u1 == units;
+            if (!begun || !ended) partial = a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (64 * C + 2));
+            if (begun) write_joined(a, done, w.last >= 0 ? make_int2((int)blockIdx.x, w.last) : make_int2(-1, -1));
+        }
+        more = next(w);
         if (more) ask();
-        exchange<C>(rows, sh);
+        exchange(rows, done, sh);
         if (more && from < stop) begin_piece();
-        finish<C>(a, done, sh, partial);
+        finish(a, done, sh, partial);
     }
+}
+
+template <int FMT, int C>
+__global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend_selected(Attend a, u32 units, u32 tiles) {
+    __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
+    __shared__ __align__(16) Entries sh_entries[SPLIT_WAVES][2];
+    const u32 cost = units + PIECE;
+    const u64 total = (u64)a.s.tokens * a.id_heads * tiles * cost;
+    const u32 parts = (u32)min((u64)gridDim.x, total);
+    if (blockIdx.x >= parts) return;
+    u64 at = share(total, parts, blockIdx.x);
+    const u64 end = share(total, parts, blockIdx.x + 1);
+    attend_lists<FMT, C, SPLIT_WAVES, false>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
+        while (at < end) {
+            const u64 part = divide(at, cost), list = divide(part, tiles);
+            const u32 c0 = (u32)(at - part * cost), c1 = (u32)min((u64)cost, c0 + (end - at));
+            at += c1 - c0;
+            p.u0 = max(c0, PIECE) - PIECE;
+            p.u1 = max(c1, PIECE) - PIECE;
+            if (p.u0 == p.u1) continue;
+            p.last = p.u0 == 0 && p.u1 < units ? (int)divide((part + 1) * cost * parts - 1, total) : -1;
+            place_list(a, p, list, (u32)(part - list * tiles));
+            return true;
+        }
+        return false;
+    });
+}
+
+template <int FMT, int C, int NW>
+__global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_selected_whole(Attend a, u32 tiles) {
+    __shared__ __align__(16) Exchange<C, NW> sh;
+    __shared__ __align__(16) Entries sh_entries[NW][2];
+    const u32 units = max((a.k + a.window + NW * TILE - 1) / (NW * TILE), 1u);
+    bool first = true;
+    attend_lists<FMT, C, NW, true>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
+        if (!first) return false;
+        first = false;
+        p.u0 = 0;
+        p.u1 = units;
+        p.last = -1;
+        place_list(a, p, blockIdx.x / tiles, blockIdx.x % tiles);
+        return true;
+    });
 }
 
 // ---- joining --------------------------------------------------------------------------------------------------------
@@ -771,27 +858,52 @@ __global__ void __launch_bounds__(256) k_join(Attend a, int groups) {
     if (a.lse && threadIdx.x == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }
 
+u64 whole_groups(const Attend& a) { return a.listed ? (u64)a.s.tokens * a.id_heads * ((a.group + ROWS - 1) / ROWS) : (u64)a.s.requests * a.c.kv_heads; }
+
+// Whether a workgroup reads all keys of its rows: lists, windows or tables that hold few keys.
+bool narrow_whole(const Attend& a, int num_cu) {
+    const u64 keys = a.listed ? (u64)a.k + a.window : std::min<u64>((u64)a.s.max_pages * a.c.page_tokens, a.window ? (u64)a.window + 2 * ROWS : ~0ull);
+    const u64 groups = whole_groups(a);
+    if (keys <= 1024) return true;
+    return a.listed ? keys <= 4096 && groups >= (u64)num_cu : keys <= 2048 && groups >= (u64)num_cu / 2;
+}
+
 u64 partial_floats(u32 width, int num_cu) { return 2ull * (u32)num_cu * groups_per_cu(width) * ROWS * (width + 2); }
+
+template <int FMT, int C, int NW>
+void run_whole(hipStream_t st, const Attend& a) {
+    if (a.listed) {
+        const u32 tiles = (a.group + ROWS - 1) / ROWS;
+        k_attend_selected_whole<FMT, C, NW><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
+    } else {
+        k_attend_whole<FMT, C, NW><<<a.s.requests * a.c.kv_heads, 64 * NW, 0, st>>>(a);
+    }
+}
 
 template <int FMT, int C>
 void run_attend(hipStream_t st, const Attend& a, int num_cu) {
-    const u32 grid = (u32)num_cu * groups_per_cu(64 * C);
-    if (a.listed) {
-        const u32 units = max((a.k + a.window + UNIT - 1) / UNIT, 1u), tiles = (a.group + ROWS - 1) / ROWS;
-        k_attend_selected<FMT, C><<<grid, 256, 0, st>>>(a, units, tiles);
-    } else {
-        k_attend<FMT, C><<<grid, 256, 0, st>>>(a);
+    if (narrow_whole(a, num_cu)) {
+        // eight waves where there are CUs enough, four where workgroups queue (and where registers last for no more)
+        if constexpr (C <= 2) {
+            if (whole_groups(a) <= (u64)num_cu) return run_whole<FMT, C, 8>(st, a);
+        }
+        return run_whole<FMT, C, 4>(st, a);
     }
+    const u32 grid = (u32)num_cu * groups_per_cu(64 * C);
+    if (a.listed) k_attend_selected<FMT, C><<<grid, 256, 0, st>>>(a, std::max<u32>((a.k + a.window + UNIT - 1) / UNIT, 1), (a.group + ROWS - 1) / ROWS);
+    else k_attend<FMT, C><<<grid, 256, 0, st>>>(a);
     k_join<C><<<a.s.tokens * a.heads, 256, 0, st>>>(a, (int)grid);
 }
 
 }  // namespace
 
-u64 narrow_workspace(u32 width, u64 rows, int num_cu) { return 4 * partial_floats(width, num_cu) + 8 * rows; }
+u64 narrow_workspace(const Attend& a, int num_cu) {
+    return narrow_whole(a, num_cu) ? 0 : 4 * partial_floats(a.c.width, num_cu) + 8 * (u64)a.s.tokens * a.heads;
+}
 
 int launch_attend(hipStream_t st, const Attend& args, int num_cu) {
     Attend a = args;
-    a.joined = (int2*)(a.partial + partial_floats(a.c.width, num_cu));
+    a.joined = narrow_whole(a, num_cu) ? nullptr : (int2*)(a.partial + partial_floats(a.c.width, num_cu));
     const u32 n = a.c.width / 64;
     if (a.c.fmt == PAG_KV_INT8) {
         if (n == 1) run_attend<PAG_KV_INT8, 1>(st, a, num_cu);

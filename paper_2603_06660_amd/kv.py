@@ -20,6 +20,7 @@ from .binding import PagError, _check, load_library
 
 _FORMATS = {"int8": 0, "fp8": 1}
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_ROW_DTYPES = (torch.float16, torch.bfloat16)
 
 
 class _Cache(C.Structure):
@@ -58,37 +59,47 @@ def _gpu(device):
 
 def _array(t, dtype, shape, device, what):
     """The address of a dense tensor of this type, shape and device."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise PagError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
     return t.data_ptr()
 
 
 def _rows(t, shape, device, what, dtypes=_DTYPES):
     """Checks a [tokens, heads, dim] tensor whose last dimension is dense; the other strides are free."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != shape or t.device != device:
         raise PagError("%s must be a tensor of shape %s on %s, of type %s" %
                        (what, tuple(shape), device, ", ".join(str(x) for x in dtypes)))
     if t.stride(2) != 1 and t.shape[2] > 1:
         raise PagError("%s: the last dimension must be dense" % what)
 
 
-class _On:
-    """Makes a GPU current if another one is, and gives its current stream."""
+# the number of a GPU's current stream, without an object around it where torch offers that
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    __slots__ = ("device", "before")
+_P, _I = C.c_void_p, C.c_int64
+_ARGTYPES = {"pag_kv_extend": [_P, _P, _P, _P], "pag_kv_release": [_P, _P, _P],
+             "pag_kv_append": [_P, C.c_uint32, _P, _I, _I, _P, _I, _I, _P, C.c_uint64, _P],
+             "pag_kv_read": [_P, _P, C.c_uint64, C.c_uint32, _P, _I, _I, _P, _I, _I, _P],
+             "pag_kv_workspace_bytes": [_P, _P, _P, C.c_int, C.c_uint32, C.c_uint32, _P],
+             "pag_kv_attend": [_P, _P, _P, _P], "pag_kv_attend_selected": [_P, _P, _P, _P, _I, _I, C.c_uint32, C.c_uint32, _P]}
+_calls = {}
 
-    def __init__(self, device):
-        self.device = device
 
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.device)
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *_):
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.before)
+def _call(name, device, *args):
+    """One call of the library with `device` current, on its current stream (the last argument of every call)."""
+    f = _calls.get(name)
+    if f is None:
+        f = C.CFUNCTYPE(C.c_int, *_ARGTYPES[name])((name, load_library()))
+        _calls[name] = f
+    index = device.index
+    before = torch.cuda.current_device()
+    if before == index:
+        rc = f(*args, _stream_of(index))
+    else:
+        with torch.cuda.device(index):
+            rc = f(*args, _stream_of(index))
+    if rc:
+        _check(rc, name)
 
 
 class KvStep:
@@ -206,9 +217,7 @@ class KvTables:
         elif out.lengths is self.lengths or out.free_count is self.free_count:
             out.lengths, out.free_count = torch.empty_like(self.lengths), torch.empty_like(self.free_count)
             s.lengths, s.free_count = out.lengths.data_ptr(), out.free_count.data_ptr()
-        with _On(self.device) as stream:
-            _check(load_library().pag_kv_extend(C.byref(self._t), C.c_void_p(_array(add, torch.int32, (self._t.requests,), self.device, "add")),
-                                                C.byref(s), C.c_void_p(stream)), "pag_kv_extend")
+        _call("pag_kv_extend", self.device, C.addressof(self._t), _array(add, torch.int32, (self._t.requests,), self.device, "add"), C.addressof(s))
         return out
 
     def commit(self, step):
@@ -219,9 +228,7 @@ class KvTables:
 
     def release(self, done):
         """The requests with done[r] != 0 (int32 [requests]) give their pages back."""
-        with _On(self.device) as stream:
-            _check(load_library().pag_kv_release(C.byref(self._t), C.c_void_p(_array(done, torch.int32, (self._t.requests,), self.device, "done")),
-                                                 C.c_void_p(stream)), "pag_kv_release")
+        _call("pag_kv_release", self.device, C.addressof(self._t), _array(done, torch.int32, (self._t.requests,), self.device, "done"))
 
 
 class KvCache:
@@ -253,9 +260,8 @@ class KvCache:
                          _array(data, torch.uint8, (pages, heads, tokens, 2, -(-self.head_dim // 64) * 64), self.device, "data"),
                          _array(exponents, torch.int8, (pages, heads, tokens // 16, 2), self.device, "exponents"))
         self.data, self.exponents = data, exponents
-        lib = load_library()
-        nothing = [C.c_void_p(None), C.c_int64(0), C.c_int64(0)]
-        _check(lib.pag_kv_read(C.byref(self._c), C.c_void_p(None), C.c_uint64(0), C.c_uint32(0), *nothing, *nothing, C.c_void_p(None)), "KvCache")
+        _check(load_library().pag_kv_read(C.byref(self._c), None, C.c_uint64(0), C.c_uint32(0), *[C.c_void_p(None), C.c_int64(0), C.c_int64(0)] * 2,
+                                          None), "KvCache")      # of nothing: looks the cache over
         self._rooms = {}        # sizes of workspaces
 
     def append(self, k, v, slots):
@@ -264,11 +270,8 @@ class KvCache:
         shape = (tokens, self.kv_heads, self.head_dim)
         _rows(k, shape, self.device, "k")
         _rows(v, shape, self.device, "v", (k.dtype,))
-        with _On(self.device) as stream:
-            _check(load_library().pag_kv_append(
-                C.byref(self._c), C.c_uint32(_DTYPES[k.dtype]), C.c_void_p(k.data_ptr()), C.c_int64(k.stride(0)), C.c_int64(k.stride(1)),
-                C.c_void_p(v.data_ptr()), C.c_int64(v.stride(0)), C.c_int64(v.stride(1)),
-                C.c_void_p(_array(slots, torch.int64, (tokens,), self.device, "slots")), C.c_uint64(tokens), C.c_void_p(stream)), "pag_kv_append")
+        _call("pag_kv_append", self.device, C.addressof(self._c), _DTYPES[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
+              v.stride(0), v.stride(1), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens)
 
     def read(self, slots, dtype=torch.float32, out=None):
         """-> (k, v) [tokens, kv_heads, head_dim]: the rows in these slots as numbers; zeros for -1.  out: (k, v) to write into, of any
@@ -287,43 +290,52 @@ class KvCache:
         args = []
         for t, what in ((k, "k"), (v, "v")):
             if t is None:
-                args += [C.c_void_p(None), C.c_int64(0), C.c_int64(0)]
+                args += [None, 0, 0]
             else:
                 _rows(t, shape, self.device, what, (dtype,))
-                args += [C.c_void_p(t.data_ptr()), C.c_int64(t.stride(0)), C.c_int64(t.stride(1))]
-        with _On(self.device) as stream:
-            _check(load_library().pag_kv_read(C.byref(self._c), C.c_void_p(_array(slots, torch.int64, (tokens,), self.device, "slots")),
-                                              C.c_uint64(tokens), C.c_uint32(_DTYPES[dtype]), *args, C.c_void_p(stream)), "pag_kv_read")
+                args += [t.data_ptr(), t.stride(0), t.stride(1)]
+        _call("pag_kv_read", self.device, C.addressof(self._c), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens, _DTYPES[dtype], *args)
         return k, v
 
-    def _attention(self, q, step, scale, window, softcap, slopes, out):
+    def _attention(self, q, step, scale, window, softcap, slopes, out, id_heads=0, k=-1):
+        """Checks a call's tensors -> out, its arguments, and its workspace, which has to live until the call is made."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise PagError("q must be a tensor [tokens, heads, head_dim]")
-        tokens, heads = q.shape[0], q.shape[1]
-        shape = (tokens, heads, self.head_dim)
-        _rows(q, shape, self.device, "q", (torch.float16, torch.bfloat16))
-        if step.table is not None and step.device != self.device:
-            raise PagError("the step is on %s, the cache on %s" % (step.device, self.device))
+        tokens, heads, dim = shape = q.shape
+        device = self.device
+        if dim != self.head_dim:
+            raise PagError("q has rows of %d numbers, the cache of %d" % (dim, self.head_dim))
+        _rows(q, shape, device, "q", _ROW_DTYPES)
+        if step.table is not None and step.device != device:
+            raise PagError("the step is on %s, the cache on %s" % (step.device, device))
         if not 0 <= window < 1 << 31:
             raise PagError("window must be between 0 and 2^31 - 1")
         if out is None:
-            out = (torch.empty(shape, dtype=q.dtype, device=self.device), torch.empty((tokens, heads), dtype=torch.float32, device=self.device))
-        o, lse = out
-        _rows(o, shape, self.device, "out", (q.dtype,))
+            o, lse = out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty((tokens, heads), dtype=torch.float32, device=device)
+        else:
+            o, lse = out
+            _rows(o, shape, device, "out", (q.dtype,))
+            if lse is not None:
+                _array(lse, torch.float32, (tokens, heads), device, "lse")
         s = step._with(tokens)
-        size = self._rooms.get((tokens, heads, s.requests, s.max_new))
+        a = _Attention(C.sizeof(_Attention), _DTYPES[q.dtype], heads, window, dim ** -0.5 if scale is None else scale, softcap,
+                       None if slopes is None else _array(slopes, torch.float32, (heads,), device, "slopes"),
+                       q.data_ptr(), q.stride(0), q.stride(1), o.data_ptr(), o.stride(0), o.stride(1), None if lse is None else lse.data_ptr())
+        key = (tokens, heads, window, s.requests, s.max_new, s.max_pages, id_heads, k)
+        size = self._rooms.get(key)
         if size is None:
-            with _On(self.device):
-                size = load_library().pag_kv_workspace_bytes(C.byref(self._c), C.byref(s), C.c_uint32(heads))
+            n = C.c_uint64()
+            with torch.cuda.device(device):
+                _check(load_library().pag_kv_workspace_bytes(C.byref(self._c), C.byref(s), C.byref(a), C.c_int(k >= 0), C.c_uint32(id_heads),
+                                                             C.c_uint32(max(k, 0)), C.byref(n)), "pag_kv_workspace_bytes")
             if len(self._rooms) > 4096:
                 self._rooms.clear()
-            self._rooms[tokens, heads, s.requests, s.max_new] = size
-        room = torch.empty(size, dtype=torch.uint8, device=self.device)
-        a = _Attention(C.sizeof(_Attention), _DTYPES[q.dtype], heads, window, self.head_dim ** -0.5 if scale is None else scale, softcap,
-                       None if slopes is None else _array(slopes, torch.float32, (heads,), self.device, "slopes"),
-                       q.data_ptr(), q.stride(0), q.stride(1), o.data_ptr(), o.stride(0), o.stride(1),
-                       None if lse is None else _array(lse, torch.float32, (tokens, heads), self.device, "lse"), room.data_ptr(), room.numel())
-        return out, s, a, room
+            size = self._rooms[key] = n.value
+        room = None
+        if size:
+            room = torch.empty(size, dtype=torch.uint8, device=device)
+            a.workspace, a.workspace_bytes = room.data_ptr(), size
+        return out, a, room
 
     def attend(self, q, step, scale=None, window=0, softcap=0.0, slopes=None, out=None):
         """-> (out like q, lse float32 [tokens, heads]): every token of q [tokens, heads, head_dim] (float16 or bfloat16) attends to its request's
@@ -331,9 +343,8 @@ class KvCache:
         slopes (float32 [heads]): minus slope * distance.  scale: head_dim ** -0.5.  out: (out, lse) to write into; lse may be None."""
         if step.offsets is None or step.context is None:
             raise PagError("attend needs the step's offsets and context")
-        out, s, a, room = self._attention(q, step, scale, window, softcap, slopes, out)
-        with _On(self.device) as stream:
-            _check(load_library().pag_kv_attend(C.byref(self._c), C.byref(s), C.byref(a), C.c_void_p(stream)), "pag_kv_attend")
+        out, a, room = self._attention(q, step, scale, window, softcap, slopes, out)
+        _call("pag_kv_attend", self.device, C.addressof(self._c), C.addressof(step._s), C.addressof(a))
         return out
 
     def attend_selected(self, q, ids, step, scale=None, window=0, softcap=0.0, slopes=None, out=None):
@@ -345,9 +356,7 @@ class KvCache:
         if not isinstance(ids, torch.Tensor) or ids.dtype != torch.int64 or ids.dim() != 3 or ids.device != self.device or ids.shape[0] != q.shape[0] or \
                 (ids.shape[2] > 1 and ids.stride(2) != 1):
             raise PagError("ids must be an int64 tensor [tokens, id_heads, k] on %s whose last dimension is dense" % self.device)
-        out, s, a, room = self._attention(q, step, scale, window, softcap, slopes, out)
-        with _On(self.device) as stream:
-            _check(load_library().pag_kv_attend_selected(C.byref(self._c), C.byref(s), C.byref(a), C.c_void_p(ids.data_ptr()), C.c_int64(ids.stride(0)),
-                                                         C.c_int64(ids.stride(1)), C.c_uint32(ids.shape[1]), C.c_uint32(ids.shape[2]),
-                                                         C.c_void_p(stream)), "pag_kv_attend_selected")
+        out, a, room = self._attention(q, step, scale, window, softcap, slopes, out, ids.shape[1], ids.shape[2])
+        _call("pag_kv_attend_selected", self.device, C.addressof(self._c), C.addressof(step._s), C.addressof(a), ids.data_ptr(), ids.stride(0), ids.stride(1),
+              ids.shape[1], ids.shape[2])
         return out
