@@ -404,7 +404,7 @@ int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* strea
  * first token is among the new ones) is cleared first; its exponent is the smallest e >= -64 at which the largest code reaches the
  * largest finite magnitude.  Another block keeps its exponent unless the new tokens need a larger one; then what it held is
  * rounded again.  Rounding is to nearest even; infinities are held as the largest code, NaN as 0.
- * pag_kv_read: rows of the cache as numbers, [tokens][kv_heads][head_dim] with strides in elements (multiples of 8 bytes); k or v may be
+ * pag_kv_read: rows of the cache as numbers, [tokens][kv_heads][head_dim] with strides in elements (multiples of 16 bytes); k or v may be
  * null.  Slots -1 or out of range give zeros.  PAG_F32 and PAG_BF16 hold every number of the cache exactly.
  */
 int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride,

@@ -865,7 +865,8 @@ bool narrow_whole(const Attend& a, int num_cu) {
     const u64 keys = a.listed ? (u64)a.k + a.window : std::min<u64>((u64)a.s.max_pages * a.c.page_tokens, a.window ? (u64)a.window + 2 * ROWS : ~0ull);
     const u64 groups = whole_groups(a);
     if (keys <= 1024) return true;
-    return a.listed ? keys <= 4096 && groups >= (u64)num_cu : keys <= 2048 && groups >= (u64)num_cu / 2;
+    if (!a.listed) return keys <= 2048 && groups >= (u64)num_cu / 2;
+    return (keys <= 2048 && groups >= (u64)num_cu / 4) || (keys <= 4096 && groups >= (u64)num_cu);
 }
 
 u64 partial_floats(u32 width, int num_cu) { return 2ull * (u32)num_cu * groups_per_cu(width) * ROWS * (width + 2); }

@@ -165,80 +165,88 @@ struct Store {
     u32 dtype;
 };
 
-// One wave writes the new tokens of one block, for one head and kind: the wave of the first of them, the others' waves have
-// nothing to do.  8 numbers of a row are a lane's; a block of 16 rows is 2 C of these pieces a lane.
+// A wave has a window of new tokens, one head and one kind.  It writes the blocks whose first new token lies in its window, with all
+// their new tokens, one block after the other.  8 numbers of a row are a lane's; a block of 16 rows is 2 C of these pieces a lane.
+// A window of one token spreads a decoding step's blocks over as many waves as there are; where that makes more waves than run at
+// once, most of a prompt's would start only to find that their token is not the first of its block (15,000 tokens, 8 heads of 128:
+// 108 us), so windows are larger then.
 template <int FMT, int C>
-__global__ void __launch_bounds__(256) k_append(Store a) {
+__global__ void __launch_bounds__(256) k_append(Store a, u32 window) {
     const u32 lane = threadIdx.x & 63, kinds = 2 * a.c.kv_heads;
-    const u64 wave = (u64)blockIdx.x * 4 + (threadIdx.x >> 6), t = wave / kinds;
-    if (t >= a.tokens) return;
+    const u64 wave = (u64)blockIdx.x * 4 + (threadIdx.x >> 6), t0 = wave / kinds * window;
+    if (t0 >= a.tokens) return;
     const u32 head = (u32)(wave % kinds) >> 1, kind = (u32)(wave % kinds) & 1;
-    // lane 0: the token before, lanes 1 .. 16: this one and the next 15
+    // lane 0: the token before, lanes 1 .. window: the window, and the next 15
     int64_t slot = -1;
-    if (lane <= BLOCK && t + lane >= 1 && t + lane - 1 < a.tokens) slot = a.slots[t + lane - 1];
+    if (lane < window + BLOCK && t0 + lane >= 1 && t0 + lane - 1 < a.tokens) slot = a.slots[t0 + lane - 1];
     if (slot >= (int64_t)a.c.num_pages * a.c.page_tokens || slot < 0) slot = -1;
     const int block = slot < 0 ? -1 : (int)(slot / BLOCK), place = (int)(slot & (BLOCK - 1));
-    const int mine = __builtin_amdgcn_readlane(block, 1);
-    if (mine < 0 || __builtin_amdgcn_readlane(block, 0) == mine) return;
-    const u64 same = __ballot(block == mine && lane >= 1 && lane <= BLOCK) >> 1;
-    const u32 run = (u32)__builtin_ctzll(~same);
-    u32 present = 0;
-    for (u32 i = 0; i < run; ++i) present |= 1u << __builtin_amdgcn_readlane(place, i + 1);
-    const bool begins = present & 1u;
-    const u32 page = (u32)mine / a.c.page_blocks, first = (u32)mine % a.c.page_blocks * BLOCK;
-    uint8_t* rows = a.c.data + (u64)row_of(a.c, page, head, first) * (2 * a.c.width) + kind * a.c.width;
-    int8_t* exponent = a.c.exponents + ((u64)(page * a.c.kv_heads + head) * a.c.page_blocks + first / BLOCK) * 2 + kind;
-    const int held = *exponent;
+    const int left = __shfl_up(block, 1);
+    u64 firsts = __ballot(lane >= 1 && lane <= window && block >= 0 && block != left);
+    for (; firsts; firsts &= firsts - 1) {
+        const u32 at_lane = (u32)__builtin_ctzll(firsts);
+        const u64 t = t0 + at_lane - 1;
+        const int mine = __builtin_amdgcn_readlane(block, (int)at_lane);
+        const u64 same = __ballot(block == mine && lane >= at_lane && lane < at_lane + BLOCK) >> at_lane;
+        const u32 run = (u32)__builtin_ctzll(~same);
+        u32 present = 0;
+        for (u32 i = 0; i < run; ++i) present |= 1u << __builtin_amdgcn_readlane(place, (int)(at_lane + i));
+        const bool begins = present & 1u;
+        const u32 page = (u32)mine / a.c.page_blocks, first = (u32)mine % a.c.page_blocks * BLOCK;
+        uint8_t* rows = a.c.data + (u64)row_of(a.c, page, head, first) * (2 * a.c.width) + kind * a.c.width;
+        int8_t* exponent = a.c.exponents + ((u64)(page * a.c.kv_heads + head) * a.c.page_blocks + first / BLOCK) * 2 + kind;
+        const int held = *exponent;
 
-    float x[2 * C][8];
-    float most = 0.f;
-#pragma unroll
-    for (int n = 0; n < 2 * C; ++n) {
-        const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[n][j] = 0.f;
-        if (row < run && at < a.c.dim) load8(a.x[kind], (t + row) * (u64)a.ts[kind] + head * (u64)a.hs[kind] + at, a.dtype, x[n]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float y = fabsf(x[n][j]);
-            if (y <= 3.402823466e38f) most = fmaxf(most, y);
-        }
-    }
-    const int least = least_exponent<FMT>(wave_max(most));
-    const int e = begins ? least : max(least, held);
-    const float down = power(-e);
-#pragma unroll
-    for (int n = 0; n < 2 * C; ++n) {
-        const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
-        const int to = __shfl(place, (int)(row + 1));
-        if (row < run) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[n][j] *= down;
-            *(uint2*)(rows + (u64)to * (2 * a.c.width) + at) = make_uint2(encode4<FMT>(x[n]), encode4<FMT>(x[n] + 4));
-        }
-    }
-    if (begins || e > held) {
-        const float again = begins ? 0.f : power(max(held - e, -126));
+        float x[2 * C][8];
+        float most = 0.f;
 #pragma unroll
         for (int n = 0; n < 2 * C; ++n) {
             const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
-            if (!(present >> row & 1u)) {
-                uint2* p = (uint2*)(rows + (u64)row * (2 * a.c.width) + at);
-                uint2 w = make_uint2(0, 0);
-                if (!begins) {
-                    w = *p;
-                    float y[8];
-                    decode4<FMT>(w.x, y);
-                    decode4<FMT>(w.y, y + 4);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] *= again;
-                    w = make_uint2(encode4<FMT>(y), encode4<FMT>(y + 4));
-                }
-                *p = w;
+            for (int j = 0; j < 8; ++j) x[n][j] = 0.f;
+            if (row < run && at < a.c.dim) load8(a.x[kind], (t + row) * (u64)a.ts[kind] + head * (u64)a.hs[kind] + at, a.dtype, x[n]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float y = fabsf(x[n][j]);
+                if (y <= 3.402823466e38f) most = fmaxf(most, y);
             }
         }
+        const int least = least_exponent<FMT>(wave_max(most));
+        const int e = begins ? least : max(least, held);
+        const float down = power(-e);
+#pragma unroll
+        for (int n = 0; n < 2 * C; ++n) {
+            const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
+            const int to = __shfl(place, (int)(row + at_lane));
+            if (row < run) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[n][j] *= down;
+                *(uint2*)(rows + (u64)to * (2 * a.c.width) + at) = make_uint2(encode4<FMT>(x[n]), encode4<FMT>(x[n] + 4));
+            }
+        }
+        if (begins || e > held) {
+            const float again = begins ? 0.f : power(max(held - e, -126));
+#pragma unroll
+            for (int n = 0; n < 2 * C; ++n) {
+                const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
+                if (!(present >> row & 1u)) {
+                    uint2* p = (uint2*)(rows + (u64)row * (2 * a.c.width) + at);
+                    uint2 w = make_uint2(0, 0);
+                    if (!begins) {
+                        w = *p;
+                        float y[8];
+                        decode4<FMT>(w.x, y);
+                        decode4<FMT>(w.y, y + 4);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] *= again;
+                        w = make_uint2(encode4<FMT>(y), encode4<FMT>(y + 4));
+                    }
+                    *p = w;
+                }
+            }
+        }
+        if (lane == 0) *exponent = (int8_t)e;
     }
-    if (lane == 0) *exponent = (int8_t)e;
 }
 
 struct Load {
@@ -246,30 +254,62 @@ struct Load {
     void* x[2];
     int64_t ts[2], hs[2];
     const int64_t* slots;
-    u64 pieces;                // tokens * kv_heads * 2 * width / 8
+    u64 rows;                  // tokens * kv_heads
     u32 dtype;
 };
 
-// Eight numbers a thread.
-template <int FMT, int C>
+// A workgroup has 16 rows, keys and values, of 16 bytes of output a thread and turn: what a wave writes is one stretch of memory, and
+// all that a thread reads is asked for before the first of it is used.
+template <int FMT, int C, typename T>
 __global__ void __launch_bounds__(256) k_read(Load a) {
-    const u64 i = (u64)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.pieces) return;
-    const u32 piece = (u32)(i % (16 * C)), kind = piece / (8 * C), at = piece % (8 * C) * 8, head = (u32)(i / (16 * C) % a.c.kv_heads);
-    const u64 t = i / (16 * C) / a.c.kv_heads;
-    if (!a.x[kind] || at >= a.c.dim) return;
-    const int64_t slot = a.slots[t];
-    float x[8] = { 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f };
-    if (slot >= 0 && slot < (int64_t)a.c.num_pages * a.c.page_tokens) {
-        const u32 page = (u32)((u64)slot / a.c.page_tokens), place = (u32)((u64)slot % a.c.page_tokens);
-        const uint2 w = *(const uint2*)(a.c.data + (u64)row_of(a.c, page, head, place) * (2 * a.c.width) + kind * a.c.width + at);
-        const float up = power(a.c.exponents[((u64)(page * a.c.kv_heads + head) * a.c.page_blocks + place / BLOCK) * 2 + kind]);
-        decode4<FMT>(w.x, x);
-        decode4<FMT>(w.y, x + 4);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= up;
+    constexpr u32 EACH = 16 / sizeof(T), PIECES = 128 * C / EACH, TURNS = 16 * PIECES / 256;      // numbers, pieces of a row, turns
+    __shared__ u32 sh_row[16];
+    __shared__ float sh_up[16][2];
+    __shared__ u64 sh_token[16];
+    __shared__ u32 sh_head[16];
+    const u64 row0 = (u64)blockIdx.x * 16;
+    if (threadIdx.x < 16) {
+        const u64 r = min(row0 + threadIdx.x, a.rows - 1), t = r / a.c.kv_heads;
+        const u32 head = (u32)(r - t * a.c.kv_heads);
+        const int64_t slot = a.slots[t];
+        u32 row = 0;
+        float k = 0.f, v = 0.f;                  // zeros for slots that are none
+        if (slot >= 0 && slot < (int64_t)a.c.num_pages * a.c.page_tokens) {
+            row = row_of(a.c, (u32)((u64)slot / a.c.page_tokens), head, (u32)((u64)slot % a.c.page_tokens));
+            const int8_t* e = a.c.exponents + (u64)(row / BLOCK) * 2;
+            k = power(e[0]);
+            v = power(e[1]);
+        }
+        sh_row[threadIdx.x] = row;
+        sh_up[threadIdx.x][0] = k;
+        sh_up[threadIdx.x][1] = v;
+        sh_token[threadIdx.x] = t;
+        sh_head[threadIdx.x] = head;
     }
-    store8(a.x[kind], t * (u64)a.ts[kind] + head * (u64)a.hs[kind] + at, a.dtype, x);
+    __syncthreads();
+    u32 w[TURNS][EACH / 4];
+#pragma unroll
+    for (u32 n = 0; n < TURNS; ++n) {
+        const u32 i = threadIdx.x + 256 * n, r = i / PIECES, at = i % PIECES * EACH;
+#pragma unroll
+        for (u32 x = 0; x < EACH / 4; ++x) w[n][x] = *(const u32*)(a.c.data + (u64)sh_row[r] * (128 * C) + at + 4 * x);
+    }
+#pragma unroll
+    for (u32 n = 0; n < TURNS; ++n) {
+        const u32 i = threadIdx.x + 256 * n, r = i / PIECES, both = i % PIECES * EACH, kind = both / (64 * C), at = both % (64 * C);
+        if (row0 + r < a.rows && at < a.c.dim && a.x[kind]) {
+            const float up = sh_up[r][kind];
+            float x[EACH];
+#pragma unroll
+            for (u32 y = 0; y < EACH / 4; ++y) decode4<FMT>(w[n][y], x + 4 * y);
+            // a slot that is none has no numbers, whatever the row that was read instead holds
+#pragma unroll
+            for (u32 y = 0; y < EACH; ++y) x[y] = up != 0.f ? x[y] * up : 0.f;
+            T* to = (T*)a.x[kind] + (int64_t)sh_token[r] * a.ts[kind] + (int64_t)sh_head[r] * a.hs[kind] + at;
+            if constexpr (sizeof(T) == 4) *(float4*)to = make_float4(x[0], x[1], x[2], x[3]);
+            else *(uint4*)to = make_uint4(pack2(x[0], x[1], a.dtype), pack2(x[2], x[3], a.dtype), pack2(x[4], x[5], a.dtype), pack2(x[6], x[7], a.dtype));
+        }
+    }
 }
 
 // f<FMT, C>() for the cache's format and row width
@@ -290,9 +330,14 @@ void for_cache(const Cache& c, A&&... args) {
 }
 
 template <int FMT, int C>
-struct RunAppend { static void run(hipStream_t st, u32 grid, const Store& a) { k_append<FMT, C><<<grid, 256, 0, st>>>(a); } };
+struct RunAppend { static void run(hipStream_t st, u32 grid, const Store& a, u32 window) { k_append<FMT, C><<<grid, 256, 0, st>>>(a, window); } };
 template <int FMT, int C>
-struct RunRead { static void run(hipStream_t st, u32 grid, const Load& a) { k_read<FMT, C><<<grid, 256, 0, st>>>(a); } };
+struct RunRead {
+    static void run(hipStream_t st, u32 grid, const Load& a) {
+        if (a.dtype == PAG_F32) k_read<FMT, C, float><<<grid, 256, 0, st>>>(a);
+        else k_read<FMT, C, uint16_t><<<grid, 256, 0, st>>>(a);
+    }
+};
 
 int launched(const char* what) {
     const hipError_t e = hipGetLastError();
@@ -319,15 +364,17 @@ int launch_release(hipStream_t st, const pag_kv_tables& t, const int32_t* done) 
 int launch_append(hipStream_t st, const Cache& c, u32 dtype, const void* k, int64_t k_ts, int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs,
                   const int64_t* slots, u64 tokens) {
     const Store a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, tokens, dtype };
-    for_cache<RunAppend>(c, st, (u32)((tokens * 2 * c.kv_heads + 3) / 4), a);
+    const u64 waves = tokens * 2 * c.kv_heads;
+    const u32 window = waves <= 8192 ? 1 : waves <= 65536 ? 4 : 16;
+    for_cache<RunAppend>(c, st, (u32)(((tokens + window - 1) / window * 2 * c.kv_heads + 3) / 4), a, window);
     return launched("pag_kv_append");
 }
 
 int launch_read(hipStream_t st, const Cache& c, const int64_t* slots, u64 tokens, u32 dtype, void* k, int64_t k_ts, int64_t k_hs, void* v,
                 int64_t v_ts, int64_t v_hs) {
-    const u64 pieces = tokens * c.kv_heads * 2 * (c.width / 8);
-    const Load a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, pieces, dtype };
-    for_cache<RunRead>(c, st, (u32)((pieces + 255) / 256), a);
+    const u64 rows = tokens * c.kv_heads;
+    const Load a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, rows, dtype };
+    for_cache<RunRead>(c, st, (u32)((rows + 15) / 16), a);
     return launched("pag_kv_read");
 }
 
