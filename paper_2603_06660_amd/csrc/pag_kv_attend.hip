@@ -140,50 +140,50 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
             s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<FMT>(tile.k[b][h].z, tile.k[b][h].w), r.q[2 * h + 1], s[b], 0, 0, 0);
         }
     }
-    // t = score * log2 e + e of the values - offset, and the largest of them
+    // t = score * log2 e + e of the values - offset
+    const float base = r.M == LOWEST ? 0.f : r.M;
     float t[8];
-    const auto exponents = [&](float offset) {
-        if (a.softcap > 0.f) {
-            // tanh(y) = 1 - 2 / (1 + e^(2 y))
-            const float in = 2.f * LOG2E * r.factor / a.softcap, cap = a.softcap * LOG2E;
+    if (a.softcap > 0.f) {
+        // tanh(y) = 1 - 2 / (1 + e^(2 y))
+        const float in = 2.f * LOG2E * r.factor / a.softcap, cap = a.softcap * LOG2E;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = LISTED ? j : j >> 2;
-                const float z = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] * (in * x.ek[n]));
-                t[j] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + z), cap + (x.ev[n] - offset));
-            }
-        } else {
-            const float f = r.factor * LOG2E;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = LISTED ? j : j >> 2;
-                t[j] = __builtin_fmaf(s[j >> 2][j & 3], f * x.ek[n], x.ev[n] - offset);
-            }
+        for (int j = 0; j < 8; ++j) {
+            const int n = LISTED ? j : j >> 2;
+            const float z = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] * (in * x.ek[n]));
+            t[j] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + z), cap + (x.ev[n] - base));
         }
-        if (a.slopes) {
+    } else {
+        const float f = r.factor * LOG2E;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] -= r.slope * (float)(r.position - (LISTED ? x.at[LISTED ? j : 0] : x.at[j >> 2] + (j & 3)));
+        for (int j = 0; j < 8; ++j) {
+            const int n = LISTED ? j : j >> 2;
+            t[j] = __builtin_fmaf(s[j >> 2][j & 3], f * x.ek[n], x.ev[n] - base);
         }
-        if (masked) {
+    }
+    if (a.slopes) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = keep >> j & 1u ? t[j] : -INFINITY;
-        }
-        float most = fmaxf(t[0], t[1]);
+        for (int j = 0; j < 8; ++j) t[j] -= r.slope * (float)(r.position - (LISTED ? x.at[LISTED ? j : 0] : x.at[j >> 2] + (j & 3)));
+    }
+    if (masked) {
 #pragma unroll
-        for (int j = 2; j < 8; ++j) most = fmaxf(most, t[j]);
-        return most;
-    };
-    if (__ballot(exponents(r.M) > HEADROOM)) {
-        float most = exponents(0.f);
+        for (int j = 0; j < 8; ++j) t[j] = keep >> j & 1u ? t[j] : -INFINITY;
+    }
+    float most = fmaxf(t[0], t[1]);
+#pragma unroll
+    for (int j = 2; j < 8; ++j) most = fmaxf(most, t[j]);
+    if (__ballot(most > (r.M == LOWEST ? LOWEST : HEADROOM))) {
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
         // rows that need not move stay as they are: a row's result does not depend on its neighbours in the tile
-        const float M = most > r.M + HEADROOM ? most - START : r.M, alpha = __builtin_amdgcn_exp2f(r.M - M);
-        r.sum *= alpha;
+        if (most > (r.M == LOWEST ? LOWEST : HEADROOM)) {
+            const float up = most - START, M = base + up, alpha = __builtin_amdgcn_exp2f(r.M - M);
 #pragma unroll
-        for (int c = 0; c < 4 * C; ++c) r.acc[c] *= alpha;
-        r.M = M;
-        exponents(M);
+            for (int j = 0; j < 8; ++j) t[j] -= up;
+            r.sum *= alpha;
+#pragma unroll
+            for (int c = 0; c < 4 * C; ++c) r.acc[c] *= alpha;
+            r.M = M;
+        }
     }
     half8_t p;
 #pragma unroll

@@ -306,8 +306,11 @@ __global__ void __launch_bounds__(256) k_read(Load a) {
 #pragma unroll
             for (u32 y = 0; y < EACH; ++y) x[y] = up != 0.f ? x[y] * up : 0.f;
             T* to = (T*)a.x[kind] + (int64_t)sh_token[r] * a.ts[kind] + (int64_t)sh_head[r] * a.hs[kind] + at;
-            if constexpr (sizeof(T) == 4) *(float4*)to = make_float4(x[0], x[1], x[2], x[3]);
-            else *(uint4*)to = make_uint4(pack2(x[0], x[1], a.dtype), pack2(x[2], x[3], a.dtype), pack2(x[4], x[5], a.dtype), pack2(x[6], x[7], a.dtype));
+            typedef u32 word4 __attribute__((ext_vector_type(4)));
+            word4 y;
+            if constexpr (sizeof(T) == 4) y = word4{ __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]) };
+            else y = word4{ pack2(x[0], x[1], a.dtype), pack2(x[2], x[3], a.dtype), pack2(x[4], x[5], a.dtype), pack2(x[6], x[7], a.dtype) };
+            __builtin_nontemporal_store(y, (word4*)to);
         }
     }
 }

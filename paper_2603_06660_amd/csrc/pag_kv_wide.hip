@@ -73,9 +73,10 @@ struct Fetch {
     u32 v[N][8];
 };
 
-template <int FMT, int C>
+template <int FMT, int C, bool CAP>
 __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, Head* heads) {
     constexpr u32 W = 64 * C, KEYS = STEP * W, VALUES = W * STEP;
+    constexpr int KEY_TURNS = C == 2 ? 7 : 3;             // which pairs of pieces trade places in key_at
     extern __shared__ __align__(16) _Float16 lds[];       // two buffers of keys and values
     __shared__ float sh_scale[2][4][2];                   // 2^e of the keys' block, e of the values'
     __shared__ u32 sh_there[2][4];
@@ -277,6 +278,8 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
             }
         };
 
+        // where this lane's pieces of keys and values lie: the piece's number turns bits of the address, the token's or number's group adds to it
+        const u32 k_lds = key_at<C>(col, hi) * 2, v_lds = value_at(col, hi) * 2;
         const u32 steps = (u32)(max(stop - start, 0) + (int)STEP - 1) / STEP;
         __syncthreads();                                        // the piece before has been read
         if (steps) {
@@ -293,8 +296,10 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
                 fetch(n + 1);
             }
             if (busy && from <= w_p1 && from + (int)STEP > w_first) {
-                const _Float16* keys = lds + buffer * (KEYS + VALUES);
-                const _Float16* values = keys + KEYS;
+                const char* keys = (const char*)(lds + buffer * (KEYS + VALUES));
+                const char* values = keys + KEYS * 2;
+                // Both halves' scores are under way before the first of them is used: the matrix unit works on one half while the vector unit has
+                // the other.
                 float16_t S[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -302,80 +307,76 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
                     for (int i = 0; i < 16; ++i) S[h][i] = 0.f;
 #pragma unroll
                     for (int i = 0; i < 4 * C; ++i)
-                        S[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(keys + key_at<C>(h * 32 + col, 2 * i + hi)), Q[i], S[h], 0, 0, 0);
+                        S[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(keys + (k_lds ^ (i & KEY_TURNS) * 32) + (i & ~KEY_TURNS) * 32 + h * (32 * W * 2)), Q[i], S[h], 0, 0, 0);
                 }
-                float ev[4];
+                const u32 found = sh_there[buffer][0] | sh_there[buffer][1] << 1 | sh_there[buffer][2] << 2 | sh_there[buffer][3] << 3;
+                const bool masked = found != 15u || from + (int)STEP > w_p0 + 1 || from < w_full;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) ev[x] = sh_scale[buffer][x][1];
-                // key 32 h + 8 (i / 4) + 4 hi + i % 4 in S[h][i]; i / 8 is its block's half
-                if (a.softcap > 0.f) {
-                    const float in = 2.f * LOG2E * factor / a.softcap, cap = a.softcap * LOG2E;
+                for (int h = 0; h < 2; ++h) {
+                    float ek[2], ev[2];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const float by = in * sh_scale[buffer][x][0], top = cap + ev[x];
+                    for (int x = 0; x < 2; ++x) {
+                        ek[x] = sh_scale[buffer][2 * h + x][0];
+                        ev[x] = sh_scale[buffer][2 * h + x][1];
+                    }
+                    // key 32 h + 8 (i / 4) + 4 hi + i % 4 in S[h][i]; i / 8 is its block's half.  S becomes the weights' exponents.
+                    const float base = M == LOWEST ? 0.f : M;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float s = S[x >> 1][8 * (x & 1) + i];
-                            S[x >> 1][8 * (x & 1) + i] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * by)), top);
+                    for (int x = 0; x < 2; ++x) {
+                        if constexpr (CAP) {
+                            const float by = 2.f * LOG2E * factor / a.softcap * ek[x], cap = a.softcap * LOG2E, top = cap + (ev[x] - base);
+#pragma unroll
+                            for (int i = 8 * x; i < 8 * x + 8; ++i)
+                                S[h][i] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(S[h][i] * by)), top);
+                        } else {
+                            const float by = factor * LOG2E * ek[x], add = ev[x] - base;
+#pragma unroll
+                            for (int i = 8 * x; i < 8 * x + 8; ++i) S[h][i] = __builtin_fmaf(S[h][i], by, add);
                         }
                     }
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const float by = factor * LOG2E * sh_scale[buffer][x][0];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            S[x >> 1][8 * (x & 1) + i] = __builtin_fmaf(S[x >> 1][8 * (x & 1) + i], by, ev[x]);
-                        }
-                    }
-                }
-                if (a.slopes) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    if (a.slopes) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) S[h][i] -= slope * (float)(position - (from + h * 32 + 8 * (i >> 2) + 4 * (int)hi + (i & 3)));
                     }
-                }
-                const bool all = sh_there[buffer][0] & sh_there[buffer][1] & sh_there[buffer][2] & sh_there[buffer][3];
-                if (!all || from + (int)STEP > w_p0 + 1 || from < w_full) {
+                    if (masked) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const bool ok = sh_there[buffer][x];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int p = from + 16 * x + 8 * (i >> 2) + 4 * (int)hi + (i & 3);
-                            if (!ok || p > position || p < oldest) S[x >> 1][8 * (x & 1) + i] = -INFINITY;
+                        for (int i = 0; i < 16; ++i) {
+                            const int k = from + h * 32 + 8 * (i >> 2) + 4 * (int)hi + (i & 3);
+                            if (!(found >> (2 * h + (i >> 3)) & 1u) || k > position || k < oldest) S[h][i] = -INFINITY;
                         }
                     }
-                }
-                float most = fmaxf(S[0][0], S[1][0]);
+                    float most = fmaxf(S[h][0], S[h][1]);
 #pragma unroll
-                for (int i = 1; i < 16; ++i) most = fmaxf(most, fmaxf(S[0][i], S[1][i]));
-                if (__ballot(most > M + HEADROOM)) {
-                    most = fmaxf(most, __shfl_xor(most, 32));
-                    const float to = most > M + HEADROOM ? most - START : M, alpha = __builtin_amdgcn_exp2f(M - to);
-                    sum *= alpha;
+                    for (int i = 2; i < 16; ++i) most = fmaxf(most, S[h][i]);
+                    if (__ballot(most > (M == LOWEST ? LOWEST : HEADROOM))) {
+                        most = fmaxf(most, __shfl_xor(most, 32));
+                        if (most > (M == LOWEST ? LOWEST : HEADROOM)) {
+                            const float up = most - START, to = base + up, alpha = __builtin_amdgcn_exp2f(M - to);
 #pragma unroll
-                    for (int n = 0; n < 2 * C; ++n) acc[n] *= alpha;
-                    M = to;
-                }
-                half8_t P[4];
+                            for (int i = 0; i < 16; ++i) S[h][i] -= up;
+                            sum *= alpha;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    float part = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float y = __builtin_amdgcn_exp2f(S[x >> 1][8 * (x & 1) + i] - M);
-                        part += y;
-                        P[x][i] = (_Float16)y;
+                            for (int d = 0; d < 2 * C; ++d) acc[d] *= alpha;
+                            M = to;
+                        }
                     }
-                    sum = __builtin_fmaf(part, power(-(int)ev[x]), sum);
-                }
+                    half8_t P[2];
 #pragma unroll
-                for (int n = 0; n < 2 * C; ++n) {
+                    for (int x = 0; x < 2; ++x) {
+                        float part = 0.f;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(values + value_at(n * 32 + col, 2 * x + hi)), P[x], acc[n], 0, 0, 0);
+                        for (int i = 0; i < 8; ++i) {
+                            const float y = __builtin_amdgcn_exp2f(S[h][8 * x + i]);
+                            part = i ? part + y : y;
+                            P[x][i] = (_Float16)y;
+                        }
+                        sum = __builtin_fmaf(part, power(-(int)ev[x]), sum);
+                    }
+#pragma unroll
+                    for (int d = 0; d < 2 * C; ++d) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(values + (v_lds ^ (2 * h + x) * 32) + d * (32 * STEP * 2)), P[x], acc[d], 0, 0, 0);
+                    }
                 }
             }
             if (n + 1 < steps) stage(n + 1, from + (int)STEP, buffer ^ 1);
@@ -460,15 +461,22 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
 constexpr u32 groups_per_cu(u32 width) { return width <= 128 ? 2 : 1; }
 constexpr u32 lds_bytes(u32 width) { return 2 * 2 * STEP * width * 2; }
 
+template <int FMT, int C, bool CAP>
+int run_wide(hipStream_t st, const Attend& a, u32 grid, Head* heads) {
+    if (lds_bytes(64 * C) >= 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void*)k_attend_wide<FMT, C, CAP>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes(64 * C));
+        if (e != hipSuccess) { pag_set_error(std::string("hipFuncSetAttribute: ") + hipGetErrorString(e)); return PAG_EHIP; }
+    }
+    k_attend_wide<FMT, C, CAP><<<grid, 256, lds_bytes(64 * C), st>>>(a, heads);
+    return PAG_OK;
+}
+
 template <int FMT, int C>
 int run(hipStream_t st, const Attend& a, int num_cu) {
     const u32 grid = (u32)num_cu * groups_per_cu(64 * C);
     Head* heads = (Head*)(a.partial + 2ull * grid * ROWS * (64 * C + 2));
-    if (lds_bytes(64 * C) >= 65536) {
-        const hipError_t e = hipFuncSetAttribute((const void*)k_attend_wide<FMT, C>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes(64 * C));
-        if (e != hipSuccess) { pag_set_error(std::string("hipFuncSetAttribute: ") + hipGetErrorString(e)); return PAG_EHIP; }
-    }
-    k_attend_wide<FMT, C><<<grid, 256, lds_bytes(64 * C), st>>>(a, heads);
+    const int rc = a.softcap > 0.f ? run_wide<FMT, C, true>(st, a, grid, heads) : run_wide<FMT, C, false>(st, a, grid, heads);
+    if (rc) return rc;
     k_join_wide<C><<<dim3(grid, ROWS / 16), 256, 0, st>>>(a, heads);
     return PAG_OK;
 }
