@@ -30,6 +30,9 @@ struct Step {
     u32 requests, max_pages, tokens;
 };
 
+// the wave's number in its workgroup, in a scalar register: what follows from it takes none of the lanes'
+__device__ __forceinline__ u32 wave_of() { return (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
 // 2^e in 32 bits, -126 <= e <= 127
 __device__ __forceinline__ float power(int e) { return __uint_as_float((u32)(e + 127) << 23); }
 

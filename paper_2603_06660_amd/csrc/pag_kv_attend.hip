@@ -27,7 +27,7 @@ constexpr u32 UNIT = SPLIT_WAVES * TILE;  // and keys of the smallest share
 
 constexpr u32 PIECE = 4;                  // what beginning and ending a piece costs, in units
 
-constexpr u32 groups_per_cu(u32 width) { return width <= 128 ? 2 : 1; }
+constexpr u32 groups_per_cu(u32 width) { return width <= 64 ? 3 : width <= 128 ? 2 : 1; }
 
 // a lane's part of 32 keys: of row lane % 16 of both halves the 16-byte pieces lane / 16 + 4 h, and of tokens 4 (lane / 16) + 0 .. 3
 // of both halves the values' numbers 4 C (lane % 16) + 0 .. 4 C - 1
@@ -227,7 +227,7 @@ struct Exchange {
 // The waves' sums, into LDS, of the rows that there are.  All waves call it; the rows are free afterwards.
 template <int C, int NW>
 __device__ __forceinline__ void exchange(const Rows<C>& r, const Where& w, Exchange<C, NW>& x) {
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     float sum = r.sum;
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -341,7 +341,7 @@ __device__ __forceinline__ void place_piece(const Attend& a, Piece& p, const Spa
 // The pieces that next(p) gives, one after the other.  WHOLE: they are whole row tiles.
 template <int FMT, int C, int NW, bool WHOLE, typename Next>
 __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& sh, Next&& next) {
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     Piece p;
     Rows<C> rows;
     RawRows<C> raw;
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C)) k_attend(Attend a)
     __shared__ u64 sh_sum[SPLIT_WAVES];
     __shared__ u64 sh_begin;
     __shared__ u32 sh_b;
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u32 lane = threadIdx.x & 63, wave = wave_of();
 
     // this workgroup's share of all units
     const u32 per = (a.s.requests + 255) / 256, b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
@@ -602,7 +602,7 @@ __device__ __forceinline__ void place_list(const Attend& a, ListPiece& p, u64 li
 // The pieces that next(p) gives; a list has `units` units of 32 NW entries.
 template <int FMT, int C, int NW, bool WHOLE, typename Next>
 __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& sh, Entries (&sh_entries)[NW][2], u32 units, Next&& next) {
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     const u32 entries = a.k + a.window;
     ListPiece w = {};
     Rows<C> rows;
@@ -789,7 +789,7 @@ template <int C>
 __global__ void __launch_bounds__(256) k_join(Attend a, int groups) {
     __shared__ float sh_max[4], sh_by[256], sh_sum[4];
     __shared__ float sh_acc[4][64 * C];
-    const u32 t = blockIdx.x / a.heads, head = blockIdx.x % a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u32 t = blockIdx.x / a.heads, head = blockIdx.x % a.heads, lane = threadIdx.x & 63, wave = wave_of();
     const int2 j = a.joined[(u64)t * a.heads + head];
     if (j.x < 0 || j.y < j.x || j.y >= groups) return;
     u32 row = head % a.group;

@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
     __shared__ u64 sh_sum[4];
     __shared__ u64 sh_begin;
     __shared__ u32 sh_b;
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, hi = lane >> 5;
+    const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 31, hi = lane >> 5;
 
     // this workgroup's share
     const u32 per = (a.s.requests + 255) / 256, b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
@@ -298,38 +298,58 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
             if (busy && from <= w_p1 && from + (int)STEP > w_first) {
                 const char* keys = (const char*)(lds + buffer * (KEYS + VALUES));
                 const char* values = keys + KEYS * 2;
+                float ek[4], ev[4];
+                u32 found = 0;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    ek[x] = sh_scale[buffer][x][0];
+                    ev[x] = sh_scale[buffer][x][1];
+                    found |= sh_there[buffer][x] << x;
+                }
                 // Both halves' scores are under way before the first of them is used: the matrix unit works on one half while the vector unit has
-                // the other.
+                // the other.  Pieces are asked for AHEAD of their products; left alone, the compiler asks for each right before it, to save
+                // registers, and a product then waits for LDS every time (uncapped chunks 603 us, with this order ORDERED).
+                constexpr int AHEAD = 4, PRODUCTS = 8 * C;
+                const auto key_piece = [&](int n) {
+                    const int h = n / (4 * C), i = n % (4 * C);
+                    return *(const half8_t*)(keys + (k_lds ^ (i & KEY_TURNS) * 32) + (i & ~KEY_TURNS) * 32 + h * (32 * W * 2));
+                };
                 float16_t S[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) S[h][i] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 4 * C; ++i)
-                        S[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(keys + (k_lds ^ (i & KEY_TURNS) * 32) + (i & ~KEY_TURNS) * 32 + h * (32 * W * 2)), Q[i], S[h], 0, 0, 0);
                 }
-                const u32 found = sh_there[buffer][0] | sh_there[buffer][1] << 1 | sh_there[buffer][2] << 2 | sh_there[buffer][3] << 3;
+                {
+                    half8_t piece[AHEAD];
+#pragma unroll
+                    for (int n = 0; n < AHEAD; ++n) piece[n] = key_piece(n);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int n = 0; n < PRODUCTS; ++n) {
+                        S[n / (4 * C)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(piece[n % AHEAD], Q[n % (4 * C)], S[n / (4 * C)], 0, 0, 0);
+                        if (n + AHEAD < PRODUCTS) piece[n % AHEAD] = key_piece(n + AHEAD);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
                 const bool masked = found != 15u || from + (int)STEP > w_p0 + 1 || from < w_full;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float ek[2], ev[2];
+                    const auto value_piece = [&](int n) { return *(const half8_t*)(values + (v_lds ^ (2 * h + n / (2 * C)) * 32) + n % (2 * C) * (32 * STEP * 2)); };
+                    half8_t piece[AHEAD];
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        ek[x] = sh_scale[buffer][2 * h + x][0];
-                        ev[x] = sh_scale[buffer][2 * h + x][1];
-                    }
+                    for (int n = 0; n < (AHEAD < 4 * C ? AHEAD : 4 * C); ++n) piece[n] = value_piece(n);
                     // key 32 h + 8 (i / 4) + 4 hi + i % 4 in S[h][i]; i / 8 is its block's half.  S becomes the weights' exponents.
                     const float base = M == LOWEST ? 0.f : M;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         if constexpr (CAP) {
-                            const float by = 2.f * LOG2E * factor / a.softcap * ek[x], cap = a.softcap * LOG2E, top = cap + (ev[x] - base);
+                            const float by = 2.f * LOG2E * factor / a.softcap * ek[2 * h + x], cap = a.softcap * LOG2E, top = cap + (ev[2 * h + x] - base);
 #pragma unroll
                             for (int i = 8 * x; i < 8 * x + 8; ++i)
                                 S[h][i] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(S[h][i] * by)), top);
                         } else {
-                            const float by = factor * LOG2E * ek[x], add = ev[x] - base;
+                            const float by = factor * LOG2E * ek[2 * h + x], add = ev[2 * h + x] - base;
 #pragma unroll
                             for (int i = 8 * x; i < 8 * x + 8; ++i) S[h][i] = __builtin_fmaf(S[h][i], by, add);
                         }
@@ -370,12 +390,14 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
                             part = i ? part + y : y;
                             P[x][i] = (_Float16)y;
                         }
-                        sum = __builtin_fmaf(part, power(-(int)ev[x]), sum);
+                        sum = __builtin_fmaf(part, power(-(int)ev[2 * h + x]), sum);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int d = 0; d < 2 * C; ++d) {
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8_t*)(values + (v_lds ^ (2 * h + x) * 32) + d * (32 * STEP * 2)), P[x], acc[d], 0, 0, 0);
+                    for (int n = 0; n < 4 * C; ++n) {
+                        acc[n % (2 * C)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(piece[n % AHEAD], P[n / (2 * C)], acc[n % (2 * C)], 0, 0, 0);
+                        if (n + AHEAD < 4 * C) piece[n % AHEAD] = value_piece(n + AHEAD);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
