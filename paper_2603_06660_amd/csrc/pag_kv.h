@@ -128,7 +128,9 @@ struct Attend {
     const float* slopes;
     const int64_t* ids;
     int64_t q_ts, q_hs, o_ts, o_hs, ids_ts, ids_hs;
-    u32 heads, group, dtype, window, id_heads, k, listed;      // listed: attention over ids and a window
+    u32 heads, group, dtype, window, id_heads, k;
+    u32 listed;                           // attention over ids and a window
+    u32 row_tiles;                        // tiles of 16 query rows that a wave has at most to a key/value head; 0: the wide kernel
     float scale, softcap;
     float* partial;                       // the workspace: two parts a workgroup, of the piece that another one began, and of the piece that it began and another one ends
     int2* joined;                         // narrow kernels: [tokens * heads] first and last workgroup of the row's pieces; first < 0: written whole
@@ -144,7 +146,7 @@ int launch_attend(hipStream_t st, const Attend& a, int num_cu);
 
 int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu);
 
-u64 narrow_workspace(const Attend& a, int num_cu);      // bytes
+u64 attend_workspace(const Attend& a, int num_cu);      // bytes
 u64 wide_workspace(u32 width, int num_cu);
 int num_cu_of_current();                        // < 0: no GPU
 

@@ -61,10 +61,10 @@ int check_tables(const pag_kv_tables* t) {
     return PAG_OK;
 }
 
-// Whether a request has more query rows to a key/value head than a tile of the narrow kernel.
-bool many_rows(const pag_kv_step* s, u32 group) {
+// How many tiles of 16 query rows a request's new tokens make for a key/value head, as far as the host can tell.
+u32 row_tiles_of(const pag_kv_step* s, u32 group) {
     const u64 tokens = s->max_new ? s->max_new : (s->tokens + s->requests - 1) / s->requests;
-    return tokens * group > 16;
+    return tokens * group <= 16 ? 1 : tokens * group <= 32 ? 2 : 0;
 }
 
 int check_rows(const void* p, int64_t token_stride, int64_t head_stride, u32 bytes, u32 to, const char* message) {
@@ -96,11 +96,8 @@ int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_a
         a->k = k;
         a->group = a->heads / id_heads;
     }
+    a->row_tiles = selected ? 1 : row_tiles_of(step, a->group);
     return PAG_OK;
-}
-
-u64 workspace_of(const Attend& a, const pag_kv_step* step, int num_cu) {
-    return !a.listed && many_rows(step, a.group) ? wide_workspace(a.c.width, num_cu) : narrow_workspace(a, num_cu);
 }
 
 int arrays_of(const pag_kv_step* step, const pag_kv_attention* args, Attend* a, int* num_cu) {
@@ -115,7 +112,7 @@ int arrays_of(const pag_kv_step* step, const pag_kv_attention* args, Attend* a, 
               "workspace is null but has a size, or is not 16-byte aligned");
     *num_cu = num_cu_of_current();
     PAG_CHECK(*num_cu > 0, PAG_EHIP, "no current GPU");
-    const u64 need = workspace_of(*a, step, *num_cu);
+    const u64 need = attend_workspace(*a, *num_cu);
     PAG_CHECK(need == 0 || (args->workspace != nullptr && args->workspace_bytes >= need), PAG_EINVAL, "workspace is null or smaller than pag_kv_workspace_bytes");
     a->q = args->q; a->q_ts = args->q_token_stride; a->q_hs = args->q_head_stride;
     a->out = args->out; a->o_ts = args->out_token_stride; a->o_hs = args->out_head_stride;
@@ -197,7 +194,7 @@ extern "C" int pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_st
         PAG_CHECK(bytes != nullptr, PAG_EINVAL, "bytes is null");
         const int num_cu = num_cu_of_current();
         PAG_CHECK(num_cu > 0, PAG_EHIP, "no current GPU");
-        *bytes = workspace_of(a, step, num_cu);
+        *bytes = attend_workspace(a, num_cu);
         return PAG_OK;
     });
 }
@@ -208,7 +205,7 @@ extern "C" int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step,
         int num_cu = 0, rc;
         if ((rc = layout_of(cache, step, args, false, 0, 0, &a)) || (rc = arrays_of(step, args, &a, &num_cu)) || step->tokens == 0) return rc;
         PAG_CHECK(step->offsets && step->context, PAG_EINVAL, "step: offsets or context is null");
-        return many_rows(step, a.group) ? launch_attend_wide((hipStream_t)stream, a, num_cu) : launch_attend((hipStream_t)stream, a, num_cu);
+        return launch_attend((hipStream_t)stream, a, num_cu);
     });
 }
 

@@ -114,3 +114,21 @@ __device__ __forceinline__ void write_padding(const Attend& a) {
 }
 
 }  // namespace pagkv
+
+namespace pagkv {
+
+// shapes of the kernels for few query rows to a key
+constexpr u32 ROWS = 16;                  // query rows of a tile
+constexpr u32 TILE = 32;                  // keys of a tile
+constexpr u32 SPLIT_WAVES = 4;            // waves of a workgroup whose keys are a share of all,
+constexpr u32 UNIT = SPLIT_WAVES * TILE;  // and keys of the smallest share
+
+constexpr u32 PIECE = 4;                  // what beginning and ending a piece costs, in units
+
+constexpr u32 groups_per_cu(u32 width, int t) { return width > 128 ? 1 : width == 64 && t == 1 ? 3 : 2; }
+
+u64 narrow_groups(const Attend& a);        // workgroups, where one reads all keys of its rows
+template <int FMT, int C>
+void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole);
+
+}  // namespace pagkv

@@ -12,7 +12,7 @@ namespace pagkv {
 namespace {
 
 constexpr u32 WROWS = 32;                   // query rows of a wave
-constexpr u32 ROWS = 4 * WROWS;             // of a workgroup
+constexpr u32 WIDE_ROWS = 4 * WROWS;             // of a workgroup
 constexpr u32 STEP = 64;                    // keys of a step, one block of 16 a wave to fetch
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
@@ -27,8 +27,8 @@ struct Range { int start, stop, p0, p1; u32 units; };
 
 __device__ __forceinline__ Range range_of(const Attend& a, const Span& s, u32 rows, u32 tile) {
     Range r;
-    r.p0 = s.first + (int)(tile * ROWS / a.group);
-    r.p1 = s.first + (int)(min(tile * ROWS + ROWS - 1, rows - 1) / a.group);
+    r.p0 = s.first + (int)(tile * WIDE_ROWS / a.group);
+    r.p1 = s.first + (int)(min(tile * WIDE_ROWS + WIDE_ROWS - 1, rows - 1) / a.group);
     r.start = a.window ? max(0, r.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) & ~(int)(BLOCK - 1) : 0;
     r.stop = max(r.p1 + 1, r.start);
     r.units = max(((u32)(r.stop - r.start) + STEP - 1) / STEP, 1u);
@@ -39,12 +39,12 @@ __device__ __forceinline__ Tiles tiles_of(const Attend& a, u32 b) {
     Tiles t;
     t.s = span_of(a, b);
     t.rows = t.s.tokens * a.group;
-    t.count = t.s.context ? (t.rows + ROWS - 1) / ROWS : 0;
+    t.count = t.s.context ? (t.rows + WIDE_ROWS - 1) / WIDE_ROWS : 0;
     t.pairs = t.count / 2;
     t.mid_units = t.count & 1 ? range_of(a, t.s, t.rows, t.pairs).units : 0;
     // no pair is longer: two ends of tiles that lie opposite add up to the same, and each is rounded up once
-    u64 most = (2 * (u64)max(t.s.first + 1, 0) + ((u64)ROWS * (t.count ? t.count - 1 : 0) + 2 * (ROWS - 1)) / a.group + 1) / STEP + 2;
-    if (a.window) most = min(most, 2 * (((u64)a.window + (ROWS - 1) / a.group + 1 + BLOCK - 1 + STEP - 1) / STEP));
+    u64 most = (2 * (u64)max(t.s.first + 1, 0) + ((u64)WIDE_ROWS * (t.count ? t.count - 1 : 0) + 2 * (WIDE_ROWS - 1)) / a.group + 1) / STEP + 2;
+    if (a.window) most = min(most, 2 * (((u64)a.window + (WIDE_ROWS - 1) / a.group + 1 + BLOCK - 1 + STEP - 1) / STEP));
     t.pair_units = (u32)max(most, (u64)2);
     t.units = (u64)t.pairs * t.pair_units + t.mid_units;
     return t;
@@ -161,10 +161,10 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         const int start = r.start + (int)(u0 * STEP), stop = min(r.stop, start + (int)((u1 - u0) * STEP));
 
         // this wave's rows
-        const u32 row = tile * ROWS + wave * WROWS + col, token = row / a.group, head = kv_head * a.group + row % a.group;
+        const u32 row = tile * WIDE_ROWS + wave * WROWS + col, token = row / a.group, head = kv_head * a.group + row % a.group;
         const bool real = row < q.rows;
         const int position = real ? q.s.first + (int)token : -1;
-        const u32 w_row = tile * ROWS + wave * WROWS;
+        const u32 w_row = tile * WIDE_ROWS + wave * WROWS;
         const bool busy = w_row < q.rows;                   // the wave has rows
         const int w_p0 = q.s.first + (int)(min(w_row, q.rows - 1) / a.group), w_p1 = q.s.first + (int)(min(w_row + WROWS - 1, q.rows - 1) / a.group);
         const int oldest = a.window ? max(0, position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
@@ -423,18 +423,18 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
                 if (a.lse && hi == 0) a.lse[(u64)(q.s.t0 + token) * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
             }
         } else {
-            float* partial = a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (ROWS * (W + 2));
+            float* partial = a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (WIDE_ROWS * (W + 2));
             const u32 r_here = wave * WROWS + col;
-            if (hi == 0) { partial[r_here] = M; partial[ROWS + r_here] = sum; }
+            if (hi == 0) { partial[r_here] = M; partial[WIDE_ROWS + r_here] = sum; }
 #pragma unroll
             for (int n = 0; n < 2 * C; ++n) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *(float4*)(partial + 2 * ROWS + r_here * W + n * 32 + 8 * i + 4 * hi) = make_float4(acc[n][4 * i], acc[n][4 * i + 1], acc[n][4 * i + 2], acc[n][4 * i + 3]);
+                    *(float4*)(partial + 2 * WIDE_ROWS + r_here * W + n * 32 + 8 * i + 4 * hi) = make_float4(acc[n][4 * i], acc[n][4 * i + 1], acc[n][4 * i + 2], acc[n][4 * i + 3]);
             }
             if (begun && threadIdx.x == 0) {
                 Head h;
-                h.t0 = q.s.t0; h.rows = q.rows; h.row0 = tile * ROWS; h.head0 = kv_head * a.group;
+                h.t0 = q.s.t0; h.rows = q.rows; h.row0 = tile * WIDE_ROWS; h.head0 = kv_head * a.group;
                 h.last = (int)(((at + r.units) * parts - 1) / total);       // the workgroup of the tile's last unit
                 heads[blockIdx.x] = h;
             }
@@ -443,44 +443,85 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
     }
 }
 
-// Adds up the pieces of a tile that several workgroups had: workgroup (g, y) rows 16 y to 16 y + 15 of the tile that g began
+// Adds up the pieces of a tile that several workgroups had: workgroup (g, y) the rows 4 y to 4 y + 3 of the tile that g began.  Its waves take
+// every fourth piece, four of them asked for at a time (a request's 32 rows over 20,000 keys are in hundreds of pieces).
 template <int C>
 __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) {
-    constexpr u32 W = 64 * C, SLOT = ROWS * (W + 2);
+    constexpr u32 W = 64 * C, SLOT = WIDE_ROWS * (W + 2), N = 4 * C, THREADS = 16;      // numbers of a lane, lanes of a row
+    __shared__ float sh_m[4][4], sh_s[4][4];
+    __shared__ __align__(16) float sh_acc[4][4][W];
     const Head h = heads[blockIdx.x];
     if (h.last <= (int)blockIdx.x || h.last >= (int)gridDim.x) return;
-    const u32 r = blockIdx.y * 16 + (threadIdx.x >> 4), first = (threadIdx.x & 15) * 4 * C, row = h.row0 + r;
-    if (row >= h.rows) return;
-    float M = LOWEST, sum = 0.f, acc[4 * C];
+    const u32 lane = threadIdx.x & 63, wave = wave_of(), r = lane / THREADS, row0 = blockIdx.y * 4, first = lane % THREADS * N;
+    if (h.row0 + row0 >= h.rows) return;
+    const int pieces = h.last - (int)blockIdx.x + 1;
+    float M = LOWEST, sum = 0.f, acc[N];
 #pragma unroll
-    for (int c = 0; c < 4 * C; ++c) acc[c] = 0.f;
-    for (int g = (int)blockIdx.x; g <= h.last; ++g) {
-        const float* p = a.partial + (2 * (u64)g + (g == (int)blockIdx.x ? 1 : 0)) * SLOT;
-        const float m = p[r], s = p[ROWS + r], top = fmaxf(M, m);
-        const float was = __builtin_amdgcn_exp2f(M - top), is = __builtin_amdgcn_exp2f(m - top);
-        sum = sum * was + s * is;
+    for (u32 n = 0; n < N; ++n) acc[n] = 0.f;
+    for (int i = (int)wave; i < pieces; i += 16) {
+        float m[4], s[4];
+        float4 y[4][C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const float4 y = *(const float4*)(p + 2 * ROWS + r * W + first + 4 * c);
-            acc[4 * c] = acc[4 * c] * was + y.x * is;
-            acc[4 * c + 1] = acc[4 * c + 1] * was + y.y * is;
-            acc[4 * c + 2] = acc[4 * c + 2] * was + y.z * is;
-            acc[4 * c + 3] = acc[4 * c + 3] * was + y.w * is;
+        for (int u = 0; u < 4; ++u) {
+            const int k = min(i + 4 * u, pieces - 1);
+            const float* p = a.partial + (2 * ((u64)blockIdx.x + (u32)k) + (k == 0 ? 1 : 0)) * SLOT;
+            m[u] = i + 4 * u < pieces ? p[row0 + r] : LOWEST;
+            s[u] = p[WIDE_ROWS + row0 + r];
+#pragma unroll
+            for (int c = 0; c < C; ++c) y[u][c] = *(const float4*)(p + 2 * WIDE_ROWS + (row0 + r) * W + first + 4 * c);
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) top = fmaxf(top, m[u]);
+        const float was = __builtin_amdgcn_exp2f(M - top);
+        sum *= was;
+#pragma unroll
+        for (u32 n = 0; n < N; ++n) acc[n] *= was;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i + 4 * u >= pieces) break;
+            const float is = __builtin_amdgcn_exp2f(m[u] - top);
+            sum = __builtin_fmaf(s[u], is, sum);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                acc[4 * c] = __builtin_fmaf(y[u][c].x, is, acc[4 * c]);
+                acc[4 * c + 1] = __builtin_fmaf(y[u][c].y, is, acc[4 * c + 1]);
+                acc[4 * c + 2] = __builtin_fmaf(y[u][c].z, is, acc[4 * c + 2]);
+                acc[4 * c + 3] = __builtin_fmaf(y[u][c].w, is, acc[4 * c + 3]);
+            }
         }
         M = top;
     }
-    const u32 t = h.t0 + row / a.group, head = h.head0 + row % a.group;
-    const float by = sum != 0.f ? 1.f / sum : 0.f;
-    uint16_t* out = (uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + first;
+    if (lane % THREADS == 0) { sh_m[wave][r] = M; sh_s[wave][r] = sum; }
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        if (first + 4 * c < a.c.dim)
-            *(uint2*)(out + 4 * c) = make_uint2(pack2(acc[4 * c] * by, acc[4 * c + 1] * by, a.dtype), pack2(acc[4 * c + 2] * by, acc[4 * c + 3] * by, a.dtype));
+    for (int c = 0; c < C; ++c) *(float4*)&sh_acc[wave][r][first + 4 * c] = make_float4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+    __syncthreads();
+    // a wave a row
+    const u32 row = h.row0 + row0 + wave;
+    if (row >= h.rows) return;
+    const float top = fmaxf(fmaxf(sh_m[0][wave], sh_m[1][wave]), fmaxf(sh_m[2][wave], sh_m[3][wave]));
+    float by[4], all = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        by[x] = __builtin_amdgcn_exp2f(sh_m[x][wave] - top);
+        all = __builtin_fmaf(sh_s[x][wave], by[x], all);
     }
-    if (a.lse && first == 0) a.lse[(u64)t * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
+    const u32 t = h.t0 + row / a.group, head = h.head0 + row % a.group;
+    const float f = all != 0.f ? 1.f / all : 0.f;
+    uint16_t* out = (uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs;
+    for (u32 d = 2 * lane; d < a.c.dim; d += 128) {
+        float o[2] = { 0.f, 0.f };
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            o[0] = __builtin_fmaf(sh_acc[x][wave][d], by[x], o[0]);
+            o[1] = __builtin_fmaf(sh_acc[x][wave][d + 1], by[x], o[1]);
+        }
+        *(u32*)(out + d) = pack2(o[0] * f, o[1] * f, a.dtype);
+    }
+    if (a.lse && lane == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }
 
-constexpr u32 groups_per_cu(u32 width) { return width <= 128 ? 2 : 1; }
+constexpr u32 wide_groups_per_cu(u32 width) { return width <= 128 ? 2 : 1; }
 constexpr u32 lds_bytes(u32 width) { return 2 * 2 * STEP * width * 2; }
 
 template <int FMT, int C, bool CAP>
@@ -495,19 +536,19 @@ int run_wide(hipStream_t st, const Attend& a, u32 grid, Head* heads) {
 
 template <int FMT, int C>
 int run(hipStream_t st, const Attend& a, int num_cu) {
-    const u32 grid = (u32)num_cu * groups_per_cu(64 * C);
-    Head* heads = (Head*)(a.partial + 2ull * grid * ROWS * (64 * C + 2));
+    const u32 grid = (u32)num_cu * wide_groups_per_cu(64 * C);
+    Head* heads = (Head*)(a.partial + 2ull * grid * WIDE_ROWS * (64 * C + 2));
     const int rc = a.softcap > 0.f ? run_wide<FMT, C, true>(st, a, grid, heads) : run_wide<FMT, C, false>(st, a, grid, heads);
     if (rc) return rc;
-    k_join_wide<C><<<dim3(grid, ROWS / 16), 256, 0, st>>>(a, heads);
+    k_join_wide<C><<<dim3(grid, WIDE_ROWS / 4), 256, 0, st>>>(a, heads);
     return PAG_OK;
 }
 
 }  // namespace
 
 u64 wide_workspace(u32 width, int num_cu) {
-    const u64 grid = (u64)num_cu * groups_per_cu(width);
-    return 4 * 2 * grid * ROWS * (width + 2) + (grid * sizeof(Head) + 15) / 16 * 16;
+    const u64 grid = (u64)num_cu * wide_groups_per_cu(width);
+    return 4 * 2 * grid * WIDE_ROWS * (width + 2) + (grid * sizeof(Head) + 15) / 16 * 16;
 }
 
 int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu) {
