@@ -64,7 +64,7 @@ int check_tables(const pag_kv_tables* t) {
 // How many tiles of 16 query rows a request's new tokens make for a key/value head, as far as the host can tell.
 u32 row_tiles_of(const pag_kv_step* s, u32 group) {
     const u64 tokens = s->max_new ? s->max_new : (s->tokens + s->requests - 1) / s->requests;
-    return tokens * group <= 16 ? 1 : tokens * group <= 32 ? 2 : 0;
+    return tokens * group <= 16 ? 1 : tokens * group <= 64 ? 2 : 0;
 }
 
 int check_rows(const void* p, int64_t token_stride, int64_t head_stride, u32 bytes, u32 to, const char* message) {
