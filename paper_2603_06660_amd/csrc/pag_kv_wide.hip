@@ -85,6 +85,9 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
     __shared__ u32 sh_b;
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 31, hi = lane >> 5;
 
+    // Workgroups go to the chip's parts (each with an L2 of its own) in turn; neighbouring shares, which read the same keys, go to one part
+    const u32 self = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+
     // this workgroup's share
     const u32 per = (a.s.requests + 255) / 256, b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
     u64 mine = 0;
@@ -103,7 +106,7 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         total += sh_sum[x];
     }
     const u32 parts = (u32)min((u64)gridDim.x, total);
-    const u64 begin = blockIdx.x < parts ? share(total, parts, blockIdx.x) : total, end = blockIdx.x < parts ? share(total, parts, blockIdx.x + 1) : total;
+    const u64 begin = self < parts ? share(total, parts, self) : total, end = self < parts ? share(total, parts, self + 1) : total;
     if (begin < end && begin >= upto - mine && begin < upto) {
         u64 before = upto - mine;
         u32 b = b0;
@@ -115,12 +118,12 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         sh_b = b;
         sh_begin = before;
     }
-    for (u32 b = blockIdx.x; b < a.s.requests; b += gridDim.x) {
+    for (u32 b = self; b < a.s.requests; b += gridDim.x) {
         const Span s = span_of(a, b);
         if (s.tokens && !s.context) write_empty(a, s.t0, s.t0 + s.tokens);
     }
     write_padding(a);
-    if (threadIdx.x == 0) heads[blockIdx.x].last = -1;
+    if (threadIdx.x == 0) heads[self].last = -1;
     if (begin >= end) return;
     __syncthreads();
     u32 b = sh_b;
@@ -423,7 +426,7 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
                 if (a.lse && hi == 0) a.lse[(u64)(q.s.t0 + token) * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
             }
         } else {
-            float* partial = a.partial + (2 * (u64)blockIdx.x + (begun ? 1 : 0)) * (WIDE_ROWS * (W + 2));
+            float* partial = a.partial + (2 * (u64)self + (begun ? 1 : 0)) * (WIDE_ROWS * (W + 2));
             const u32 r_here = wave * WROWS + col;
             if (hi == 0) { partial[r_here] = M; partial[WIDE_ROWS + r_here] = sum; }
 #pragma unroll
@@ -436,7 +439,7 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
                 Head h;
                 h.t0 = q.s.t0; h.rows = q.rows; h.row0 = tile * WIDE_ROWS; h.head0 = kv_head * a.group;
                 h.last = (int)(((at + r.units) * parts - 1) / total);       // the workgroup of the tile's last unit
-                heads[blockIdx.x] = h;
+                heads[self] = h;
             }
         }
         at += u1 - u0;
