@@ -131,6 +131,7 @@ struct Attend {
     u32 heads, group, dtype, window, id_heads, k;
     u32 listed;                           // attention over ids and a window
     u32 row_tiles;                        // tiles of 16 query rows that a wave has at most to a key/value head; 0: the wide kernel
+    u32 many_rows;                        // the wide kernel: a request has more rows than four of its waves
     float scale, softcap;
     float* partial;                       // the workspace: two parts a workgroup, of the piece that another one began, and of the piece that it began and another one ends
     int2* joined;                         // narrow kernels: [tokens * heads] first and last workgroup of the row's pieces; first < 0: written whole

@@ -61,12 +61,6 @@ int check_tables(const pag_kv_tables* t) {
     return PAG_OK;
 }
 
-// How many tiles of 16 query rows a request's new tokens make for a key/value head, as far as the host can tell.
-u32 row_tiles_of(const pag_kv_step* s, u32 group) {
-    const u64 tokens = s->max_new ? s->max_new : (s->tokens + s->requests - 1) / s->requests;
-    return tokens * group <= 16 ? 1 : tokens * group <= 64 ? 2 : 0;
-}
-
 int check_rows(const void* p, int64_t token_stride, int64_t head_stride, u32 bytes, u32 to, const char* message) {
     PAG_CHECK(aligned(p, to) && token_stride * (int64_t)bytes % (int64_t)to == 0 && head_stride * (int64_t)bytes % (int64_t)to == 0, PAG_EINVAL, message);
     return PAG_OK;
@@ -96,7 +90,10 @@ int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_a
         a->k = k;
         a->group = a->heads / id_heads;
     }
-    a->row_tiles = selected ? 1 : row_tiles_of(step, a->group);
+    // query rows that a request's new tokens make for a key/value head, as far as the host can tell
+    const u64 rows = (step->max_new ? step->max_new : (step->tokens + step->requests - 1) / step->requests) * (u64)a->group;
+    a->row_tiles = selected || rows <= 16 ? 1 : rows <= 64 ? 2 : 0;
+    a->many_rows = rows > 128;
     return PAG_OK;
 }
 

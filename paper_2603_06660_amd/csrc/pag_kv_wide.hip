@@ -6,13 +6,14 @@
 // so that weights go back in from their registers as in the narrow kernel.  The next 64 keys are on their way from memory
 // meanwhile.  Shares are counted in steps of 64 keys of the tiles' own causal lengths: tile j and the j-th from the end make a pair,
 // and all pairs of a request are equally long, so that a share is found without adding up tiles.
+#include <algorithm>
+
 #include "pag_kv_attend.h"
 
 namespace pagkv {
 namespace {
 
 constexpr u32 WROWS = 32;                   // query rows of a wave
-constexpr u32 WIDE_ROWS = 4 * WROWS;             // of a workgroup
 constexpr u32 STEP = 64;                    // keys of a step, one block of 16 a wave to fetch
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
@@ -25,26 +26,28 @@ struct Tiles {
 
 struct Range { int start, stop, p0, p1; u32 units; };
 
+template <int NW>
 __device__ __forceinline__ Range range_of(const Attend& a, const Span& s, u32 rows, u32 tile) {
     Range r;
-    r.p0 = s.first + (int)(tile * WIDE_ROWS / a.group);
-    r.p1 = s.first + (int)(min(tile * WIDE_ROWS + WIDE_ROWS - 1, rows - 1) / a.group);
+    r.p0 = s.first + (int)(tile * (NW * WROWS) / a.group);
+    r.p1 = s.first + (int)(min(tile * (NW * WROWS) + (NW * WROWS) - 1, rows - 1) / a.group);
     r.start = a.window ? max(0, r.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) & ~(int)(BLOCK - 1) : 0;
     r.stop = max(r.p1 + 1, r.start);
     r.units = max(((u32)(r.stop - r.start) + STEP - 1) / STEP, 1u);
     return r;
 }
 
+template <int NW>
 __device__ __forceinline__ Tiles tiles_of(const Attend& a, u32 b) {
     Tiles t;
     t.s = span_of(a, b);
     t.rows = t.s.tokens * a.group;
-    t.count = t.s.context ? (t.rows + WIDE_ROWS - 1) / WIDE_ROWS : 0;
+    t.count = t.s.context ? (t.rows + (NW * WROWS) - 1) / (NW * WROWS) : 0;
     t.pairs = t.count / 2;
-    t.mid_units = t.count & 1 ? range_of(a, t.s, t.rows, t.pairs).units : 0;
+    t.mid_units = t.count & 1 ? range_of<NW>(a, t.s, t.rows, t.pairs).units : 0;
     // no pair is longer: two ends of tiles that lie opposite add up to the same, and each is rounded up once
-    u64 most = (2 * (u64)max(t.s.first + 1, 0) + ((u64)WIDE_ROWS * (t.count ? t.count - 1 : 0) + 2 * (WIDE_ROWS - 1)) / a.group + 1) / STEP + 2;
-    if (a.window) most = min(most, 2 * (((u64)a.window + (WIDE_ROWS - 1) / a.group + 1 + BLOCK - 1 + STEP - 1) / STEP));
+    u64 most = (2 * (u64)max(t.s.first + 1, 0) + ((u64)(NW * WROWS) * (t.count ? t.count - 1 : 0) + 2 * ((NW * WROWS) - 1)) / a.group + 1) / STEP + 2;
+    if (a.window) most = min(most, 2 * (((u64)a.window + ((NW * WROWS) - 1) / a.group + 1 + BLOCK - 1 + STEP - 1) / STEP));
     t.pair_units = (u32)max(most, (u64)2);
     t.units = (u64)t.pairs * t.pair_units + t.mid_units;
     return t;
@@ -65,22 +68,51 @@ __device__ __forceinline__ u32 key_at(u32 token, u32 piece) {
 
 __device__ __forceinline__ u32 value_at(u32 d, u32 piece) { return d * STEP + (piece ^ (d >> 2 & 7u) ^ (d & 2u)) * 8; }
 
-// what a thread fetches of the next 64 keys: 16 C bytes of a key, and 8 tokens' words of the values
-template <int C>
+// What a thread fetches of the next 64 keys.  NW waves share them, NW / 4 of them a block of 16: 64 C / NW bytes of a key, and words of eight
+// tokens' values.  With four waves a word's four numbers are one lane's, with eight two lanes have the same word and two numbers each.
+template <int C, int NW>
 struct Fetch {
+    static constexpr int PIECES = 8 * C / NW;            // of 8 numbers of a key
     static constexpr int N = (32 * C + 63) / 64;         // words of values a lane has at most
-    uint4 k[C];
+    static constexpr int COLUMNS = 16 / NW;              // numbers of a word
+    uint2 k[PIECES];
     u32 v[N][8];
 };
 
-template <int FMT, int C, bool CAP>
-__global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, Head* heads) {
+// bytes first and first + 1 of eight words: columns of eight tokens
+template <int FMT>
+__device__ __forceinline__ void two_columns(const u32* w, u32 first, half8_t* out) {
+    if constexpr (FMT == PAG_KV_INT8) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const u32 pick = 0x0c040c00u + 0x00010001u * (first + c);
+            half2_t h[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) h[p] = widen_int8(perm(w[2 * p + 1], w[2 * p], pick));
+            out[c] = half8_t{ h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y };
+        }
+    } else {
+        const u32 pick = 0x05010400u + 0x02020202u * (first / 2);
+        u32 t[2][2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const u32 lo = perm(w[4 * q + 1], w[4 * q], pick), hi = perm(w[4 * q + 3], w[4 * q + 2], pick);
+            t[q][0] = perm(hi, lo, 0x05040100);
+            t[q][1] = perm(hi, lo, 0x07060302);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) out[c] = widen8<FMT>(t[0][c], t[1][c]);
+    }
+}
+
+template <int FMT, int C, bool CAP, int NW>
+__global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend a, Head* heads) {
     constexpr u32 W = 64 * C, KEYS = STEP * W, VALUES = W * STEP;
     constexpr int KEY_TURNS = C == 2 ? 7 : 3;             // which pairs of pieces trade places in key_at
     extern __shared__ __align__(16) _Float16 lds[];       // two buffers of keys and values
     __shared__ float sh_scale[2][4][2];                   // 2^e of the keys' block, e of the values'
     __shared__ u32 sh_there[2][4];
-    __shared__ u64 sh_sum[4];
+    __shared__ u64 sh_sum[NW];
     __shared__ u64 sh_begin;
     __shared__ u32 sh_b;
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 31, hi = lane >> 5;
@@ -89,9 +121,9 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
     const u32 self = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
 
     // this workgroup's share
-    const u32 per = (a.s.requests + 255) / 256, b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
+    const u32 per = (a.s.requests + 64 * NW - 1) / (64 * NW), b0 = min(threadIdx.x * per, a.s.requests), b1 = min(b0 + per, a.s.requests);
     u64 mine = 0;
-    for (u32 b = b0; b < b1; ++b) mine += tiles_of(a, b).units * a.c.kv_heads;
+    for (u32 b = b0; b < b1; ++b) mine += tiles_of<NW>(a, b).units * a.c.kv_heads;
     u64 upto = mine;
 #pragma unroll
     for (u32 o = 1; o < 64; o <<= 1) {
@@ -101,7 +133,7 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
     if (lane == 63) sh_sum[wave] = upto;
     __syncthreads();
     u64 total = 0;
-    for (u32 x = 0; x < 4; ++x) {
+    for (u32 x = 0; x < NW; ++x) {
         if (x < wave) upto += sh_sum[x];
         total += sh_sum[x];
     }
@@ -111,7 +143,7 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         u64 before = upto - mine;
         u32 b = b0;
         for (;; ++b) {
-            const u64 n = tiles_of(a, b).units * a.c.kv_heads;
+            const u64 n = tiles_of<NW>(a, b).units * a.c.kv_heads;
             if (begin < before + n) break;
             before += n;
         }
@@ -128,13 +160,13 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
     __syncthreads();
     u32 b = sh_b;
     u64 before = sh_begin, at = begin;
-    Tiles q = tiles_of(a, b);
+    Tiles q = tiles_of<NW>(a, b);
 
     while (at < end) {
         while (at >= before + q.units * a.c.kv_heads) {
             before += q.units * a.c.kv_heads;
             ++b;
-            q = tiles_of(a, b);
+            q = tiles_of<NW>(a, b);
         }
         const u32 kv_head = (u32)((at - before) / q.units);
         const u64 in = (at - before) % q.units;
@@ -143,16 +175,16 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         if (in >= (u64)q.pairs * q.pair_units) {
             tile = q.pairs;
             u0 = (u32)(in - (u64)q.pairs * q.pair_units);
-            r = range_of(a, q.s, q.rows, tile);
+            r = range_of<NW>(a, q.s, q.rows, tile);
         } else {
             const u32 pair = (u32)(in / q.pair_units);
             u0 = (u32)(in % q.pair_units);
             tile = q.count - 1 - pair;                      // the longer one first
-            r = range_of(a, q.s, q.rows, tile);
+            r = range_of<NW>(a, q.s, q.rows, tile);
             if (u0 >= r.units) {
                 u0 -= r.units;
                 tile = pair;
-                r = range_of(a, q.s, q.rows, tile);
+                r = range_of<NW>(a, q.s, q.rows, tile);
                 if (u0 >= r.units) skip = (u32)(q.pair_units - in % q.pair_units);
             }
         }
@@ -164,10 +196,10 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         const int start = r.start + (int)(u0 * STEP), stop = min(r.stop, start + (int)((u1 - u0) * STEP));
 
         // this wave's rows
-        const u32 row = tile * WIDE_ROWS + wave * WROWS + col, token = row / a.group, head = kv_head * a.group + row % a.group;
+        const u32 row = tile * (NW * WROWS) + wave * WROWS + col, token = row / a.group, head = kv_head * a.group + row % a.group;
         const bool real = row < q.rows;
         const int position = real ? q.s.first + (int)token : -1;
-        const u32 w_row = tile * WIDE_ROWS + wave * WROWS;
+        const u32 w_row = tile * (NW * WROWS) + wave * WROWS;
         const bool busy = w_row < q.rows;                   // the wave has rows
         const int w_p0 = q.s.first + (int)(min(w_row, q.rows - 1) / a.group), w_p1 = q.s.first + (int)(min(w_row + WROWS - 1, q.rows - 1) / a.group);
         const int oldest = a.window ? max(0, position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
@@ -212,12 +244,13 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         }
 
         const int32_t* table = a.s.table + b * a.s.table_stride;
-        // this wave's blocks of the next 64 steps, a lane each
+        // this wave's blocks of the next 64 steps, a lane each; NW / 4 waves share one
+        const u32 block = wave / (NW / 4), part = wave % (NW / 4);
         u32 block_row = 0;
         int ek_mine = 0, ev_mine = 0;
         u64 there = 0;
         const auto look_up = [&](int from) {
-            const int at_key = from + (int)(lane * STEP + wave * BLOCK);
+            const int at_key = from + (int)(lane * STEP + block * BLOCK);
             bool ok = false;
             block_row = 0;
             ek_mine = ev_mine = 0;
@@ -233,16 +266,26 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
             }
             there = __ballot(ok);
         };
-        Fetch<C> f;
+        Fetch<C, NW> f;
+        const u32 key = part * (64 / NW) + lane / NW, key_piece0 = lane % NW * Fetch<C, NW>::PIECES;
+        const auto word_of = [&](int i, u32& word, u32& half, u32& first) -> bool {
+            const u32 item = lane + 64 * i;
+            if (NW == 4) {
+                word = item % (16 * C); half = item / (16 * C); first = 0;
+                return half < 2;
+            }
+            word = item / 2; half = part; first = item % 2 * 2;
+            return word < 16 * C;
+        };
         const auto fetch = [&](u32 n) {
             const uint8_t* rows = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, (int)(n & 63)) * (2 * W);
-            const uint8_t* k = rows + (lane >> 2) * (2 * W) + (lane & 3) * (16 * C);
+            const uint8_t* k = rows + key * (2 * W) + key_piece0 * 8;
 #pragma unroll
-            for (int i = 0; i < C; ++i) f.k[i] = *(const uint4*)(k + 16 * i);
+            for (int i = 0; i < Fetch<C, NW>::PIECES; ++i) f.k[i] = *(const uint2*)(k + 8 * i);
 #pragma unroll
-            for (int i = 0; i < Fetch<C>::N; ++i) {
-                const u32 item = lane + 64 * i, word = item % (16 * C), half = item / (16 * C);
-                if (half < 2) {
+            for (int i = 0; i < Fetch<C, NW>::N; ++i) {
+                u32 word, half, first;
+                if (word_of(i, word, half, first)) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) f.v[i][j] = *(const u32*)(rows + (8 * (j >> 2) + 4 * half + (j & 3)) * (2 * W) + W + word * 4);
                 }
@@ -251,33 +294,31 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
         const auto stage = [&](u32 n, int from, u32 buffer) {
             _Float16* keys = lds + buffer * (KEYS + VALUES);
             _Float16* values = keys + KEYS;
-            const u32 token = wave * BLOCK + (lane >> 2), piece = (lane & 3) * (2 * C);
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                *(half8_t*)(keys + key_at<C>(token, piece + 2 * i)) = widen8<FMT>(f.k[i].x, f.k[i].y);
-                *(half8_t*)(keys + key_at<C>(token, piece + 2 * i + 1)) = widen8<FMT>(f.k[i].z, f.k[i].w);
-            }
+            for (int i = 0; i < Fetch<C, NW>::PIECES; ++i)
+                *(half8_t*)(keys + key_at<C>(block * BLOCK + key, key_piece0 + i)) = widen8<FMT>(f.k[i].x, f.k[i].y);
             const bool ok = there >> (n & 63) & 1;
-            const int base = from + (int)(wave * BLOCK);
+            const int base = from + (int)(block * BLOCK);
 #pragma unroll
-            for (int i = 0; i < Fetch<C>::N; ++i) {
-                const u32 item = lane + 64 * i, word = item % (16 * C), half = item / (16 * C);
-                if (half < 2) {
+            for (int i = 0; i < Fetch<C, NW>::N; ++i) {
+                u32 word, half, first;
+                if (word_of(i, word, half, first)) {
                     if (!ok || base + (int)BLOCK > stop) {      // the memory behind the last token may hold anything
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             if (!ok || base + (int)(8 * (j >> 2) + 4 * half + (j & 3)) >= stop) f.v[i][j] = 0;
                     }
                     half8_t v[4];
-                    columns<FMT>(f.v[i], v);
+                    if constexpr (NW == 4) columns<FMT>(f.v[i], v);
+                    else two_columns<FMT>(f.v[i], first, v);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) *(half8_t*)(values + value_at(word * 4 + c, wave * 2 + half)) = v[c];
+                    for (int c = 0; c < Fetch<C, NW>::COLUMNS; ++c) *(half8_t*)(values + value_at(word * 4 + first + c, block * 2 + half)) = v[c];
                 }
             }
-            if (lane == 0) {
-                sh_scale[buffer][wave][0] = power(__builtin_amdgcn_readlane(ek_mine, (int)(n & 63)));
-                sh_scale[buffer][wave][1] = (float)__builtin_amdgcn_readlane(ev_mine, (int)(n & 63));
-                sh_there[buffer][wave] = ok && base < stop ? 1u : 0u;
+            if (lane == 0 && part == 0) {
+                sh_scale[buffer][block][0] = power(__builtin_amdgcn_readlane(ek_mine, (int)(n & 63)));
+                sh_scale[buffer][block][1] = (float)__builtin_amdgcn_readlane(ev_mine, (int)(n & 63));
+                sh_there[buffer][block] = ok && base < stop ? 1u : 0u;
             }
         };
 
@@ -426,18 +467,18 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
                 if (a.lse && hi == 0) a.lse[(u64)(q.s.t0 + token) * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
             }
         } else {
-            float* partial = a.partial + (2 * (u64)self + (begun ? 1 : 0)) * (WIDE_ROWS * (W + 2));
+            float* partial = a.partial + (2 * (u64)self + (begun ? 1 : 0)) * ((NW * WROWS) * (W + 2));
             const u32 r_here = wave * WROWS + col;
-            if (hi == 0) { partial[r_here] = M; partial[WIDE_ROWS + r_here] = sum; }
+            if (hi == 0) { partial[r_here] = M; partial[(NW * WROWS) + r_here] = sum; }
 #pragma unroll
             for (int n = 0; n < 2 * C; ++n) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *(float4*)(partial + 2 * WIDE_ROWS + r_here * W + n * 32 + 8 * i + 4 * hi) = make_float4(acc[n][4 * i], acc[n][4 * i + 1], acc[n][4 * i + 2], acc[n][4 * i + 3]);
+                    *(float4*)(partial + 2 * (NW * WROWS) + r_here * W + n * 32 + 8 * i + 4 * hi) = make_float4(acc[n][4 * i], acc[n][4 * i + 1], acc[n][4 * i + 2], acc[n][4 * i + 3]);
             }
             if (begun && threadIdx.x == 0) {
                 Head h;
-                h.t0 = q.s.t0; h.rows = q.rows; h.row0 = tile * WIDE_ROWS; h.head0 = kv_head * a.group;
+                h.t0 = q.s.t0; h.rows = q.rows; h.row0 = tile * (NW * WROWS); h.head0 = kv_head * a.group;
                 h.last = (int)(((at + r.units) * parts - 1) / total);       // the workgroup of the tile's last unit
                 heads[self] = h;
             }
@@ -448,9 +489,9 @@ __global__ void __launch_bounds__(256, C <= 2 ? 2 : 1) k_attend_wide(Attend a, H
 
 // Adds up the pieces of a tile that several workgroups had: workgroup (g, y) the rows 4 y to 4 y + 3 of the tile that g began.  Its waves take
 // every fourth piece, four of them asked for at a time (a request's 32 rows over 20,000 keys are in hundreds of pieces).
-template <int C>
+template <int C, int NW>
 __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) {
-    constexpr u32 W = 64 * C, SLOT = WIDE_ROWS * (W + 2), N = 4 * C, THREADS = 16;      // numbers of a lane, lanes of a row
+    constexpr u32 W = 64 * C, SLOT = (NW * WROWS) * (W + 2), N = 4 * C, THREADS = 16;      // numbers of a lane, lanes of a row
     __shared__ float sh_m[4][4], sh_s[4][4];
     __shared__ __align__(16) float sh_acc[4][4][W];
     const Head h = heads[blockIdx.x];
@@ -469,9 +510,9 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
             const int k = min(i + 4 * u, pieces - 1);
             const float* p = a.partial + (2 * ((u64)blockIdx.x + (u32)k) + (k == 0 ? 1 : 0)) * SLOT;
             m[u] = i + 4 * u < pieces ? p[row0 + r] : LOWEST;
-            s[u] = p[WIDE_ROWS + row0 + r];
+            s[u] = p[(NW * WROWS) + row0 + r];
 #pragma unroll
-            for (int c = 0; c < C; ++c) y[u][c] = *(const float4*)(p + 2 * WIDE_ROWS + (row0 + r) * W + first + 4 * c);
+            for (int c = 0; c < C; ++c) y[u][c] = *(const float4*)(p + 2 * (NW * WROWS) + (row0 + r) * W + first + 4 * c);
         }
         float top = M;
 #pragma unroll
@@ -524,50 +565,54 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
     if (a.lse && lane == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }
 
-constexpr u32 wide_groups_per_cu(u32 width) { return width <= 128 ? 2 : 1; }
+// workgroups of a CU: as many as its registers last for
+constexpr u32 wide_groups_per_cu(u32 width, int waves) { return waves == 4 && width <= 128 ? 2 : 1; }
 constexpr u32 lds_bytes(u32 width) { return 2 * 2 * STEP * width * 2; }
 
-template <int FMT, int C, bool CAP>
-int run_wide(hipStream_t st, const Attend& a, u32 grid, Head* heads) {
+// Eight waves share a step's keys where there are rows for them, and registers: they are widened half as often
+constexpr int MANY = 8;
+
+template <int FMT, int C, bool CAP, int NW>
+int run_wide(hipStream_t st, const Attend& a, int num_cu) {
+    const u32 grid = (u32)num_cu * wide_groups_per_cu(64 * C, NW);
+    Head* heads = (Head*)(a.partial + 2ull * grid * (NW * WROWS) * (64 * C + 2));
     if (lds_bytes(64 * C) >= 65536) {
-        const hipError_t e = hipFuncSetAttribute((const void*)k_attend_wide<FMT, C, CAP>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes(64 * C));
+        const hipError_t e = hipFuncSetAttribute((const void*)k_attend_wide<FMT, C, CAP, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes(64 * C));
         if (e != hipSuccess) { pag_set_error(std::string("hipFuncSetAttribute: ") + hipGetErrorString(e)); return PAG_EHIP; }
     }
-    k_attend_wide<FMT, C, CAP><<<grid, 256, lds_bytes(64 * C), st>>>(a, heads);
+    k_attend_wide<FMT, C, CAP, NW><<<grid, 64 * NW, lds_bytes(64 * C), st>>>(a, heads);
+    k_join_wide<C, NW><<<dim3(grid, NW * WROWS / 4), 256, 0, st>>>(a, heads);
     return PAG_OK;
 }
 
-template <int FMT, int C>
+template <int FMT, int C, bool CAP>
 int run(hipStream_t st, const Attend& a, int num_cu) {
-    const u32 grid = (u32)num_cu * wide_groups_per_cu(64 * C);
-    Head* heads = (Head*)(a.partial + 2ull * grid * WIDE_ROWS * (64 * C + 2));
-    const int rc = a.softcap > 0.f ? run_wide<FMT, C, true>(st, a, grid, heads) : run_wide<FMT, C, false>(st, a, grid, heads);
-    if (rc) return rc;
-    k_join_wide<C><<<dim3(grid, WIDE_ROWS / 4), 256, 0, st>>>(a, heads);
-    return PAG_OK;
+    if constexpr (C <= 2) {
+        if (a.many_rows) return run_wide<FMT, C, CAP, MANY>(st, a, num_cu);
+    }
+    return run_wide<FMT, C, CAP, 4>(st, a, num_cu);
+}
+
+template <int FMT>
+int run_format(hipStream_t st, const Attend& a, int num_cu) {
+    const u32 n = a.c.width / 64;
+    const bool cap = a.softcap > 0.f;
+    if (n == 1) return cap ? run<FMT, 1, true>(st, a, num_cu) : run<FMT, 1, false>(st, a, num_cu);
+    if (n == 2) return cap ? run<FMT, 2, true>(st, a, num_cu) : run<FMT, 2, false>(st, a, num_cu);
+    if (n == 3) return cap ? run<FMT, 3, true>(st, a, num_cu) : run<FMT, 3, false>(st, a, num_cu);
+    return cap ? run<FMT, 4, true>(st, a, num_cu) : run<FMT, 4, false>(st, a, num_cu);
 }
 
 }  // namespace
 
 u64 wide_workspace(u32 width, int num_cu) {
-    const u64 grid = (u64)num_cu * wide_groups_per_cu(width);
-    return 4 * 2 * grid * WIDE_ROWS * (width + 2) + (grid * sizeof(Head) + 15) / 16 * 16;
+    // twice the workgroups have half the rows, or the other way round
+    const u64 grid = (u64)num_cu * wide_groups_per_cu(width, 4), rows = std::max(grid * 4 * WROWS, width <= 128 ? (u64)num_cu * MANY * WROWS : 0);
+    return 4 * 2 * rows * (width + 2) + (grid * sizeof(Head) + 15) / 16 * 16;
 }
 
 int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu) {
-    const u32 n = a.c.width / 64;
-    int rc;
-    if (a.c.fmt == PAG_KV_INT8) {
-        if (n == 1) rc = run<PAG_KV_INT8, 1>(st, a, num_cu);
-        else if (n == 2) rc = run<PAG_KV_INT8, 2>(st, a, num_cu);
-        else if (n == 3) rc = run<PAG_KV_INT8, 3>(st, a, num_cu);
-        else rc = run<PAG_KV_INT8, 4>(st, a, num_cu);
-    } else {
-        if (n == 1) rc = run<PAG_KV_FP8, 1>(st, a, num_cu);
-        else if (n == 2) rc = run<PAG_KV_FP8, 2>(st, a, num_cu);
-        else if (n == 3) rc = run<PAG_KV_FP8, 3>(st, a, num_cu);
-        else rc = run<PAG_KV_FP8, 4>(st, a, num_cu);
-    }
+    const int rc = a.c.fmt == PAG_KV_INT8 ? run_format<PAG_KV_INT8>(st, a, num_cu) : run_format<PAG_KV_FP8>(st, a, num_cu);
     if (rc) return rc;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { pag_set_error(std::string("pag_kv_attend: ") + hipGetErrorString(e)); return PAG_EHIP; }
