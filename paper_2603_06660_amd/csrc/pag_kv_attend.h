@@ -67,6 +67,13 @@ __device__ __forceinline__ void columns(const u32* w, half8_t* out) {
     }
 }
 
+// LDS traffic only: loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // what fits 32 bits is divided in 32 bits, in a tenth of the instructions
 __device__ __forceinline__ u64 divide(u64 a, u64 b) {
     if ((a | b) >> 32) return a / b;

@@ -223,13 +223,6 @@ __device__ __forceinline__ Where tile_of(const Where& w, u32 y) {
     return x;
 }
 
-// LDS traffic only: loads from memory stay in flight
-__device__ __forceinline__ void lds_barrier() {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 template <int C, int NW>
 struct Exchange {
     static constexpr u32 STRIDE = 64 * C + 4;

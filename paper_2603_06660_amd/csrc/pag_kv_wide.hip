@@ -326,19 +326,28 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
         const u32 k_lds = key_at<C>(col, hi) * 2, v_lds = value_at(col, hi) * 2;
         const u32 steps = (u32)(max(stop - start, 0) + (int)STEP - 1) / STEP;
         __syncthreads();                                        // the piece before has been read
+        // step n + 1 into LDS, and step n + 2 on its way
+        const auto prepare = [&](u32 n) {
+            if (n + 1 < steps) stage(n + 1, start + (int)((n + 1) * STEP), (n + 1) & 1);
+            if (n + 2 < steps) {
+                if (((n + 2) & 63) == 0) look_up(start + (int)((n + 2) * STEP));
+                fetch(n + 2);
+            }
+        };
+        // Two waves of eight are on a SIMD: one widens the next keys before its products, the other after them, so that one has the vector unit
+        // while the other has the matrix unit.
+        const bool early = NW == 8 && wave >= 4;
         if (steps) {
             look_up(start);
             fetch(0);
             stage(0, start, 0);
+            if (steps > 1) fetch(1);
         }
         __syncthreads();
         for (u32 n = 0; n < steps; ++n) {
             const int from = start + (int)(n * STEP);
             const u32 buffer = n & 1;
-            if (n + 1 < steps) {
-                if (((n + 1) & 63) == 0) look_up(from + (int)STEP);
-                fetch(n + 1);
-            }
+            if (early) prepare(n);
             if (busy && from <= w_p1 && from + (int)STEP > w_first) {
                 const char* keys = (const char*)(lds + buffer * (KEYS + VALUES));
                 const char* values = keys + KEYS * 2;
@@ -445,8 +454,8 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                     }
                 }
             }
-            if (n + 1 < steps) stage(n + 1, from + (int)STEP, buffer ^ 1);
-            __syncthreads();
+            if (!early) prepare(n);
+            lds_barrier();
         }
 
         sum += __shfl_xor(sum, 32);
