@@ -341,7 +341,7 @@ typedef struct {
     uint32_t max_pages;    /* columns of table in use */
     uint32_t page_tokens;
     uint64_t table_stride; /* entries from row to row */
-    uint64_t num_pages;    /* entries of free_pages */
+    uint64_t num_pages;    /* entries of free_pages: room for every page that may be given back */
     int32_t* table;        /* [requests * table_stride] */
     int32_t* lengths;      /* [requests] tokens held */
     int32_t* free_pages;   /* [num_pages] */

@@ -69,7 +69,7 @@ __device__ __forceinline__ void fill_token(const Extend& e, u64 t, u64 free_befo
                 page = *entry;
             }
             position = (int32_t)p;
-            if (page >= 0 && (u32)page < e.num_pages) slot = (int64_t)page * e.page_tokens + (int64_t)place;
+            if (page >= 0) slot = (int64_t)page * e.page_tokens + (int64_t)place;
         }
     }
     e.request[t] = request;

@@ -97,6 +97,23 @@ def test_extend_in_place_and_release(kv):
     assert len(free) < 150
 
 
+def test_extend_with_a_stack_of_the_free_pages_alone(kv):
+    """The stack need not have room for pages that are held: their numbers may lie beyond its size."""
+    rng = np.random.default_rng(8)
+    pages, order = 60, np.random.default_rng(9).permutation(60)
+    lengths = np.array([100, 3, 0, 64, 250])
+    table, first = np.full((5, 20), -1), 0
+    for r, n in enumerate(-(-lengths // 16)):
+        table[r, :n] = order[first:first + n]
+        first += n
+    free = order[first:]
+    for add in ([1, 1, 1, 1, 1], [40, 0, 60, 16, 3], rng.integers(0, 30, 5).tolist()):
+        mine = table.copy()
+        tables = kv.KvTables.from_tensors(ints(lengths), ints(table), ints(free), ints([len(free)]), 16)
+        want = plain.extend(lengths, mine, free, len(free), add, 16, sum(add))
+        check_step(tables.extend(ints(add), sum(add)), tables, want, mine)
+
+
 def test_extend_of_no_tokens_at_all(kv):
     tables = kv.KvTables(2, 2, 2, 16)
     step = tables.extend(ints([0, -3]), 0)
