@@ -254,7 +254,7 @@ struct Load {
     void* x[2];
     int64_t ts[2], hs[2];
     const int64_t* slots;
-    u64 rows;                  // tokens * kv_heads
+    u64 tokens;
     u32 dtype;
 };
 
@@ -265,13 +265,10 @@ __global__ void __launch_bounds__(256) k_read(Load a) {
     constexpr u32 EACH = 16 / sizeof(T), PIECES = 128 * C / EACH, TURNS = 16 * PIECES / 256;      // numbers, pieces of a row, turns
     __shared__ u32 sh_row[16];
     __shared__ float sh_up[16][2];
-    __shared__ u64 sh_token[16];
-    __shared__ u32 sh_head[16];
-    const u64 row0 = (u64)blockIdx.x * 16;
+    const u32 head = blockIdx.x % a.c.kv_heads;
+    const u64 token0 = (u64)(blockIdx.x / a.c.kv_heads) * 16;
     if (threadIdx.x < 16) {
-        const u64 r = min(row0 + threadIdx.x, a.rows - 1), t = r / a.c.kv_heads;
-        const u32 head = (u32)(r - t * a.c.kv_heads);
-        const int64_t slot = a.slots[t];
+        const int64_t slot = a.slots[min(token0 + threadIdx.x, a.tokens - 1)];
         u32 row = 0;
         float k = 0.f, v = 0.f;                  // zeros for slots that are none
         if (slot >= 0 && slot < (int64_t)a.c.num_pages * a.c.page_tokens) {
@@ -283,8 +280,6 @@ __global__ void __launch_bounds__(256) k_read(Load a) {
         sh_row[threadIdx.x] = row;
         sh_up[threadIdx.x][0] = k;
         sh_up[threadIdx.x][1] = v;
-        sh_token[threadIdx.x] = t;
-        sh_head[threadIdx.x] = head;
     }
     __syncthreads();
     u32 w[TURNS][EACH / 4];
@@ -297,7 +292,7 @@ __global__ void __launch_bounds__(256) k_read(Load a) {
 #pragma unroll
     for (u32 n = 0; n < TURNS; ++n) {
         const u32 i = threadIdx.x + 256 * n, r = i / PIECES, both = i % PIECES * EACH, kind = both / (64 * C), at = both % (64 * C);
-        if (row0 + r < a.rows && at < a.c.dim && a.x[kind]) {
+        if (token0 + r < a.tokens && at < a.c.dim && a.x[kind]) {
             const float up = sh_up[r][kind];
             float x[EACH];
 #pragma unroll
@@ -305,7 +300,7 @@ __global__ void __launch_bounds__(256) k_read(Load a) {
             // a slot that is none has no numbers, whatever the row that was read instead holds
 #pragma unroll
             for (u32 y = 0; y < EACH; ++y) x[y] = up != 0.f ? x[y] * up : 0.f;
-            T* to = (T*)a.x[kind] + (int64_t)sh_token[r] * a.ts[kind] + (int64_t)sh_head[r] * a.hs[kind] + at;
+            T* to = (T*)a.x[kind] + (int64_t)(token0 + r) * a.ts[kind] + (int64_t)head * a.hs[kind] + at;
             typedef u32 word4 __attribute__((ext_vector_type(4)));
             word4 y;
             if constexpr (sizeof(T) == 4) y = word4{ __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]) };
@@ -375,9 +370,8 @@ int launch_append(hipStream_t st, const Cache& c, u32 dtype, const void* k, int6
 
 int launch_read(hipStream_t st, const Cache& c, const int64_t* slots, u64 tokens, u32 dtype, void* k, int64_t k_ts, int64_t k_hs, void* v,
                 int64_t v_ts, int64_t v_hs) {
-    const u64 rows = tokens * c.kv_heads;
-    const Load a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, rows, dtype };
-    for_cache<RunRead>(c, st, (u32)((rows + 15) / 16), a);
+    const Load a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, tokens, dtype };
+    for_cache<RunRead>(c, st, (u32)((tokens + 15) / 16 * c.kv_heads), a);
     return launched("pag_kv_read");
 }
 
