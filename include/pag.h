@@ -353,7 +353,7 @@ typedef struct {
     uint32_t struct_size;
     uint32_t requests;
     uint32_t max_pages;        /* as in pag_kv_tables */
-    uint32_t max_new;          /* no request has more new tokens than this (0: not known); a hint, results never depend on it */
+    uint32_t max_new;          /* no request has more new tokens than this (0: not known); a hint: it decides how work is split, so the last bits of a result may differ with it */
     uint64_t table_stride;
     uint64_t tokens;           /* rows of the step's arrays, padding behind the last request included */
     const int32_t* table;

@@ -199,6 +199,34 @@ def test_append_of_values_at_the_edges(kv, fmt):
             same_cache(cache, data, exponents)
 
 
+@pytest.mark.parametrize("tokens, heads", [(300, 12), (700, 8), (5000, 8)])
+def test_append_of_prompts(kv, tokens, heads):
+    """Waves with one new token, with 4 and with 16; runs that begin and end anywhere in a block, with slots that are none between them."""
+    rng = np.random.default_rng(tokens)
+    dim, page, pages = 16, 32, tokens // 8 + 40
+    cache, data, exponents = new_cache(kv, pages, heads, dim, page, "fp8", tokens)
+    order, slots, first = rng.permutation(pages), [], 0
+    while len(slots) < tokens:                       # a request: some tokens from some place on, in pages of its own
+        n, start = int(rng.integers(1, 70)), int(rng.integers(0, page))
+        at = np.arange(start, start + n)
+        need = int(at[-1]) // page + 1
+        if first + need > pages:
+            break
+        slots += (order[first + at // page] * page + at % page).tolist() + [-1] * int(rng.integers(0, 3) == 0)
+        first += need
+    slots = (slots + [-1] * tokens)[:tokens]
+    x = [torch.tensor(rng.standard_normal((tokens, heads, dim)) * 2.0 ** rng.integers(-6, 7, (tokens, heads, 1))).to(torch.bfloat16) for _ in range(2)]
+    cache.append(x[0].cuda(), x[1].cuda(), torch.tensor(slots).cuda())
+    plain.append(data, exponents, dim, "fp8", wide(x[0]), wide(x[1]), slots)
+    same_cache(cache, data, exponents)
+    numbers = plain.numbers(data, exponents, dim, "fp8")
+    at = np.maximum(slots, 0)
+    want = torch.tensor(np.where(np.asarray(slots)[:, None, None, None] < 0, 0.0, numbers[at // page, :, at % page]))
+    got = cache.read(torch.tensor(slots).cuda(), dtype=torch.bfloat16)
+    for kind in range(2):
+        assert torch.equal(got[kind].cpu(), want[:, :, kind].to(torch.bfloat16))
+
+
 def test_append_leaves_out_slots_that_are_none(kv):
     cache, data, exponents = new_cache(kv, 3, 2, 64, 16, "int8", 9)
     slots = np.array([-1, 5, 6, -7, 48, 1 << 40, 17, 32, -(1 << 62)])
@@ -289,7 +317,7 @@ def check_attention(memory, q, out, lse, dtype, requests, positions, keys_of, sc
     return worst
 
 
-def attend_case(kv, contexts, news, heads, kv_heads, dim, page, fmt, dtype, window=0, softcap=0.0, slopes=False, pad=0, seed=1, scale=None):
+def attend_case(kv, contexts, news, heads, kv_heads, dim, page, fmt, dtype, window=0, softcap=0.0, slopes=False, pad=0, seed=1, scale=None, max_new=None):
     m = Memory(kv, contexts, kv_heads, dim, page, fmt, seed)
     tokens = sum(news) + pad
     gen = torch.Generator().manual_seed(seed)
@@ -297,7 +325,7 @@ def attend_case(kv, contexts, news, heads, kv_heads, dim, page, fmt, dtype, wind
     slope = np.exp2(-8.0 * (1 + np.arange(heads)) / heads).astype(np.float32) if slopes else None
     requests = [b for b, a in enumerate(news) for _ in range(a)] + [-1] * pad
     positions = [p for c, a in zip(contexts, news) for p in range(c - a, c)] + [-1] * pad
-    step = kv.KvStep(ints(m.table), offsets=ints(np.concatenate([[0], np.cumsum(news)])), context=ints(contexts), max_new=max(news))
+    step = kv.KvStep(ints(m.table), offsets=ints(np.concatenate([[0], np.cumsum(news)])), context=ints(contexts), max_new=max(news) if max_new is None else max_new)
     out = (torch.full((tokens, heads, dim), 7.0, dtype=DTYPES[dtype], device="cuda"), torch.full((tokens, heads), 7.0, device="cuda"))
     got = m.cache.attend(q.cuda(), step, window=window, softcap=softcap, slopes=None if slope is None else torch.tensor(slope).cuda(), out=out, scale=scale)
     assert got[0] is out[0] and got[1] is out[1]
@@ -350,6 +378,46 @@ def test_attend_many_requests(kv):
 def test_attend_pieces_of_several_units(kv):
     attend_case(kv, [20_000, 9000, 30_011], [1, 2, 1], 8, 8, 64, 64, "int8", "fp16")
     attend_case(kv, [5000, 2000, 3011], [40, 70, 100], 8, 8, 64, 64, "fp8", "fp16")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+def test_attend_two_tiles_of_rows_in_pieces(kv, fmt, dim):
+    """17 to 64 rows to a key over more keys than one workgroup reads."""
+    attend_case(kv, [4100, 2300, 900], [1, 2, 0], 20, 1, dim, 64, fmt, "bf16")
+    attend_case(kv, [3000, 40], [8, 8], 8, 1, dim, 64, fmt, "fp16", window=2500, softcap=20.0)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("dim", [40, 128])
+@pytest.mark.parametrize("softcap, slopes, window", [(0.0, False, 0), (30.0, False, 0), (0.0, True, 90), (5.0, True, 0)])
+def test_attend_long_chunks(kv, fmt, dim, softcap, slopes, window):
+    """More than 128 rows to a key, in one request of several."""
+    attend_case(kv, [400, 33, 0, 150], [300, 33, 0, 1], 2, 1, dim, 32, fmt, "fp16", softcap=softcap, slopes=slopes, window=window, pad=2)
+
+
+@pytest.mark.parametrize("max_new", [0, 1, 4, 16, 20, 37, 300])
+def test_attend_with_any_hint(kv, max_new):
+    """max_new decides which kernels run, and not what they compute, also where it is wrong."""
+    attend_case(kv, [2900, 40, 700], [37, 5, 1], 4, 1, 64, 64, "int8", "fp16", max_new=max_new)
+
+
+def test_attend_of_a_long_chunk(kv):
+    """Pieces of many thousand keys, by each of the kernels: rows here and there against the plain form, all rows against each other."""
+    context, new, heads, kv_heads, dim = 20_003, 448, 32, 8, 64
+    m = Memory(kv, [context], kv_heads, dim, 64, "fp8", 4)
+    q = torch.randn(new, heads, dim, generator=torch.Generator().manual_seed(4)).half()
+    some = [0, 1, 200, 447]
+    first = None
+    for max_new in (1, 16, 20, 448):
+        step = kv.KvStep(ints(m.table), offsets=ints([0, new]), context=ints([context]), max_new=max_new)
+        out, lse = m.cache.attend(q.cuda(), step)
+        check_attention(m, q[some], out[some], lse[some], "fp16", [0] * len(some), [context - new + t for t in some],
+                        lambda t, h: np.arange(context - new + some[t] + 1), dim ** -0.5)
+        if first is None:
+            first = out, lse
+        # weights of 11 bits and an output of 11 bits on each side, of numbers that are below 8 in magnitude
+        assert (out.float() - first[0].float()).abs().max() <= 4 * 2.0 ** -11 * 8 and (lse - first[1]).abs().max() <= 2.0 ** -10
 
 
 def test_attend_scores_far_apart(kv):
@@ -516,6 +584,19 @@ def test_selected_nothing_at_all(kv):
 
 def test_selected_long_lists(kv):
     selected_case(kv, [5000, 3000, 1500], 4, 2, 2, 64, 1024, 600, "int8", "fp16")
+
+
+@pytest.mark.parametrize("fmt, dim", [("int8", 128), ("fp8", 64), ("fp8", 256)])
+def test_selected_of_many_tokens(kv, fmt, dim):
+    """More lists than workgroups run at once."""
+    rng = np.random.default_rng(6)
+    selected_case(kv, rng.integers(1, 400, 45).tolist(), 16, 8, 8, dim, 90, 20, fmt, "bf16")
+
+
+@pytest.mark.parametrize("tokens, k, window", [(1, 2500, 0), (3, 1200, 300), (5, 1900, 100), (5, 2600, 64), (17, 2600, 64)])
+def test_selected_longer_lists(kv, tokens, k, window):
+    """Lists that one workgroup reads, and lists that several share."""
+    selected_case(kv, [3000 - 7 * i for i in range(tokens)], 16, 1, 16, 64, k, window, "int8", "fp16", page=64)
 
 
 def test_selected_everything_is_attention(kv):
