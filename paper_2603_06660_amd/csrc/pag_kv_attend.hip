@@ -85,7 +85,10 @@ __global__ void __launch_bounds__(256) k_join(Attend a, int groups) {
     if (a.lse && threadIdx.x == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }
 
-// Whether a workgroup reads all keys of its rows: lists, windows or tables that hold few keys.  WHOLE
+// Whether a workgroup reads all keys of its rows, without shares to find and a second kernel to join them.  Split and whole, in us, heads of 128:
+//   tables and windows: one request of 777 tokens 12.3, 8.8; 16 of 100 to 2,000 tokens 17.9, 16.2; 32 of 2,000 tokens 34.9, 27; 96 of 300 to 2,000 tokens
+//   51.8, 47.8; one of 2,000 tokens 14.0, 18.3, whose 8 workgroups leave the chip idle
+//   lists: 384 of 1,256 keys 38.6, 29.6; 1,536 of 164 keys 36, 27; 64 of 1,064 keys 19, 15; 32 of 1,064 keys 13.3, 14.3
 bool narrow_whole(const Attend& a, int num_cu) {
     const u64 keys = a.listed ? (u64)a.k + a.window : std::min<u64>((u64)a.s.max_pages * a.c.page_tokens, a.window ? (u64)a.window + 2 * ROWS : ~0ull);
     const u64 groups = narrow_groups(a);

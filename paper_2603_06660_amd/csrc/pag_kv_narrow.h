@@ -827,9 +827,11 @@ void run_whole(hipStream_t st, const Attend& a) {
 template <int FMT, int C>
 void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
     if (whole) {
-        if (!a.listed && a.row_tiles == 2) {
-            k_attend_whole<FMT, C, 2, 4><<<a.s.requests * a.c.kv_heads, 256, 0, st>>>(a);
-            return;
+        if constexpr (C <= 3) {
+            if (!a.listed && a.row_tiles == 2) {
+                k_attend_whole<FMT, C, 2, 4><<<a.s.requests * a.c.kv_heads, 256, 0, st>>>(a);
+                return;
+            }
         }
         // eight waves where there are CUs enough, four where workgroups queue (and where registers last for no more)
         if constexpr (C <= 2) {
@@ -838,9 +840,11 @@ void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
         return run_whole<FMT, C, 4>(st, a);
     }
     const u32 grid = (u32)num_cu * groups_per_cu(64 * C, a.row_tiles);
-    if (a.listed) k_attend_selected<FMT, C><<<grid, 256, 0, st>>>(a, std::max<u32>((a.k + a.window + UNIT - 1) / UNIT, 1), (a.group + ROWS - 1) / ROWS);
-    else if (a.row_tiles == 2) k_attend<FMT, C, 2><<<grid, 256, 0, st>>>(a);
-    else k_attend<FMT, C, 1><<<grid, 256, 0, st>>>(a);
+    if (a.listed) return k_attend_selected<FMT, C><<<grid, 256, 0, st>>>(a, std::max<u32>((a.k + a.window + UNIT - 1) / UNIT, 1), (a.group + ROWS - 1) / ROWS);
+    if constexpr (C <= 3) {
+        if (a.row_tiles == 2) return k_attend<FMT, C, 2><<<grid, 256, 0, st>>>(a);
+    }
+    k_attend<FMT, C, 1><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace pagkv

@@ -167,9 +167,11 @@ struct Store {
 
 // A wave has a window of new tokens, one head and one kind.  It writes the blocks whose first new token lies in its window, with all
 // their new tokens, one block after the other.  8 numbers of a row are a lane's; a block of 16 rows is 2 C of these pieces a lane.
-// A window of one token spreads a decoding step's blocks over as many waves as there are; where that makes more waves than run at
-// once, most of a prompt's would start only to find that their token is not the first of its block (15,000 tokens, 8 heads of 128:
-// 108 us), so windows are larger then.
+// A window of one token spreads a decoding step's blocks over as many waves as there are; the more tokens, the more of the waves of
+// prompts start only to find that their token is not the first of its block.  Windows of 1, 4 and 16 tokens, 8 heads of 128, in us:
+// one token each: 256 requests 6.0, 9.3, 28; 512 requests 9.1, 10.5, 28; 2,048 requests 29, 25, 35; 4,096 requests 53, 44, 47;
+// prompts: 256 tokens 8.5, 5.9, 5.9; 512 tokens 9.8, 6.5, 5.9; 2,048 tokens 18, 12.5, 11; 4,096 tokens 35, 20, 14; 15,000 tokens 139, 53, 36.
+// Bound by memory where there are many tokens (60,000: 370 MB in 124 us), by the waits for a slot, an exponent and a row where there are few.
 template <int FMT, int C>
 __global__ void __launch_bounds__(256) k_append(Store a, u32 window) {
     const u32 lane = threadIdx.x & 63, kinds = 2 * a.c.kv_heads;
@@ -350,7 +352,8 @@ int launched(const char* what) {
 int launch_extend(hipStream_t st, const pag_kv_tables& t, const int32_t* add, const pag_kv_step& s) {
     const Extend e{ add, t.lengths, t.free_pages, t.free_count, t.table, t.table_stride, s.tokens, t.requests, t.max_pages, t.page_tokens,
                     (u32)t.num_pages, s.offsets, s.context, s.granted, s.lengths, s.free_count, s.scratch, s.request, s.positions, s.slots };
-    const bool alone = s.tokens <= 4 * PLAN_THREADS;
+    // one launch or two: 1,024 tokens 7.6 and 8.7 us, 2,048 tokens 9.0 and 9.2, 4,096 tokens 12.3 and 9.5
+    const bool alone = s.tokens <= 2 * PLAN_THREADS;
     k_extend<<<1, PLAN_THREADS, 0, st>>>(e, alone ? s.tokens : 0);
     if (!alone) k_extend_tokens<<<(u32)((s.tokens + 255) / 256), 256, 0, st>>>(e);
     return launched("pag_kv_extend");
@@ -365,7 +368,7 @@ int launch_append(hipStream_t st, const Cache& c, u32 dtype, const void* k, int6
                   const int64_t* slots, u64 tokens) {
     const Store a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, tokens, dtype };
     const u64 waves = tokens * 2 * c.kv_heads;
-    const u32 window = waves <= 8192 ? 1 : waves <= 65536 ? 4 : 16;
+    const u32 window = waves <= 4096 ? 1 : waves <= 32768 ? 4 : 16;
     for_cache<RunAppend>(c, st, (u32)(((tokens + window - 1) / window * 2 * c.kv_heads + 3) / 4), a, window);
     return launched("pag_kv_append");
 }

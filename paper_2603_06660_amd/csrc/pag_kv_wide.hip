@@ -361,7 +361,8 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                 }
                 // Both halves' scores are under way before the first of them is used: the matrix unit works on one half while the vector unit has
                 // the other.  Pieces are asked for AHEAD of their products; left alone, the compiler asks for each right before it, to save
-                // registers, and a product then waits for LDS every time (uncapped chunks 603 us, with this order ORDERED).
+                // registers, and a product then waits for LDS every time (4 chunks of 700 to 2,000 tokens with a cap
+                // 735 us, with this order 715; 256 numbers a head 957 and 854).
                 constexpr int AHEAD = 4, PRODUCTS = 8 * C;
                 const auto key_piece = [&](int n) {
                     const int h = n / (4 * C), i = n % (4 * C);
@@ -496,18 +497,20 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
     }
 }
 
-// Adds up the pieces of a tile that several workgroups had: workgroup (g, y) the rows 4 y to 4 y + 3 of the tile that g began.  Its waves take
-// every fourth piece, four of them asked for at a time (a request's 32 rows over 20,000 keys are in hundreds of pieces).
+// Adds up the pieces of a tile that several workgroups had: workgroup (y, g) the rows 4 y to 4 y + 3 of the tile that g began.  Its waves take
+// every fourth piece, four of them asked for at a time (a request's 32 rows over 20,000 keys are in hundreds of pieces).  The rows come first in
+// the grid: workgroups go to the chip's parts in turn, and the tiles that have pieces begin at every 64th workgroup where a few requests
+// are as long as the rest of the chip's work, so that with g first one part alone adds up (both kernels, 128 rows over 30,000 keys: 89 us, this way 52).
 template <int C, int NW>
 __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) {
     constexpr u32 W = 64 * C, SLOT = (NW * WROWS) * (W + 2), N = 4 * C, THREADS = 16;      // numbers of a lane, lanes of a row
     __shared__ float sh_m[4][4], sh_s[4][4];
     __shared__ __align__(16) float sh_acc[4][4][W];
-    const Head h = heads[blockIdx.x];
-    if (h.last <= (int)blockIdx.x || h.last >= (int)gridDim.x) return;
-    const u32 lane = threadIdx.x & 63, wave = wave_of(), r = lane / THREADS, row0 = blockIdx.y * 4, first = lane % THREADS * N;
+    const Head h = heads[blockIdx.y];
+    if (h.last <= (int)blockIdx.y || h.last >= (int)gridDim.y) return;
+    const u32 lane = threadIdx.x & 63, wave = wave_of(), r = lane / THREADS, row0 = blockIdx.x * 4, first = lane % THREADS * N;
     if (h.row0 + row0 >= h.rows) return;
-    const int pieces = h.last - (int)blockIdx.x + 1;
+    const int pieces = h.last - (int)blockIdx.y + 1;
     float M = LOWEST, sum = 0.f, acc[N];
 #pragma unroll
     for (u32 n = 0; n < N; ++n) acc[n] = 0.f;
@@ -517,7 +520,7 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int k = min(i + 4 * u, pieces - 1);
-            const float* p = a.partial + (2 * ((u64)blockIdx.x + (u32)k) + (k == 0 ? 1 : 0)) * SLOT;
+            const float* p = a.partial + (2 * ((u64)blockIdx.y + (u32)k) + (k == 0 ? 1 : 0)) * SLOT;
             m[u] = i + 4 * u < pieces ? p[row0 + r] : LOWEST;
             s[u] = p[(NW * WROWS) + row0 + r];
 #pragma unroll
@@ -578,7 +581,9 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
 constexpr u32 wide_groups_per_cu(u32 width, int waves) { return waves == 4 && width <= 128 ? 2 : 1; }
 constexpr u32 lds_bytes(u32 width) { return 2 * 2 * STEP * width * 2; }
 
-// Eight waves share a step's keys where there are rows for them, and registers: they are widened half as often
+// Eight waves share a step's keys where there are rows for them, and registers: they are widened half as often.  Four and eight waves, in us: 4 chunks of
+// 700 to 2,000 tokens 605, 587; 256 rows over 30,000 keys 70, 65; 32 requests of 256 rows over 3,000 keys 155, 140;
+// where a request has up to 128 rows half of the waves have none (32 requests of 64 rows, 300 to 12,000 keys: 118, 165).
 constexpr int MANY = 8;
 
 template <int FMT, int C, bool CAP, int NW>
@@ -590,7 +595,7 @@ int run_wide(hipStream_t st, const Attend& a, int num_cu) {
         if (e != hipSuccess) { pag_set_error(std::string("hipFuncSetAttribute: ") + hipGetErrorString(e)); return PAG_EHIP; }
     }
     k_attend_wide<FMT, C, CAP, NW><<<grid, 64 * NW, lds_bytes(64 * C), st>>>(a, heads);
-    k_join_wide<C, NW><<<dim3(grid, NW * WROWS / 4), 256, 0, st>>>(a, heads);
+    k_join_wide<C, NW><<<dim3(NW * WROWS / 4, grid), 256, 0, st>>>(a, heads);
     return PAG_OK;
 }
 
