@@ -406,6 +406,7 @@ int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* strea
  * rounded again.  Rounding is to nearest even; infinities are held as the largest code, NaN as 0.
  * pag_kv_read: rows of the cache as numbers, [tokens][kv_heads][head_dim] with strides in elements (multiples of 16 bytes); k or v may be
  * null.  Slots -1 or out of range give zeros.  PAG_F32 and PAG_BF16 hold every number of the cache exactly.
+ * tokens * kv_heads of a call has to be below 2^27.
  */
 int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride,
                   const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, uint64_t tokens, void* stream);
@@ -419,7 +420,7 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
  * pag_kv_attend_selected: it attends to the last `window` tokens and to the tokens whose positions ids lists (dev int64
  * [tokens][id_heads][k], strides in elements, last dimension dense): id_heads is kv_heads (the heads of a group share a list), heads, or a
  * multiple of kv_heads that divides heads.  Ids below 0, in the window or beyond the token itself are passed over (the window's tokens count
- * once); an id listed twice counts twice.
+ * once); an id listed twice counts twice.  tokens * heads and requests * kv_heads have to be below 2^23 there, below 2^31 in pag_kv_attend.
  * A token that finds nothing to attend to gets zeros and an lse of -inf; so does padding.
  * Sums, maxima and scores are held in 32 bits; softmax weights are rounded to 16-bit floats for their product with the values.
  */

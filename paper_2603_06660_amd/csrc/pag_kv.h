@@ -109,16 +109,6 @@ __device__ __forceinline__ u32 pack2(float a, float b, u32 dtype) {       // to 
     return __builtin_bit_cast(u32, __builtin_convertvector(x, half2_t));
 }
 
-__device__ __forceinline__ void store8(void* p, u64 at, u32 dtype, const float* x) {
-    if (dtype == PAG_F32) {
-        float* o = (float*)p + at;
-        *(float4*)o = make_float4(x[0], x[1], x[2], x[3]);
-        *(float4*)(o + 4) = make_float4(x[4], x[5], x[6], x[7]);
-        return;
-    }
-    *(uint4*)((uint16_t*)p + at) = make_uint4(pack2(x[0], x[1], dtype), pack2(x[2], x[3], dtype), pack2(x[4], x[5], dtype), pack2(x[6], x[7], dtype));
-}
-
 struct Attend {
     Cache c;
     Step s;

@@ -101,6 +101,10 @@ int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_a
     const bool two = a->c.width <= 192;
     a->row_tiles = selected || rows <= (two ? 16u : 32u) ? 1 : two && rows <= 64 ? 2 : 0;
     a->many_rows = rows > 128;
+    // a launch has fewer than 2^32 threads: these kernels have up to 512 for a list, a request's head or a row to join; the wide kernel's grid is the chip's
+    const bool fits = step->tokens * args->heads < (1ull << 23) && (u64)step->requests * a->c.kv_heads < (1ull << 23);
+    PAG_CHECK(!selected || fits, PAG_EUNSUPPORTED, "attention over ids needs tokens * heads and requests * kv_heads below 2^23");
+    if (!fits) a->row_tiles = 0;
     return PAG_OK;
 }
 
@@ -162,7 +166,7 @@ extern "C" int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const vo
         int rc = cache_of(cache, &c);
         if (rc) return rc;
         PAG_CHECK(dtype <= PAG_BF16, PAG_EINVAL, "unknown dtype");
-        PAG_CHECK(tokens * c.kv_heads < (1ull << 31) && tokens < (1ull << 31), PAG_EUNSUPPORTED, "tokens * kv_heads must be below 2^31");
+        PAG_CHECK(tokens < (1ull << 27) && tokens * c.kv_heads < (1ull << 27), PAG_EUNSUPPORTED, "tokens * kv_heads must be below 2^27");
         if (tokens == 0) return PAG_OK;
         PAG_CHECK(k && v && slots, PAG_EINVAL, "k, v or slots is null");
         const u32 bytes = dtype == PAG_F32 ? 4 : 2;
@@ -179,7 +183,7 @@ extern "C" int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint
         int rc = cache_of(cache, &c);
         if (rc) return rc;
         PAG_CHECK(dtype <= PAG_BF16, PAG_EINVAL, "unknown dtype");
-        PAG_CHECK(tokens * c.kv_heads < (1ull << 31) && tokens < (1ull << 31), PAG_EUNSUPPORTED, "tokens * kv_heads must be below 2^31");
+        PAG_CHECK(tokens < (1ull << 27) && tokens * c.kv_heads < (1ull << 27), PAG_EUNSUPPORTED, "tokens * kv_heads must be below 2^27");
         if (tokens == 0 || (!k && !v)) return PAG_OK;
         PAG_CHECK(slots != nullptr, PAG_EINVAL, "slots is null");
         const u32 bytes = dtype == PAG_F32 ? 4 : 2;

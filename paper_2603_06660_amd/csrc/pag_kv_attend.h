@@ -96,7 +96,6 @@ __device__ __forceinline__ void write_empty(const Attend& a, u32 t0, u32 t1) {
     }
 }
 
-
 // tokens of a request, tokens that it holds (no more than its row of the table), and where its first new token stands
 struct Span {
     u32 t0, tokens;
@@ -119,10 +118,6 @@ __device__ __forceinline__ void write_padding(const Attend& a) {
     const u32 from = last + (u32)((u64)pad * blockIdx.x / gridDim.x), to = last + (u32)((u64)pad * (blockIdx.x + 1) / gridDim.x);
     if (from < to) write_empty(a, from, to);
 }
-
-}  // namespace pagkv
-
-namespace pagkv {
 
 // shapes of the kernels for few query rows to a key
 constexpr u32 ROWS = 16;                  // query rows of a tile

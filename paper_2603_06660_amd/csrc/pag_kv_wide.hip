@@ -1,6 +1,6 @@
 // Attention of many query rows over the same keys: pag_kv_attend for chunks of prompts and wide groups.
 //
-// The mathematics is that of pag_kv_attend.hip; what bounds it is different.  With 16 rows a tile a key is widened to 16-bit floats
+// The mathematics is that of pag_kv_narrow.h; what bounds it is different.  With 16 rows a tile a key is widened to 16-bit floats
 // once for each of them, and the vector units are what a long chunk waits for.  Here four waves have 32 rows each, and 64 keys are
 // widened once for all 128, into LDS: keys row by row, values transposed, in the order in which the scores leave the matrix unit,
 // so that weights go back in from their registers as in the narrow kernel.  The next 64 keys are on their way from memory
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
             }
         };
         // Two waves of eight are on a SIMD: one widens the next keys before its products, the other after them, so that one has the vector unit
-        // while the other has the matrix unit.
+        // while the other has the matrix unit (4 chunks of 700 to 2,000 tokens 547 us with all of them after, this way 536; 8-bit integers 590, 567).
         const bool early = NW == 8 && wave >= 4;
         if (steps) {
             look_up(start);

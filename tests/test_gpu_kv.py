@@ -420,6 +420,25 @@ def test_attend_of_a_long_chunk(kv):
         assert (out.float() - first[0].float()).abs().max() <= 4 * 2.0 ** -11 * 8 and (lse - first[1]).abs().max() <= 2.0 ** -10
 
 
+def test_attend_of_more_rows_than_a_launch_has_threads_for(kv):
+    """2^19 requests of 16 heads: the results are those of the requests a thousand at a time, to 11 bits of weights and 11 of output on both sides."""
+    requests, heads, dim = 1 << 19, 16, 8
+    m = Memory(kv, [48] * 8, 1, dim, 16, "int8", 12)
+    order = torch.randint(0, 8, (requests,), generator=torch.Generator().manual_seed(12))
+    table = torch.tensor(m.table, dtype=torch.int32)[order].cuda()
+    context = (torch.arange(requests, dtype=torch.int32, device="cuda") * 7) % 49
+    offsets = torch.arange(requests + 1, dtype=torch.int32, device="cuda")
+    q = torch.randn(requests, heads, dim, device="cuda").half()
+    out, lse = m.cache.attend(q, kv.KvStep(table, offsets=offsets, context=context, max_new=1))
+    for first in (0, 262_000, requests - 1000):
+        step = kv.KvStep(table[first:first + 1000], offsets=offsets[:1001].clone(), context=context[first:first + 1000].clone(), max_new=1)
+        some, some_lse = m.cache.attend(q[first:first + 1000], step)
+        there = context[first:first + 1000] > 0
+        most = some.float().abs().max()
+        assert (out[first:first + 1000].float() - some.float()).abs().max() <= 4 * 2.0 ** -11 * max(float(most), 1.0)
+        assert (lse[first:first + 1000] - some_lse)[there].abs().max() <= 2.0 ** -10 and (lse[first:first + 1000][~there] == -math.inf).all()
+
+
 def test_attend_scores_far_apart(kv):
     """A running maximum that rises by a lot, late; scores that leave one key only; scale 0, where all weights are equal."""
     for scale in (20.0, -3.0, 0.0):

@@ -95,6 +95,18 @@ def test_wrong_attention_arguments_are_refused(kv, step, args, code, word):
     assert rc == code and word in lib.pag_last_error()
 
 
+def test_more_than_a_launch_has_threads_for_is_refused(kv):
+    lib, c, a = kv.load_library(), _cache(kv), _attention(kv)
+    rows = [C.c_void_p(4096), C.c_int64(128), C.c_int64(64)]
+    for tokens in (1 << 26, 1 << 27, 1 << 63):                 # of 2 heads
+        assert lib.pag_kv_append(C.byref(c), C.c_uint32(1), *rows, *rows, C.c_void_p(4096), C.c_uint64(tokens), None) == -5 and b"2^27" in lib.pag_last_error()
+        assert lib.pag_kv_read(C.byref(c), C.c_void_p(4096), C.c_uint64(tokens), C.c_uint32(1), *rows, *rows, None) == -5 and b"2^27" in lib.pag_last_error()
+    for change in (dict(tokens=1 << 21), dict(requests=1 << 22)):
+        rc = lib.pag_kv_attend_selected(C.byref(c), C.byref(_step(kv, **change)), C.byref(a), C.c_void_p(4096), C.c_int64(8), C.c_int64(4), C.c_uint32(2),
+                                        C.c_uint32(4), None)
+        assert rc == -5 and b"2^23" in lib.pag_last_error()
+
+
 def test_null_arguments_and_empty_calls(kv):
     lib = kv.load_library()
     c, s, a, t = _cache(kv), _step(kv), _attention(kv), _tables(kv)
