@@ -362,7 +362,7 @@ typedef struct {
     int32_t* request;          /* [tokens] request of a token, -1 for padding (pag_kv_attend_selected reads it, pag_kv_attend does not) */
     int32_t* positions;        /* [tokens] position in the request, -1 for padding and for refused requests (likewise) */
     int64_t* slots;            /* [tokens] where its key and value go, -1 likewise (only pag_kv_extend uses the fields from here on) */
-    int32_t* granted;          /* [requests] 1, or 0 if there were not enough pages */
+    int32_t* granted;          /* [requests] 1, or 0 if there were not enough pages, or not enough rows in the step */
     int32_t* lengths;          /* [requests] lengths after the step; may be pag_kv_tables.lengths itself */
     int32_t* free_count;       /* [1] likewise */
     int32_t* scratch;          /* [requests + 1] */
@@ -388,7 +388,9 @@ typedef struct {
 /*
  * pag_kv_extend: request r gets add[r] (dev int32 [requests], negative counts as 0) new tokens.  Requests are served in order; one
  * that needs more pages than its row of the table or the stack has left is refused as a whole (granted 0, slots -1), and so
- * is every later one that needs a page once the stack could not serve one before it.  Writes the new entries of the tables
+ * is every later one that needs a page once the stack could not serve one before it.  Refused as a whole is also a request whose new
+ * tokens do not all have rows in the step (the sum of add up to it is above step->tokens), and with it every later one that gets tokens; it
+ * takes no page and keeps its length.  offsets count the tokens of refused requests too.  Writes the new entries of the tables
  * and all arrays of `step`; the rest of `tables` changes only where step->lengths and step->free_count are its own arrays, so
  * a step can be looked at before it is taken over.
  * pag_kv_release: the requests with done[r] != 0 (dev int32 [requests]) give back their pages, first page first, in order of

@@ -97,7 +97,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_extend(Extend e, u64 fill) {
         const Want w = want_of(e, r);
         const u64 before = upto;
         if (w.fits) upto += w.need;
-        const bool granted = w.fits && (w.need == 0 || upto <= avail);
+        // all of its new tokens need rows in the step: the token that begins a page writes the table's entry and one without a row would leave
+        // there what an earlier holder of the row's place wrote.  After a request without rows only those that want none are served, so upto stands
+        const bool rows = w.add == 0 || first + w.add <= e.tokens;
+        const bool granted = w.fits && rows && (w.need == 0 || upto <= avail);
         if (granted && w.need) taken = upto;
         e.offsets[r] = (int32_t)min(first, (u64)0x7FFFFFFF);
         first += w.add;

@@ -197,7 +197,8 @@ class KvTables:
         self.lengths, self.free_count = lengths, free_count
 
     def extend(self, add, total, max_new=0, out=None, commit=False):
-        """-> KvStep for add[r] (int32 [requests]) new tokens of each request, `total` rows in all (more than the sum: padding).
+        """-> KvStep for add[r] (int32 [requests]) new tokens of each request, `total` rows in all (more than the sum: padding; fewer: the
+        requests whose tokens do not all have rows are refused, as those are for which there are no pages).
         max_new: no request gets more tokens (0: not known).  out: a step whose arrays are written again.  The tables keep their
         lengths and free pages until commit(step); commit=True writes them in place, as a captured loop needs it."""
         if out is None:
