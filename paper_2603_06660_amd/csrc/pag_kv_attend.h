@@ -112,6 +112,12 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 b) {
     return s;
 }
 
+// The first position that a row at `position` reads.  Positions are negative where a request holds fewer tokens than it has rows: such a row reads
+// nothing, and position - window would leave 32 bits.
+__device__ __forceinline__ int oldest_of(const Attend& a, int position) {
+    return a.window && position >= 0 && (u32)position >= a.window ? position - (int)a.window + 1 : 0;
+}
+
 // zeros for tokens behind the last request; this workgroup's part of them
 __device__ __forceinline__ void write_padding(const Attend& a) {
     const u32 last = min((u32)max(a.s.offsets[a.s.requests], 0), a.s.tokens), pad = a.s.tokens - last;

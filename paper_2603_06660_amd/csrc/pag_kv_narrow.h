@@ -343,8 +343,7 @@ __device__ __forceinline__ void place_piece(const Attend& a, Piece& p, const Spa
     p.w.head0 = kv_head * a.group;
     p.p0 = s.first + (int)(p.w.row0 / a.group);
     p.p1 = s.first + (int)(min(p.w.row0 + T * ROWS - 1, p.w.rows - 1) / a.group);
-    const int low = a.window ? max(0, p.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
-    p.start = (low & ~(int)(BLOCK - 1)) + (int)(p.u0 * unit);
+    p.start = (oldest_of(a, p.p0) & ~(int)(BLOCK - 1)) + (int)(p.u0 * unit);
     p.stop = (int)min((int64_t)p.p1 + 1, (int64_t)p.start + (int64_t)(p.u1 - p.u0) * unit);
 }
 
@@ -400,7 +399,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             x.at[s] = pos + s * (int)BLOCK + 4 * (int)g;
         }
         const u32 two = (u32)(there >> (2 * i)) & 3u;
-        const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos <= p.p1 - (int)min(a.window - 1, 0x7FFFFFFEu) - 1;
+        const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos < oldest_of(a, p.p1);
         u32 keep[T];
 #pragma unroll
         for (int y = 0; y < T; ++y) keep[y] = 0xFF;
@@ -411,8 +410,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 const bool exists = (two >> (j >> 2) & 1u) && k < p.stop;
 #pragma unroll
                 for (int y = 0; y < T; ++y) {
-                    const int oldest = a.window ? rows[y].position - (int)min(a.window, 0x7FFFFFFFu) + 1 : 0;
-                    if (!exists || k > rows[y].position || k < oldest) keep[y] &= ~(1u << j);
+                    if (!exists || k > rows[y].position || k < oldest_of(a, rows[y].position)) keep[y] &= ~(1u << j);
                 }
                 if (!exists) {
 #pragma unroll

@@ -33,7 +33,7 @@ __device__ __forceinline__ Range range_of(const Attend& a, const Span& s, u32 ro
     Range r;
     r.p0 = s.first + (int)(tile * (NW * WROWS) / a.group);
     r.p1 = s.first + (int)(min(tile * (NW * WROWS) + (NW * WROWS) - 1, rows - 1) / a.group);
-    r.start = a.window ? max(0, r.p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) & ~(int)(BLOCK - 1) : 0;
+    r.start = oldest_of(a, r.p0) & ~(int)(BLOCK - 1);
     r.stop = max(r.p1 + 1, r.start);
     r.units = max(((u32)(r.stop - r.start) + STEP - 1) / STEP, 1u);
     return r;
@@ -204,9 +204,9 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
         const u32 w_row = tile * (NW * WROWS) + wave * WROWS;
         const bool busy = w_row < q.rows;                   // the wave has rows
         const int w_p0 = q.s.first + (int)(min(w_row, q.rows - 1) / a.group), w_p1 = q.s.first + (int)(min(w_row + WROWS - 1, q.rows - 1) / a.group);
-        const int oldest = a.window ? max(0, position - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
-        const int w_first = a.window ? max(0, w_p0 - (int)min(a.window, 0x7FFFFFFFu) + 1) : 0;
-        const int w_full = a.window ? w_p1 - (int)min(a.window - 1, 0x7FFFFFFEu) : 0;      // keys from here on are in the window of all rows
+        const int oldest = oldest_of(a, position);
+        const int w_first = oldest_of(a, w_p0);
+        const int w_full = oldest_of(a, w_p1);      // keys from here on are in the window of all rows
         const float slope = real && a.slopes ? a.slopes[head] * LOG2E : 0.f;
 
         half8_t Q[4 * C];                                   // numbers 16 n + 8 hi + 0 .. 7 in Q[n]

@@ -93,3 +93,65 @@ def test_extend_by_more_tokens_than_32_bits_count(kv):
     assert step.requests.tolist() == [0] * 5 + [1] * 15 and step.positions.tolist() == list(range(5)) + [-1] * 15
     assert step.slots.tolist() == list(range(5)) + [-1] * 15
     assert step.free_count.tolist() == [7]
+
+
+# ---- attention ----------------------------------------------------------------------------------------------------------------
+
+
+class Memory:
+    """One cache whose tokens are given, in pages in some order; numpy copies of what it holds."""
+
+    def __init__(self, kv, k, v, page, fmt, seed=1):
+        n, self.kv_heads, self.dim = k.shape
+        self.page, self.fmt = page, fmt
+        pages = -(-n // page)
+        self.order = np.random.default_rng(seed).permutation(pages)
+        data = np.zeros((pages, self.kv_heads, page, 2, -(-self.dim // 64) * 64), np.uint8)
+        exponents = np.zeros((pages, self.kv_heads, page // 16, 2), np.int8)
+        at = np.arange(n)
+        plain.append(data, exponents, self.dim, fmt, np.asarray(k, np.float64), np.asarray(v, np.float64), self.order[at // page] * page + at % page)
+        self.numbers = plain.numbers(data, exponents, self.dim, fmt)
+        self.cache = kv.KvCache.from_tensors(torch.tensor(data).cuda(), torch.tensor(exponents).cuda(), self.dim, fmt)
+
+    def rows(self, at, head):
+        p, t = self.order[at // self.page], at % self.page
+        return self.numbers[p, head, t, 0], self.numbers[p, head, t, 1]
+
+
+def check_rows(memory, q, out, lse, bits, positions, keys_of, scale, softcap=0.0, slopes=None, slack=0.0):
+    """Each row against 64 bits.  The cap counts in a score's error up to 64, where another form of it begins, whose error is the score's;
+    a slope counts with the distance between the keys that a row reads, not with their distance from the row: only lse, a number of 32
+    bits, is off by its own size.  slack: added to out's tolerance, times the largest |value|."""
+    q, out, lse = wide(q), wide(out), wide(lse)
+    heads = q.shape[1]
+    for t in range(q.shape[0]):
+        for h in range(heads):
+            at = keys_of(t, h)
+            if len(at) == 0:
+                assert (out[t, h] == 0).all() and lse[t, h] == -math.inf, (t, h)
+                continue
+            k, v = memory.rows(at, h * memory.kv_heads // heads)
+            slope = 0.0 if slopes is None else float(slopes[h])
+            o, l, spread, products = plain.attend_row(q[t, h], k, v, scale, softcap, slope, positions[t] - at)
+            tol_o, tol_l = plain.tolerance(memory.dim, bits, o, spread, products, min(softcap, 64.0), abs(slope) * float(at.max() - at.min()))
+            assert abs(lse[t, h] - l) <= tol_l + 2.0 ** -22 * abs(l), (t, h, lse[t, h], l, tol_l)
+            assert (np.abs(out[t, h] - o) <= tol_o + slack * np.abs(v).max()).all(), (t, h, np.abs(out[t, h] - o).max(), tol_o.min())
+
+
+def normal(shape, seed, scale=1.0):
+    return np.random.default_rng(seed).standard_normal(shape) * scale
+
+
+@pytest.mark.parametrize("window", [0, 1, 4, 7, (1 << 31) - 17, (1 << 31) - 1])
+@pytest.mark.parametrize("max_new", [1, 20, 300])
+def test_requests_that_hold_fewer_tokens_than_they_have_rows(kv, max_new, window):
+    """Rows in front of a request's first token read nothing, whatever the window; the others read what there is."""
+    for n, rows in ((5, 10), (1, 70), (40, 41), (1200, 1290)):
+        m = Memory(kv, normal((n, 2, 64), 1), normal((n, 2, 64), 2), 16, "int8")
+        q = torch.tensor(normal((rows + 2, 4, 64), 3)).half()
+        positions = list(range(n - rows, n)) + [n - 2, n - 1]
+        step = kv.KvStep(ints([m.order] * 2), offsets=ints([0, rows, rows + 2]), context=ints([n, n]), max_new=max_new)
+        out, lse = m.cache.attend(q.cuda(), step, window=window)
+        some = [t for t in range(rows + 2) if rows < 100 or t % 41 == 0 or t >= rows - 2]
+        check_rows(m, q[some], out[some], lse[some], 11, [positions[t] for t in some],
+                   lambda t, h: np.arange(max(0, positions[some[t]] - window + 1) if window else 0, positions[some[t]] + 1), 0.125)
