@@ -96,7 +96,8 @@ __device__ __forceinline__ void write_empty(const Attend& a, u32 t0, u32 t1) {
     }
 }
 
-// tokens of a request, tokens that it holds (no more than its row of the table), and where its first new token stands
+// rows of a request, tokens that it holds (no more than its row of the table), and where its first new token stands: counted from all of its new
+// tokens, also where the step has rows for some of them only
 struct Span {
     u32 t0, tokens;
     int context, first;
@@ -106,9 +107,10 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 b) {
     Span s;
     const int32_t from = a.s.offsets[b], to = a.s.offsets[b + 1];
     s.t0 = min((u32)max(from, 0), a.s.tokens);
-    s.tokens = max(min((u32)max(to, 0), a.s.tokens), s.t0) - s.t0;
+    const u32 end = max((u32)max(to, 0), s.t0);
+    s.tokens = min(end, a.s.tokens) - s.t0;
     s.context = (int)min((u64)(u32)max(a.s.context[b], 0), (u64)a.s.max_pages * a.c.page_tokens);
-    s.first = s.context - (int)s.tokens;
+    s.first = s.context - (int)(end - s.t0);
     return s;
 }
 

@@ -155,3 +155,15 @@ def test_requests_that_hold_fewer_tokens_than_they_have_rows(kv, max_new, window
         some = [t for t in range(rows + 2) if rows < 100 or t % 41 == 0 or t >= rows - 2]
         check_rows(m, q[some], out[some], lse[some], 11, [positions[t] for t in some],
                    lambda t, h: np.arange(max(0, positions[some[t]] - window + 1) if window else 0, positions[some[t]] + 1), 0.125)
+
+
+@pytest.mark.parametrize("max_new", [1, 16, 20, 37, 300])
+def test_a_step_with_fewer_rows_than_its_requests_have_tokens(kv, max_new):
+    """The rows that there are stand where they stood."""
+    n = 900
+    m = Memory(kv, normal((n, 1, 64), 1), normal((n, 1, 64), 2), 16, "int8")
+    q = torch.tensor(normal((37, 4, 64), 3)).half()
+    step = kv.KvStep(ints([m.order] * 3), offsets=ints([0, 5, 70, 90]), context=ints([n, 500, 40]), max_new=max_new)
+    out, lse = m.cache.attend(q.cuda(), step)
+    positions = list(range(n - 5, n)) + list(range(500 - 65, 500 - 65 + 32))
+    check_rows(m, q, out, lse, 11, positions, lambda t, h: np.arange(positions[t] + 1), 0.125)
