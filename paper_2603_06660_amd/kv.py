@@ -112,7 +112,7 @@ class KvStep:
 
     def __init__(self, table, offsets=None, context=None, requests=None, positions=None, slots=None, max_new=0, granted=None,
                  lengths=None, free_count=None, scratch=None, tokens=None):
-        self.table, self.offsets, self.context = table, offsets, context
+        self.table, self.offsets, self.context = None, offsets, context
         self.requests, self.positions, self.slots = requests, positions, slots
         self.granted, self.lengths, self.free_count, self.scratch = granted, lengths, free_count, scratch
         self.max_new = int(max_new)
@@ -139,19 +139,21 @@ class KvStep:
         if not isinstance(table, torch.Tensor) or table.dtype != torch.int32 or table.dim() != 2 or not table.is_cuda or \
                 (table.stride(1) != 1 and table.shape[1] > 1) or table.shape[0] == 0 or table.shape[1] == 0:
             raise PagError("table must be an int32 CUDA tensor [requests, max_pages] with dense rows")
-        device, n, s = table.device, table.shape[0], self._s
-        self.table, self.device = table, device
-        s.requests, s.max_pages = n, table.shape[1]
-        s.table_stride = table.stride(0) if n > 1 else max(table.stride(0), table.shape[1])
-        s.table = table.data_ptr()
+        device, n = table.device, table.shape[0]
+        fields = dict(requests=n, max_pages=table.shape[1], table_stride=table.stride(0) if n > 1 else max(table.stride(0), table.shape[1]),
+                      table=table.data_ptr())
         for name, shape, field in (("offsets", (n + 1,), "offsets"), ("context", (n,), "context"), ("granted", (n,), "granted"),
                                    ("lengths", (n,), "lengths"), ("free_count", (1,), "free_count"), ("scratch", (n + 1,), "scratch"),
                                    ("requests", (self.tokens,), "request"), ("positions", (self.tokens,), "positions")):
             t = getattr(self, name)
             if t is not None:
-                setattr(s, field, _array(t, torch.int32, shape, device, name))
+                fields[field] = _array(t, torch.int32, shape, device, name)
         if self.slots is not None:
-            s.slots = _array(self.slots, torch.int64, (self.tokens,), device, "slots")
+            fields["slots"] = _array(self.slots, torch.int64, (self.tokens,), device, "slots")
+        # everything fits: a step that is refused stays what it was
+        for field, value in fields.items():
+            setattr(self._s, field, value)
+        self.table, self.device = table, device
 
     def _with(self, tokens):
         if self.table is None:
@@ -192,8 +194,9 @@ class KvTables:
         self._take(lengths, free_count)
 
     def _take(self, lengths, free_count):
-        self._t.lengths = _array(lengths, torch.int32, (self._t.requests,), self.device, "lengths")
-        self._t.free_count = _array(free_count, torch.int32, (1,), self.device, "free_count")
+        where = (_array(lengths, torch.int32, (self._t.requests,), self.device, "lengths"),
+                 _array(free_count, torch.int32, (1,), self.device, "free_count"))
+        self._t.lengths, self._t.free_count = where
         self.lengths, self.free_count = lengths, free_count
 
     def extend(self, add, total, max_new=0, out=None, commit=False):

@@ -95,6 +95,16 @@ def test_extend_by_more_tokens_than_32_bits_count(kv):
     assert step.free_count.tolist() == [7]
 
 
+def test_a_step_of_fewer_requests_than_the_tables_is_refused_every_time(kv):
+    two, three, step = kv.KvTables(2, 4, 8, 16), kv.KvTables(3, 4, 8, 16), kv.KvStep.empty(2, 6)
+    for _ in range(2):
+        for _ in range(2):
+            with pytest.raises(kv.PagError):
+                three.extend(ints([1, 1, 1]), 6, out=step)
+        assert two.extend(ints([2, 3]), 6, out=step).context.tolist() == [2, 3]
+    assert three.table.eq(-1).all() and three.lengths.tolist() == [0, 0, 0]
+
+
 # ---- attention ----------------------------------------------------------------------------------------------------------------
 
 

@@ -1,0 +1,50 @@
+"""What steps and tables hand to the library, with tensors that say they are on a GPU and a library call that only looks at its arguments."""
+import ctypes as C
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+class OnGpu(torch.Tensor):
+    is_cuda = True
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """-> (module, the steps of the calls that were made)"""
+    from paper_2603_06660_amd import kv
+    made = []
+    monkeypatch.setattr(kv, "_call", lambda name, device, *a: made.append((name, kv._Step.from_buffer_copy(C.string_at(a[2], C.sizeof(kv._Step))))
+                                                                          if name == "pag_kv_extend" else (name, None)))
+    return kv, made
+
+
+def ints(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def tables_of(kv, requests, max_pages=3):
+    return kv.KvTables.from_tensors(ints(requests), ints(requests, max_pages).as_subclass(OnGpu), ints(9), ints(1), 16)
+
+
+def step_of(kv, requests, total):
+    return kv.KvStep(None, ints(requests + 1), ints(requests), ints(total), ints(total), torch.zeros(total, dtype=torch.int64), granted=ints(requests),
+                     lengths=ints(requests), free_count=ints(1), scratch=ints(requests + 1), tokens=total)
+
+
+def test_a_step_that_does_not_fit_is_refused_every_time_and_stays_as_it_was(calls):
+    kv, made = calls
+    two, three, step = tables_of(kv, 2), tables_of(kv, 3), step_of(kv, 2, 4)
+    for _ in range(3):                       # unbound, then bound to the tables that it fits
+        for _ in range(2):
+            with pytest.raises(kv.PagError):
+                three.extend(ints(3), 4, out=step)
+        before = len(made)
+        two.extend(ints(2), 4, out=step)
+        assert len(made) == before + 1 and made[-1][1].requests == 2 and made[-1][1].table == two.table.data_ptr()
+        assert step.table is two.table and made[-1][1].offsets == step.offsets.data_ptr()
+    assert len(made) == 3
+    with pytest.raises(kv.PagError):
+        step._with(3)
+    assert step._with(4).requests == 2
