@@ -121,6 +121,7 @@ class KvStep:
                 tokens = t.shape[0]
         self._s = _Step(struct_size=C.sizeof(_Step), max_new=self.max_new)
         self.tokens = tokens
+        self._holders = []          # tables that took over lengths and free_count
         if table is not None:
             self._bind(table)
 
@@ -210,6 +211,7 @@ class KvTables:
             raise PagError("the step has %s tokens, not %d" % (out.tokens, total))
         if out.slots is None or out.granted is None or out.scratch is None:
             raise PagError("out has no room for slots: use KvStep.empty")
+        add = _array(add, torch.int32, (self._t.requests,), self.device, "add")
         if out.table is not self.table:
             out._bind(self.table)
         s = out._s
@@ -218,10 +220,12 @@ class KvTables:
         if commit:
             out.lengths, out.free_count = self.lengths, self.free_count
             s.lengths, s.free_count = self._t.lengths, self._t.free_count
-        elif out.lengths is self.lengths or out.free_count is self.free_count:
+            out._holders = [self]
+        elif any(t.lengths is out.lengths or t.free_count is out.free_count for t in (self, *out._holders)):
             out.lengths, out.free_count = torch.empty_like(self.lengths), torch.empty_like(self.free_count)
             s.lengths, s.free_count = out.lengths.data_ptr(), out.free_count.data_ptr()
-        _call("pag_kv_extend", self.device, C.addressof(self._t), _array(add, torch.int32, (self._t.requests,), self.device, "add"), C.addressof(s))
+            out._holders = []
+        _call("pag_kv_extend", self.device, C.addressof(self._t), add, C.addressof(s))
         return out
 
     def commit(self, step):
@@ -229,6 +233,7 @@ class KvTables:
         if step.table is not self.table or step.lengths is None or step.free_count is None:
             raise PagError("the step belongs to other tables")
         self._take(step.lengths, step.free_count)
+        step._holders = [t for t in step._holders if t is not self] + [self]
 
     def release(self, done):
         """The requests with done[r] != 0 (int32 [requests]) give their pages back."""

@@ -48,3 +48,46 @@ def test_a_step_that_does_not_fit_is_refused_every_time_and_stays_as_it_was(call
     with pytest.raises(kv.PagError):
         step._with(3)
     assert step._with(4).requests == 2
+
+
+def test_lengths_that_tables_took_over_are_not_written_for_others(calls):
+    """A committed step's arrays are the tables' own from then on: the next step in it, of any tables, gets new ones."""
+    kv, made = calls
+    for in_place in (False, True):
+        a, b, step = tables_of(kv, 2), tables_of(kv, 2), step_of(kv, 2, 4)
+        a.extend(ints(2), 4, out=step, commit=in_place)
+        if not in_place:
+            a.commit(step)
+        held = (a.lengths.data_ptr(), a.free_count.data_ptr())
+        assert (step.lengths.data_ptr(), step.free_count.data_ptr()) == held == (a._t.lengths, a._t.free_count)
+        for tables in (b, a):
+            tables.extend(ints(2), 4, out=step)
+            s = made[-1][1]
+            assert s.lengths not in held and s.free_count not in held
+            assert (s.lengths, s.free_count) == (step.lengths.data_ptr(), step.free_count.data_ptr())
+        # nobody has taken these over: they are written again
+        again = step.lengths
+        a.extend(ints(2), 4, out=step)
+        assert step.lengths is again
+        # in place for the second tables: theirs, and only theirs
+        b.extend(ints(2), 4, out=step, commit=True)
+        assert (made[-1][1].lengths, made[-1][1].free_count) == (b._t.lengths, b._t.free_count) and (a._t.lengths, a._t.free_count) == held
+
+
+def test_two_steps_in_turn_keep_their_arrays(calls):
+    kv, made = calls
+    a, steps = tables_of(kv, 2), [step_of(kv, 2, 4) for _ in range(2)]
+    mine = [s.lengths for s in steps]
+    for i in range(6):
+        a.extend(ints(2), 4, out=steps[i % 2])
+        a.commit(steps[i % 2])
+        assert steps[i % 2].lengths is mine[i % 2] and len(steps[i % 2]._holders) == 1
+
+
+def test_a_refused_call_hands_nothing_over(calls):
+    kv, made = calls
+    a, step = tables_of(kv, 2), step_of(kv, 2, 4)
+    mine = step.lengths
+    with pytest.raises(kv.PagError):
+        a.extend(ints(3), 4, out=step, commit=True)
+    assert step.lengths is mine and not made
