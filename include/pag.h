@@ -357,7 +357,7 @@ typedef struct {
     uint64_t table_stride;
     uint64_t tokens;           /* rows of the step's arrays, padding behind the last request included */
     const int32_t* table;
-    int32_t* offsets;          /* [requests + 1] first new token of each request */
+    int32_t* offsets;          /* [requests + 1] first new token of each request, ascending; rows before the first and behind the last are padding */
     int32_t* context;          /* [requests] tokens that it holds once the new ones are written; 0 if it was refused */
     int32_t* request;          /* [tokens] request of a token, -1 for padding (pag_kv_attend_selected reads it, pag_kv_attend does not) */
     int32_t* positions;        /* [tokens] position in the request, -1 for padding and for refused requests (likewise) */

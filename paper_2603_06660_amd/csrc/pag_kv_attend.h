@@ -120,11 +120,12 @@ __device__ __forceinline__ int oldest_of(const Attend& a, int position) {
     return a.window && position >= 0 && (u32)position >= a.window ? position - (int)a.window + 1 : 0;
 }
 
-// zeros for tokens behind the last request; this workgroup's part of them
+// zeros for tokens before the first request and behind the last one; this workgroup's part of them
 __device__ __forceinline__ void write_padding(const Attend& a) {
-    const u32 last = min((u32)max(a.s.offsets[a.s.requests], 0), a.s.tokens), pad = a.s.tokens - last;
-    const u32 from = last + (u32)((u64)pad * blockIdx.x / gridDim.x), to = last + (u32)((u64)pad * (blockIdx.x + 1) / gridDim.x);
-    if (from < to) write_empty(a, from, to);
+    const u32 last = min((u32)max(a.s.offsets[a.s.requests], 0), a.s.tokens), first = min((u32)max(a.s.offsets[0], 0), last), pad = first + a.s.tokens - last;
+    const u32 from = (u32)((u64)pad * blockIdx.x / gridDim.x), to = (u32)((u64)pad * (blockIdx.x + 1) / gridDim.x);
+    if (from < min(to, first)) write_empty(a, from, min(to, first));
+    if (max(from, first) < to) write_empty(a, max(from, first) - first + last, to - first + last);
 }
 
 // shapes of the kernels for few query rows to a key

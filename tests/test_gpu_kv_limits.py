@@ -177,3 +177,17 @@ def test_a_step_with_fewer_rows_than_its_requests_have_tokens(kv, max_new):
     out, lse = m.cache.attend(q.cuda(), step)
     positions = list(range(n - 5, n)) + list(range(500 - 65, 500 - 65 + 32))
     check_rows(m, q, out, lse, 11, positions, lambda t, h: np.arange(positions[t] + 1), 0.125)
+
+
+@pytest.mark.parametrize("max_new, n", [(1, 200), (1, 3000), (20, 200), (20, 3000), (300, 200), (300, 3000)])
+def test_rows_before_the_first_request_are_zeros(kv, max_new, n):
+    """offsets that begin behind row 0; in one workgroup and in shares, with few and with many rows."""
+    m = Memory(kv, normal((n, 2, 64), 1), normal((n, 2, 64), 2), 16, "fp8")
+    q = torch.tensor(normal((9, 4, 64), 3)).half()
+    step = kv.KvStep(ints([m.order] * 2), offsets=ints([4, 5, 7]), context=ints([n, n - 3]), max_new=max_new)
+    positions = [-1] * 4 + [n - 1, n - 5, n - 4] + [-1] * 2
+    for _ in range(2):
+        room = torch.full((1 << 22,), 1, dtype=torch.int32, device="cuda")      # what the workspace holds afterwards
+        del room
+        out, lse = m.cache.attend(q.cuda(), step, out=(torch.full((9, 4, 64), 7.0).half().cuda(), torch.full((9, 4), 7.0).cuda()))
+        check_rows(m, q, out, lse, 11, positions, lambda t, h: np.arange(positions[t] + 1), 0.125)
