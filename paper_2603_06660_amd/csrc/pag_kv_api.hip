@@ -127,7 +127,8 @@ int arrays_of(const pag_kv_step* step, const pag_kv_attention* args, Attend* a, 
     a->lse = args->lse;
     a->slopes = args->slopes;
     a->scale = args->scale;
-    a->softcap = args->softcap;
+    // scores below 2^-64 are all the same to a weight of 32 bits, and the reciprocal of a smaller cap leaves them
+    a->softcap = args->softcap > 0.f ? std::max(args->softcap, 0x1p-64f) : 0.f;
     a->partial = (float*)args->workspace;
     return PAG_OK;
 }

@@ -11,6 +11,24 @@ constexpr float START = 7.f;              // and are 2^7 at most when M moves: 1
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LN2 = 0.69314718055994530942f;
 
+// Up to this cap a capped score is cap - 2 cap / (1 + e^(2 score / cap)), one exponential and one reciprocal, whose error is 2^-22 of the cap (of 64 a
+// hundredth of what a weight's rounding to 11 bits does).  Above it the error has to be the score's own, see capped().
+constexpr float NEAR_CAP = 64.f;
+
+// cap * tanh(x / cap), by: 1 / cap; x and cap are a score and its cap, both times log2 e.  Below half the cap by tanh's series, x - x^3 / 3 + ..., whose
+// first term left out is 2^-23 of x there; above it as for small caps.  A cap beyond all scores leaves x as it is.
+__device__ __forceinline__ float capped(float x, float cap, float by) {
+    const float y = x * by, u = y * y;
+    float p = 21844.f / 6081075.f;
+    p = __builtin_fmaf(p, u, -1382.f / 155925.f);
+    p = __builtin_fmaf(p, u, 62.f / 2835.f);
+    p = __builtin_fmaf(p, u, -17.f / 315.f);
+    p = __builtin_fmaf(p, u, 2.f / 15.f);
+    p = __builtin_fmaf(p, u, -1.f / 3.f);
+    const float low = __builtin_fmaf(x, u * p, x), high = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * LOG2E * y)), cap);
+    return fabsf(y) < 0.5f ? low : high;
+}
+
 __device__ __forceinline__ u32 perm(u32 hi, u32 lo, u32 sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
 
 // two codes, bytes 0 and 2 of a word whose other bytes are zero, as 16-bit floats: 1024 + (code + 128) has the code's bits, with the

@@ -148,7 +148,14 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
         // t = score * log2 e + e of the values - offset
         const float base = r.M == LOWEST ? 0.f : r.M;
         float t[8];
-        if (a.softcap > 0.f) {
+        if (a.softcap > NEAR_CAP) {
+            const float f = r.factor * LOG2E, cap = a.softcap * LOG2E, by = 1.f / cap;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int n = LISTED ? j : j >> 2;
+                t[j] = capped(s[y][j >> 2][j & 3] * (f * x.ek[n]), cap, by) + (x.ev[n] - base);
+            }
+        } else if (a.softcap > 0.f) {
             // tanh(y) = 1 - 2 / (1 + e^(2 y))
             const float in = 2.f * LOG2E * r.factor / a.softcap, cap = a.softcap * LOG2E;
 #pragma unroll

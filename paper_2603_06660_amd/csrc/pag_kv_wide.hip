@@ -107,7 +107,8 @@ __device__ __forceinline__ void two_columns(const u32* w, u32 first, half8_t* ou
     }
 }
 
-template <int FMT, int C, bool CAP, int NW>
+// CAP: 0 none, 1 up to NEAR_CAP, 2 above it
+template <int FMT, int C, int CAP, int NW>
 __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend a, Head* heads) {
     constexpr u32 W = 64 * C, KEYS = STEP * W, VALUES = W * STEP;
     constexpr int KEY_TURNS = C == 2 ? 7 : 3;             // which pairs of pieces trade places in key_at
@@ -399,7 +400,11 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                     const float base = M == LOWEST ? 0.f : M;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        if constexpr (CAP) {
+                        if constexpr (CAP == 2) {
+                            const float by = factor * LOG2E * ek[2 * h + x], add = ev[2 * h + x] - base, cap = a.softcap * LOG2E, per = 1.f / cap;
+#pragma unroll
+                            for (int i = 8 * x; i < 8 * x + 8; ++i) S[h][i] = capped(S[h][i] * by, cap, per) + add;
+                        } else if constexpr (CAP == 1) {
                             const float by = 2.f * LOG2E * factor / a.softcap * ek[2 * h + x], cap = a.softcap * LOG2E, top = cap + (ev[2 * h + x] - base);
 #pragma unroll
                             for (int i = 8 * x; i < 8 * x + 8; ++i)
@@ -588,7 +593,7 @@ constexpr u32 lds_bytes(u32 width) { return 2 * 2 * STEP * width * 2; }
 // where a request has up to 128 rows half of the waves have none (32 requests of 64 rows, 300 to 12,000 keys: 118, 165).
 constexpr int MANY = 8;
 
-template <int FMT, int C, bool CAP, int NW>
+template <int FMT, int C, int CAP, int NW>
 int run_wide(hipStream_t st, const Attend& a, int num_cu) {
     const u32 grid = (u32)num_cu * wide_groups_per_cu(64 * C, NW);
     Head* heads = (Head*)(a.partial + 2ull * grid * (NW * WROWS) * (64 * C + 2));
@@ -601,7 +606,7 @@ int run_wide(hipStream_t st, const Attend& a, int num_cu) {
     return PAG_OK;
 }
 
-template <int FMT, int C, bool CAP>
+template <int FMT, int C, int CAP>
 int run(hipStream_t st, const Attend& a, int num_cu) {
     if constexpr (C <= 2) {
         if (a.many_rows) return run_wide<FMT, C, CAP, MANY>(st, a, num_cu);
@@ -609,14 +614,18 @@ int run(hipStream_t st, const Attend& a, int num_cu) {
     return run_wide<FMT, C, CAP, 4>(st, a, num_cu);
 }
 
-template <int FMT>
+template <int FMT, int CAP>
 int run_format(hipStream_t st, const Attend& a, int num_cu) {
     const u32 n = a.c.width / 64;
-    const bool cap = a.softcap > 0.f;
-    if (n == 1) return cap ? run<FMT, 1, true>(st, a, num_cu) : run<FMT, 1, false>(st, a, num_cu);
-    if (n == 2) return cap ? run<FMT, 2, true>(st, a, num_cu) : run<FMT, 2, false>(st, a, num_cu);
-    if (n == 3) return cap ? run<FMT, 3, true>(st, a, num_cu) : run<FMT, 3, false>(st, a, num_cu);
-    return cap ? run<FMT, 4, true>(st, a, num_cu) : run<FMT, 4, false>(st, a, num_cu);
+    if (n == 1) return run<FMT, 1, CAP>(st, a, num_cu);
+    if (n == 2) return run<FMT, 2, CAP>(st, a, num_cu);
+    if (n == 3) return run<FMT, 3, CAP>(st, a, num_cu);
+    return run<FMT, 4, CAP>(st, a, num_cu);
+}
+
+template <int CAP>
+int run_cap(hipStream_t st, const Attend& a, int num_cu) {
+    return a.c.fmt == PAG_KV_INT8 ? run_format<PAG_KV_INT8, CAP>(st, a, num_cu) : run_format<PAG_KV_FP8, CAP>(st, a, num_cu);
 }
 
 }  // namespace
@@ -628,7 +637,7 @@ u64 wide_workspace(u32 width, int num_cu) {
 }
 
 int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu) {
-    const int rc = a.c.fmt == PAG_KV_INT8 ? run_format<PAG_KV_INT8>(st, a, num_cu) : run_format<PAG_KV_FP8>(st, a, num_cu);
+    const int rc = a.softcap > NEAR_CAP ? run_cap<2>(st, a, num_cu) : a.softcap > 0.f ? run_cap<1>(st, a, num_cu) : run_cap<0>(st, a, num_cu);
     if (rc) return rc;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { pag_set_error(std::string("pag_kv_attend: ") + hipGetErrorString(e)); return PAG_EHIP; }

@@ -191,3 +191,50 @@ def test_rows_before_the_first_request_are_zeros(kv, max_new, n):
         del room
         out, lse = m.cache.attend(q.cuda(), step, out=(torch.full((9, 4, 64), 7.0).half().cuda(), torch.full((9, 4), 7.0).cuda()))
         check_rows(m, q, out, lse, 11, positions, lambda t, h: np.arange(positions[t] + 1), 0.125)
+
+
+CAPS = [65.0, 1e3, 1e4, 1e6, 1e30, 3e38]
+
+
+@pytest.mark.parametrize("softcap", CAPS + [1e-3, 1e-30])
+@pytest.mark.parametrize("dim, new", [(64, 1), (128, 40), (192, 3), (256, 33)])
+def test_attend_with_any_cap(kv, softcap, dim, new):
+    """A cap far above the scores leaves them as they are, to the rounding of a score; one far below makes all weights equal.  One row a
+    key, two tiles of rows, the wide kernel; in one workgroup and in shares."""
+    for n, fmt in ((300, "int8"), (2600, "fp8")):
+        m = Memory(kv, normal((n, 1, dim), 1, 2.0), normal((n, 1, dim), 2), 64, fmt)
+        q = torch.tensor(normal((new, 5, dim), 3)).half()
+        step = kv.KvStep(ints([m.order]), offsets=ints([0, new]), context=ints([n]), max_new=new)
+        out, lse = m.cache.attend(q.cuda(), step, softcap=softcap)
+        some = sorted({0, new // 2, new - 1})
+        positions = [n - new + t for t in some]
+        check_rows(m, q[some], out[some], lse[some], 11, positions, lambda t, h: np.arange(positions[t] + 1), dim ** -0.5, softcap)
+
+
+@pytest.mark.parametrize("softcap", CAPS + [1e-3, 1e-30])
+def test_selected_with_any_cap(kv, softcap):
+    m = Memory(kv, normal((400, 2, 96), 1, 2.0), normal((400, 2, 96), 2), 32, "int8")
+    q = torch.tensor(normal((2, 6, 96), 3)).half()
+    for k in (50, 2900):
+        ids = np.random.default_rng(k).integers(0, 400, (2, 2, k))
+        step = kv.KvStep(ints([m.order]), requests=ints([0, 0]), positions=ints([398, 399]))
+        out, lse = m.cache.attend_selected(q.cuda(), torch.tensor(ids).cuda(), step, window=7, softcap=softcap)
+
+        def keys_of(t, h):
+            p, row = 398 + t, ids[t, h // 3]
+            return np.concatenate([row[row <= p - 7], np.arange(p - 6, p + 1)])
+
+        check_rows(m, q, out, lse, 11, [398, 399], keys_of, 96 ** -0.5, softcap)
+
+
+def test_a_cap_of_nearly_nothing_and_keys_of_zeros(kv):
+    """Scores of zero under a cap that 32 bits hardly hold."""
+    m = Memory(kv, np.zeros((40, 1, 64)), normal((40, 1, 64), 2), 16, "int8")
+    q = torch.tensor(normal((33, 4, 64), 3)).half()
+    for new in (1, 33):
+        step = kv.KvStep(ints([m.order]), offsets=ints([0, new]), context=ints([40]), requests=ints([0] * new), positions=ints(np.arange(40 - new, 40)))
+        out, lse = m.cache.attend(q[:new].cuda(), step, softcap=1e-44)
+        check_rows(m, q[:new], out, lse, 11, list(range(40 - new, 40)), lambda t, h: np.arange(40 - new + t + 1), 64 ** -0.5)
+        ids = torch.arange(40).expand(new, 1, 40).contiguous().cuda()
+        out, lse = m.cache.attend_selected(q[:new].cuda(), ids, step, softcap=1e-44)
+        check_rows(m, q[:new], out, lse, 11, list(range(40 - new, 40)), lambda t, h: np.arange(40 - new + t + 1), 64 ** -0.5)
