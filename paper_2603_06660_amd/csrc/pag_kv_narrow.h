@@ -123,8 +123,9 @@ struct Scales {
     int at[N];
 };
 
-// T tiles of rows against one of keys.  keep: bit j set if the row may read key j; looked at only if `masked`
-template <int FMT, int C, int T, bool LISTED>
+// T tiles of rows against one of keys.  keep: bit j set if the row may read key j; looked at only if `masked`.  SLOPES: of lists, whether the call
+// has slopes; otherwise that is looked up
+template <int FMT, int C, int T, bool LISTED, bool SLOPES>
 __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, Rows<C> (&rows)[T], const Scales<LISTED>& x, bool masked, const u32 (&keep)[T]) {
     float4_t s[T][2];
 #pragma unroll
@@ -145,56 +146,91 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
 #pragma unroll
     for (int y = 0; y < T; ++y) {
         Rows<C>& r = rows[y];
-        // t = score * log2 e + e of the values - offset
-        const float base = r.M == LOWEST ? 0.f : r.M;
+        // t = score * log2 e + e of the values - offset.  Listed keys may all be far away, slope * distance 10^5 and more, of which the distances from each
+        // other are a small part: with slopes of lists the difference from the offset comes out of one rounding, before the score is added.
+        constexpr bool APART = LISTED && SLOPES;
         float t[8];
-        if (a.softcap > NEAR_CAP) {
-            const float f = r.factor * LOG2E, cap = a.softcap * LOG2E, by = 1.f / cap;
+        const auto exponents = [&](float base) {
+            if (a.softcap > NEAR_CAP) {
+                const float f = r.factor * LOG2E, cap = a.softcap * LOG2E, by = 1.f / cap;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = LISTED ? j : j >> 2;
-                t[j] = capped(s[y][j >> 2][j & 3] * (f * x.ek[n]), cap, by) + (x.ev[n] - base);
+                for (int j = 0; j < 8; ++j) {
+                    const int n = LISTED ? j : j >> 2;
+                    t[j] = capped(s[y][j >> 2][j & 3] * (f * x.ek[n]), cap, by) + (APART ? 0.f : x.ev[n] - base);
+                }
+            } else if (a.softcap > 0.f) {
+                // tanh(y) = 1 - 2 / (1 + e^(2 y))
+                const float in = 2.f * LOG2E * r.factor / a.softcap, cap = a.softcap * LOG2E;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int n = LISTED ? j : j >> 2;
+                    const float z = __builtin_amdgcn_exp2f(s[y][j >> 2][j & 3] * (in * x.ek[n]));
+                    t[j] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + z), cap + (APART ? 0.f : x.ev[n] - base));
+                }
+            } else {
+                const float f = r.factor * LOG2E;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int n = LISTED ? j : j >> 2;
+                    t[j] = __builtin_fmaf(s[y][j >> 2][j & 3], f * x.ek[n], APART ? 0.f : x.ev[n] - base);
+                }
             }
-        } else if (a.softcap > 0.f) {
-            // tanh(y) = 1 - 2 / (1 + e^(2 y))
-            const float in = 2.f * LOG2E * r.factor / a.softcap, cap = a.softcap * LOG2E;
+            if constexpr (APART) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = LISTED ? j : j >> 2;
-                const float z = __builtin_amdgcn_exp2f(s[y][j >> 2][j & 3] * (in * x.ek[n]));
-                t[j] = __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + z), cap + (x.ev[n] - base));
+                for (int j = 0; j < 8; ++j) {
+                    const int distance = r.position - x.at[j];          // in two parts that a float holds
+                    t[j] += __builtin_fmaf(-r.slope, (float)(distance & 4095), __builtin_fmaf(-r.slope, (float)(distance & ~4095), -base)) + x.ev[j];
+                }
+            } else if (!LISTED && a.slopes) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) t[j] -= r.slope * (float)(r.position - (x.at[LISTED ? 0 : j >> 2] + (j & 3)));
             }
-        } else {
-            const float f = r.factor * LOG2E;
+            if (masked) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = LISTED ? j : j >> 2;
-                t[j] = __builtin_fmaf(s[y][j >> 2][j & 3], f * x.ek[n], x.ev[n] - base);
+                for (int j = 0; j < 8; ++j) t[j] = keep[y] >> j & 1u ? t[j] : -INFINITY;
             }
-        }
-        if (a.slopes) {
+        };
+        const auto largest = [&]() {
+            float most = fmaxf(t[0], t[1]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] -= r.slope * (float)(r.position - (LISTED ? x.at[LISTED ? j : 0] : x.at[j >> 2] + (j & 3)));
-        }
-        if (masked) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = keep[y] >> j & 1u ? t[j] : -INFINITY;
-        }
-        float most = fmaxf(t[0], t[1]);
-#pragma unroll
-        for (int j = 2; j < 8; ++j) most = fmaxf(most, t[j]);
-        if (__ballot(most > (r.M == LOWEST ? LOWEST : HEADROOM))) {
+            for (int j = 2; j < 8; ++j) most = fmaxf(most, t[j]);
+            return most;
+        };
+        const auto of_row = [&](float most) {
             most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
+            return fmaxf(most, __shfl_xor(most, 32));
+        };
+        const auto move = [&](float M) {
+            const float alpha = __builtin_amdgcn_exp2f(r.M - M);
+            r.sum *= alpha;
+#pragma unroll
+            for (int c = 0; c < 4 * C; ++c) r.acc[c] *= alpha;
+            r.M = M;
+        };
+        const float base = r.M == LOWEST ? 0.f : r.M;
+        exponents(base);
+        float most = largest();
+        if (__ballot(most > (r.M == LOWEST ? LOWEST : HEADROOM))) {
+            most = of_row(most);
             // rows that need not move stay as they are: a row's result does not depend on its neighbours in the tile
             if (most > (r.M == LOWEST ? LOWEST : HEADROOM)) {
-                const float up = most - START, M = base + up, alpha = __builtin_amdgcn_exp2f(r.M - M);
+                const float up = most - START, M = base + up, by = APART ? M - base : up;
+                move(M);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] -= up;
-                r.sum *= alpha;
+                for (int j = 0; j < 8; ++j) t[j] -= by;
+                if constexpr (APART) {
+                    // numbers of 512 and more were rounded to 2^-15 and more: once again, from the offset where it is now.  Beyond 2^20 the offset is
+                    // off by that rounding itself and is put right first; beyond 2^28 its own is more than the weights have room for.
+                    if (fabsf(up) > 512.f) {
+                        exponents(r.M);
+                        if (fabsf(r.M) > 0x1p20f) {
+                            move(r.M + (of_row(largest()) - START));
+                            exponents(r.M);
 #pragma unroll
-                for (int c = 0; c < 4 * C; ++c) r.acc[c] *= alpha;
-                r.M = M;
+                            for (int j = 0; j < 8; ++j) t[j] = fminf(t[j], HEADROOM);
+                        }
+                    }
+                }
             }
         }
 #pragma unroll
@@ -425,7 +461,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 }
             }
         }
-        add_tile<FMT, C, T, false>(a, tile, rows, x, masked, keep);
+        add_tile<FMT, C, T, false, false>(a, tile, rows, x, masked, keep);
     };
     const auto start = [&]() {
 #pragma unroll
@@ -638,7 +674,7 @@ __device__ __forceinline__ void place_list(const Attend& a, ListPiece& p, u64 li
 }
 
 // The pieces that next(p) gives; a list has `units` units of 32 NW entries.
-template <int FMT, int C, int NW, bool WHOLE, typename Next>
+template <int FMT, int C, int NW, bool WHOLE, bool SLOPES, typename Next>
 __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& sh, Entries (&sh_entries)[NW][2], u32 units, Next&& next) {
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     const u32 entries = a.k + a.window;
@@ -730,7 +766,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
                 }
             }
         }
-        add_tile<FMT, C, 1, true>(a, tile, rows, scales, masked, keep);
+        add_tile<FMT, C, 1, true, SLOPES>(a, tile, rows, scales, masked, keep);
     };
     Tile<C> even, odd;
     u32 buffer = 0;
@@ -776,8 +812,11 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
     }
 }
 
-template <int FMT, int C>
-__global__ void __launch_bounds__(256, groups_per_cu(64 * C, 1)) k_attend_selected(Attend a, u32 units, u32 tiles) {
+// Slopes need registers that three workgroups a CU leave none of: 8 lists of 5,064 keys of 64 numbers, 4 of 40,000, in us, three 24.9, 44.7, two 20.3, 39.9
+constexpr u32 list_groups_per_cu(u32 width, bool slopes) { return slopes ? std::min(groups_per_cu(width, 1), 2u) : groups_per_cu(width, 1); }
+
+template <int FMT, int C, bool SLOPES>
+__global__ void __launch_bounds__(256, list_groups_per_cu(64 * C, SLOPES)) k_attend_selected(Attend a, u32 units, u32 tiles) {
     __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
     __shared__ __align__(16) Entries sh_entries[SPLIT_WAVES][2];
     const u32 cost = units + PIECE;
@@ -786,7 +825,7 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C, 1)) k_attend_select
     if (blockIdx.x >= parts) return;
     u64 at = share(total, parts, blockIdx.x);
     const u64 end = share(total, parts, blockIdx.x + 1);
-    attend_lists<FMT, C, SPLIT_WAVES, false>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
+    attend_lists<FMT, C, SPLIT_WAVES, false, SLOPES>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
         while (at < end) {
             const u64 part = divide(at, cost), list = divide(part, tiles);
             const u32 c0 = (u32)(at - part * cost), c1 = (u32)min((u64)cost, c0 + (end - at));
@@ -802,13 +841,13 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C, 1)) k_attend_select
     });
 }
 
-template <int FMT, int C, int NW>
+template <int FMT, int C, int NW, bool SLOPES>
 __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_selected_whole(Attend a, u32 tiles) {
     __shared__ __align__(16) Exchange<C, NW> sh;
     __shared__ __align__(16) Entries sh_entries[NW][2];
     const u32 units = max((a.k + a.window + NW * TILE - 1) / (NW * TILE), 1u);
     bool first = true;
-    attend_lists<FMT, C, NW, true>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
+    attend_lists<FMT, C, NW, true, SLOPES>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
         if (!first) return false;
         first = false;
         p.u0 = 0;
@@ -823,7 +862,8 @@ template <int FMT, int C, int NW>
 void run_whole(hipStream_t st, const Attend& a) {
     if (a.listed) {
         const u32 tiles = (a.group + ROWS - 1) / ROWS;
-        k_attend_selected_whole<FMT, C, NW><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
+        if (a.slopes) k_attend_selected_whole<FMT, C, NW, true><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
+        else k_attend_selected_whole<FMT, C, NW, false><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
     } else {
         k_attend_whole<FMT, C, 1, NW><<<a.s.requests * a.c.kv_heads, 64 * NW, 0, st>>>(a);
     }
@@ -849,7 +889,11 @@ void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
         return run_whole<FMT, C, 4>(st, a);
     }
     const u32 grid = (u32)num_cu * groups_per_cu(64 * C, a.row_tiles);
-    if (a.listed) return k_attend_selected<FMT, C><<<grid, 256, 0, st>>>(a, std::max<u32>((a.k + a.window + UNIT - 1) / UNIT, 1), (a.group + ROWS - 1) / ROWS);
+    if (a.listed) {
+        const u32 units = std::max<u32>((a.k + a.window + UNIT - 1) / UNIT, 1), tiles = (a.group + ROWS - 1) / ROWS;
+        if (a.slopes) return k_attend_selected<FMT, C, true><<<(u32)num_cu * list_groups_per_cu(64 * C, true), 256, 0, st>>>(a, units, tiles);
+        return k_attend_selected<FMT, C, false><<<grid, 256, 0, st>>>(a, units, tiles);
+    }
     if constexpr (C <= 3) {
         if (a.row_tiles == 2) return k_attend<FMT, C, 2><<<grid, 256, 0, st>>>(a);
     }

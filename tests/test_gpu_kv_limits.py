@@ -238,3 +238,21 @@ def test_a_cap_of_nearly_nothing_and_keys_of_zeros(kv):
         ids = torch.arange(40).expand(new, 1, 40).contiguous().cuda()
         out, lse = m.cache.attend_selected(q[:new].cuda(), ids, step, softcap=1e-44)
         check_rows(m, q[:new], out, lse, 11, list(range(40 - new, 40)), lambda t, h: np.arange(40 - new + t + 1), 64 ** -0.5)
+
+
+@pytest.mark.parametrize("page, position", [(16, 5000), (64, 300_000), (1 << 20, 5_000_000), (1 << 20, 1_000_000_000)])
+@pytest.mark.parametrize("softcap", [0.0, 30.0])
+def test_selected_far_away_with_slopes(kv, page, position, softcap):
+    """A list of tokens that all lie far from the one that reads them, without a window: their distances' differences decide, and these are small
+    numbers.  Slopes up to where slope * distance is some 10^8."""
+    n, dim, heads = 300, 64, 4
+    m = Memory(kv, normal((n, 1, dim), 1), normal((n, 1, dim), 2), page, "int8")
+    table = np.full((1, position // page + 1), -1)
+    table[0, :len(m.order)] = m.order
+    slopes = np.array([1.0, 0.25, 0.1, 0.003], np.float32) * min(1.0, 1e8 / position)
+    q = torch.tensor(normal((1, heads, dim), 3)).half()
+    for k in (1, 33, 300, 3000):
+        ids = np.random.default_rng(k).integers(0, n, (1, 1, k))
+        step = kv.KvStep(ints(table), requests=ints([0]), positions=ints([position]))
+        out, lse = m.cache.attend_selected(q.cuda(), torch.tensor(ids).cuda(), step, slopes=torch.tensor(slopes).cuda(), softcap=softcap)
+        check_rows(m, q, out, lse, 11, [position], lambda t, h: ids[0, 0], dim ** -0.5, softcap, slopes)
