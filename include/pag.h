@@ -407,7 +407,9 @@ int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* strea
  * largest finite magnitude.  Another block keeps its exponent unless the new tokens need a larger one; then what it held is
  * rounded again.  Rounding is to nearest even; infinities are held as the largest code, NaN as 0.
  * pag_kv_read: rows of the cache as numbers, [tokens][kv_heads][head_dim] with strides in elements (multiples of 16 bytes); k or v may be
- * null.  Slots -1 or out of range give zeros.  PAG_F32 and PAG_BF16 hold every number of the cache exactly.
+ * null.  Slots -1 or out of range give zeros.  PAG_F32 and PAG_BF16 hold every number of the cache exactly, but for what a block near the end of
+ * 32 bits rounds up to 2^128 and infinities held as the largest code there: that is read as the largest finite PAG_BF16, 255 * 2^120, where
+ * attention's results end as well.
  * tokens * kv_heads of a call has to be below 2^27.
  */
 int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride,

@@ -103,6 +103,13 @@ __device__ __forceinline__ void load8(const void* p, u64 at, u32 dtype, float* x
     widen_row8(*(const uint4*)((const uint16_t*)p + at), dtype, x);
 }
 
+// Blocks near the end of 32 bits hold their largest numbers rounded up to 2^128 (255.99 * 2^120 at 2^122 is 64 of these); what comes out, and means
+// of such numbers, ends at the largest that bf16 holds.  NaN stays what it is.
+__device__ __forceinline__ float finite(float x) {
+    constexpr float MOST = 0x1.fep127f;
+    return fabsf(x) > MOST ? copysignf(MOST, x) : x;
+}
+
 __device__ __forceinline__ u32 pack2(float a, float b, u32 dtype) {       // to nearest even
     const float2_t x = { a, b };
     if (dtype == PAG_BF16) return __builtin_bit_cast(u32, __builtin_convertvector(x, bf16x2_t));

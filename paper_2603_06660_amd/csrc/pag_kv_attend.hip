@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(256) k_join(Attend a, int groups) {
     if (d < a.c.dim) {
         const float by = all != 0.f ? 1.f / all : 0.f;
         const float x = sh_acc[0][d] + sh_acc[1][d] + sh_acc[2][d] + sh_acc[3][d], y = sh_acc[0][d + 1] + sh_acc[1][d + 1] + sh_acc[2][d + 1] + sh_acc[3][d + 1];
-        *(u32*)((uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + d) = pack2(x * by, y * by, a.dtype);
+        *(u32*)((uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + d) = pack2(finite(x * by), finite(y * by), a.dtype);
     }
     if (a.lse && threadIdx.x == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }

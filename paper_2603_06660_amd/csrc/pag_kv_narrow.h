@@ -331,7 +331,7 @@ __device__ __forceinline__ void finish(const Attend& a, const Where& w, const Ex
             uint16_t* out = (uint16_t*)a.out + (int64_t)t * a.o_ts + (int64_t)head * a.o_hs + first;
 #pragma unroll
             for (u32 n = 0; n < N; n += 2) {
-                if (first + n < a.c.dim) *(u32*)(out + n) = pack2(o[n] * f, o[n + 1] * f, a.dtype);
+                if (first + n < a.c.dim) *(u32*)(out + n) = pack2(finite(o[n] * f), finite(o[n + 1] * f), a.dtype);
             }
             if (a.lse && first == 0) a.lse[(u64)t * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
         }

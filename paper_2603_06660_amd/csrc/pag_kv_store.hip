@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(256) k_read(Load a) {
             for (u32 y = 0; y < EACH / 4; ++y) decode4<FMT>(w[n][y], x + 4 * y);
             // a slot that is none has no numbers, whatever the row that was read instead holds
 #pragma unroll
-            for (u32 y = 0; y < EACH; ++y) x[y] = up != 0.f ? x[y] * up : 0.f;
+            for (u32 y = 0; y < EACH; ++y) x[y] = up != 0.f ? finite(x[y] * up) : 0.f;
             T* to = (T*)a.x[kind] + (int64_t)(token0 + r) * a.ts[kind] + (int64_t)head * a.hs[kind] + at;
             typedef u32 word4 __attribute__((ext_vector_type(4)));
             word4 y;

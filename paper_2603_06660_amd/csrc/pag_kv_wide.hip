@@ -478,7 +478,8 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                     for (int i = 0; i < 4; ++i) {
                         const u32 d = n * 32 + 8 * i + 4 * hi;
                         if (d < a.c.dim)
-                            *(uint2*)(out + d) = make_uint2(pack2(acc[n][4 * i] * by, acc[n][4 * i + 1] * by, a.dtype), pack2(acc[n][4 * i + 2] * by, acc[n][4 * i + 3] * by, a.dtype));
+                            *(uint2*)(out + d) = make_uint2(pack2(finite(acc[n][4 * i] * by), finite(acc[n][4 * i + 1] * by), a.dtype),
+                                                               pack2(finite(acc[n][4 * i + 2] * by), finite(acc[n][4 * i + 3] * by), a.dtype));
                     }
                 }
                 if (a.lse && hi == 0) a.lse[(u64)(q.s.t0 + token) * a.heads + head] = sum != 0.f ? LN2 * (M + __builtin_amdgcn_logf(sum)) : -INFINITY;
@@ -579,7 +580,7 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
             o[0] = __builtin_fmaf(sh_acc[x][wave][d], by[x], o[0]);
             o[1] = __builtin_fmaf(sh_acc[x][wave][d + 1], by[x], o[1]);
         }
-        *(u32*)(out + d) = pack2(o[0] * f, o[1] * f, a.dtype);
+        *(u32*)(out + d) = pack2(finite(o[0] * f), finite(o[1] * f), a.dtype);
     }
     if (a.lse && lane == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }

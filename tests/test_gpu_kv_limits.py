@@ -256,3 +256,40 @@ def test_selected_far_away_with_slopes(kv, page, position, softcap):
         step = kv.KvStep(ints(table), requests=ints([0]), positions=ints([position]))
         out, lse = m.cache.attend_selected(q.cuda(), torch.tensor(ids).cuda(), step, slopes=torch.tensor(slopes).cuda(), softcap=softcap)
         check_rows(m, q, out, lse, 11, [position], lambda t, h: ids[0, 0], dim ** -0.5, softcap, slopes)
+
+
+FINITE = 255.0 * 2.0 ** 120      # the largest finite bf16
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_the_largest_numbers_stay_finite(kv, fmt):
+    """A block whose largest magnitude lies near the end of 32 bits is rounded up to 2^128: what is read back, and attention's mean of it, ends at
+    the largest number that 16 bits of bf16 hold."""
+    top = float(torch.finfo(torch.float32).max)
+    for big, new in ((top, 1), (FINITE, 1), (math.inf, 1), (top, 40), (FINITE, 300)):
+        n = max(3000 if new == 1 else 40, new)
+        v = normal((n, 1, 64), 2)
+        v[::3] = np.where(np.arange(64) % 2, big, -big)
+        v[1::3] = np.where(np.arange(64) % 4 < 2, top, -top)
+        k = torch.tensor(normal((n, 1, 64), 1))
+        cache = kv.KvCache(-(-n // 16), 1, 64, 16, fmt)
+        slots = torch.arange(n).cuda()
+        cache.append(k.float().cuda(), torch.tensor(v).float().cuda(), slots)
+        numbers = plain.numbers(cache.data.cpu().numpy(), cache.exponents.cpu().numpy(), 64, fmt).reshape(-1, 16, 2, 64).reshape(-1, 2, 64)[:n]
+        assert np.abs(numbers[:, 1]).max() >= 2.0 ** 128
+        held = np.clip(numbers, -FINITE, FINITE)
+        for dtype in (torch.float32, torch.bfloat16):
+            got = cache.read(slots, dtype=dtype)
+            assert (wide(got[0][:, 0]) == numbers[:, 0]).all() and (wide(got[1][:, 0]) == held[:, 1]).all()
+        q = torch.tensor(normal((new, 2, 64), 3)).to(torch.bfloat16)
+        positions = np.arange(n - new, n)
+        step = kv.KvStep(ints([np.arange(-(-n // 16))]), offsets=ints([0, new]), context=ints([n]), requests=ints([0] * new), positions=ints(positions), max_new=new)
+        one = torch.full((new, 1, 1), 3, dtype=torch.int64).cuda()
+        for (out, lse), keys in ((cache.attend(q.cuda(), step), None), (cache.attend(q.cuda(), step, window=1), 1), (cache.attend_selected(q.cuda(), one, step), 3)):
+            for t in range(0, new, 13):
+                p = positions[t]
+                at = np.arange(p + 1) if keys is None else np.array([p]) if keys == 1 else np.array([3] if p >= 3 else [], int)
+                for h in range(2):
+                    o, l, spread, products = plain.attend_row(wide(q[t, h]), numbers[at, 0], numbers[at, 1], 0.125)
+                    tol_o, tol_l = plain.tolerance(64, 8, o, spread, products)
+                    assert (np.abs(wide(out[t, h]) - np.clip(o, -FINITE, FINITE)) <= tol_o).all() and (l == lse[t, h] or abs(float(lse[t, h]) - l) <= tol_l)
