@@ -426,7 +426,9 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
  * multiple of kv_heads that divides heads.  Ids below 0, in the window or beyond the token itself are passed over (the window's tokens count
  * once); an id listed twice counts twice.  tokens * heads and requests * kv_heads have to be below 2^23 there, below 2^31 in pag_kv_attend.
  * A token that finds nothing to attend to gets zeros and an lse of -inf; so does padding.
- * Sums, maxima and scores are held in 32 bits; softmax weights are rounded to 16-bit floats for their product with the values.
+ * Sums, maxima and scores are held in 32 bits.  Rounded to 16-bit floats (11 bits) are the softmax weights for their product with the values,
+ * together with the values' scale: what lies below 2^-31 of a row's largest weight * 2^exponent is lost from out, not from lse or from the sum
+ * that out is divided by; and q, as multiples of 2^-32 of its row's largest magnitude at least.
  */
 int pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, int selected, uint32_t id_heads,
                            uint32_t k, uint64_t* bytes);

@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(256) k_join(Attend a, int groups) {
             const float* p = piece(first + (int)threadIdx.x);
             const float by = __builtin_amdgcn_exp2f(p[row] - top);
             sh_by[threadIdx.x] = by;
-            sum = __builtin_fmaf(p[ROWS + row], by, sum);
+            sum = add_scaled(sum, p[ROWS + row], p[row] - top);
         }
         __syncthreads();
         for (int i = (int)wave; i < n; i += 32) {

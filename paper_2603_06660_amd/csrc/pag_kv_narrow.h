@@ -114,7 +114,7 @@ __device__ __forceinline__ void start_rows(const Attend& a, const Where& w, int 
     for (int c = 0; c < 4 * C; ++c) r.acc[c] = float4_t{ 0.f, 0.f, 0.f, 0.f };
 }
 
-// What this lane's 8 keys are scaled by: 2^e of the keys, e of the values and 2^-e of the values.
+// What this lane's 8 keys are scaled by: 2^e of the keys, e of the values and 2^-e of the values (0 where the sum takes none, see FAR_EXPONENT).
 // LISTED: every key has its own and its position; otherwise keys 0 .. 3 and 4 .. 7 share theirs, and at holds the first one's position
 template <bool LISTED>
 struct Scales {
@@ -123,10 +123,11 @@ struct Scales {
     int at[N];
 };
 
-// T tiles of rows against one of keys.  keep: bit j set if the row may read key j; looked at only if `masked`.  SLOPES: of lists, whether the call
+// T tiles of rows against one of keys.  keep: bit j set if the row may read key j; looked at only if `masked`.  far: the
+// sum takes weights without their values' scale.  SLOPES: of lists, whether the call
 // has slopes; otherwise that is looked up
 template <int FMT, int C, int T, bool LISTED, bool SLOPES>
-__device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, Rows<C> (&rows)[T], const Scales<LISTED>& x, bool masked, const u32 (&keep)[T]) {
+__device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, Rows<C> (&rows)[T], const Scales<LISTED>& x, bool masked, const u32 (&keep)[T], bool far) {
     float4_t s[T][2];
 #pragma unroll
     for (int y = 0; y < T; ++y) s[y][0] = s[y][1] = float4_t{ 0.f, 0.f, 0.f, 0.f };
@@ -202,7 +203,7 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
         };
         const auto move = [&](float M) {
             const float alpha = __builtin_amdgcn_exp2f(r.M - M);
-            r.sum *= alpha;
+            r.sum = LISTED ? add_scaled(0.f, r.sum, r.M - M) : r.sum * alpha;
 #pragma unroll
             for (int c = 0; c < 4 * C; ++c) r.acc[c] *= alpha;
             r.M = M;
@@ -232,6 +233,10 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
                     }
                 }
             }
+        }
+        if (LISTED && far) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r.sum += __builtin_amdgcn_exp2f(t[j] - x.ev[LISTED ? j : 0]);
         }
 #pragma unroll
         for (int n = 0; n < Scales<LISTED>::N; ++n) {
@@ -313,7 +318,7 @@ __device__ __forceinline__ void finish(const Attend& a, const Where& w, const Ex
 #pragma unroll
         for (u32 v = 0; v < NW; ++v) {
             const float by = __builtin_amdgcn_exp2f(x.m[v][row] - M);
-            sum = __builtin_fmaf(x.sum[v][row], by, sum);
+            sum = add_scaled(sum, x.sum[v][row], x.m[v][row] - M);
 #pragma unroll
             for (u32 n = 0; n < N; n += 2) {
                 const float2 y = *(const float2*)&x.acc[v][row][first + n];
@@ -404,12 +409,14 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
     u32 page = 0, block_row = 0;
     uint16_t exponents = 0;
     u64 there = 0;
+    bool far = false;
     const auto page_of = [&](int at_key) -> u32 {
         return at_key < p.stop ? (u32)a.s.table[p.b * a.s.table_stride + (u32)at_key / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
     };
     const auto ask = [&]() {                  // what does not depend on each other is asked for together: pages and rows,
         from = p.start + (int)(wave * TILE);
         page = page_of(from + mine_at);
+        far = false;
         if (T == 1) fetch_rows<C>(a, p.w, raw);
     };
     const auto look_up = [&]() {              // then exponents and the first tile
@@ -417,6 +424,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
         block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)(from + mine_at) / BLOCK % a.c.page_blocks * BLOCK) : 0;
         exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
         there = __ballot(ok);
+        far = far || __ballot((int)(int8_t)(exponents >> 8) > FAR_EXPONENT);
         page = page_of(from + 32 * (int)(NW * TILE) + mine_at);
     };
     const u32 k_at = col * (128 * C) + g * 16, v_at = 4 * g * (128 * C) + 64 * C + col * (4 * C);
@@ -461,7 +469,20 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 }
             }
         }
-        add_tile<FMT, C, T, false, false>(a, tile, rows, x, masked, keep);
+        add_tile<FMT, C, T, false, false>(a, tile, rows, x, masked, keep, false);
+    };
+    const auto end = [&]() {                  // behind the last tile
+        if (!far) return;
+#pragma unroll
+        for (int y = 0; y < T; ++y) {
+            const Where w = tile_of(p.w, y);
+            const u32 row = w.row0 + col;
+            const uint16_t* row_at = (lane & 16) || row >= w.rows ? nullptr
+                : (const uint16_t*)a.q + (int64_t)(w.t0 + row / a.group) * a.q_ts + (int64_t)(w.head0 + row % a.group) * a.q_hs;
+            const float sum = far_sum<FMT, C>(far_rows(a, a.s.table + p.b * a.s.table_stride, p.w.kv_head, row_at, p.start + (int)(wave * TILE), p.stop, (int)(NW * TILE),
+                                                       lane & 16 ? -1 : rows[y].position, rows[y].slope, rows[y].M));
+            rows[y].sum = lane & 16 ? 0.f : sum;
+        }
     };
     const auto start = [&]() {
 #pragma unroll
@@ -488,6 +509,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 }
                 from += 32 * (int)(NW * TILE);
             }
+            end();
             const bool begun = p.u0 == 0, ended = p.u1 == p.units;
             float* partial = nullptr;
             if (!WHOLE) {
@@ -530,6 +552,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 load(even, 0);
             }
         }
+        end();
         // the next piece's first tile is on its way while this one's waves are added up
         const Where w = p.w;
         const bool begun = p.u0 == 0, ended = p.u1 == p.units;
@@ -687,6 +710,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
     int key = -1;                                // the positions and pages of the next one
     u32 page = 0;
     u64 there = 0;                               // which of this batch are keys
+    bool far = false;
     const u32 mine = (lane & 31) + (lane >> 5) * (NW * TILE);
     const auto id_of = [&](u32 n) -> int64_t { return n < a.k && n < stop ? a.ids[(int64_t)w.t0 * a.ids_ts + (int64_t)w.id_head * a.ids_hs + n] : -1; };
     const auto key_of = [&](u32 n) {             // from id
@@ -714,6 +738,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
         const u32 row = ok ? row_of(a.c, page, w.kv_head, (u32)key / BLOCK % a.c.page_blocks * BLOCK + ((u32)key & (BLOCK - 1))) : 0;
         const u32 e = ok ? *(const uint16_t*)(a.c.exponents + (u64)(row / BLOCK) * 2) : 0;
         there = __ballot(ok);
+        far = far || __ballot((int)(int8_t)(e >> 8) > FAR_EXPONENT);
         x.row[lane] = row;
         x.at[lane] = key;
         const u32 next = from + 2 * (NW * TILE) + mine;
@@ -724,7 +749,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
         const int ev = (int)(int8_t)(e >> 8);
         x.ek[lane] = power((int)(int8_t)e);
         x.ev[lane] = (float)ev;
-        x.down[lane] = power(-ev);
+        x.down[lane] = far ? 0.f : power(-ev);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -742,7 +767,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
             for (int j = 0; j < 4; ++j) load_words<C>(a.c.data + (u64)v[j] * (128 * C) + 64 * C + col * (4 * C), tile.v[4 * s + j]);
         }
     };
-    const auto add = [&](Tile<C>& tile, u32 buffer, int i, u32 found) {
+    const auto add = [&](Tile<C>& tile, u32 buffer, int i, u32 found, bool far_now) {
         const Entries& x = sh_entries[wave][buffer];
         Scales<true> scales;
 #pragma unroll
@@ -766,12 +791,13 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
                 }
             }
         }
-        add_tile<FMT, C, 1, true, SLOPES>(a, tile, rows, scales, masked, keep);
+        add_tile<FMT, C, 1, true, SLOPES>(a, tile, rows, scales, masked, keep, far_now);
     };
     Tile<C> even, odd;
     u32 buffer = 0;
     const auto begin_piece = [&]() {
         check();
+        far = false;
         key_of(from + mine);
         id = id_of(from + 2 * (NW * TILE) + mine);
         look_up(buffer);
@@ -787,15 +813,16 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
         start_rows<C>(a, w, position, raw, rows[0]);
         while (from < stop) {
             const u32 lo = (u32)there, hi = (u32)(there >> 32), now = buffer;
+            const bool far_now = far;
             load(odd, now, 1);
-            if (lo) add(even, now, 0, lo);
+            if (lo) add(even, now, 0, lo, far_now);
             from += 2 * (NW * TILE);
             if (from < stop) {
                 buffer ^= 1;
                 look_up(buffer);
                 load(even, buffer, 0);
             }
-            if (hi) add(odd, now, 1, hi);
+            if (hi) add(odd, now, 1, hi, far_now);
         }
         const Where done = w;
         float* partial = nullptr;

@@ -18,8 +18,6 @@ namespace {
 constexpr u32 WROWS = 32;                   // query rows of a wave
 constexpr u32 STEP = 64;                    // keys of a step, one block of 16 a wave to fetch
 
-typedef float float16_t __attribute__((ext_vector_type(16)));
-
 struct Tiles {
     Span s;
     u32 rows, count, pairs, pair_units, mid_units;
@@ -115,6 +113,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
     extern __shared__ __align__(16) _Float16 lds[];       // two buffers of keys and values
     __shared__ float sh_scale[2][4][2];                   // 2^e of the keys' block, e of the values'
     __shared__ u32 sh_there[2][4];
+    __shared__ u32 sh_far[2];                             // this piece, and the next: a block's values have an e above FAR_EXPONENT
     __shared__ u64 sh_sum[NW];
     __shared__ u64 sh_begin;
     __shared__ u32 sh_b;
@@ -158,11 +157,15 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
         if (s.tokens && !s.context) write_empty(a, s.t0, s.t0 + s.tokens);
     }
     write_padding(a);
-    if (threadIdx.x == 0) heads[self].last = -1;
+    if (threadIdx.x == 0) {
+        heads[self].last = -1;
+        sh_far[0] = sh_far[1] = 0;
+    }
     if (begin >= end) return;
     __syncthreads();
     u32 b = sh_b;
     u64 before = sh_begin, at = begin;
+    u32 turn = 0;                                           // of sh_far
     Tiles q = tiles_of<NW>(a, b);
 
     while (at < end) {
@@ -252,6 +255,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
         u32 block_row = 0;
         int ek_mine = 0, ev_mine = 0;
         u64 there = 0;
+        u64 far = 0;
         const auto look_up = [&](int from) {
             const int at_key = from + (int)(lane * STEP + block * BLOCK);
             bool ok = false;
@@ -268,6 +272,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                 }
             }
             there = __ballot(ok);
+            far |= __ballot(ev_mine > FAR_EXPONENT);
         };
         Fetch<C, NW> f;
         const u32 key = part * (64 / NW) + lane / NW, key_piece0 = lane % NW * Fetch<C, NW>::PIECES;
@@ -329,6 +334,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
         const u32 k_lds = key_at<C>(col, hi) * 2, v_lds = value_at(col, hi) * 2;
         const u32 steps = (u32)(max(stop - start, 0) + (int)STEP - 1) / STEP;
         __syncthreads();                                        // the piece before has been read
+        if (threadIdx.x == 0) sh_far[turn ^ 1] = 0;
         // step n + 1 into LDS, and step n + 2 on its way
         const auto prepare = [&](u32 n) {
             if (n + 1 < steps) stage(n + 1, start + (int)((n + 1) * STEP), (n + 1) & 1);
@@ -466,6 +472,13 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
             lds_barrier();
         }
 
+        if (far) sh_far[turn] = 1;
+        lds_barrier();
+        if (__builtin_amdgcn_readfirstlane((int)sh_far[turn])) {
+            const uint16_t* row_at = real ? (const uint16_t*)a.q + (int64_t)(q.s.t0 + token) * a.q_ts + (int64_t)head * a.q_hs : nullptr;
+            sum = far_sum<FMT, C>(far_rows(a, table, kv_head, row_at, start, busy ? min(stop, w_p1 + 1) : start, 32, position, slope, M));
+        }
+        turn ^= 1;
         sum += __shfl_xor(sum, 32);
         const bool begun = u0 == 0, ended = u1 == r.units;
         if (begun && ended) {
@@ -538,14 +551,14 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
 #pragma unroll
         for (int u = 0; u < 4; ++u) top = fmaxf(top, m[u]);
         const float was = __builtin_amdgcn_exp2f(M - top);
-        sum *= was;
+        sum = add_scaled(0.f, sum, M - top);
 #pragma unroll
         for (u32 n = 0; n < N; ++n) acc[n] *= was;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             if (i + 4 * u >= pieces) break;
             const float is = __builtin_amdgcn_exp2f(m[u] - top);
-            sum = __builtin_fmaf(s[u], is, sum);
+            sum = add_scaled(sum, s[u], m[u] - top);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 acc[4 * c] = __builtin_fmaf(y[u][c].x, is, acc[4 * c]);
@@ -568,7 +581,7 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
         by[x] = __builtin_amdgcn_exp2f(sh_m[x][wave] - top);
-        all = __builtin_fmaf(sh_s[x][wave], by[x], all);
+        all = add_scaled(all, sh_s[x][wave], sh_m[x][wave] - top);
     }
     const u32 t = h.t0 + row / a.group, head = h.head0 + row % a.group;
     const float f = all != 0.f ? 1.f / all : 0.f;

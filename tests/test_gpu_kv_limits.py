@@ -293,3 +293,28 @@ def test_the_largest_numbers_stay_finite(kv, fmt):
                     o, l, spread, products = plain.attend_row(wide(q[t, h]), numbers[at, 0], numbers[at, 1], 0.125)
                     tol_o, tol_l = plain.tolerance(64, 8, o, spread, products)
                     assert (np.abs(wide(out[t, h]) - np.clip(o, -FINITE, FINITE)) <= tol_o).all() and (l == lse[t, h] or abs(float(lse[t, h]) - l) <= tol_l)
+
+
+@pytest.mark.parametrize("new, heads", [(1, 2), (1, 20), (40, 4), (300, 2)])
+@pytest.mark.parametrize("n", [160, 3200])
+def test_values_whose_exponents_are_as_far_apart_as_they_can_be(kv, new, heads, n):
+    """The sum of the weights is that of all keys, whatever their values' sizes: zeros beside numbers near the end of 32 bits, in any order, in one wave's
+    tiles, in several waves' and in several workgroups'.  A weight that is less than 2^-31 of the row's largest times its block's scale is lost from
+    the values' sum, as a 16-bit float cannot hold it."""
+    dim, n = 64, max(n, new + 20)
+    for seed in range(3):
+        rng = np.random.default_rng(seed)
+        v = rng.standard_normal((n, 1, dim))
+        for block in range(0, n, 16):
+            v[block:block + 16] *= [0.0, 2.0 ** -80, 1.0, 2.0 ** 40, 2.0 ** 90, 2.0 ** 120][rng.integers(0, 6) if seed else min(5, block * 6 // n)]
+        for fmt in ("int8", "fp8"):
+            m = Memory(kv, rng.standard_normal((n, 1, dim)), v, 32, fmt)
+            q = torch.tensor(normal((new, heads, dim), 3)).to(torch.bfloat16)
+            positions = np.arange(n - new, n)
+            step = kv.KvStep(ints([m.order]), offsets=ints([0, new]), context=ints([n]), requests=ints([0] * new), positions=ints(positions), max_new=new)
+            some = sorted({0, new // 2, new - 1})
+            out, lse = m.cache.attend(q.cuda(), step)
+            check_rows(m, q[some], out[some], lse[some], 8, positions[some], lambda t, h: np.arange(positions[some][t] + 1), dim ** -0.5, slack=2.0 ** -18)
+            ids = rng.integers(0, n - new + 1, (new, 1, 200))
+            out, lse = m.cache.attend_selected(q.cuda(), torch.tensor(ids).cuda(), step, window=0)
+            check_rows(m, q[some], out[some], lse[some], 8, positions[some], lambda t, h: ids[some][t, 0], dim ** -0.5, slack=2.0 ** -18)
