@@ -9,6 +9,8 @@ A decoding step, in order (every call goes onto the current stream and returns w
     out, lse = cache.attend(q, step)                                    # reads everything
     out, lse = cache.attend_selected(q, ids, step, window=64)           # reads what a search found, and the last 64 tokens
     tables.commit(step)
+
+None of it has a backward: tensors that require a gradient are refused unless gradients are switched off (torch.no_grad).
 """
 from __future__ import annotations
 
@@ -57,10 +59,17 @@ def _gpu(device):
     return device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
 
 
+def _no_graph(t, what):
+    """The cache is 8 bits, written once, and its calls have no backward: a graph that ends here would be a silent zero."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise PagError("%s requires a gradient, and the cache has no backward: detach it, or call under torch.no_grad()" % what)
+
+
 def _array(t, dtype, shape, device, what):
     """The address of a dense tensor of this type, shape and device."""
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise PagError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
+    _no_graph(t, what)
     return t.data_ptr()
 
 
@@ -71,6 +80,7 @@ def _rows(t, shape, device, what, dtypes=_DTYPES):
                        (what, tuple(shape), device, ", ".join(str(x) for x in dtypes)))
     if t.stride(2) != 1 and t.shape[2] > 1:
         raise PagError("%s: the last dimension must be dense" % what)
+    _no_graph(t, what)
 
 
 # the number of a GPU's current stream, without an object around it where torch offers that

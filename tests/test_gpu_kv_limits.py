@@ -318,3 +318,18 @@ def test_values_whose_exponents_are_as_far_apart_as_they_can_be(kv, new, heads, 
             ids = rng.integers(0, n - new + 1, (new, 1, 200))
             out, lse = m.cache.attend_selected(q.cuda(), torch.tensor(ids).cuda(), step, window=0)
             check_rows(m, q[some], out[some], lse[some], 8, positions[some], lambda t, h: ids[some][t, 0], dim ** -0.5, slack=2.0 ** -18)
+
+
+def test_calls_on_tensors_that_require_a_gradient_are_refused(kv):
+    cache, tables = kv.KvCache(4, 2, 64, 16), kv.KvTables(1, 4, 4, 16)
+    step = tables.extend(ints([3]), 3)
+    x, q = torch.randn(3, 2, 64, device="cuda").half(), torch.randn(3, 4, 64, device="cuda").half()
+    ids = torch.zeros(3, 2, 2, dtype=torch.int64, device="cuda")
+    slopes = torch.ones(4, device="cuda", requires_grad=True)
+    asks = lambda t: t.clone().requires_grad_()
+    for call in (lambda: cache.append(asks(x), x, step.slots), lambda: cache.append(x, asks(x), step.slots), lambda: cache.attend(asks(q), step),
+                 lambda: cache.attend_selected(asks(q), ids, step), lambda: cache.attend(q, step, slopes=slopes)):
+        with pytest.raises(kv.PagError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()

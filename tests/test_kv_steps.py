@@ -91,3 +91,17 @@ def test_a_refused_call_hands_nothing_over(calls):
     with pytest.raises(kv.PagError):
         a.extend(ints(3), 4, out=step, commit=True)
     assert step.lengths is mine and not made
+
+
+def test_tensors_that_require_a_gradient_are_refused(calls):
+    kv, _ = calls
+    x, slopes = torch.zeros(3, 2, 8, requires_grad=True), torch.zeros(2, requires_grad=True)
+    for t in (x, x * 2.0):
+        with pytest.raises(kv.PagError, match="gradient"):
+            kv._rows(t, (3, 2, 8), x.device, "q")
+        kv._rows(t.detach(), (3, 2, 8), x.device, "q")
+        with torch.no_grad():
+            kv._rows(t, (3, 2, 8), x.device, "q")
+    with pytest.raises(kv.PagError, match="gradient"):
+        kv._array(slopes, torch.float32, (2,), slopes.device, "slopes")
+    assert kv._array(slopes.detach(), torch.float32, (2,), slopes.device, "slopes") == slopes.data_ptr()
