@@ -314,7 +314,7 @@ int pag_searcher_free(pag_searcher* s);
  * A cache has a row of keys and a row of values side by side for every page, head and token, W = head_dim rounded up to a
  * multiple of 64 bytes each (zeros behind head_dim), and an exponent per block of 16 tokens, head and kind:
  *     data      uint8 [num_pages][kv_heads][page_tokens][2][W]
- *     exponents int8  [num_pages][kv_heads][page_tokens / 16][2]            number = code * 2^exponent
+ *     exponents int8  [num_pages][kv_heads][page_tokens / 16][2]            number = code * 2^exponent, exponents of -126 to 126
  * Codes are signed integers (largest 127) or floats of 4 exponent and 3 mantissa bits without infinities (largest 448).
  * A power of two as scale means that a product with it never rounds and that a block which outgrows its exponent is rounded
  * again at most once per doubling.  slot = page * page_tokens + place in the page; a request's token p is in page table[p / page_tokens].
@@ -394,7 +394,7 @@ typedef struct {
  * and all arrays of `step`; the rest of `tables` changes only where step->lengths and step->free_count are its own arrays, so
  * a step can be looked at before it is taken over.
  * pag_kv_release: the requests with done[r] != 0 (dev int32 [requests]) give back their pages, first page first, in order of
- * their numbers, and hold nothing then.
+ * their numbers, and hold nothing then.  Pages for which free_pages has no room (num_pages) are not put anywhere.
  */
 int pag_kv_extend(const pag_kv_tables* tables, const int32_t* add, const pag_kv_step* step, void* stream);
 int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* stream);
@@ -402,7 +402,8 @@ int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* strea
 /*
  * pag_kv_append: writes the keys and values of `tokens` tokens (dev, dtype PAG_F32 / F16 / BF16, [tokens][kv_heads][head_dim], strides in
  * elements, multiples of 16 bytes) into their slots (dev int64 [tokens]; -1 or out of range: left out).  The tokens of one block have to
- * follow each other in the call, in ascending order, as pag_kv_extend numbers them.  A block that begins with the call (its
+ * follow each other in the call, in ascending order, with no other ones and none that are left out between them, as pag_kv_extend numbers them:
+ * otherwise several waves write the block, and what it holds then is not defined.  A block that begins with the call (its
  * first token is among the new ones) is cleared first; its exponent is the smallest e >= -64 at which the largest code reaches the
  * largest finite magnitude.  Another block keeps its exponent unless the new tokens need a larger one; then what it held is
  * rounded again.  Rounding is to nearest even; infinities are held as the largest code, NaN as 0.
@@ -424,7 +425,8 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
  * pag_kv_attend_selected: it attends to the last `window` tokens and to the tokens whose positions ids lists (dev int64
  * [tokens][id_heads][k], strides in elements, last dimension dense): id_heads is kv_heads (the heads of a group share a list), heads, or a
  * multiple of kv_heads that divides heads.  Ids below 0, in the window or beyond the token itself are passed over (the window's tokens count
- * once); an id listed twice counts twice.  tokens * heads and requests * kv_heads have to be below 2^23 there, below 2^31 in pag_kv_attend.
+ * once); an id listed twice counts twice.  tokens * heads and requests * kv_heads have to be below 2^23 there, below 2^31 in pag_kv_attend; k + window
+ * below 2^30.
  * A token that finds nothing to attend to gets zeros and an lse of -inf; so does padding.
  * Sums, maxima and scores are held in 32 bits.  Rounded to 16-bit floats (11 bits) are the softmax weights for their product with the values,
  * together with the values' scale: what lies below 2^-31 of a row's largest weight * 2^exponent is lost from out, not from lse or from the sum

@@ -333,3 +333,92 @@ def test_calls_on_tensors_that_require_a_gradient_are_refused(kv):
             call()
         with torch.no_grad():
             call()
+
+
+# ---- layouts --------------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("max_new", [1, 20, 300])
+@pytest.mark.parametrize("n", [150, 3000])
+def test_strided_rows_and_tables(kv, max_new, n):
+    """q and out that are slices of larger arrays, heads before tokens; a table that is a slice of a wider one.  Bit for bit what dense ones give."""
+    m = Memory(kv, normal((n, 2, 64), 1), normal((n, 2, 64), 2), 32, "int8")
+    heads, tokens = 6, 9
+    dense = torch.tensor(normal((tokens, heads, 64), 3)).half().cuda()
+    news, contexts = [4, 0, 5], [n, 0, n - 7]
+    positions = list(range(n - 4, n)) + list(range(n - 12, n - 7))
+    wide_table = torch.full((3, len(m.order) + 5), 1 << 30, dtype=torch.int32, device="cuda")
+    wide_table[:, 2:-3] = ints([m.order] * 3)
+    arrays = dict(offsets=ints([0, 4, 4, 9]), context=ints(contexts), requests=ints([0] * 4 + [2] * 5), positions=ints(positions), max_new=max_new)
+    ids = torch.randint(0, n - 20, (tokens, 2, 40), generator=torch.Generator().manual_seed(1)).cuda()
+    wide_ids = torch.full((2, tokens, 50), 5, dtype=torch.int64, device="cuda")
+    wide_ids[:, :, 3:43] = ids.transpose(0, 1)
+    one, two = kv.KvStep(ints([m.order] * 3), **arrays), kv.KvStep(wide_table[:, 2:-3], **arrays)
+    want = m.cache.attend(dense, one), m.cache.attend_selected(dense, ids, one, window=5)
+    check_rows(m, dense, *want[0], 11, positions, lambda t, h: np.arange(positions[t] + 1), 0.125)
+    some = ids.cpu().numpy()
+    check_rows(m, dense, *want[1], 11, positions, lambda t, h: np.concatenate([some[t, h // 3], np.arange(positions[t] - 4, positions[t] + 1)]), 0.125)
+    fused = torch.full((tokens, 3 * heads, 80), 9.0, dtype=torch.float16, device="cuda")
+    by_head = torch.full((heads, tokens, 64), 9.0, dtype=torch.float16, device="cuda")
+    fused[:, heads:2 * heads, 8:72] = dense
+    by_head.copy_(dense.transpose(0, 1))
+    for q in (fused[:, heads:2 * heads, 8:72], by_head.transpose(0, 1)):
+        rest = torch.full((tokens, 2 * heads, 72), 7.0, dtype=torch.float16, device="cuda")
+        heads_first = torch.full((heads + 1, tokens, 64), 7.0, dtype=torch.float16, device="cuda")
+        for out in (rest[:, heads:, :64], heads_first[1:].transpose(0, 1)):
+            got = m.cache.attend(q, two, out=(out, None))
+            assert got[0] is out and torch.equal(out, want[0][0])
+            out.fill_(7.0)
+            lse = torch.empty(tokens, heads, device="cuda")
+            m.cache.attend_selected(q, wide_ids[:, :, 3:43].transpose(0, 1), two, window=5, out=(out, lse))
+            assert torch.equal(out, want[1][0]) and torch.equal(lse, want[1][1])
+        assert (rest[:, :heads] == 7.0).all() and (rest[:, :, 64:] == 7.0).all() and (heads_first[0] == 7.0).all()
+
+
+@pytest.mark.parametrize("id_heads, k, window", [(2, 40, 0), (2, 40, 5), (6, 7, 30), (2, 3000, 64)])
+def test_selected_of_several_tokens_of_a_request(kv, id_heads, k, window):
+    """Each of a request's new tokens has a list and a window of its own; lists may name tokens that are new themselves."""
+    n = 3100 if k > 1000 else 260
+    m = Memory(kv, normal((n, 2, 64), 1), normal((n, 2, 64), 2), 16, "fp8")
+    news, ends = [5, 1, 17], [n, 100, n - 50]
+    requests = [r for r, a in enumerate(news) for _ in range(a)]
+    positions = [p for a, e in zip(news, ends) for p in range(e - a, e)]
+    rng = np.random.default_rng(k)
+    ids = rng.integers(-1, n, (len(positions), id_heads, k))
+    for t, p in enumerate(positions):
+        ids[t, :, ::3] = rng.integers(max(0, p - 60), p + 3, ids[t, :, ::3].shape)
+    q = torch.tensor(normal((len(positions), 6, 64), 3)).to(torch.bfloat16)
+    step = kv.KvStep(ints([m.order] * 3), requests=ints(requests), positions=ints(positions))
+    out, lse = m.cache.attend_selected(q.cuda(), torch.tensor(ids).cuda(), step, window=window)
+
+    def keys_of(t, h):
+        p, row = positions[t], ids[t, h * id_heads // 6]
+        return np.concatenate([row[(row >= 0) & (row <= p - window)], np.arange(max(0, p - window + 1), p + 1)]).astype(int)
+
+    check_rows(m, q, out, lse, 8, positions, keys_of, 0.125)
+
+
+# ---- pages that come back -------------------------------------------------------------------------------------------------------
+
+
+def test_release_of_long_requests(kv):
+    """Thousands of pages of one request, and requests of one page on both sides of it."""
+    tables = kv.KvTables(5, 7000, 9000, 16)
+    add = [3, 6250 * 16, 0, 1500 * 16 + 1, 16]
+    tables.commit(tables.extend(ints(add), sum(add)))
+    table, count = tables.table.cpu().numpy(), int(tables.free_count)
+    assert count == 9000 - (1 + 6250 + 1501 + 1) and sorted(table[table >= 0].tolist()) == list(range(9000 - count))
+    free = tables.free_pages[:count].tolist()
+    tables.release(ints([0, 1, 1, 1, 0]))
+    free += table[1, :6250].tolist() + table[3, :1501].tolist()
+    assert tables.lengths.tolist() == [3, 0, 0, 0, 16] and tables.free_pages[:int(tables.free_count)].tolist() == free
+
+
+def test_release_onto_a_stack_without_room(kv):
+    """Pages for which the stack has no room are not put anywhere."""
+    lengths, table, free = ints([40, 16, 0]), ints([[7, 8, 9], [5, -1, -1], [1, 2, 3]]), ints([11, 12, 13, 99])
+    guard = torch.full((12,), -7, dtype=torch.int32, device="cuda")
+    guard[4:8] = free
+    tables = kv.KvTables.from_tensors(lengths, table, guard[4:8], ints([2]), 16)
+    tables.release(ints([1, 1, 1]))
+    assert guard.tolist() == [-7] * 4 + [11, 12, 7, 8] + [-7] * 4 and tables.free_count.tolist() == [4] and tables.lengths.tolist() == [0, 0, 0]
