@@ -5,8 +5,6 @@
 
 namespace pagkv {
 
-typedef float float16_t __attribute__((ext_vector_type(16)));
-
 constexpr float LOWEST = -3.0e38f;        // M before the first key
 constexpr float HEADROOM = 15.f;          // weights stay below 2^15
 constexpr float START = 7.f;              // and are 2^7 at most when M moves: 16-bit floats then hold 2^-31 of the largest
@@ -14,7 +12,7 @@ constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LN2 = 0.69314718055994530942f;
 
 // Up to this cap a capped score is cap - 2 cap / (1 + e^(2 score / cap)), one exponential and one reciprocal, whose error is 2^-22 of the cap (of 64 a
-// hundredth of what a weight's rounding to 11 bits does).  Above it the error has to be the score's own, see capped().
+// twentieth of what a weight's rounding to 11 bits does).  Above it the error has to be the score's own, see capped().
 constexpr float NEAR_CAP = 64.f;
 
 // cap * tanh(x / cap), by: 1 / cap; x and cap are a score and its cap, both times log2 e.  Below half the cap by tanh's series, x - x^3 / 3 + ..., whose
@@ -35,7 +33,7 @@ __device__ __forceinline__ u32 perm(u32 hi, u32 lo, u32 sel) { return __builtin_
 
 // A weight is carried with its values' scale, w = 2^(t) with t = score * log2 e + e - M, and 2^-e takes that off again in the weights' sum.  32 bits hold
 // weights down to 2^-126, so that a key whose e lies 120 below the largest would be missing there: once a wave has seen an e above this one
-// (values of 2^31 and more; e is -64 at least), 2^(t - e) itself is summed up, beside the weights in lists, otherwise by far_sum() once all keys are added.
+// (values of 2^31 and more; e is -64 at least), 2^(t - e) itself is summed up, in the narrow kernels beside the weights, in the wide one once all keys are added.
 constexpr int FAR_EXPONENT = 24;
 
 // sum + x * 2^d, d <= 0 or so, also where 2^d alone leaves 32 bits
@@ -149,73 +147,6 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 b) {
 // nothing, and position - window would leave 32 bits.
 __device__ __forceinline__ int oldest_of(const Attend& a, int position) {
     return a.window && position >= 0 && (u32)position >= a.window ? position - (int)a.window + 1 : 0;
-}
-
-// What far_sum looks at: a piece's keys and this lane's row.
-struct FarRows {
-    const uint8_t* data;
-    const int8_t* exponents;
-    const int32_t* table;
-    const uint16_t* q;                      // row lane % 32; null: no such row
-    u32 dim, dtype, page_blocks, kv_heads, kv_head, page_tokens, num_pages;
-    int start, stop, stride, position, oldest;
-    float scale, cap, slope, M;
-};
-
-__device__ __forceinline__ FarRows far_rows(const Attend& a, const int32_t* table, u32 kv_head, const uint16_t* q, int start, int stop, int stride, int position, float slope, float M) {
-    return FarRows{ a.c.data, a.c.exponents, table, q, a.c.dim, a.dtype, a.c.page_blocks, a.c.kv_heads, kv_head, a.c.page_tokens, a.c.num_pages,
-                    start, stop, stride, position, oldest_of(a, position), a.scale, a.softcap, slope, M };
-}
-
-// This lane's part, every other four keys, of the sum of 2^(score log2 e - M) over keys start .. stop - 1, 32 of each `stride`, straight from memory: for
-// pieces with values' exponents above FAR_EXPONENT.  A call of its own: with this code, or a sum of its own, in a kernel's loop the loop's
-// registers are shared out otherwise (4 chunks of 700 to 2,000 tokens, heads of 64: 455 -> 471 us, with the call 456 to 462).
-template <int FMT, int C>
-__device__ __attribute__((noinline)) float far_sum(FarRows r) {
-    constexpr u32 W = 64 * C;
-    const u32 lane = threadIdx.x & 63, col = lane & 31, hi = lane >> 5;
-    const auto numbers = [&](int n, float* x) {
-        if (r.q && n * 16 + hi * 8 < r.dim) return load8(r.q, n * 16 + hi * 8, r.dtype, x);
-        for (int j = 0; j < 8; ++j) x[j] = 0.f;
-    };
-    float x[8], most = 0.f;
-    for (int n = 0; n < 4 * C; ++n) {
-        numbers(n, x);
-        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
-    }
-    most = fmaxf(most, __shfl_xor(most, 32));
-    const int up = min(max((int)(__float_as_uint(most) >> 23) - 127 - 7, -100), 100);       // as the loop's rows
-    const float down = power(-up), factor = r.scale * power(up) * LOG2E, cap = r.cap * LOG2E;
-    float sum = 0.f;
-    for (int from = r.start; from < r.stop; from += r.stride) {
-        const int first = from + (int)(col & BLOCK);
-        const u32 page = first < r.stop ? (u32)r.table[(u32)first / BLOCK / r.page_blocks] : 0xFFFFFFFFu;
-        const bool ok = page < r.num_pages;
-        const u32 row = ok ? (page * r.kv_heads + r.kv_head) * r.page_tokens + (u32)first / BLOCK % r.page_blocks * BLOCK : 0;
-        const int e = ok ? r.exponents[(u64)(row / BLOCK) * 2] : 0;
-        const u64 there = __ballot(ok);
-        const uint8_t* k = r.data + (u64)(row + (col & (BLOCK - 1))) * (2 * W) + hi * 8;
-        float16_t S;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = 0.f;
-        for (int n = 0; n < 4 * C; ++n) {
-            const uint2 codes = *(const uint2*)(k + 16 * n);
-            half8_t q;
-            numbers(n, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = (_Float16)(x[j] * down);
-            S = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8<FMT>(codes.x, codes.y), q, S, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int key = from + 8 * (i >> 2) + 4 * (int)hi + (i & 3);
-            float t = S[i] * (factor * power(__builtin_amdgcn_readlane(e, (i >> 3) * (int)BLOCK)));
-            if (r.cap > 0.f) t = capped(t, cap, 1.f / cap);
-            t -= r.slope * (float)(r.position - key);
-            if ((there >> ((i >> 3) * BLOCK) & 1u) && key <= r.position && key >= r.oldest) sum += __builtin_amdgcn_exp2f(t - r.M);
-        }
-    }
-    return sum;
 }
 
 // zeros for tokens before the first request and behind the last one; this workgroup's part of them

@@ -124,9 +124,10 @@ struct Scales {
 };
 
 // T tiles of rows against one of keys.  keep: bit j set if the row may read key j; looked at only if `masked`.  far: the
-// sum takes weights without their values' scale.  SLOPES: of lists, whether the call
-// has slopes; otherwise that is looked up
-template <int FMT, int C, int T, bool LISTED, bool SLOPES>
+// sum takes weights without their values' scale.  SLOPES: of lists, whether the call has slopes; otherwise that is looked up.  CAPPED: by a cap above
+// NEAR_CAP.  Both are kernels of their own: code that a call does not run lies between code that it does, and short calls wait for
+// its fetch (one request of 500 tokens 10.1 us with the large caps' code, 9.6 without).
+template <int FMT, int C, int T, bool LISTED, bool SLOPES, bool CAPPED>
 __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, Rows<C> (&rows)[T], const Scales<LISTED>& x, bool masked, const u32 (&keep)[T], bool far) {
     float4_t s[T][2];
 #pragma unroll
@@ -152,7 +153,7 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
         constexpr bool APART = LISTED && SLOPES;
         float t[8];
         const auto exponents = [&](float base) {
-            if (a.softcap > NEAR_CAP) {
+            if constexpr (CAPPED) {
                 const float f = r.factor * LOG2E, cap = a.softcap * LOG2E, by = 1.f / cap;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -203,7 +204,7 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
         };
         const auto move = [&](float M) {
             const float alpha = __builtin_amdgcn_exp2f(r.M - M);
-            r.sum = LISTED ? add_scaled(0.f, r.sum, r.M - M) : r.sum * alpha;
+            r.sum = add_scaled(0.f, r.sum, r.M - M);
 #pragma unroll
             for (int c = 0; c < 4 * C; ++c) r.acc[c] *= alpha;
             r.M = M;
@@ -234,9 +235,9 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
                 }
             }
         }
-        if (LISTED && far) {
+        if (far) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r.sum += __builtin_amdgcn_exp2f(t[j] - x.ev[LISTED ? j : 0]);
+            for (int j = 0; j < 8; ++j) r.sum += __builtin_amdgcn_exp2f(t[j] - x.ev[LISTED ? j : j >> 2]);
         }
 #pragma unroll
         for (int n = 0; n < Scales<LISTED>::N; ++n) {
@@ -397,7 +398,7 @@ __device__ __forceinline__ void place_piece(const Attend& a, Piece& p, const Spa
 
 // The pieces that next(p) gives, one after the other.  A wave has T tiles of rows: keys are widened once for all of them.  WHOLE: the pieces
 // are whole row tiles.
-template <int FMT, int C, int T, int NW, bool WHOLE, typename Next>
+template <int FMT, int C, int T, int NW, bool WHOLE, bool CAPPED, typename Next>
 __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& sh, Next&& next) {
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     Piece p;
@@ -424,7 +425,6 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
         block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)(from + mine_at) / BLOCK % a.c.page_blocks * BLOCK) : 0;
         exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
         there = __ballot(ok);
-        far = far || __ballot((int)(int8_t)(exponents >> 8) > FAR_EXPONENT);
         page = page_of(from + 32 * (int)(NW * TILE) + mine_at);
     };
     const u32 k_at = col * (128 * C) + g * 16, v_at = 4 * g * (128 * C) + 64 * C + col * (4 * C);
@@ -446,9 +446,11 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             const int e = __builtin_amdgcn_readlane((int)exponents, 2 * i + s), ev = (int)(int8_t)(e >> 8);
             x.ek[s] = power((int)(int8_t)e);
             x.ev[s] = (float)ev;
+            far = far || ev > FAR_EXPONENT;
             x.down[s] = power(-ev);
             x.at[s] = pos + s * (int)BLOCK + 4 * (int)g;
         }
+        if (far) x.down[0] = x.down[1] = 0.f;
         const u32 two = (u32)(there >> (2 * i)) & 3u;
         const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos < oldest_of(a, p.p1);
         u32 keep[T];
@@ -469,20 +471,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 }
             }
         }
-        add_tile<FMT, C, T, false, false>(a, tile, rows, x, masked, keep, false);
-    };
-    const auto end = [&]() {                  // behind the last tile
-        if (!far) return;
-#pragma unroll
-        for (int y = 0; y < T; ++y) {
-            const Where w = tile_of(p.w, y);
-            const u32 row = w.row0 + col;
-            const uint16_t* row_at = (lane & 16) || row >= w.rows ? nullptr
-                : (const uint16_t*)a.q + (int64_t)(w.t0 + row / a.group) * a.q_ts + (int64_t)(w.head0 + row % a.group) * a.q_hs;
-            const float sum = far_sum<FMT, C>(far_rows(a, a.s.table + p.b * a.s.table_stride, p.w.kv_head, row_at, p.start + (int)(wave * TILE), p.stop, (int)(NW * TILE),
-                                                       lane & 16 ? -1 : rows[y].position, rows[y].slope, rows[y].M));
-            rows[y].sum = lane & 16 ? 0.f : sum;
-        }
+        add_tile<FMT, C, T, false, false, CAPPED>(a, tile, rows, x, masked, keep, far);
     };
     const auto start = [&]() {
 #pragma unroll
@@ -509,7 +498,6 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 }
                 from += 32 * (int)(NW * TILE);
             }
-            end();
             const bool begun = p.u0 == 0, ended = p.u1 == p.units;
             float* partial = nullptr;
             if (!WHOLE) {
@@ -552,7 +540,6 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 load(even, 0);
             }
         }
-        end();
         // the next piece's first tile is on its way while this one's waves are added up
         const Where w = p.w;
         const bool begun = p.u0 == 0, ended = p.u1 == p.units;
@@ -569,7 +556,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
     }
 }
 
-template <int FMT, int C, int T>
+template <int FMT, int C, int T, bool CAPPED>
 __global__ void __launch_bounds__(256, groups_per_cu(64 * C, T)) k_attend(Attend a) {
     __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
     __shared__ u64 sh_sum[SPLIT_WAVES];
@@ -644,11 +631,11 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C, T)) k_attend(Attend
         }
         return false;
     };
-    attend_pieces<FMT, C, T, SPLIT_WAVES, false>(a, sh, next_piece);
+    attend_pieces<FMT, C, T, SPLIT_WAVES, false, CAPPED>(a, sh, next_piece);
 }
 
 // A workgroup for each request and key/value head, which reads all of its keys: nothing to share out and nothing to join.
-template <int FMT, int C, int T, int NW>
+template <int FMT, int C, int T, int NW, bool CAPPED>
 __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_whole(Attend a) {
     __shared__ __align__(16) Exchange<C, NW> sh;
     const u32 b = blockIdx.x / a.c.kv_heads, kv_head = blockIdx.x % a.c.kv_heads;
@@ -661,7 +648,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_whole(Attend
     }
     const u32 tiles = (s.tokens * a.group + T * ROWS - 1) / (T * ROWS);
     u32 tile = 0;
-    attend_pieces<FMT, C, T, NW, true>(a, sh, [&](Piece& p) -> bool {
+    attend_pieces<FMT, C, T, NW, true, CAPPED>(a, sh, [&](Piece& p) -> bool {
         if (tile == tiles) return false;
         p.b = b;
         p.units = p.u1 = 1;
@@ -697,7 +684,7 @@ __device__ __forceinline__ void place_list(const Attend& a, ListPiece& p, u64 li
 }
 
 // The pieces that next(p) gives; a list has `units` units of 32 NW entries.
-template <int FMT, int C, int NW, bool WHOLE, bool SLOPES, typename Next>
+template <int FMT, int C, int NW, bool WHOLE, bool SLOPES, bool CAPPED, typename Next>
 __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& sh, Entries (&sh_entries)[NW][2], u32 units, Next&& next) {
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     const u32 entries = a.k + a.window;
@@ -791,7 +778,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
                 }
             }
         }
-        add_tile<FMT, C, 1, true, SLOPES>(a, tile, rows, scales, masked, keep, far_now);
+        add_tile<FMT, C, 1, true, SLOPES, CAPPED>(a, tile, rows, scales, masked, keep, far_now);
     };
     Tile<C> even, odd;
     u32 buffer = 0;
@@ -842,7 +829,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
 // Slopes need registers that three workgroups a CU leave none of: 8 lists of 5,064 keys of 64 numbers, 4 of 40,000, in us, three 24.9, 44.7, two 20.3, 39.9
 constexpr u32 list_groups_per_cu(u32 width, bool slopes) { return slopes ? std::min(groups_per_cu(width, 1), 2u) : groups_per_cu(width, 1); }
 
-template <int FMT, int C, bool SLOPES>
+template <int FMT, int C, bool SLOPES, bool CAPPED>
 __global__ void __launch_bounds__(256, list_groups_per_cu(64 * C, SLOPES)) k_attend_selected(Attend a, u32 units, u32 tiles) {
     __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
     __shared__ __align__(16) Entries sh_entries[SPLIT_WAVES][2];
@@ -852,7 +839,7 @@ __global__ void __launch_bounds__(256, list_groups_per_cu(64 * C, SLOPES)) k_att
     if (blockIdx.x >= parts) return;
     u64 at = share(total, parts, blockIdx.x);
     const u64 end = share(total, parts, blockIdx.x + 1);
-    attend_lists<FMT, C, SPLIT_WAVES, false, SLOPES>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
+    attend_lists<FMT, C, SPLIT_WAVES, false, SLOPES, CAPPED>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
         while (at < end) {
             const u64 part = divide(at, cost), list = divide(part, tiles);
             const u32 c0 = (u32)(at - part * cost), c1 = (u32)min((u64)cost, c0 + (end - at));
@@ -868,13 +855,13 @@ __global__ void __launch_bounds__(256, list_groups_per_cu(64 * C, SLOPES)) k_att
     });
 }
 
-template <int FMT, int C, int NW, bool SLOPES>
+template <int FMT, int C, int NW, bool SLOPES, bool CAPPED>
 __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_selected_whole(Attend a, u32 tiles) {
     __shared__ __align__(16) Exchange<C, NW> sh;
     __shared__ __align__(16) Entries sh_entries[NW][2];
     const u32 units = max((a.k + a.window + NW * TILE - 1) / (NW * TILE), 1u);
     bool first = true;
-    attend_lists<FMT, C, NW, true, SLOPES>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
+    attend_lists<FMT, C, NW, true, SLOPES, CAPPED>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {
         if (!first) return false;
         first = false;
         p.u0 = 0;
@@ -885,25 +872,23 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_selected_who
     });
 }
 
-template <int FMT, int C, int NW>
+template <int FMT, int C, int NW, bool CAPPED>
 void run_whole(hipStream_t st, const Attend& a) {
     if (a.listed) {
         const u32 tiles = (a.group + ROWS - 1) / ROWS;
-        if (a.slopes) k_attend_selected_whole<FMT, C, NW, true><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
-        else k_attend_selected_whole<FMT, C, NW, false><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
+        if (a.slopes) k_attend_selected_whole<FMT, C, NW, true, CAPPED><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
+        else k_attend_selected_whole<FMT, C, NW, false, CAPPED><<<a.s.tokens * a.id_heads * tiles, 64 * NW, 0, st>>>(a, tiles);
     } else {
-        k_attend_whole<FMT, C, 1, NW><<<a.s.requests * a.c.kv_heads, 64 * NW, 0, st>>>(a);
+        k_attend_whole<FMT, C, 1, NW, CAPPED><<<a.s.requests * a.c.kv_heads, 64 * NW, 0, st>>>(a);
     }
 }
 
-}  // namespace
-
-template <int FMT, int C>
-void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
+template <int FMT, int C, bool CAPPED>
+void run_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
     if (whole) {
         if constexpr (C <= 3) {
             if (!a.listed && a.row_tiles == 2) {
-                k_attend_whole<FMT, C, 2, 4><<<a.s.requests * a.c.kv_heads, 256, 0, st>>>(a);
+                k_attend_whole<FMT, C, 2, 4, CAPPED><<<a.s.requests * a.c.kv_heads, 256, 0, st>>>(a);
                 return;
             }
         }
@@ -911,20 +896,28 @@ void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
         // 777 tokens 9.7, 8.3; 16 of 500 tokens 10.7, 9.9; 64 lists of 1,064 keys 17.2, 14.4; 64 requests of 10 to 100 tokens 8.7, 12.9; 96 of 300 to 1,000
         // tokens 32, 37; 1,536 lists of 164 keys 27, 44
         if constexpr (C <= 2) {
-            if (narrow_groups(a) <= (u64)num_cu) return run_whole<FMT, C, 8>(st, a);
+            if (narrow_groups(a) <= (u64)num_cu) return run_whole<FMT, C, 8, CAPPED>(st, a);
         }
-        return run_whole<FMT, C, 4>(st, a);
+        return run_whole<FMT, C, 4, CAPPED>(st, a);
     }
     const u32 grid = (u32)num_cu * groups_per_cu(64 * C, a.row_tiles);
     if (a.listed) {
         const u32 units = std::max<u32>((a.k + a.window + UNIT - 1) / UNIT, 1), tiles = (a.group + ROWS - 1) / ROWS;
-        if (a.slopes) return k_attend_selected<FMT, C, true><<<(u32)num_cu * list_groups_per_cu(64 * C, true), 256, 0, st>>>(a, units, tiles);
-        return k_attend_selected<FMT, C, false><<<grid, 256, 0, st>>>(a, units, tiles);
+        if (a.slopes) return k_attend_selected<FMT, C, true, CAPPED><<<(u32)num_cu * list_groups_per_cu(64 * C, true), 256, 0, st>>>(a, units, tiles);
+        return k_attend_selected<FMT, C, false, CAPPED><<<grid, 256, 0, st>>>(a, units, tiles);
     }
     if constexpr (C <= 3) {
-        if (a.row_tiles == 2) return k_attend<FMT, C, 2><<<grid, 256, 0, st>>>(a);
+        if (a.row_tiles == 2) return k_attend<FMT, C, 2, CAPPED><<<grid, 256, 0, st>>>(a);
     }
-    k_attend<FMT, C, 1><<<grid, 256, 0, st>>>(a);
+    k_attend<FMT, C, 1, CAPPED><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace
+
+template <int FMT, int C>
+void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
+    if (a.softcap > NEAR_CAP) run_narrow<FMT, C, true>(st, a, num_cu, whole);
+    else run_narrow<FMT, C, false>(st, a, num_cu, whole);
 }
 
 }  // namespace pagkv

@@ -18,6 +18,8 @@ namespace {
 constexpr u32 WROWS = 32;                   // query rows of a wave
 constexpr u32 STEP = 64;                    // keys of a step, one block of 16 a wave to fetch
 
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
 struct Tiles {
     Span s;
     u32 rows, count, pairs, pair_units, mid_units;
@@ -103,6 +105,73 @@ __device__ __forceinline__ void two_columns(const u32* w, u32 first, half8_t* ou
 #pragma unroll
         for (int c = 0; c < 2; ++c) out[c] = widen8<FMT>(t[0][c], t[1][c]);
     }
+}
+
+// What far_sum looks at: a piece's keys and this lane's row.
+struct FarRows {
+    const uint8_t* data;
+    const int8_t* exponents;
+    const int32_t* table;
+    const uint16_t* q;                      // row lane % 32; null: no such row
+    u32 dim, dtype, page_blocks, kv_heads, kv_head, page_tokens, num_pages;
+    int start, stop, position, oldest;
+    float scale, cap, slope, M;
+};
+
+__device__ __forceinline__ FarRows far_rows(const Attend& a, const int32_t* table, u32 kv_head, const uint16_t* q, int start, int stop, int position, float slope, float M) {
+    return FarRows{ a.c.data, a.c.exponents, table, q, a.c.dim, a.dtype, a.c.page_blocks, a.c.kv_heads, kv_head, a.c.page_tokens, a.c.num_pages,
+                    start, stop, position, oldest_of(a, position), a.scale, a.softcap, slope, M };
+}
+
+// This lane's part, every other four keys, of the sum of 2^(score log2 e - M) over keys start .. stop - 1, straight from memory: for
+// pieces with values' exponents above FAR_EXPONENT.  A call of its own: with this code, or a sum of its own, in a kernel's loop the loop's
+// registers are shared out otherwise (4 chunks of 700 to 2,000 tokens, heads of 64: 455 -> 471 us, with the call 456 to 462).
+template <int FMT, int C>
+__device__ __attribute__((noinline)) float far_sum(FarRows r) {
+    constexpr u32 W = 64 * C;
+    const u32 lane = threadIdx.x & 63, col = lane & 31, hi = lane >> 5;
+    const auto numbers = [&](int n, float* x) {
+        if (r.q && n * 16 + hi * 8 < r.dim) return load8(r.q, n * 16 + hi * 8, r.dtype, x);
+        for (int j = 0; j < 8; ++j) x[j] = 0.f;
+    };
+    float x[8], most = 0.f;
+    for (int n = 0; n < 4 * C; ++n) {
+        numbers(n, x);
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
+    }
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const int up = min(max((int)(__float_as_uint(most) >> 23) - 127 - 7, -100), 100);       // as the loop's rows
+    const float down = power(-up), factor = r.scale * power(up) * LOG2E, cap = r.cap * LOG2E;
+    float sum = 0.f;
+    for (int from = r.start; from < r.stop; from += 32) {
+        const int first = from + (int)(col & BLOCK);
+        const u32 page = first < r.stop ? (u32)r.table[(u32)first / BLOCK / r.page_blocks] : 0xFFFFFFFFu;
+        const bool ok = page < r.num_pages;
+        const u32 row = ok ? (page * r.kv_heads + r.kv_head) * r.page_tokens + (u32)first / BLOCK % r.page_blocks * BLOCK : 0;
+        const int e = ok ? r.exponents[(u64)(row / BLOCK) * 2] : 0;
+        const u64 there = __ballot(ok);
+        const uint8_t* k = r.data + (u64)(row + (col & (BLOCK - 1))) * (2 * W) + hi * 8;
+        float16_t S;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[i] = 0.f;
+        for (int n = 0; n < 4 * C; ++n) {
+            const uint2 codes = *(const uint2*)(k + 16 * n);
+            half8_t q;
+            numbers(n, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = (_Float16)(x[j] * down);
+            S = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8<FMT>(codes.x, codes.y), q, S, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int key = from + 8 * (i >> 2) + 4 * (int)hi + (i & 3);
+            float t = S[i] * (factor * power(__builtin_amdgcn_readlane(e, (i >> 3) * (int)BLOCK)));
+            if (r.cap > 0.f) t = capped(t, cap, 1.f / cap);
+            t -= r.slope * (float)(r.position - key);
+            if ((there >> ((i >> 3) * BLOCK) & 1u) && key <= r.position && key >= r.oldest) sum += __builtin_amdgcn_exp2f(t - r.M);
+        }
+    }
+    return sum;
 }
 
 // CAP: 0 none, 1 up to NEAR_CAP, 2 above it
@@ -272,7 +341,6 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                 }
             }
             there = __ballot(ok);
-            far |= __ballot(ev_mine > FAR_EXPONENT);
         };
         Fetch<C, NW> f;
         const u32 key = part * (64 / NW) + lane / NW, key_piece0 = lane % NW * Fetch<C, NW>::PIECES;
@@ -339,7 +407,10 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
         const auto prepare = [&](u32 n) {
             if (n + 1 < steps) stage(n + 1, start + (int)((n + 1) * STEP), (n + 1) & 1);
             if (n + 2 < steps) {
-                if (((n + 2) & 63) == 0) look_up(start + (int)((n + 2) * STEP));
+                if (((n + 2) & 63) == 0) {
+                    far |= __ballot(ev_mine > FAR_EXPONENT);
+                    look_up(start + (int)((n + 2) * STEP));
+                }
                 fetch(n + 2);
             }
         };
@@ -472,11 +543,11 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
             lds_barrier();
         }
 
-        if (far) sh_far[turn] = 1;
+        if (far | __ballot(ev_mine > FAR_EXPONENT)) sh_far[turn] = 1;
         lds_barrier();
         if (__builtin_amdgcn_readfirstlane((int)sh_far[turn])) {
             const uint16_t* row_at = real ? (const uint16_t*)a.q + (int64_t)(q.s.t0 + token) * a.q_ts + (int64_t)head * a.q_hs : nullptr;
-            sum = far_sum<FMT, C>(far_rows(a, table, kv_head, row_at, start, busy ? min(stop, w_p1 + 1) : start, 32, position, slope, M));
+            sum = far_sum<FMT, C>(far_rows(a, table, kv_head, row_at, start, busy ? min(stop, w_p1 + 1) : start, position, slope, M));
         }
         turn ^= 1;
         sum += __shfl_xor(sum, 32);
