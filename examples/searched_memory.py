@@ -46,7 +46,8 @@ class SearchedMemory:
         self.cache.read(slots, out=(points[..., :self.dim].transpose(0, 1), None))
         lengths = points.square().sum(2)
         if self.indexes is None:
-            self.radius = 1.2 * lengths.amax(1, keepdim=True)       # of later keys too; a longer one is indexed as if it ended there
+            # of later keys too; a longer one gets no coordinate, and is ranked as farther away than its inner product says
+            self.radius = 1.2 * lengths.amax(1, keepdim=True)
         points[..., self.dim] = (self.radius - lengths).clamp(min=0.0).sqrt()
         return points
 

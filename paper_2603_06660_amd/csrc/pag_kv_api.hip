@@ -92,11 +92,12 @@ int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_a
     }
     // Query rows that a request's new tokens make for a key/value head, as far as the host can tell.  One or two tiles of 16 rows a wave, each
     // of which widens its own keys, or the wide kernel, whose waves share them; in us, 8 key/value heads of 128, as one, two, wide:
-    //   32 requests of 300 to 12,000 tokens: 16 rows 49, 51, 103; 20 rows 79, 54, 103; 64 rows 144, 95, 118; 96 rows 206, 126, 124; 256 rows 494, 276, 208
-    //   one of 30,000 tokens: 16 rows 24, 27, 50; 64 rows 40, 36, 50; 128 rows 59, 48, 52; 256 rows 104, 77, 65
-    //   32 of 3,000 tokens: 64 rows -, 75, 92; 96 rows -, 122, 95.  With few keys the wide kernel is not better before some 500 rows (one request of
-    //   3,000 tokens, 128 rows: 22, 25, 33), but those are the short calls.
-    // Rows of more than 192 numbers leave no registers for two tiles: 32 requests of 4,000 tokens, 256 numbers a head: 32 rows 207, 225, 256; 48 rows 301, 429, 264.
+    //   32 requests of 300 to 12,000 tokens: 16 rows 50, 51, 114; 20 rows 79, 54, 114; 64 rows 143, 92, 126; 96 rows 203, 125, 128; 256 rows 483, 278, 223
+    //   one of 30,000 tokens: 16 rows 23, 27, 45; 64 rows 39, 35, 49; 128 rows 60, 47, 52; 256 rows 102, 73, 64
+    //   32 of 3,000 tokens: 64 rows 130, 74, 90; 96 rows 192, 119, 92.  With few keys the wide kernel is not better before some 500 rows (one request of
+    //   3,000 tokens, 128 rows: 21, 24, 36), but those are the short calls.
+    // Rows of more than 192 numbers leave no registers for two tiles, which spill: 32 requests of 4,000 tokens, 256 numbers a head: 32 rows 201, (225), 259;
+    // 48 rows 288, (429), 265.
     const u64 rows = (step->max_new ? step->max_new : (step->tokens + step->requests - 1) / step->requests) * (u64)a->group;
     const bool two = a->c.width <= 192;
     a->row_tiles = selected || rows <= (two ? 16u : 32u) ? 1 : two && rows <= 64 ? 2 : 0;

@@ -14,7 +14,7 @@
 // Work is split evenly over a fixed number of workgroups, in units of 128 keys, across requests of any lengths: each finds its share by
 // one sum over the requests' lengths.  A row block whose keys went to several workgroups is joined by a second kernel.
 // Bound by memory: 64 requests of 300 to 12,000 tokens, 8 heads of 128 numbers, 485 MB in 103 us with the joining, 400,000 tokens of one request 819 MB in
-// 146 us (5.6 TB/s; a kernel that only reads reaches 6.0).  Up to 16 rows cost what one costs.
+// 146 us with it (5.6 TB/s; a kernel that only reads reaches 6.0).  Up to 16 rows cost what one costs.
 #pragma once
 
 #include <algorithm>

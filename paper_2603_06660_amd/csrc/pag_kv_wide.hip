@@ -7,7 +7,9 @@
 // meanwhile.  Shares are counted in steps of 64 keys of the tiles' own causal lengths: tile j and the j-th from the end make a pair,
 // and all pairs of a request are equally long, so that a share is found without adding up tiles.
 // 4 chunks of 700 to 2,000 tokens that end at 2,500 to 9,000, 32 heads over 8 of 128 numbers: 540 us, 810 TFLOP/s, with the cap's tanh 640 us; a product of
-// 8192 x 8192 x 8192 reaches 1,160.  The matrix units are busy for 40 % of it and the vector units for 49 %, two waves taking turns on each SIMD.
+// 8192 x 8192 x 8192 reaches 1,160.  The matrix units are busy for 40 % of it and the vector units for 50 %: in a wave scores, weights and values' products
+// follow one another, and all waves meet every 64 keys, so that the two waves of a SIMD overlap in part only.  (No third wave: 250 of 256 registers are taken;
+// the four-wave kernel for 72 to 128 numbers spills 8 to 17.)
 #include <algorithm>
 
 #include "pag_kv_attend.h"
