@@ -179,6 +179,27 @@ def test_a_step_with_fewer_rows_than_its_requests_have_tokens(kv, max_new):
     check_rows(m, q, out, lse, 11, positions, lambda t, h: np.arange(positions[t] + 1), 0.125)
 
 
+@pytest.mark.parametrize("dim, new, heads", [(64, 100, 1), (128, 20, 5), (128, 1, 24), (128, 70, 4), (192, 25, 4), (192, 1, 3), (256, 100, 1), (256, 1, 30), (80, 40, 2)])
+@pytest.mark.parametrize("softcap, slopes, window", [(0.0, False, 0), (20.0, True, 0), (500.0, False, 90)])
+def test_values_far_apart_in_every_kernel(kv, dim, new, heads, softcap, slopes, window):
+    """Rows of every width, in one tile, in two, by four waves and by eight: a few blocks of values of 2^40 to 2^120 among zeros and usual ones, with a cap, with slopes, with a window."""
+    n = 1500
+    rng = np.random.default_rng(dim + new)
+    v = rng.standard_normal((n, 1, dim))
+    for block in range(0, n, 16):
+        v[block:block + 16] *= rng.choice([0.0, 1.0, 1.0, 1.0, 2.0 ** 40, 2.0 ** 120])
+    for fmt in ("int8", "fp8"):
+        m = Memory(kv, rng.standard_normal((n, 1, dim)), v, 48, fmt)
+        slope = np.exp2(-8.0 * (1 + np.arange(heads)) / heads).astype(np.float32) if slopes else None
+        q = torch.tensor(normal((new, heads, dim), 3)).to(torch.bfloat16)
+        some = sorted({0, new // 2, new - 1})
+        positions = np.arange(n - new, n)[some]
+        step = kv.KvStep(ints([m.order]), offsets=ints([0, new]), context=ints([n]), max_new=new)
+        out, lse = m.cache.attend(q.cuda(), step, softcap=softcap, window=window, slopes=None if slope is None else torch.tensor(slope).cuda())
+        check_rows(m, q[some], out[some], lse[some], 8, positions, lambda t, h: np.arange(max(0, positions[t] - window + 1) if window else 0, positions[t] + 1),
+                   dim ** -0.5, softcap, slope, slack=2.0 ** -18)
+
+
 @pytest.mark.parametrize("max_new, n", [(1, 200), (1, 3000), (20, 200), (20, 3000), (300, 200), (300, 3000)])
 def test_rows_before_the_first_request_are_zeros(kv, max_new, n):
     """offsets that begin behind row 0; in one workgroup and in shares, with few and with many rows."""
