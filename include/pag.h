@@ -301,9 +301,9 @@ int pag_searcher_get_counters(const pag_searcher* s, pag_counters* out);
 int pag_searcher_free(pag_searcher* s);
 
 /*
- * A memory that is searched: the keys and values of a language model's tokens in 8 bits, in pages, and attention over all of
- * them or over the tokens that a search returned (pag_search on an index over the keys; its ids, -1 where there is none, go
- * into pag_kv_attend_selected as they are).
+ * A memory that is searched: the keys and values of a language model's tokens in 8 or 4 bits, in pages, and attention over all of
+ * them, over the tokens that a search returned (pag_search on an index over the keys; its ids, -1 where there is none, go
+ * into pag_kv_attend_selected as they are), or over blocks of tokens that a cheap score selects.
  *
  * These calls belong into a decoding loop, many to a step, so they differ from the ones above in two points: they enqueue
  * their work on the stream that they are given and return without waiting for it, and they allocate nothing, so that a loop
@@ -318,8 +318,12 @@ int pag_searcher_free(pag_searcher* s);
  * Codes are signed integers (largest 127) or floats of 4 exponent and 3 mantissa bits without infinities (largest 448).
  * A power of two as scale means that a product with it never rounds and that a block which outgrows its exponent is rounded
  * again at most once per doubling.  slot = page * page_tokens + place in the page; a request's token p is in page table[p / page_tokens].
+ * A cache of 4 bits a number (PAG_KV_FP4: a sign, 2 exponent and 1 mantissa bits: 0, 1/2, 1, 3/2, 2, 3, 4, 6) has rows of W / 2 bytes, number 2 i in the
+ * low bits of byte i and number 2 i + 1 above it, and an exponent per 32 numbers of a row, those of 16 tokens side by side:
+ *     data      uint8 [num_pages][kv_heads][page_tokens][2][W / 2]
+ *     exponents int8  [num_pages][kv_heads][page_tokens / 16][2][W / 32][16]
  */
-typedef enum { PAG_KV_INT8 = 0, PAG_KV_FP8 = 1 } pag_kv_format;
+typedef enum { PAG_KV_INT8 = 0, PAG_KV_FP8 = 1, PAG_KV_FP4 = 4 } pag_kv_format;
 typedef enum { PAG_F32 = 0, PAG_F16 = 1, PAG_BF16 = 2 } pag_dtype;
 
 typedef struct {
@@ -331,7 +335,7 @@ typedef struct {
     uint32_t reserved;     /* 0 */
     uint64_t num_pages;    /* num_pages * kv_heads * page_tokens < 2^32 */
     uint8_t* data;         /* dev, 16-byte aligned */
-    int8_t*  exponents;    /* dev, 2-byte aligned */
+    int8_t*  exponents;    /* dev, 2-byte aligned (PAG_KV_FP4: 16-byte) */
 } pag_kv_cache;
 
 /* The block tables of `requests` requests and the pages that nobody holds (a stack: the last one is taken first).  All dev. */
@@ -407,6 +411,8 @@ int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* strea
  * first token is among the new ones) is cleared first; its exponent is the smallest e >= -64 at which the largest code reaches the
  * largest finite magnitude.  Another block keeps its exponent unless the new tokens need a larger one; then what it held is
  * rounded again.  Rounding is to nearest even; infinities are held as the largest code, NaN as 0.
+ * Of PAG_KV_FP4 the tokens of a call may come in any order, as long as no slot is there twice, and nothing but their own rows changes: each 32 numbers
+ * get the smallest e >= -64 at which their largest finite magnitude is at most 7, which is rounded to the largest code by no more than half a step.
  * pag_kv_read: rows of the cache as numbers, [tokens][kv_heads][head_dim] with strides in elements (multiples of 16 bytes); k or v may be
  * null.  Slots -1 or out of range give zeros.  PAG_F32 and PAG_BF16 hold every number of the cache exactly, but for what a block near the end of
  * 32 bits rounds up to 2^128 and infinities held as the largest code there: that is read as the largest finite PAG_BF16, 255 * 2^120, where
@@ -417,6 +423,31 @@ int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const void* k, int6
                   const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, uint64_t tokens, void* stream);
 int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens, uint32_t dtype, void* k, int64_t k_token_stride,
                 int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride, void* stream);
+
+/*
+ * pag_kv_append_rotated: pag_kv_append of keys that are turned by their positions, and of values as they are; and the same turn for queries.
+ * Of the first `turned` numbers of a row at position p each pair (x, y), numbers i and i + turned / 2 or 2 i and 2 i + 1, becomes
+ * (x cos a - y sin a, y cos a + x sin a) with the angle a = p * frequencies[i], a product in 64 bits.  Angles below 2^31 in magnitude are turned by as
+ * computed in 64 bits, so what is held and what comes out is rounded once.  A pair with an infinity or NaN becomes whatever these formulas give.
+ */
+typedef enum { PAG_KV_HALVES = 0, PAG_KV_NEIGHBOURS = 1 } pag_kv_pairs;
+
+typedef struct {
+    uint32_t struct_size;
+    uint32_t pairs;                /* pag_kv_pairs */
+    uint32_t turned;               /* a multiple of 8, at most head_dim */
+    uint32_t heads;                /* of q; 0: no q */
+    const float* frequencies;      /* dev [turned / 2] */
+    const int32_t* positions;      /* dev [tokens], of any sign; also those of tokens that are left out of the cache count, for q */
+    const void* q;                 /* dev [tokens][heads][head_dim] of the call's dtype, strides in elements, multiples of 16 bytes */
+    int64_t q_token_stride, q_head_stride;
+    void* out;                     /* dev, like q: the turned rows; q itself, with q's strides, or apart from it */
+    int64_t out_token_stride, out_head_stride;
+} pag_kv_rotation;
+
+int pag_kv_append_rotated(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                          const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, uint64_t tokens,
+                          const pag_kv_rotation* rotation, void* stream);
 
 /*
  * pag_kv_workspace_bytes: the workspace of such a call of pag_kv_attend (selected = 0, id_heads and k are not looked at) or pag_kv_attend_selected;

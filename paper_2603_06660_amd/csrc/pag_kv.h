@@ -1,4 +1,4 @@
-// The 8-bit key/value cache: what its kernels share.
+// The key/value cache of 8 or 4 bits: what its kernels share.
 #pragma once
 
 #include "pag_internal.h"
@@ -6,7 +6,8 @@
 namespace pagkv {
 
 constexpr int LOWEST_EXPONENT = -64;   // blocks of zeros, and what is too small to matter beside them
-constexpr u32 BLOCK = 16;              // tokens that share an exponent
+constexpr u32 BLOCK = 16;              // tokens that share an exponent (of 8-bit codes), or whose exponents lie side by side
+constexpr u32 PART = 32;               // numbers of a row that share one (of 4-bit codes)
 
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
@@ -39,6 +40,14 @@ __device__ __forceinline__ float power(int e) { return __uint_as_float((u32)(e +
 // row of a token of a page and head; fits 32 bits (checked by the host)
 __device__ __forceinline__ u32 row_of(const Cache& c, u32 page, u32 head, u32 place) { return (page * c.kv_heads + head) * c.page_tokens + place; }
 
+// bytes of a row of keys or of values, for C = width / 64
+template <int FMT, int C>
+constexpr u32 row_bytes() { return FMT == PAG_KV_FP4 ? 32 * C : 64 * C; }
+
+// Exponents of 4-bit codes: of a block of 16 tokens (rows / 16, as row_of counts them) and kind, W / 32 parts of 16 bytes
+template <int C>
+__device__ __forceinline__ const int8_t* parts_of(const Cache& c, u32 block, u32 kind) { return c.exponents + ((u64)block * 2 + kind) * (2 * C * BLOCK); }
+
 // four codes of a word as numbers without their exponent
 template <int FMT>
 __device__ __forceinline__ void decode4(u32 w, float* x) {
@@ -69,13 +78,32 @@ __device__ __forceinline__ u32 encode4(const float* x) {
     }
 }
 
-// the smallest exponent at which the largest code reaches `most` (127 = 1.984375 * 2^6, 448 = 1.75 * 2^8)
+// the smallest exponent at which the largest code reaches `most` (127 = 1.984375 * 2^6, 448 = 1.75 * 2^8), or, of 4 bits, at which `most` is
+// rounded to the largest code by no more than half a step (7 = 1.75 * 2^2)
 template <int FMT>
 __device__ __forceinline__ int least_exponent(float most) {
     const u32 bits = __float_as_uint(most);
     constexpr u32 FRACTION = FMT == PAG_KV_INT8 ? 0x7E0000u : 0x600000u;
-    const int e = (int)(bits >> 23) - 127 - (FMT == PAG_KV_INT8 ? 6 : 8) + ((bits & 0x7FFFFFu) > FRACTION ? 1 : 0);
+    const int e = (int)(bits >> 23) - 127 - (FMT == PAG_KV_INT8 ? 6 : FMT == PAG_KV_FP8 ? 8 : 2) + ((bits & 0x7FFFFFu) > FRACTION ? 1 : 0);
     return e < LOWEST_EXPONENT ? LOWEST_EXPONENT : e;
+}
+
+// eight codes of 4 bits; x and NaN as for encode4
+__device__ __forceinline__ u32 encode8_fp4(const float* x) {
+    u32 w = 0;
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -6.f), 6.f) : 0.f;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], 1.f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], 1.f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], 1.f, 3);
+}
+
+// four codes of 4 bits, the low half of a word, times a power of two
+__device__ __forceinline__ void decode4_fp4(u32 w, float scale, float* x) {
+    const float2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+    x[0] = lo.x; x[1] = lo.y; x[2] = hi.x; x[3] = hi.y;
 }
 
 __device__ __forceinline__ void widen_row8(const uint4& r, u32 dtype, float* x) {      // PAG_F16 or PAG_BF16
@@ -110,6 +138,28 @@ __device__ __forceinline__ float finite(float x) {
     return fabsf(x) > MOST ? copysignf(MOST, x) : x;
 }
 
+// four numbers of an input row in 32 bits, at a multiple of 4
+__device__ __forceinline__ void load4(const void* p, u64 at, u32 dtype, float* x) {
+    if (dtype == PAG_F32) {
+        const float4 a = *(const float4*)((const float*)p + at);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        return;
+    }
+    const uint2 r = *(const uint2*)((const uint16_t*)p + at);
+    const u32 w[2] = { r.x, r.y };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (dtype == PAG_BF16) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        } else {
+            const half2_t h = __builtin_bit_cast(half2_t, w[i]);
+            x[2 * i] = (float)h.x;
+            x[2 * i + 1] = (float)h.y;
+        }
+    }
+}
+
 __device__ __forceinline__ u32 pack2(float a, float b, u32 dtype) {       // to nearest even
     const float2_t x = { a, b };
     if (dtype == PAG_BF16) return __builtin_bit_cast(u32, __builtin_convertvector(x, bf16x2_t));
@@ -136,8 +186,24 @@ struct Attend {
 
 int launch_extend(hipStream_t st, const pag_kv_tables& t, const int32_t* add, const pag_kv_step& s);
 int launch_release(hipStream_t st, const pag_kv_tables& t, const int32_t* done);
-int launch_append(hipStream_t st, const Cache& c, u32 dtype, const void* k, int64_t k_ts, int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs,
-                  const int64_t* slots, u64 tokens);
+
+// new tokens of a call, keys and values, and what turns them
+struct Store {
+    Cache c;
+    const void* x[2];
+    int64_t ts[2], hs[2];
+    const int64_t* slots;
+    u64 tokens;
+    u32 dtype;
+    u32 pairs, turned, heads;                       // pag_kv_rotation; turned 0: rows stay as they are
+    const float* frequencies;
+    const int32_t* positions;
+    const void* q;
+    void* out;
+    int64_t q_ts, q_hs, o_ts, o_hs;
+};
+
+int launch_append(hipStream_t st, const Store& a);
 int launch_read(hipStream_t st, const Cache& c, const int64_t* slots, u64 tokens, u32 dtype, void* k, int64_t k_ts, int64_t k_hs, void* v,
                 int64_t v_ts, int64_t v_hs);
 int launch_attend(hipStream_t st, const Attend& a, int num_cu);

@@ -1,4 +1,4 @@
-// C ABI of the 8-bit key/value cache: argument checking; everything that computes runs in the kernels.
+// C ABI of the key/value cache: argument checking; everything that computes runs in the kernels.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -24,7 +24,7 @@ bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 
 int cache_of(const pag_kv_cache* c, Cache* out) {
     PAG_CHECK(c != nullptr, PAG_EINVAL, "cache is null");
     PAG_CHECK(c->struct_size == sizeof(pag_kv_cache), PAG_EINVAL, "pag_kv_cache.struct_size does not match this library");
-    PAG_CHECK(c->format <= PAG_KV_FP8, PAG_EINVAL, "unknown cache format");
+    PAG_CHECK(c->format <= PAG_KV_FP8 || c->format == PAG_KV_FP4, PAG_EINVAL, "unknown cache format");
     PAG_CHECK(c->kv_heads > 0 && c->head_dim > 0 && c->page_tokens > 0 && c->num_pages > 0, PAG_EINVAL,
               "kv_heads, head_dim, page_tokens and num_pages must be positive");
     PAG_CHECK(c->head_dim % 8 == 0 && c->head_dim <= 256, PAG_EUNSUPPORTED, "this build needs head_dim % 8 == 0 and head_dim <= 256");
@@ -33,7 +33,8 @@ int cache_of(const pag_kv_cache* c, Cache* out) {
     PAG_CHECK(c->num_pages <= 0xFFFFFFFFull / c->page_tokens / c->kv_heads && c->num_pages < (1ull << 31), PAG_EUNSUPPORTED,
               "num_pages * kv_heads * page_tokens must be below 2^32");
     PAG_CHECK(c->data != nullptr && c->exponents != nullptr, PAG_EINVAL, "cache data or exponents is null");
-    PAG_CHECK(aligned(c->data, 16) && aligned(c->exponents, 2), PAG_EINVAL, "cache data must be 16-byte aligned, exponents 2-byte");
+    PAG_CHECK(aligned(c->data, 16) && aligned(c->exponents, c->format == PAG_KV_FP4 ? 16 : 2), PAG_EINVAL,
+              "cache data must be 16-byte aligned, exponents 2-byte (of 4-bit codes 16-byte)");
     *out = Cache{ c->data, c->exponents, c->kv_heads, c->head_dim, (c->head_dim + 63) / 64 * 64, c->page_tokens, c->page_tokens / BLOCK,
                   (u32)c->num_pages, c->format };
     return PAG_OK;
@@ -70,6 +71,7 @@ int check_rows(const void* p, int64_t token_stride, int64_t head_stride, u32 byt
 int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, bool selected, uint32_t id_heads, uint32_t k, Attend* a) {
     int rc;
     if ((rc = cache_of(cache, &a->c)) || (rc = check_step(step))) return rc;
+    PAG_CHECK(a->c.fmt != PAG_KV_FP4, PAG_EUNSUPPORTED, "attention over 4-bit codes is not built");
     PAG_CHECK(args != nullptr, PAG_EINVAL, "args is null");
     PAG_CHECK(args->struct_size == sizeof(pag_kv_attention), PAG_EINVAL, "pag_kv_attention.struct_size does not match this library");
     PAG_CHECK(args->dtype == PAG_F16 || args->dtype == PAG_BF16, PAG_EUNSUPPORTED, "attention takes PAG_F16 or PAG_BF16");
@@ -161,20 +163,75 @@ extern "C" int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, 
     });
 }
 
+namespace pagkv {
+namespace {
+
+int store_of(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+             int64_t v_head_stride, const int64_t* slots, uint64_t tokens, Store* a) {
+    int rc = cache_of(cache, &a->c);
+    if (rc) return rc;
+    PAG_CHECK(dtype <= PAG_BF16, PAG_EINVAL, "unknown dtype");
+    PAG_CHECK(tokens < (1ull << 27) && tokens * a->c.kv_heads < (1ull << 27), PAG_EUNSUPPORTED, "tokens * kv_heads must be below 2^27");
+    // a launch has fewer than 2^32 threads, and these have 64 a token
+    PAG_CHECK(cache->format != PAG_KV_FP4 || tokens < (1ull << 25), PAG_EUNSUPPORTED, "calls of 2^25 tokens or more are not built for PAG_KV_FP4");
+    a->tokens = tokens;
+    a->dtype = dtype;
+    if (tokens == 0) return PAG_OK;
+    PAG_CHECK(k && v && slots, PAG_EINVAL, "k, v or slots is null");
+    const u32 bytes = dtype == PAG_F32 ? 4 : 2;
+    if ((rc = check_rows(k, k_token_stride, k_head_stride, bytes, 16, "k and its strides must be multiples of 16 bytes"))) return rc;
+    if ((rc = check_rows(v, v_token_stride, v_head_stride, bytes, 16, "v and its strides must be multiples of 16 bytes"))) return rc;
+    a->x[0] = k; a->ts[0] = k_token_stride; a->hs[0] = k_head_stride;
+    a->x[1] = v; a->ts[1] = v_token_stride; a->hs[1] = v_head_stride;
+    a->slots = slots;
+    return PAG_OK;
+}
+
+}  // namespace
+}  // namespace pagkv
+
 extern "C" int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
                              int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, uint64_t tokens, void* stream) {
     return guarded("pag_kv_append", [&]() -> int {
-        Cache c;
-        int rc = cache_of(cache, &c);
+        Store a = {};
+        const int rc = store_of(cache, dtype, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, slots, tokens, &a);
+        if (rc || tokens == 0) return rc;
+        return launch_append((hipStream_t)stream, a);
+    });
+}
+
+extern "C" int pag_kv_append_rotated(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                                     int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, uint64_t tokens, const pag_kv_rotation* r,
+                                     void* stream) {
+    return guarded("pag_kv_append_rotated", [&]() -> int {
+        Store a = {};
+        int rc = store_of(cache, dtype, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, slots, tokens, &a);
         if (rc) return rc;
-        PAG_CHECK(dtype <= PAG_BF16, PAG_EINVAL, "unknown dtype");
-        PAG_CHECK(tokens < (1ull << 27) && tokens * c.kv_heads < (1ull << 27), PAG_EUNSUPPORTED, "tokens * kv_heads must be below 2^27");
+        PAG_CHECK(r != nullptr, PAG_EINVAL, "rotation is null");
+        PAG_CHECK(r->struct_size == sizeof(pag_kv_rotation), PAG_EINVAL, "pag_kv_rotation.struct_size does not match this library");
+        PAG_CHECK(r->pairs <= PAG_KV_NEIGHBOURS, PAG_EINVAL, "unknown pairs");
+        PAG_CHECK(r->turned > 0 && r->turned % 8 == 0 && r->turned <= a.c.dim, PAG_EUNSUPPORTED, "this build needs turned % 8 == 0 and 0 < turned <= head_dim");
+        PAG_CHECK(tokens < (1ull << 25) && r->heads <= 65536 && tokens * r->heads < (1ull << 31), PAG_EUNSUPPORTED,
+                  "tokens must be below 2^25, heads at most 65536, tokens * heads below 2^31");
         if (tokens == 0) return PAG_OK;
-        PAG_CHECK(k && v && slots, PAG_EINVAL, "k, v or slots is null");
-        const u32 bytes = dtype == PAG_F32 ? 4 : 2;
-        if ((rc = check_rows(k, k_token_stride, k_head_stride, bytes, 16, "k and its strides must be multiples of 16 bytes"))) return rc;
-        if ((rc = check_rows(v, v_token_stride, v_head_stride, bytes, 16, "v and its strides must be multiples of 16 bytes"))) return rc;
-        return launch_append((hipStream_t)stream, c, dtype, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, slots, tokens);
+        PAG_CHECK(r->frequencies && r->positions && aligned(r->frequencies, 4) && aligned(r->positions, 4), PAG_EINVAL,
+                  "frequencies or positions is null or not 4-byte aligned");
+        a.pairs = r->pairs;
+        a.turned = r->turned;
+        a.frequencies = r->frequencies;
+        a.positions = r->positions;
+        if (r->heads) {
+            PAG_CHECK(r->q && r->out, PAG_EINVAL, "q or out is null");
+            const u32 bytes = dtype == PAG_F32 ? 4 : 2;
+            if ((rc = check_rows(r->q, r->q_token_stride, r->q_head_stride, bytes, 16, "q and its strides must be multiples of 16 bytes"))) return rc;
+            if ((rc = check_rows(r->out, r->out_token_stride, r->out_head_stride, bytes, 16, "out and its strides must be multiples of 16 bytes"))) return rc;
+            PAG_CHECK(r->q != r->out || (r->q_token_stride == r->out_token_stride && r->q_head_stride == r->out_head_stride), PAG_EINVAL,
+                      "q may be turned in place with its own strides only");
+            a.heads = r->heads;
+            a.q = r->q; a.q_ts = r->q_token_stride; a.q_hs = r->q_head_stride;
+            a.out = r->out; a.o_ts = r->out_token_stride; a.o_hs = r->out_head_stride;
+        }
+        return launch_append((hipStream_t)stream, a);
     });
 }
 

@@ -1,4 +1,4 @@
-// Block tables and slots of a step, and what goes into the 8-bit cache and comes out of it.
+// Block tables and slots of a step, and what goes into the cache and comes out of it.
 #include "pag_kv.h"
 
 namespace pagkv {
@@ -159,14 +159,153 @@ __device__ __forceinline__ float wave_max(float x) {
     return x;
 }
 
-struct Store {
-    Cache c;
-    const void* x[2];
-    int64_t ts[2], hs[2];
-    const int64_t* slots;
-    u64 tokens;
-    u32 dtype;
-};
+// ---- rotation ---------------------------------------------------------------------------------------------------------
+
+// cos and sin of an angle below 2^31 or so, to 2^-50: the nearest multiple of pi / 2 is taken off in two parts, which leaves r with |r| <= pi / 4
+// exact to 2^-70, and of r Taylor's series, whose first terms left out, r^17 / 17! and r^18 / 18!, are below 2^-54.
+__device__ __forceinline__ double2 spin_of(double angle) {
+    const double n = __builtin_rint(angle * 0.63661977236758134308);
+    double r = __builtin_fma(n, -1.57079632679489655800, angle);
+    r = __builtin_fma(n, -6.12323399573676603587e-17, r);
+    const double u = r * r;
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+    s = __builtin_fma(s, u, 1.0 / 6227020800.0);
+    c = __builtin_fma(c, u, -1.0 / 87178291200.0);
+    s = __builtin_fma(s, u, -1.0 / 39916800.0);
+    c = __builtin_fma(c, u, 1.0 / 479001600.0);
+    s = __builtin_fma(s, u, 1.0 / 362880.0);
+    c = __builtin_fma(c, u, -1.0 / 3628800.0);
+    s = __builtin_fma(s, u, -1.0 / 5040.0);
+    c = __builtin_fma(c, u, 1.0 / 40320.0);
+    s = __builtin_fma(s, u, 1.0 / 120.0);
+    c = __builtin_fma(c, u, -1.0 / 720.0);
+    s = __builtin_fma(s, u, -1.0 / 6.0);
+    c = __builtin_fma(c, u, 1.0 / 24.0);
+    s = __builtin_fma(s * u, r, r);
+    c = __builtin_fma(c, u, -0.5);
+    c = __builtin_fma(c, u, 1.0);
+    const int q = (int)(n - 4.0 * __builtin_floor(n * 0.25));
+    const double x = q & 1 ? s : c, y = q & 1 ? c : s;
+    return make_double2(q == 1 || q == 2 ? -x : x, q >= 2 ? -y : y);
+}
+
+// A number of 64 bits on its way to fewer than 24: rounded to 32 bits towards zero, and the last bit set if that took anything off, so that rounding
+// it again gives what rounding once would have given.
+__device__ __forceinline__ float odd(double x) {
+    const float f = (float)x;
+    const double y = (double)f;
+    const u32 bits = __float_as_uint(f);
+    if (y == x || x != x) return f;
+    return __uint_as_float((bits - (fabs(y) > fabs(x) ? 1u : 0u)) | 1u);
+}
+
+// the angles of tokens t0 to t0 + n - 1, into LDS, by the workgroup
+__device__ __forceinline__ void spin_tokens(const Store& a, u64 t0, u32 n, double2* spin) {
+    const u32 half = a.turned / 2;
+    for (u32 i = threadIdx.x; i < n * half; i += blockDim.x) spin[i] = spin_of((double)a.positions[t0 + i / half] * (double)a.frequencies[i % half]);
+}
+
+// Numbers at to at + 7 of a row, which x holds as they came, turned.  row: the element that the row begins with.
+__device__ __forceinline__ void turn8(const Store& a, const void* p, u64 row, u32 at, const double2* spin, float* x) {
+    if (at >= a.turned) return;
+    if (a.pairs == PAG_KV_NEIGHBOURS) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double2 by = spin[at / 2 + j];
+            const double u = x[2 * j], v = x[2 * j + 1];
+            x[2 * j] = odd(__builtin_fma(u, by.x, -v * by.y));
+            x[2 * j + 1] = odd(__builtin_fma(v, by.x, u * by.y));
+        }
+        return;
+    }
+    // four at a time lie on one side of the middle, and so do their partners
+    const u32 half = a.turned / 2;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        const u32 first = at + 4 * z;
+        const bool low = first < half;
+        float y[4];
+        load4(p, row + (low ? first + half : first - half), a.dtype, y);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double2 by = spin[(low ? first : first - half) + j];
+            x[4 * z + j] = odd(__builtin_fma((double)x[4 * z + j], by.x, (double)(low ? -y[j] : y[j]) * by.y));
+        }
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void load_numbers(const void* p, u64 at, u32 dtype, float* x) {
+    if constexpr (N == 8) load8(p, at, dtype, x);
+    else load4(p, at, dtype, x);
+}
+
+// N numbers in the call's type, each rounded once
+template <int N>
+__device__ __forceinline__ void store_numbers(void* p, u64 at, u32 dtype, const double* x) {
+    if (dtype == PAG_F32) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) *(float4*)((float*)p + at + j) = make_float4((float)x[j], (float)x[j + 1], (float)x[j + 2], (float)x[j + 3]);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; j += 4)
+        *(uint2*)((uint16_t*)p + at + j) = make_uint2(pack2(odd(x[j]), odd(x[j + 1]), dtype), pack2(odd(x[j + 2]), odd(x[j + 3]), dtype));
+}
+
+// N pairs whose first numbers lie at x_at and second ones at y_at of a row
+template <int N>
+__device__ __forceinline__ void turn_halves(const Store& a, u64 from, u64 to, u32 x_at, u32 y_at, const double2* spin) {
+    float x[N], y[N];
+    load_numbers<N>(a.q, from + x_at, a.dtype, x);
+    load_numbers<N>(a.q, from + y_at, a.dtype, y);
+    double u[N], v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const double2 by = spin[x_at + j];
+        u[j] = __builtin_fma((double)x[j], by.x, -(double)y[j] * by.y);
+        v[j] = __builtin_fma((double)y[j], by.x, (double)x[j] * by.y);
+    }
+    store_numbers<N>(a.out, to + x_at, a.dtype, u);
+    store_numbers<N>(a.out, to + y_at, a.dtype, v);
+}
+
+// q's rows of tokens t0 to t0 + n - 1, by the workgroup.  A pair is one thread's, so that rows may be turned in place.
+__device__ __forceinline__ void turn_queries(const Store& a, u64 t0, u32 n, const double2* spin) {
+    const u32 half = a.turned / 2, each = half % 8 == 0 ? 8 : 4;
+    const u32 pairs = a.pairs == PAG_KV_NEIGHBOURS ? a.turned / 8 : half / each, pieces = pairs + (a.c.dim - a.turned) / 8, all = n * a.heads * pieces;
+    for (u32 i = threadIdx.x; i < all; i += blockDim.x) {
+        const u32 piece = i % pieces, head = i / pieces % a.heads, token = i / pieces / a.heads;
+        const u64 from = (t0 + token) * (u64)a.q_ts + head * (u64)a.q_hs, to = (t0 + token) * (u64)a.o_ts + head * (u64)a.o_hs;
+        const double2* by = spin + token * half;
+        if (piece >= pairs) {
+            const u32 at = a.turned + (piece - pairs) * 8;
+            float x[8];
+            double y[8];
+            load8(a.q, from + at, a.dtype, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = x[j];
+            store_numbers<8>(a.out, to + at, a.dtype, y);
+        } else if (a.pairs == PAG_KV_NEIGHBOURS) {
+            float x[8];
+            double y[8];
+            load8(a.q, from + piece * 8, a.dtype, x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const double2 s = by[piece * 4 + j];
+                y[2 * j] = __builtin_fma((double)x[2 * j], s.x, -(double)x[2 * j + 1] * s.y);
+                y[2 * j + 1] = __builtin_fma((double)x[2 * j + 1], s.x, (double)x[2 * j] * s.y);
+            }
+            store_numbers<8>(a.out, to + piece * 8, a.dtype, y);
+        } else if (each == 8) {
+            turn_halves<8>(a, from, to, piece * 8, half + piece * 8, by);
+        } else {
+            turn_halves<4>(a, from, to, piece * 4, half + piece * 4, by);
+        }
+    }
+}
+
+constexpr u32 QUERY_TOKENS = 4;       // of a workgroup that turns queries, where there are many
 
 // A wave has a window of new tokens, one head and one kind.  It writes the blocks whose first new token lies in its window, with all
 // their new tokens, one block after the other.  8 numbers of a row are a lane's; a block of 16 rows is 2 C of these pieces a lane.
@@ -175,12 +314,34 @@ struct Store {
 // one token each: 256 requests 6.0, 9.3, 28; 512 requests 9.1, 10.5, 28; 2,048 requests 29, 25, 35; 4,096 requests 53, 44, 47;
 // prompts: 256 tokens 8.5, 5.9, 5.9; 512 tokens 9.8, 6.5, 5.9; 2,048 tokens 18, 12.5, 11; 4,096 tokens 35, 20, 14; 15,000 tokens 139, 53, 36.
 // Bound by memory where there are many tokens (60,000: 370 MB in 124 us), by the waits for a slot, an exponent and a row where there are few.
-template <int FMT, int C>
-__global__ void __launch_bounds__(256) k_append(Store a, u32 window) {
+// TURN: keys are turned.  The four waves of a workgroup then have one window and kind, and four heads, and share their tokens' angles; the workgroups from
+// number `writers` on turn queries.
+template <int FMT, int C, bool TURN>
+__global__ void __launch_bounds__(256) k_append(Store a, u32 window, u32 writers, u32 each) {
+    extern __shared__ double2 spin[];
     const u32 lane = threadIdx.x & 63, kinds = 2 * a.c.kv_heads;
-    const u64 wave = (u64)blockIdx.x * 4 + (threadIdx.x >> 6), t0 = wave / kinds * window;
-    if (t0 >= a.tokens) return;
-    const u32 head = (u32)(wave % kinds) >> 1, kind = (u32)(wave % kinds) & 1;
+    u64 t0;
+    u32 head, kind;
+    if constexpr (TURN) {
+        if (blockIdx.x >= writers) {
+            const u64 first = (u64)(blockIdx.x - writers) * each;
+            const u32 n = (u32)min((u64)each, a.tokens - first);
+            spin_tokens(a, first, n, spin);
+            __syncthreads();
+            turn_queries(a, first, n, spin);
+            return;
+        }
+        const u32 fours = (a.c.kv_heads + 3) / 4, part = blockIdx.x % (2 * fours);
+        t0 = (u64)(blockIdx.x / (2 * fours)) * window;
+        head = (part >> 1) * 4 + (threadIdx.x >> 6);
+        kind = part & 1;
+    } else {
+        const u64 wave = (u64)blockIdx.x * 4 + (threadIdx.x >> 6);
+        t0 = wave / kinds * window;
+        if (t0 >= a.tokens) return;
+        head = (u32)(wave % kinds) >> 1;
+        kind = (u32)(wave % kinds) & 1;
+    }
     // lane 0: the token before, lanes 1 .. window: the window, and the next 15
     int64_t slot = -1;
     if (lane < window + BLOCK && t0 + lane >= 1 && t0 + lane - 1 < a.tokens) slot = a.slots[t0 + lane - 1];
@@ -196,6 +357,14 @@ __global__ void __launch_bounds__(256) k_append(Store a, u32 window) {
         const u32 run = (u32)__builtin_ctzll(~same);
         u32 present = 0;
         for (u32 i = 0; i < run; ++i) present |= 1u << __builtin_amdgcn_readlane(place, (int)(at_lane + i));
+        if constexpr (TURN) {
+            if (kind == 0) {                     // the whole workgroup comes here: its waves see the same slots
+                __syncthreads();
+                spin_tokens(a, t, run, spin);
+                __syncthreads();
+            }
+            if (head >= a.c.kv_heads) continue;
+        }
         const bool begins = present & 1u;
         const u32 page = (u32)mine / a.c.page_blocks, first = (u32)mine % a.c.page_blocks * BLOCK;
         uint8_t* rows = a.c.data + (u64)row_of(a.c, page, head, first) * (2 * a.c.width) + kind * a.c.width;
@@ -209,7 +378,13 @@ __global__ void __launch_bounds__(256) k_append(Store a, u32 window) {
             const u32 i = lane + 64 * n, row = i / (8 * C), at = i % (8 * C) * 8;
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[n][j] = 0.f;
-            if (row < run && at < a.c.dim) load8(a.x[kind], (t + row) * (u64)a.ts[kind] + head * (u64)a.hs[kind] + at, a.dtype, x[n]);
+            if (row < run && at < a.c.dim) {
+                const u64 from = (t + row) * (u64)a.ts[kind] + head * (u64)a.hs[kind];
+                load8(a.x[kind], from + at, a.dtype, x[n]);
+                if constexpr (TURN) {
+                    if (kind == 0) turn8(a, a.x[0], from, at, spin + row * (a.turned / 2), x[n]);
+                }
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float y = fabsf(x[n][j]);
@@ -252,6 +427,49 @@ __global__ void __launch_bounds__(256) k_append(Store a, u32 window) {
         }
         if (lane == 0) *exponent = (int8_t)e;
     }
+}
+
+// 4-bit codes: a row's parts have their exponents to themselves, so that 8 numbers of a row are a thread's, whatever else the call writes, and four
+// threads share a part.  A workgroup has `each` tokens, all their heads, keys and values, and their queries.
+template <int C, bool TURN>
+__global__ void __launch_bounds__(256) k_append_fp4(Store a, u32 each) {
+    extern __shared__ double2 spin[];
+    const u64 first = (u64)blockIdx.x * each;
+    const u32 n = (u32)min((u64)each, a.tokens - first);
+    if constexpr (TURN) {
+        spin_tokens(a, first, n, spin);
+        __syncthreads();
+    }
+    const u32 pieces = 8 * C, all = n * a.c.kv_heads * 2 * pieces;
+    for (u32 i = threadIdx.x; i < all; i += 256) {
+        const u32 at = i % pieces * 8, kind = i / pieces & 1, head = i / (2 * pieces) % a.c.kv_heads, token = i / (2 * pieces) / a.c.kv_heads;
+        const int64_t slot = a.slots[first + token];
+        if (slot < 0 || slot >= (int64_t)a.c.num_pages * a.c.page_tokens) continue;
+        float x[8] = { 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f };
+        if (at < a.c.dim) {
+            const u64 from = (first + token) * (u64)a.ts[kind] + head * (u64)a.hs[kind];
+            load8(a.x[kind], from + at, a.dtype, x);
+            if constexpr (TURN) {
+                if (kind == 0) turn8(a, a.x[0], from, at, spin + token * (a.turned / 2), x);
+            }
+        }
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float y = fabsf(x[j]);
+            if (y <= 3.402823466e38f) most = fmaxf(most, y);
+        }
+        most = fmaxf(most, __shfl_xor(most, 1));
+        most = fmaxf(most, __shfl_xor(most, 2));
+        const int e = least_exponent<PAG_KV_FP4>(most);
+        const float down = power(-e);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= down;
+        const u32 page = (u32)((u64)slot / a.c.page_tokens), row = row_of(a.c, page, head, (u32)((u64)slot % a.c.page_tokens));
+        *(u32*)(a.c.data + (u64)row * (64 * C) + kind * (32 * C) + at / 2) = encode8_fp4(x);
+        if (at % PART == 0) a.c.exponents[((u64)(row / BLOCK) * 2 + kind) * (2 * C * BLOCK) + at / PART * BLOCK + row % BLOCK] = (int8_t)e;
+    }
+    if constexpr (TURN) turn_queries(a, first, n, spin);
 }
 
 struct Load {
@@ -317,30 +535,100 @@ __global__ void __launch_bounds__(256) k_read(Load a) {
     }
 }
 
-// f<FMT, C>() for the cache's format and row width
-template <template <int, int> class F, typename... A>
-void for_cache(const Cache& c, A&&... args) {
-    const u32 n = c.width / 64;
-    if (c.fmt == PAG_KV_INT8) {
-        if (n == 1) F<PAG_KV_INT8, 1>::run(args...);
-        else if (n == 2) F<PAG_KV_INT8, 2>::run(args...);
-        else if (n == 3) F<PAG_KV_INT8, 3>::run(args...);
-        else F<PAG_KV_INT8, 4>::run(args...);
-    } else {
-        if (n == 1) F<PAG_KV_FP8, 1>::run(args...);
-        else if (n == 2) F<PAG_KV_FP8, 2>::run(args...);
-        else if (n == 3) F<PAG_KV_FP8, 3>::run(args...);
-        else F<PAG_KV_FP8, 4>::run(args...);
+// The same of 4-bit codes; every 16 bytes of output are numbers of one part.
+template <int C, typename T>
+__global__ void __launch_bounds__(256) k_read_fp4(Load a) {
+    constexpr u32 EACH = 16 / sizeof(T), PIECES = 128 * C / EACH, TURNS = 16 * PIECES / 256;
+    __shared__ u32 sh_row[16];
+    __shared__ u32 sh_there[16];
+    const u32 head = blockIdx.x % a.c.kv_heads;
+    const u64 token0 = (u64)(blockIdx.x / a.c.kv_heads) * 16;
+    if (threadIdx.x < 16) {
+        const int64_t slot = a.slots[min(token0 + threadIdx.x, a.tokens - 1)];
+        const bool there = slot >= 0 && slot < (int64_t)a.c.num_pages * a.c.page_tokens;
+        sh_row[threadIdx.x] = there ? row_of(a.c, (u32)((u64)slot / a.c.page_tokens), head, (u32)((u64)slot % a.c.page_tokens)) : 0;
+        sh_there[threadIdx.x] = there;
+    }
+    __syncthreads();
+    u32 w[TURNS];
+    int8_t e[TURNS];
+#pragma unroll
+    for (u32 n = 0; n < TURNS; ++n) {
+        const u32 i = threadIdx.x + 256 * n, r = i / PIECES, both = i % PIECES * EACH, row = sh_row[r];
+        const uint8_t* p = a.c.data + (u64)row * (64 * C) + both / 2;
+        if constexpr (EACH == 4) w[n] = *(const uint16_t*)p;
+        else w[n] = *(const u32*)p;
+        e[n] = parts_of<C>(a.c, row / BLOCK, both / (64 * C))[both % (64 * C) / PART * BLOCK + row % BLOCK];
+    }
+#pragma unroll
+    for (u32 n = 0; n < TURNS; ++n) {
+        const u32 i = threadIdx.x + 256 * n, r = i / PIECES, both = i % PIECES * EACH, kind = both / (64 * C), at = both % (64 * C);
+        if (token0 + r < a.tokens && at < a.c.dim && a.x[kind]) {
+            const float up = power(e[n]);
+            float x[EACH];
+#pragma unroll
+            for (u32 y = 0; y < EACH / 4; ++y) decode4_fp4(w[n] >> (16 * y), 1.f, x + 4 * y);
+#pragma unroll
+            for (u32 y = 0; y < EACH; ++y) x[y] = sh_there[r] ? finite(x[y] * up) : 0.f;
+            T* to = (T*)a.x[kind] + (int64_t)(token0 + r) * a.ts[kind] + (int64_t)head * a.hs[kind] + at;
+            typedef u32 word4 __attribute__((ext_vector_type(4)));
+            word4 y;
+            if constexpr (sizeof(T) == 4) y = word4{ __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]) };
+            else y = word4{ pack2(x[0], x[1], a.dtype), pack2(x[2], x[3], a.dtype), pack2(x[4], x[5], a.dtype), pack2(x[6], x[7], a.dtype) };
+            __builtin_nontemporal_store(y, (word4*)to);
+        }
     }
 }
 
+// f<FMT, C>() for the cache's format and row width
+template <template <int, int> class F, int FMT, typename... A>
+void for_width(const Cache& c, A&&... args) {
+    const u32 n = c.width / 64;
+    if (n == 1) F<FMT, 1>::run(args...);
+    else if (n == 2) F<FMT, 2>::run(args...);
+    else if (n == 3) F<FMT, 3>::run(args...);
+    else F<FMT, 4>::run(args...);
+}
+
+template <template <int, int> class F, typename... A>
+void for_cache(const Cache& c, A&&... args) {
+    if (c.fmt == PAG_KV_INT8) for_width<F, PAG_KV_INT8>(c, args...);
+    else if (c.fmt == PAG_KV_FP8) for_width<F, PAG_KV_FP8>(c, args...);
+    else for_width<F, PAG_KV_FP4>(c, args...);
+}
+
 template <int FMT, int C>
-struct RunAppend { static void run(hipStream_t st, u32 grid, const Store& a, u32 window) { k_append<FMT, C><<<grid, 256, 0, st>>>(a, window); } };
+struct RunAppend {
+    static void run(hipStream_t st, const Store& a) {
+        const u64 waves = a.tokens * 2 * a.c.kv_heads;
+        const u32 spins = (u32)sizeof(double2) * (a.turned / 2);
+        const u32 each = a.tokens <= 1024 ? 1 : QUERY_TOKENS;
+        if constexpr (FMT == PAG_KV_FP4) {
+            const u32 grid = (u32)((a.tokens + each - 1) / each);
+            if (a.turned) k_append_fp4<C, true><<<grid, 256, each * spins, st>>>(a, each);
+            else k_append_fp4<C, false><<<grid, 256, 0, st>>>(a, each);
+        } else {
+            const u32 window = waves <= 4096 ? 1 : waves <= 32768 ? 4 : 16;
+            const u64 windows = (a.tokens + window - 1) / window;
+            if (a.turned) {
+                const u32 writers = (u32)(windows * 2 * ((a.c.kv_heads + 3) / 4)), turners = a.heads ? (u32)((a.tokens + each - 1) / each) : 0;
+                k_append<FMT, C, true><<<writers + turners, 256, BLOCK * spins, st>>>(a, window, writers, each);
+            } else {
+                k_append<FMT, C, false><<<(u32)((windows * 2 * a.c.kv_heads + 3) / 4), 256, 0, st>>>(a, window, 0, 0);
+            }
+        }
+    }
+};
 template <int FMT, int C>
 struct RunRead {
     static void run(hipStream_t st, u32 grid, const Load& a) {
-        if (a.dtype == PAG_F32) k_read<FMT, C, float><<<grid, 256, 0, st>>>(a);
-        else k_read<FMT, C, uint16_t><<<grid, 256, 0, st>>>(a);
+        if constexpr (FMT == PAG_KV_FP4) {
+            if (a.dtype == PAG_F32) k_read_fp4<C, float><<<grid, 256, 0, st>>>(a);
+            else k_read_fp4<C, uint16_t><<<grid, 256, 0, st>>>(a);
+        } else {
+            if (a.dtype == PAG_F32) k_read<FMT, C, float><<<grid, 256, 0, st>>>(a);
+            else k_read<FMT, C, uint16_t><<<grid, 256, 0, st>>>(a);
+        }
     }
 };
 
@@ -367,12 +655,8 @@ int launch_release(hipStream_t st, const pag_kv_tables& t, const int32_t* done) 
     return launched("pag_kv_release");
 }
 
-int launch_append(hipStream_t st, const Cache& c, u32 dtype, const void* k, int64_t k_ts, int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs,
-                  const int64_t* slots, u64 tokens) {
-    const Store a{ c, { k, v }, { k_ts, v_ts }, { k_hs, v_hs }, slots, tokens, dtype };
-    const u64 waves = tokens * 2 * c.kv_heads;
-    const u32 window = waves <= 4096 ? 1 : waves <= 32768 ? 4 : 16;
-    for_cache<RunAppend>(c, st, (u32)(((tokens + window - 1) / window * 2 * c.kv_heads + 3) / 4), a, window);
+int launch_append(hipStream_t st, const Store& a) {
+    for_cache<RunAppend>(a.c, st, a);
     return launched("pag_kv_append");
 }
 

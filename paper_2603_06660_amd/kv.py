@@ -1,4 +1,4 @@
-"""The 8-bit key/value cache of include/pag.h: argument marshalling only.
+"""The key/value cache of include/pag.h, 8 or 4 bits a number: argument marshalling only.
 
 A decoding step, in order (every call goes onto the current stream and returns without waiting):
 
@@ -20,7 +20,8 @@ import torch
 
 from .binding import PagError, _check, load_library
 
-_FORMATS = {"int8": 0, "fp8": 1}
+_FORMATS = {"int8": 0, "fp8": 1, "fp4": 4}
+_PAIRS = {"halves": 0, "neighbours": 1}
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _ROW_DTYPES = (torch.float16, torch.bfloat16)
 
@@ -50,6 +51,12 @@ class _Attention(C.Structure):
                 ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
                 ("out", C.c_void_p), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
                 ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class _Rotation(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("pairs", C.c_uint32), ("turned", C.c_uint32), ("heads", C.c_uint32), ("frequencies", C.c_void_p),
+                ("positions", C.c_void_p), ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64)]
 
 
 def _gpu(device):
@@ -89,6 +96,7 @@ _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda ind
 _P, _I = C.c_void_p, C.c_int64
 _ARGTYPES = {"pag_kv_extend": [_P, _P, _P, _P], "pag_kv_release": [_P, _P, _P],
              "pag_kv_append": [_P, C.c_uint32, _P, _I, _I, _P, _I, _I, _P, C.c_uint64, _P],
+             "pag_kv_append_rotated": [_P, C.c_uint32, _P, _I, _I, _P, _I, _I, _P, C.c_uint64, _P, _P],
              "pag_kv_read": [_P, _P, C.c_uint64, C.c_uint32, _P, _I, _I, _P, _I, _I, _P],
              "pag_kv_workspace_bytes": [_P, _P, _P, C.c_int, C.c_uint32, C.c_uint32, _P],
              "pag_kv_attend": [_P, _P, _P, _P], "pag_kv_attend_selected": [_P, _P, _P, _P, _I, _I, C.c_uint32, C.c_uint32, _P]}
@@ -250,19 +258,42 @@ class KvTables:
         _call("pag_kv_release", self.device, C.addressof(self._t), _array(done, torch.int32, (self._t.requests,), self.device, "done"))
 
 
+class KvRotation:
+    """How rows are turned by their positions (pag_kv_rotation): frequencies float32 [turned / 2] on the GPU, of the first `turned` numbers of a row;
+    pairs: "halves" (numbers i and i + turned / 2) or "neighbours" (2 i and 2 i + 1)."""
+
+    def __init__(self, frequencies, pairs="halves"):
+        if pairs not in _PAIRS:
+            raise PagError("pairs must be one of %s" % ", ".join(sorted(_PAIRS)))
+        if not isinstance(frequencies, torch.Tensor) or frequencies.dim() != 1 or not frequencies.is_cuda or frequencies.numel() == 0:
+            raise PagError("frequencies must be a float32 CUDA tensor [turned / 2]")
+        self.device, self.pairs, self.turned = frequencies.device, pairs, 2 * frequencies.numel()
+        self._where = _array(frequencies, torch.float32, (frequencies.numel(),), self.device, "frequencies")
+        self.frequencies = frequencies
+
+
+def _cache_shapes(num_pages, kv_heads, page_tokens, head_dim, format):
+    """Of data and exponents."""
+    width = -(-head_dim // 64) * 64
+    if format == "fp4":
+        return (num_pages, kv_heads, page_tokens, 2, width // 2), (num_pages, kv_heads, page_tokens // 16, 2, width // 32, 16)
+    return (num_pages, kv_heads, page_tokens, 2, width), (num_pages, kv_heads, page_tokens // 16, 2)
+
+
 class KvCache:
-    """Keys and values in 8 bits, in pages (pag_kv_cache).  format: "int8" or "fp8" (4 exponent and 3 mantissa bits)."""
+    """Keys and values in pages (pag_kv_cache).  format: "int8", "fp8" (4 exponent and 3 mantissa bits), each with an exponent for 16 tokens, or
+    "fp4" (2 exponent bits and 1 mantissa bit) with one for 32 numbers of a row."""
 
     def __init__(self, num_pages, kv_heads, head_dim, page_tokens=64, format="int8", device=None):
         device = _gpu(device)
-        width = -(-head_dim // 64) * 64
-        self._set(torch.zeros((num_pages, kv_heads, page_tokens, 2, width), dtype=torch.uint8, device=device),
-                  torch.zeros((num_pages, kv_heads, page_tokens // 16, 2), dtype=torch.int8, device=device), head_dim, format)
+        data, exponents = _cache_shapes(num_pages, kv_heads, page_tokens, head_dim, format)
+        self._set(torch.zeros(data, dtype=torch.uint8, device=device), torch.zeros(exponents, dtype=torch.int8, device=device), head_dim, format)
 
     @classmethod
     def from_tensors(cls, data, exponents, head_dim, format="int8"):
         """A cache over the caller's tensors: uint8 [num_pages, kv_heads, page_tokens, 2, width], int8 [num_pages, kv_heads, page_tokens / 16, 2];
-        width is head_dim rounded up to a multiple of 64, with zeros behind head_dim."""
+        width is head_dim rounded up to a multiple of 64, with zeros behind head_dim.  "fp4": uint8 [num_pages, kv_heads, page_tokens, 2, width / 2], int8
+        [num_pages, kv_heads, page_tokens / 16, 2, width / 32, 16]."""
         self = cls.__new__(cls)
         self._set(data, exponents, head_dim, format)
         return self
@@ -271,13 +302,13 @@ class KvCache:
         if format not in _FORMATS:
             raise PagError("format must be one of %s" % ", ".join(sorted(_FORMATS)))
         if not isinstance(data, torch.Tensor) or data.dim() != 5 or not data.is_cuda:
-            raise PagError("data must be a uint8 CUDA tensor [num_pages, kv_heads, page_tokens, 2, width]")
+            raise PagError("data must be a uint8 CUDA tensor [num_pages, kv_heads, page_tokens, 2, bytes of a row]")
         pages, heads, tokens = data.shape[:3]
         self.device = data.device
+        data_shape, exponents_shape = _cache_shapes(pages, heads, tokens, int(head_dim), format)
         self.num_pages, self.kv_heads, self.page_tokens, self.head_dim, self.format = pages, heads, tokens, int(head_dim), format
         self._c = _Cache(C.sizeof(_Cache), _FORMATS[format], heads, self.head_dim, tokens, 0, pages,
-                         _array(data, torch.uint8, (pages, heads, tokens, 2, -(-self.head_dim // 64) * 64), self.device, "data"),
-                         _array(exponents, torch.int8, (pages, heads, tokens // 16, 2), self.device, "exponents"))
+                         _array(data, torch.uint8, data_shape, self.device, "data"), _array(exponents, torch.int8, exponents_shape, self.device, "exponents"))
         self.data, self.exponents = data, exponents
         _check(load_library().pag_kv_read(C.byref(self._c), None, C.c_uint64(0), C.c_uint32(0), *[C.c_void_p(None), C.c_int64(0), C.c_int64(0)] * 2,
                                           None), "KvCache")      # of nothing: looks the cache over
@@ -291,6 +322,36 @@ class KvCache:
         _rows(v, shape, self.device, "v", (k.dtype,))
         _call("pag_kv_append", self.device, C.addressof(self._c), _DTYPES[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
               v.stride(0), v.stride(1), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens)
+
+    def append_rotated(self, k, v, slots, positions, rotation, q=None, out=None):
+        """append() of k turned by `rotation` (a KvRotation) at positions (int32 [tokens]; a step's, or others) and of v as it is.
+        -> q [tokens, heads, head_dim], of k's type, turned likewise: a new tensor, or `out` (q itself: in place); None if there is no q."""
+        tokens = slots.shape[0]
+        shape = (tokens, self.kv_heads, self.head_dim)
+        _rows(k, shape, self.device, "k")
+        _rows(v, shape, self.device, "v", (k.dtype,))
+        if not isinstance(rotation, KvRotation) or rotation.device != self.device:
+            raise PagError("rotation must be a KvRotation on %s" % self.device)
+        r = _Rotation(C.sizeof(_Rotation), _PAIRS[rotation.pairs], rotation.turned, 0, rotation._where,
+                      _array(positions, torch.int32, (tokens,), self.device, "positions"))
+        if q is None:
+            if out is not None:
+                raise PagError("out is for a q")
+        else:
+            if not isinstance(q, torch.Tensor) or q.dim() != 3:
+                raise PagError("q must be a tensor [tokens, heads, head_dim]")
+            rows = (tokens, q.shape[1], self.head_dim)
+            _rows(q, rows, self.device, "q", (k.dtype,))
+            if out is None:
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            else:
+                _rows(out, rows, self.device, "out", (k.dtype,))
+            r.heads = q.shape[1]
+            r.q, r.q_token_stride, r.q_head_stride = q.data_ptr(), q.stride(0), q.stride(1)
+            r.out, r.out_token_stride, r.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
+        _call("pag_kv_append_rotated", self.device, C.addressof(self._c), _DTYPES[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
+              v.stride(0), v.stride(1), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens, C.addressof(r))
+        return out
 
     def read(self, slots, dtype=torch.float32, out=None):
         """-> (k, v) [tokens, kv_heads, head_dim]: the rows in these slots as numbers; zeros for -1.  out: (k, v) to write into, of any

@@ -1,0 +1,197 @@
+"""Keys and queries turned by their positions on the way into the cache, and the 4-bit cache's codes, against 64 bits: bit for bit, since what is
+held and what comes out is rounded once."""
+import math
+
+import numpy as np
+import pytest
+
+import kv_more_plain as more
+import kv_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+DTYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def kv():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2603_06660_amd import kv, load_library
+    load_library()
+    return kv
+
+
+def wide(x):
+    return x.double().cpu().numpy()
+
+
+def new_cache(kv, pages, heads, dim, page, fmt, seed):
+    """A cache over memory that was used for something else before (zeros behind head_dim, which the format asks for)."""
+    gen = torch.Generator().manual_seed(seed)
+    data_shape, exponent_shape = more.shapes(pages, heads, page, dim, fmt)
+    data = torch.randint(0, 256, data_shape, generator=gen, dtype=torch.uint8)
+    data[..., dim // 2 if fmt == "fp4" else dim:] = 0
+    exponents = torch.randint(-64, 64, exponent_shape, generator=gen).to(torch.int8)
+    return kv.KvCache.from_tensors(data.cuda(), exponents.cuda(), dim, fmt), data.numpy().copy(), exponents.numpy().copy()
+
+
+def same_cache(cache, data, exponents):
+    assert (cache.exponents.cpu().numpy() == exponents).all()
+    got = cache.data.cpu().numpy()
+    if cache.format == "fp8":        # -0 and 0 are one number
+        got, data = np.where(got == 128, 0, got), np.where(data == 128, 0, data)
+    if cache.format == "fp4":
+        fold = lambda x: np.where(x & 0x70 == 0, x & 0x7F, x) & np.where(x & 7 == 0, 0xF7, 0xFF)
+        got, data = fold(got), fold(data)
+    assert (got == data).all()
+
+
+@pytest.mark.parametrize("dim, heads, page, dtype", [(64, 1, 16, "bf16"), (128, 2, 32, "fp16"), (80, 3, 48, "fp32"), (192, 2, 16, "fp32"),
+                                                     (256, 1, 64, "bf16"), (8, 2, 16, "fp16")])
+def test_fp4_append_and_read_bit_for_bit(kv, dim, heads, page, dtype):
+    """Tokens in order and out of order, steps of one and of many; nothing beside them is touched."""
+    rng = np.random.default_rng(dim + page)
+    pages = 9
+    cache, data, exponents = new_cache(kv, pages, heads, dim, page, "fp4", dim)
+    free = rng.permutation(pages * page)
+    for n in (1, 1, 3, 12, 1, 37, 20):
+        slots, free = free[:n].copy(), free[n:]
+        if n == 12:
+            slots.sort()
+            slots[[2, 5]] = -1, pages * page
+        x = [torch.tensor(rng.standard_normal((n, heads, dim)) * 2.0 ** rng.integers(-6, 7, (n, heads, 1))).to(DTYPES[dtype]) for _ in range(2)]
+        if n == 3:
+            x[0][1, 0] = 0.0
+            x[1][:] = 0.0
+        cache.append(x[0].cuda(), x[1].cuda(), torch.tensor(slots).cuda())
+        more.append(data, exponents, dim, "fp4", wide(x[0]), wide(x[1]), slots)
+        same_cache(cache, data, exponents)
+    slots = np.concatenate([rng.permutation(pages * page)[:50], [-1, pages * page, 1 << 40]])
+    at = np.where(slots < pages * page, np.maximum(slots, 0), 0)
+    want = more.numbers(data, exponents, dim, "fp4")[at // page, :, at % page]                       # [tokens, heads, 2, dim]
+    want[50:] = 0.0
+    for name in ("fp32", "bf16", "fp16"):
+        got = cache.read(torch.tensor(slots).cuda(), dtype=DTYPES[name])
+        for kind in range(2):
+            exact = torch.tensor(want[:, :, kind]).to(DTYPES[name])         # the first two hold every number; the third rounds some
+            assert got[kind].dtype == DTYPES[name] and (got[kind].cpu() == exact).all()
+
+
+def test_fp4_append_of_values_at_the_edges(kv):
+    """Zeros, infinities, NaN, the smallest and largest numbers, halfway cases, numbers that reach 7 and pass it."""
+    rows = [[0.0] * 8, [math.nan] * 8, [math.inf, -math.inf, 1.0, -2.0, math.nan, 0.0, 3.0, 6.0], [1e-38, -1e-40, 0, 0, 0, 0, 0, 2.0 ** -126],
+            [3.0e38, -3.4e38, 1.0, 0, 0, 0, 0, 0], [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0], [-0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5.0, 7.0],
+            [7.0001, 5.0, 10.0, 3.0, 1.0, 0.5, 0.49, 0], [7.0 * 2.0 ** -64, 2.0 ** -66, -(2.0 ** -65), 0, 0, 0, 0, 0],
+            [-0.0, 0.2500001, 0.7499999, 1.2500001, 1.7499999, 2.5000002, 3.4999998, 5.0000005]]
+    x = torch.tensor(rows, dtype=torch.float32)[:, None]
+    cache, data, exponents = new_cache(kv, 1, 1, 8, 16, "fp4", 3)
+    slots = np.arange(len(rows))
+    cache.append(x.cuda(), -x.cuda(), torch.tensor(slots).cuda())
+    more.append(data, exponents, 8, "fp4", wide(x), -wide(x), slots)
+    same_cache(cache, data, exponents)
+    # what rounds up to 2^128 is read as the largest finite bf16
+    assert cache.read(torch.tensor([4]).cuda())[0][0, 0, :2].tolist() == [255.0 * 2.0 ** 120, -255.0 * 2.0 ** 120]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8", "fp4"])
+@pytest.mark.parametrize("dim, turned, kv_heads, heads, page, dtype, pairs", [
+    (64, 64, 1, 1, 16, "bf16", "halves"), (128, 128, 8, 32, 32, "bf16", "halves"), (128, 64, 5, 10, 32, "fp16", "neighbours"), (80, 80, 3, 9, 48, "fp32", "halves"),
+    (72, 72, 2, 2, 16, "fp16", "halves"), (192, 8, 2, 3, 16, "fp32", "neighbours"), (256, 256, 1, 16, 64, "bf16", "halves"), (8, 8, 2, 0, 16, "fp16", "halves"),
+    (256, 256, 2, 4, 16, "fp32", "neighbours"), (96, 24, 4, 4, 16, "bf16", "halves")])
+def test_rotated_write_bit_for_bit(kv, fmt, dim, turned, kv_heads, heads, page, dtype, pairs):
+    """Steps of one and of many tokens of a request whose positions lie anywhere, also before 0 and near the end of 32 bits."""
+    rng = np.random.default_rng(dim + page + turned)
+    pages = 9
+    cache, data, exponents = new_cache(kv, pages, kv_heads, dim, page, fmt, dim)
+    f = (10000.0 ** (-np.arange(turned // 2) / (turned // 2))).astype(np.float32)
+    rotation = kv.KvRotation(torch.tensor(f).cuda(), pairs)
+    order = rng.permutation(pages)
+    length = 0
+    for n, far in ((1, 0), (1, 130_000), (3, -5), (12, 1_000_000), (37, 2 ** 31 - 37), (20, 77)):
+        at = np.arange(length, length + n)
+        slots = order[at // page] * page + at % page
+        positions = far + np.arange(n)
+        if n == 20:
+            slots[-1] = -1                   # (between a block's tokens none may be left out)
+            positions = rng.integers(-2 ** 31, 2 ** 31, n)
+        x = [torch.tensor(rng.standard_normal((n, kv_heads, dim)) * 2.0 ** rng.integers(-6, 7, (n, kv_heads, 1))).to(DTYPES[dtype]) for _ in range(2)]
+        q = torch.tensor(rng.standard_normal((n, heads, dim))).to(DTYPES[dtype]) if heads else None
+        where = torch.tensor(positions, dtype=torch.int32).cuda()
+        got = cache.append_rotated(x[0].cuda(), x[1].cuda(), torch.tensor(slots).cuda(), where, rotation, q=None if q is None else q.cuda())
+        more.append(data, exponents, dim, fmt, more.turn(wide(x[0]), positions, f, pairs), wide(x[1]), slots)
+        same_cache(cache, data, exponents)
+        if q is None:
+            assert got is None
+        else:
+            assert (wide(got) == more.rounded(more.turn(wide(q), positions, f, pairs), dtype)).all()
+        length += n
+
+
+@pytest.mark.parametrize("fmt, tokens, heads", [("fp8", 300, 12), ("int8", 700, 8), ("int8", 5000, 6), ("fp4", 1200, 8)])
+def test_rotated_write_of_prompts(kv, fmt, tokens, heads):
+    """Windows of one new token, of 4 and of 16; runs that begin and end anywhere in a block, with slots that are none between them."""
+    rng = np.random.default_rng(tokens)
+    dim, page, pages = 16, 32, tokens // 8 + 40
+    cache, data, exponents = new_cache(kv, pages, heads, dim, page, fmt, tokens)
+    order, slots, first = rng.permutation(pages), [], 0
+    while len(slots) < tokens:
+        n, start = int(rng.integers(1, 70)), int(rng.integers(0, page))
+        at = np.arange(start, start + n)
+        need = int(at[-1]) // page + 1
+        if first + need > pages:
+            break
+        slots += (order[first + at // page] * page + at % page).tolist() + [-1] * int(rng.integers(0, 3) == 0)
+        first += need
+    slots = (slots + [-1] * tokens)[:tokens]
+    f = (500.0 ** (-np.arange(8) / 8)).astype(np.float32)
+    positions = rng.integers(0, 200_000, tokens)
+    x = [torch.tensor(rng.standard_normal((tokens, heads, dim))).to(torch.bfloat16) for _ in range(2)]
+    q = torch.tensor(rng.standard_normal((tokens, 2 * heads, dim))).to(torch.bfloat16).cuda()
+    before = q.clone()
+    got = cache.append_rotated(x[0].cuda(), x[1].cuda(), torch.tensor(slots).cuda(), torch.tensor(positions, dtype=torch.int32).cuda(),
+                               kv.KvRotation(torch.tensor(f).cuda()), q=q, out=q)
+    assert got is q
+    more.append(data, exponents, dim, fmt, more.turn(wide(x[0]), positions, f, "halves"), wide(x[1]), slots)
+    same_cache(cache, data, exponents)
+    assert (wide(q) == more.rounded(more.turn(wide(before), positions, f, "halves"), "bf16")).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp4"])
+def test_rotated_strides(kv, fmt):
+    """Slices of a fused projection go in; turned queries come out head by head."""
+    tokens, heads, dim = 37, 3, 64
+    fused = torch.randn(tokens, 8 * heads, dim + 8, device="cuda", dtype=torch.bfloat16)
+    q, k, v = fused[:, :2 * heads, 8:], fused[:, 3 * heads:4 * heads, :dim], fused[:, 5 * heads:6 * heads, 8:]
+    slots, at = torch.arange(tokens, device="cuda"), torch.arange(100, 100 + tokens, device="cuda", dtype=torch.int32)
+    rotation = kv.KvRotation(torch.rand(16, device="cuda"), "neighbours")
+    one, two = kv.KvCache(3, heads, dim, 16, fmt), kv.KvCache(3, heads, dim, 16, fmt)
+    want = one.append_rotated(k.contiguous(), v.contiguous(), slots, at, rotation, q=q.contiguous())
+    by_head = torch.full((2 * heads, tokens, dim), 7.0, device="cuda", dtype=torch.bfloat16)
+    two.append_rotated(k, v, slots, at, rotation, q=q, out=by_head.transpose(0, 1))
+    assert torch.equal(one.data, two.data) and torch.equal(one.exponents, two.exponents) and torch.equal(by_head, want.transpose(0, 1))
+    before = fused.clone()
+    two.append_rotated(k, v, slots, at, rotation, q=q, out=q)
+    assert torch.equal(q, want)
+    fused[:, :2 * heads, 8:] = before[:, :2 * heads, 8:]
+    assert torch.equal(fused, before)
+
+
+def test_rotated_refusals(kv):
+    cache = kv.KvCache(2, 2, 64, 16)
+    f = torch.rand(32, device="cuda")
+    k, slots, at = torch.zeros(4, 2, 64, device="cuda", dtype=torch.bfloat16), torch.arange(4, device="cuda"), torch.zeros(4, device="cuda", dtype=torch.int32)
+    rotation = kv.KvRotation(f)
+    for bad in (lambda: kv.KvRotation(f, "pairs"), lambda: kv.KvRotation(f.cpu()), lambda: kv.KvRotation(f.double()), lambda: kv.KvRotation(f[::2]),
+                lambda: kv.KvRotation(f[:0]), lambda: cache.append_rotated(k, k, slots, at, kv.KvRotation(torch.rand(36, device="cuda"))),
+                lambda: cache.append_rotated(k, k, slots, at, kv.KvRotation(f[:30].contiguous())), lambda: cache.append_rotated(k, k, slots, at.long(), rotation),
+                lambda: cache.append_rotated(k, k, slots, at[:3], rotation), lambda: cache.append_rotated(k, k, slots, at, f),
+                lambda: cache.append_rotated(k, k, slots, at, rotation, q=k.float()), lambda: cache.append_rotated(k, k, slots, at, rotation, q=k[:3]),
+                lambda: cache.append_rotated(k, k, slots, at, rotation, out=k), lambda: cache.append_rotated(k, k.half(), slots, at, rotation),
+                lambda: cache.append_rotated(k, k, slots, at, rotation, q=k, out=k.view(2, 4, 64).transpose(0, 1)),
+                lambda: cache.append_rotated(k.clone().requires_grad_(), k, slots, at, rotation)):
+        with pytest.raises(kv.PagError):
+            bad()
+    assert cache.append_rotated(k[:0], k[:0], slots[:0], at[:0], rotation, q=k[:0]).shape == (0, 2, 64)
