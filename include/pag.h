@@ -469,6 +469,41 @@ int pag_kv_attend(const pag_kv_cache* cache, const pag_kv_step* step, const pag_
 int pag_kv_attend_selected(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, const int64_t* ids,
                            int64_t ids_token_stride, int64_t ids_head_stride, uint32_t id_heads, uint32_t k, void* stream);
 
+/*
+ * Blocks of block_tokens tokens (a multiple of 16 that divides page_tokens; block b of a request holds its tokens b * block_tokens and on), of which
+ * a token reads the k best.  A block's summary for a key/value head is, of each number of its keys as the cache holds them, the largest and the smallest, as integers with one
+ * power of two: e is the smallest >= -64 at which 127 * 2^e reaches the largest magnitude, the largest is rounded up to a multiple of 2^e and the smallest down.
+ * With a row of q as integers (nearest, at the smallest such power of two; infinities as 127, NaN as 0) a block's score for a query head is
+ *     sum over the numbers of largest * max(q, 0) + smallest * min(q, 0),
+ * which no key of the block exceeds, but for q's rounding; an integer below 2^23 times a power of two, so that which blocks are chosen is the same
+ * on every run and by every path (scores beyond 32 bits count as equal).
+ */
+typedef struct {
+    uint32_t struct_size;
+    uint32_t block_tokens;
+    int8_t* codes;             /* dev [num_pages][kv_heads][page_tokens / block_tokens][2: largest, smallest][W], 16-byte aligned */
+    int8_t* exponents;         /* dev [num_pages][kv_heads][page_tokens / block_tokens] */
+} pag_kv_blocks;
+
+/*
+ * pag_kv_blocks_update: after pag_kv_append of these slots (dev int64 [tokens]; the same rules): writes the summaries of the blocks that they lie in, of all tokens
+ * from the block's first one to the last one in the call, which has to be the last one that the block holds.
+ * pag_kv_blocks_select: for each token and list the k best of the blocks that begin before the token's window (args->window; 0: up to the token itself), of a list's heads by the
+ * largest of their scores, of equal ones the first; their numbers in ascending order, -1 behind them (dev int32 [tokens][id_heads][k], strides in elements, last dimension dense).
+ * Blocks in pages that are none are left out.  id_heads as in pag_kv_attend_selected.  Of args it reads dtype, heads, window, q and its strides,
+ * and the workspace.  tokens * heads < 2^23.
+ * pag_kv_attend_blocks: pag_kv_attend_selected over the tokens of the listed blocks: those in the window or behind the token are passed over, a block listed twice counts
+ * twice; k * block_tokens + window below 2^30.
+ * pag_kv_blocks_workspace_bytes: the workspaces of these two; either pointer may be null.
+ */
+int pag_kv_blocks_update(const pag_kv_cache* cache, const pag_kv_blocks* blocks, const int64_t* slots, uint64_t tokens, void* stream);
+int pag_kv_blocks_select(const pag_kv_cache* cache, const pag_kv_blocks* blocks, const pag_kv_step* step, const pag_kv_attention* args, uint32_t id_heads,
+                         uint32_t k, int32_t* ids, int64_t ids_token_stride, int64_t ids_head_stride, void* stream);
+int pag_kv_attend_blocks(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, const int32_t* ids, int64_t ids_token_stride,
+                         int64_t ids_head_stride, uint32_t id_heads, uint32_t k, uint32_t block_tokens, void* stream);
+int pag_kv_blocks_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, uint32_t id_heads, uint32_t k,
+                                  uint32_t block_tokens, uint64_t* select_bytes, uint64_t* attend_bytes);
+
 const char* pag_last_error(void);
 
 #ifdef __cplusplus

@@ -18,7 +18,7 @@ from .binding import (PagIndex, PagError, load_library, library_path, EXPORTED_S
 
 
 def __getattr__(name):      # these need torch, which importing the package does not
-    if name in ("KvCache", "KvRotation", "KvStep", "KvTables"):
+    if name in ("KvBlocks", "KvCache", "KvRotation", "KvStep", "KvTables"):
         from . import kv
         return getattr(kv, name)
     raise AttributeError("module %r has no attribute %r" % (__name__, name))

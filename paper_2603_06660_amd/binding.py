@@ -26,6 +26,7 @@ EXPORTED_SYMBOLS = (
     "pag_search_layout", "pag_measure_row_reads",
     "pag_searcher_create", "pag_searcher_search", "pag_searcher_get_counters", "pag_searcher_free",
     "pag_kv_extend", "pag_kv_release", "pag_kv_append", "pag_kv_append_rotated", "pag_kv_read", "pag_kv_workspace_bytes", "pag_kv_attend", "pag_kv_attend_selected",
+    "pag_kv_blocks_update", "pag_kv_blocks_select", "pag_kv_attend_blocks", "pag_kv_blocks_workspace_bytes",
     "pag_last_error",
 )
 

@@ -106,6 +106,12 @@ __device__ __forceinline__ void decode4_fp4(u32 w, float scale, float* x) {
     x[0] = lo.x; x[1] = lo.y; x[2] = hi.x; x[3] = hi.y;
 }
 
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+    return x;
+}
+
 __device__ __forceinline__ void widen_row8(const uint4& r, u32 dtype, float* x) {      // PAG_F16 or PAG_BF16
     const u32 w[4] = { r.x, r.y, r.z, r.w };
 #pragma unroll
@@ -174,14 +180,33 @@ struct Attend {
     float* lse;
     const float* slopes;
     const int64_t* ids;
+    const int32_t* blocks;                // numbers of listed blocks instead, strides as of ids
     int64_t q_ts, q_hs, o_ts, o_hs, ids_ts, ids_hs;
     u32 heads, group, dtype, window, id_heads, k;
-    u32 listed;                           // attention over ids and a window
+    u32 block;                            // tokens of a listed block; 0: ids are tokens
+    u32 listed;                           // attention over ids or blocks and a window
     u32 row_tiles;                        // tiles of 16 query rows that a wave has at most to a key/value head; 0: the wide kernel
     u32 many_rows;                        // the wide kernel: a request has more rows than four of its waves
     float scale, softcap;
     float* partial;                       // the workspace: two parts a workgroup, of the piece that another one began, and of the piece that it began and another one ends
     int2* joined;                         // narrow kernels: [tokens * heads] first and last workgroup of the row's pieces; first < 0: written whole
+};
+
+// summaries of blocks (pag_kv_blocks)
+struct Blocks {
+    int8_t *codes, *exponents;
+    u32 tokens, page_blocks;              // of a block; blocks of a page
+};
+
+struct Choose {
+    Cache c;
+    Step s;
+    Blocks b;
+    const void* q;
+    int64_t q_ts, q_hs, ids_ts, ids_hs;
+    int32_t* ids;
+    u32* keys;                            // the workspace: scores [tokens * id_heads][most_blocks]
+    u32 heads, group, dtype, window, id_heads, k, most_blocks;      // group: heads of a key/value head; most_blocks: of a request
 };
 
 int launch_extend(hipStream_t st, const pag_kv_tables& t, const int32_t* add, const pag_kv_step& s);
@@ -208,10 +233,12 @@ int launch_read(hipStream_t st, const Cache& c, const int64_t* slots, u64 tokens
                 int64_t v_ts, int64_t v_hs);
 int launch_attend(hipStream_t st, const Attend& a, int num_cu);
 
-int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu);
+int launch_summarise(hipStream_t st, const Cache& c, const Blocks& b, const int64_t* slots, u64 tokens);
+int launch_choose(hipStream_t st, const Choose& a);
+u64 choose_workspace(const Choose& a);          // bytes
+u64 choose_groups(const Choose& a);             // workgroups of 256 threads of its largest launch
 
 u64 attend_workspace(const Attend& a, int num_cu);      // bytes
-u64 wide_workspace(u32 width, int num_cu);
 int num_cu_of_current();                        // < 0: no GPU
 
 }  // namespace pagkv

@@ -68,10 +68,10 @@ int check_rows(const void* p, int64_t token_stride, int64_t head_stride, u32 byt
 }
 
 // What decides how a call is laid out: everything but its arrays.
-int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, bool selected, uint32_t id_heads, uint32_t k, Attend* a) {
+int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, bool selected, uint32_t id_heads, uint32_t k, Attend* a,
+              uint32_t block = 0) {
     int rc;
     if ((rc = cache_of(cache, &a->c)) || (rc = check_step(step))) return rc;
-    PAG_CHECK(a->c.fmt != PAG_KV_FP4, PAG_EUNSUPPORTED, "attention over 4-bit codes is not built");
     PAG_CHECK(args != nullptr, PAG_EINVAL, "args is null");
     PAG_CHECK(args->struct_size == sizeof(pag_kv_attention), PAG_EINVAL, "pag_kv_attention.struct_size does not match this library");
     PAG_CHECK(args->dtype == PAG_F16 || args->dtype == PAG_BF16, PAG_EUNSUPPORTED, "attention takes PAG_F16 or PAG_BF16");
@@ -86,7 +86,8 @@ int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_a
     a->group = a->heads / a->c.kv_heads;
     if (selected) {
         PAG_CHECK(id_heads > 0 && id_heads % a->c.kv_heads == 0 && args->heads % id_heads == 0, PAG_EINVAL, "id_heads must be a multiple of kv_heads that divides heads");
-        PAG_CHECK((u64)k + args->window < (1ull << 30), PAG_EUNSUPPORTED, "k + window must be below 2^30");
+        PAG_CHECK((u64)k * std::max(block, 1u) + args->window < (1ull << 30), PAG_EUNSUPPORTED, "listed tokens and window must be below 2^30");
+        a->block = block;
         a->listed = 1;
         a->id_heads = id_heads;
         a->k = k;
@@ -108,6 +109,42 @@ int layout_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_a
     const bool fits = step->tokens * args->heads < (1ull << 23) && (u64)step->requests * a->c.kv_heads < (1ull << 23);
     PAG_CHECK(!selected || fits, PAG_EUNSUPPORTED, "attention over ids needs tokens * heads and requests * kv_heads below 2^23");
     if (!fits) a->row_tiles = 0;
+    return PAG_OK;
+}
+
+int check_block(const Cache& c, uint32_t block) {
+    PAG_CHECK(block > 0 && block % BLOCK == 0 && c.page_tokens % block == 0, PAG_EINVAL, "block_tokens must be a multiple of 16 that divides page_tokens");
+    return PAG_OK;
+}
+
+int blocks_of(const Cache& c, const pag_kv_blocks* b, Blocks* out) {
+    PAG_CHECK(b != nullptr, PAG_EINVAL, "blocks is null");
+    PAG_CHECK(b->struct_size == sizeof(pag_kv_blocks), PAG_EINVAL, "pag_kv_blocks.struct_size does not match this library");
+    const int rc = check_block(c, b->block_tokens);
+    if (rc) return rc;
+    PAG_CHECK(b->codes != nullptr && b->exponents != nullptr && aligned(b->codes, 16), PAG_EINVAL, "blocks: codes or exponents is null, or codes not 16-byte aligned");
+    *out = Blocks{ b->codes, b->exponents, b->block_tokens, c.page_tokens / b->block_tokens };
+    return PAG_OK;
+}
+
+// What decides how a choice is laid out.
+int choice_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, uint32_t id_heads, uint32_t k, uint32_t block, Choose* a) {
+    Attend x = {};
+    int rc = layout_of(cache, step, args, true, id_heads, k, &x, std::max(block, 1u));
+    if (rc || (rc = check_block(x.c, block))) return rc;
+    a->c = x.c;
+    a->s = x.s;
+    a->dtype = x.dtype;
+    a->heads = x.heads;
+    a->group = x.heads / x.c.kv_heads;
+    a->window = x.window;
+    a->id_heads = id_heads;
+    a->k = k;
+    a->most_blocks = step->max_pages * (x.c.page_tokens / block);
+    a->b.tokens = block;
+    a->b.page_blocks = x.c.page_tokens / block;
+    // a launch has fewer than 2^32 threads
+    PAG_CHECK(choose_groups(*a) < (1ull << 23), PAG_EUNSUPPORTED, "tokens * kv_heads * blocks of a request is too large for one launch");
     return PAG_OK;
 }
 
@@ -288,5 +325,74 @@ extern "C" int pag_kv_attend_selected(const pag_kv_cache* cache, const pag_kv_st
         a.ids_ts = ids_token_stride;
         a.ids_hs = ids_head_stride;
         return launch_attend((hipStream_t)stream, a, num_cu);
+    });
+}
+
+extern "C" int pag_kv_blocks_update(const pag_kv_cache* cache, const pag_kv_blocks* blocks, const int64_t* slots, uint64_t tokens, void* stream) {
+    return guarded("pag_kv_blocks_update", [&]() -> int {
+        Cache c;
+        Blocks b;
+        int rc = cache_of(cache, &c);
+        if (rc || (rc = blocks_of(c, blocks, &b))) return rc;
+        PAG_CHECK(tokens < (1ull << 27) && tokens * c.kv_heads < (1ull << 27), PAG_EUNSUPPORTED, "tokens * kv_heads must be below 2^27");
+        if (tokens == 0) return PAG_OK;
+        PAG_CHECK(slots != nullptr, PAG_EINVAL, "slots is null");
+        return launch_summarise((hipStream_t)stream, c, b, slots, tokens);
+    });
+}
+
+extern "C" int pag_kv_blocks_select(const pag_kv_cache* cache, const pag_kv_blocks* blocks, const pag_kv_step* step, const pag_kv_attention* args, uint32_t id_heads,
+                                    uint32_t k, int32_t* ids, int64_t ids_token_stride, int64_t ids_head_stride, void* stream) {
+    return guarded("pag_kv_blocks_select", [&]() -> int {
+        Choose a = {};
+        PAG_CHECK(blocks != nullptr, PAG_EINVAL, "blocks is null");
+        int rc = choice_of(cache, step, args, id_heads, k, blocks->block_tokens, &a);
+        if (rc || (rc = blocks_of(a.c, blocks, &a.b)) || step->tokens == 0 || k == 0) return rc;
+        PAG_CHECK(args->q != nullptr && ids != nullptr && aligned(ids, 4), PAG_EINVAL, "q or ids is null, or ids not 4-byte aligned");
+        if ((rc = check_rows(args->q, args->q_token_stride, args->q_head_stride, 2, 16, "q must be 16-byte aligned, its strides multiples of 8 elements"))) return rc;
+        PAG_CHECK(step->request && step->positions, PAG_EINVAL, "step: request or positions is null");
+        const u64 need = choose_workspace(a);
+        PAG_CHECK(need == 0 || (args->workspace != nullptr && aligned(args->workspace, 16) && args->workspace_bytes >= need), PAG_EINVAL,
+                  "workspace is null, not 16-byte aligned, or smaller than pag_kv_blocks_workspace_bytes");
+        a.q = args->q; a.q_ts = args->q_token_stride; a.q_hs = args->q_head_stride;
+        a.ids = ids; a.ids_ts = ids_token_stride; a.ids_hs = ids_head_stride;
+        a.keys = (u32*)args->workspace;
+        return launch_choose((hipStream_t)stream, a);
+    });
+}
+
+extern "C" int pag_kv_attend_blocks(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, const int32_t* ids, int64_t ids_token_stride,
+                                    int64_t ids_head_stride, uint32_t id_heads, uint32_t k, uint32_t block_tokens, void* stream) {
+    return guarded("pag_kv_attend_blocks", [&]() -> int {
+        Attend a = {};
+        int num_cu = 0, rc;
+        if ((rc = layout_of(cache, step, args, true, id_heads, k, &a, std::max(block_tokens, 1u))) || (rc = check_block(a.c, block_tokens)) ||
+            (rc = arrays_of(step, args, &a, &num_cu)) || step->tokens == 0) return rc;
+        PAG_CHECK(step->request && step->positions, PAG_EINVAL, "step: request or positions is null");
+        PAG_CHECK(k == 0 || (ids != nullptr && aligned(ids, 4)), PAG_EINVAL, "ids is null or not 4-byte aligned");
+        a.blocks = ids;
+        a.ids_ts = ids_token_stride;
+        a.ids_hs = ids_head_stride;
+        return launch_attend((hipStream_t)stream, a, num_cu);
+    });
+}
+
+extern "C" int pag_kv_blocks_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, uint32_t id_heads, uint32_t k,
+                                             uint32_t block_tokens, uint64_t* select_bytes, uint64_t* attend_bytes) {
+    return guarded("pag_kv_blocks_workspace_bytes", [&]() -> int {
+        int rc;
+        if (select_bytes) {
+            Choose a = {};
+            if ((rc = choice_of(cache, step, args, id_heads, k, block_tokens, &a))) return rc;
+            *select_bytes = choose_workspace(a);
+        }
+        if (attend_bytes) {
+            Attend a = {};
+            if ((rc = layout_of(cache, step, args, true, id_heads, k, &a, std::max(block_tokens, 1u))) || (rc = check_block(a.c, block_tokens))) return rc;
+            const int num_cu = num_cu_of_current();
+            PAG_CHECK(num_cu > 0, PAG_EHIP, "no current GPU");
+            *attend_bytes = attend_workspace(a, num_cu);
+        }
+        return PAG_OK;
     });
 }

@@ -67,6 +67,61 @@ __device__ __forceinline__ half8_t widen8(u32 lo, u32 hi) {
     return half8_t{ h[0].x, h[0].y, h[1].x, h[1].y, h[2].x, h[2].y, h[3].x, h[3].y };
 }
 
+// two 4-bit codes, byte B of a word, times a power of two
+template <int B>
+__device__ __forceinline__ half2_t widen2_fp4(u32 w, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, B); }
+
+// eight 4-bit codes in their order, times a power of two
+__device__ __forceinline__ half8_t widen8_fp4(u32 w, float scale) {
+    const half2_t a = widen2_fp4<0>(w, scale), b = widen2_fp4<1>(w, scale), c = widen2_fp4<2>(w, scale), d = widen2_fp4<3>(w, scale);
+    return half8_t{ a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y };
+}
+
+// Four 4-bit codes, half B of eight words, each word with a scale of its own: a column of eight tokens for each of the four numbers.
+template <int B>
+__device__ __forceinline__ void columns_fp4(const u32 (&w)[8], const float (&scale)[8], half8_t* out) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        u32 lo[4], hi[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const u32 x = __builtin_bit_cast(u32, c ? widen2_fp4<2 * B + 1>(w[2 * p], scale[2 * p]) : widen2_fp4<2 * B>(w[2 * p], scale[2 * p]));
+            const u32 y = __builtin_bit_cast(u32, c ? widen2_fp4<2 * B + 1>(w[2 * p + 1], scale[2 * p + 1]) : widen2_fp4<2 * B>(w[2 * p + 1], scale[2 * p + 1]));
+            lo[p] = perm(y, x, 0x05040100);
+            hi[p] = perm(y, x, 0x07060302);
+        }
+        out[2 * c] = __builtin_bit_cast(half8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        out[2 * c + 1] = __builtin_bit_cast(half8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+    }
+}
+
+// The largest of the exponents of 16 tokens' parts of one kind (parts_of), of the first n tokens: what the block's numbers are held as multiples of in
+// 16-bit floats.  What those behind the last token hold may be anything.  Bytes are compared as the upper halves of 16-bit words; LOWEST_EXPONENT if n is 0.
+template <int C>
+__device__ __forceinline__ int most_of_parts(const int8_t* parts, int n) {
+    typedef uint16_t half2u __attribute__((ext_vector_type(2)));
+    uint4 e[2 * C];
+#pragma unroll
+    for (int b = 0; b < 2 * C; ++b) e[b] = *(const uint4*)(parts + b * BLOCK);
+    half2u even = { 0, 0 }, odd = { 0, 0 };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int bytes = min(max(n - 4 * i, 0), 4);
+        const u32 mask = bytes == 4 ? 0xFFFFFFFFu : (1u << (8 * bytes)) - 1;
+#pragma unroll
+        for (int b = 0; b < 2 * C; ++b) {
+            const u32 w = i == 0 ? e[b].x : i == 1 ? e[b].y : i == 2 ? e[b].z : e[b].w, x = (w ^ 0x80808080u) & mask;
+            odd = __builtin_elementwise_max(odd, __builtin_bit_cast(half2u, x));
+            even = __builtin_elementwise_max(even, __builtin_bit_cast(half2u, x << 8));
+        }
+    }
+    const half2u both = __builtin_elementwise_max(odd, even);
+    return max((int)(max(both.x, both.y) >> 8) - 128, LOWEST_EXPONENT);
+}
+
+// byte i of a word of exponents as a power of two, 0 for -127
+__device__ __forceinline__ float power_of_byte(u32 w, int i) { return power((int)(int8_t)(w >> (8 * i))); }
+
 // byte c of eight words, c = 0 .. 3: a column of eight tokens for each of four numbers of a row
 template <int FMT>
 __device__ __forceinline__ void columns(const u32* w, half8_t* out) {
@@ -170,8 +225,25 @@ constexpr u32 PIECE = 4;
 // workgroups of a CU: as many as its registers and LDS last for
 constexpr u32 groups_per_cu(u32 width, int t) { return width > 128 ? 1 : width == 64 && t == 1 ? 3 : 2; }
 
+// shapes of the kernel for many query rows
+constexpr u32 WROWS = 32;                 // query rows of a wave
+constexpr u32 MANY_WAVES = 8;             // waves of a workgroup where requests have rows for them
+
+// workgroups of a CU: as many as its registers last for
+constexpr u32 wide_groups_per_cu(u32 width, int waves) { return waves == 4 && width <= 128 ? 2 : 1; }
+
+struct Head {                             // of a piece that another workgroup goes on with
+    u32 t0, rows, row0, head0;
+    int last;                             // workgroup that ends it; -1: none
+};
+
+template <int FMT>
+int launch_wide(hipStream_t st, const Attend& a, int num_cu);
+
 u64 narrow_groups(const Attend& a);        // workgroups, where one reads all keys of its rows
 template <int FMT, int C>
 void launch_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole);
+template <int FMT, int C>
+void launch_blocks(hipStream_t st, const Attend& a, int num_cu, bool whole);
 
 }  // namespace pagkv

@@ -1,4 +1,4 @@
-// Attention over the 8-bit cache: which kernels a call runs, and the joining of rows whose keys went to several workgroups.
+// Attention over the cache: which kernels a call runs, and the joining of rows whose keys went to several workgroups.
 #include <algorithm>
 
 #include "pag_kv_attend.h"
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(256) k_join(Attend a, int groups) {
 //   51.8, 47.8; one of 2,000 tokens 14.0, 18.3, whose 8 workgroups leave the chip idle
 //   lists: 384 of 1,256 keys 38.6, 29.6; 1,536 of 164 keys 36, 27; 64 of 1,064 keys 19, 15; 32 of 1,064 keys 13.3, 14.3
 bool narrow_whole(const Attend& a, int num_cu) {
-    const u64 keys = a.listed ? (u64)a.k + a.window : std::min<u64>((u64)a.s.max_pages * a.c.page_tokens, a.window ? (u64)a.window + 2 * ROWS : ~0ull);
+    const u64 keys = a.listed ? (u64)a.k * std::max(a.block, 1u) + a.window : std::min<u64>((u64)a.s.max_pages * a.c.page_tokens, a.window ? (u64)a.window + 2 * ROWS : ~0ull);
     const u64 groups = narrow_groups(a);
     if (keys <= 1024) return true;
     if (!a.listed) return keys <= 2048 && groups >= (u64)num_cu / 2;
@@ -104,9 +104,40 @@ u64 partial_floats(const Attend& a, int num_cu) {
 template <int C>
 void run(hipStream_t st, const Attend& a, int num_cu) {
     const bool whole = narrow_whole(a, num_cu);
-    if (a.c.fmt == PAG_KV_INT8) launch_narrow<PAG_KV_INT8, C>(st, a, num_cu, whole);
-    else launch_narrow<PAG_KV_FP8, C>(st, a, num_cu, whole);
+    if (a.block) {
+        if (a.c.fmt == PAG_KV_INT8) launch_blocks<PAG_KV_INT8, C>(st, a, num_cu, whole);
+        else if (a.c.fmt == PAG_KV_FP8) launch_blocks<PAG_KV_FP8, C>(st, a, num_cu, whole);
+        else launch_blocks<PAG_KV_FP4, C>(st, a, num_cu, whole);
+    } else if (a.c.fmt == PAG_KV_INT8) {
+        launch_narrow<PAG_KV_INT8, C>(st, a, num_cu, whole);
+    } else if (a.c.fmt == PAG_KV_FP8) {
+        launch_narrow<PAG_KV_FP8, C>(st, a, num_cu, whole);
+    } else {
+        launch_narrow<PAG_KV_FP4, C>(st, a, num_cu, whole);
+    }
     if (!whole) k_join<C><<<a.s.tokens * a.heads, 256, 0, st>>>(a, num_cu * (int)groups_per_cu(64 * C, (int)a.row_tiles));
+}
+
+u64 wide_workspace(u32 width, int num_cu) {
+    // twice the workgroups have half the rows, or the other way round
+    const u64 grid = (u64)num_cu * wide_groups_per_cu(width, 4), rows = std::max(grid * 4 * WROWS, width <= 128 ? (u64)num_cu * MANY_WAVES * WROWS : 0);
+    return 4 * 2 * rows * (width + 2) + (grid * sizeof(Head) + 15) / 16 * 16;
+}
+
+int launch_all(hipStream_t st, const Attend& args, int num_cu) {
+    if (args.row_tiles == 0) {
+        if (args.c.fmt == PAG_KV_INT8) return launch_wide<PAG_KV_INT8>(st, args, num_cu);
+        if (args.c.fmt == PAG_KV_FP8) return launch_wide<PAG_KV_FP8>(st, args, num_cu);
+        return launch_wide<PAG_KV_FP4>(st, args, num_cu);
+    }
+    Attend a = args;
+    a.joined = narrow_whole(a, num_cu) ? nullptr : (int2*)(a.partial + partial_floats(a, num_cu));
+    const u32 n = a.c.width / 64;
+    if (n == 1) run<1>(st, a, num_cu);
+    else if (n == 2) run<2>(st, a, num_cu);
+    else if (n == 3) run<3>(st, a, num_cu);
+    else run<4>(st, a, num_cu);
+    return PAG_OK;
 }
 
 }  // namespace
@@ -116,15 +147,9 @@ u64 attend_workspace(const Attend& a, int num_cu) {
     return narrow_whole(a, num_cu) ? 0 : 4 * partial_floats(a, num_cu) + 8 * (u64)a.s.tokens * a.heads;
 }
 
-int launch_attend(hipStream_t st, const Attend& args, int num_cu) {
-    if (args.row_tiles == 0) return launch_attend_wide(st, args, num_cu);
-    Attend a = args;
-    a.joined = narrow_whole(a, num_cu) ? nullptr : (int2*)(a.partial + partial_floats(a, num_cu));
-    const u32 n = a.c.width / 64;
-    if (n == 1) run<1>(st, a, num_cu);
-    else if (n == 2) run<2>(st, a, num_cu);
-    else if (n == 3) run<3>(st, a, num_cu);
-    else run<4>(st, a, num_cu);
+int launch_attend(hipStream_t st, const Attend& a, int num_cu) {
+    const int rc = launch_all(st, a, num_cu);
+    if (rc) return rc;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { pag_set_error(std::string("pag_kv_attend: ") + hipGetErrorString(e)); return PAG_EHIP; }
     return PAG_OK;

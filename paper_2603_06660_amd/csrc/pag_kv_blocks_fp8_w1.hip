@@ -1,0 +1,4 @@
+// Instantiations of attention over listed blocks: 8-bit float codes, rows of up to 64 numbers.
+#include "pag_kv_blocks.h"
+
+template void pagkv::launch_blocks<PAG_KV_FP8, 1>(hipStream_t, const pagkv::Attend&, int, bool);

@@ -1,4 +1,4 @@
-// Attention over the 8-bit cache: the kernels of pag_kv_attend for few query rows to a key, and of pag_kv_attend_selected.
+// Attention over the cache: the kernels of pag_kv_attend for few query rows to a key, and of pag_kv_attend_selected.
 //
 // Rows of a token's heads that read the same keys (a group, and a request's neighbouring tokens) are taken 16 at a time, as the columns of
 // a matrix product.  Per tile of 32 keys a wave computes S^T = K Q^T (the keys are rows: a lane ends up with 8 scores of one query row), the
@@ -26,11 +26,29 @@ namespace {
 
 // a lane's part of 32 keys: of row lane % 16 of both halves the 16-byte pieces lane / 16 + 4 h, and of tokens 4 (lane / 16) + 0 .. 3
 // of both halves the values' numbers 4 C (lane % 16) + 0 .. 4 C - 1
-template <int C>
+template <int FMT, int C>
 struct Tile {
     uint4 k[2][C];
     u32 v[8][C];
 };
+
+// 4-bit codes: pieces of 16 bytes, one part each, where rows are a multiple of 64 bytes, and of 8 bytes otherwise
+template <int C>
+struct Tile<PAG_KV_FP4, C> {
+    static constexpr int PIECES = C % 2 ? C : C / 2, WORDS = 2 * C / PIECES;       // of a lane's row of keys, words of a piece
+    static constexpr int PARTS = C == 3 ? 3 : 1;                                   // parts that a lane's numbers of a row of values lie in
+    u32 k[2][2 * C];
+    u32 v[8][(C + 1) / 2];
+    int ke[2][PIECES];         // exponents of the pieces' parts; of listed keys less their largest
+    u32 ve[2][PARTS];          // of tokens 4 (lane / 16) + 0 .. 3
+};
+
+// the first number of eight that a lane with g = lane / 16 has of a row for its product number n
+template <int FMT, int C>
+__device__ __forceinline__ u32 number_of(int n, u32 g) {
+    if constexpr (FMT == PAG_KV_FP4 && C % 2 == 0) return (n >> 2) * 128 + g * 32 + (n & 3) * 8;
+    else return (n >> 1) * 64 + g * 16 + (n & 1) * 8;
+}
 
 template <int C>
 __device__ __forceinline__ void load_words(const uint8_t* p, u32* w) {
@@ -48,10 +66,51 @@ __device__ __forceinline__ void load_words(const uint8_t* p, u32* w) {
     }
 }
 
+// 4-bit codes: 2 C bytes of a row of values, at a multiple of 2 C, in the low ends of words
+template <int C>
+__device__ __forceinline__ void load_halves(const uint8_t* p, u32* w) {
+    if constexpr (C == 1) {
+        w[0] = *(const uint16_t*)p;
+    } else if constexpr (C == 2) {
+        w[0] = *(const u32*)p;
+    } else if constexpr (C == 3) {
+        const uint16_t* x = (const uint16_t*)p;
+        w[0] = x[0] | (u32)x[1] << 16;
+        w[1] = x[2];
+    } else {
+        const uint2 x = *(const uint2*)p;
+        w[0] = x.x; w[1] = x.y;
+    }
+}
+
+// A lane's part of a tile of 4-bit codes.  k: its row of keys; v(j): the rows of values of its 8 tokens
+template <int C, typename V>
+__device__ __forceinline__ void load_codes(Tile<PAG_KV_FP4, C>& tile, int s, const uint8_t* k, V&& v, u32 col, u32 g) {
+    typedef Tile<PAG_KV_FP4, C> Tile4;
+#pragma unroll
+    for (int h = 0; h < Tile4::PIECES; ++h) {
+        if constexpr (Tile4::WORDS == 4) {
+            const uint4 x = *(const uint4*)(k + g * 16 + h * 64);
+            tile.k[s][4 * h] = x.x; tile.k[s][4 * h + 1] = x.y; tile.k[s][4 * h + 2] = x.z; tile.k[s][4 * h + 3] = x.w;
+        } else {
+            const uint2 x = *(const uint2*)(k + g * 8 + h * 32);
+            tile.k[s][2 * h] = x.x; tile.k[s][2 * h + 1] = x.y;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) load_halves<C>(v(j) + 32 * C + col * (2 * C), tile.v[4 * s + j]);
+}
+
+// parts of a lane's pieces of keys and numbers of values
+template <int C>
+__device__ __forceinline__ u32 key_part(int h, u32 g) { return C % 2 ? 2 * h + g / 2 : g + 4 * h; }
+template <int C>
+__device__ __forceinline__ u32 value_part(int w, u32 col) { return C == 3 ? (3 * col + w) / 8 : C * col / 8; }
+
 // what a wave knows of its 16 rows and has summed up
 template <int C>
 struct Rows {
-    half8_t q[2 * C];          // row lane % 16, numbers 64 h + 16 (lane / 16) + 8 s + 0 .. 7 in q[2 h + s]
+    half8_t q[2 * C];          // row lane % 16, numbers number_of(n, lane / 16) + 0 .. 7 in q[n]
     float factor;              // of this row: scale, and the power of two that q was divided by
     float slope;               // times log2 e
     int position;              // -1: no such row
@@ -68,13 +127,13 @@ struct Where {
 template <int C>
 struct RawRows { uint4 x[2 * C]; };
 
-template <int C>
+template <int FMT, int C>
 __device__ __forceinline__ void fetch_rows(const Attend& a, const Where& w, RawRows<C>& raw) {
     const u32 lane = threadIdx.x & 63, row = w.row0 + (lane & 15), g = lane >> 4;
     const u64 from = (u64)(w.t0 + row / a.group) * (u64)a.q_ts + (w.head0 + row % a.group) * (u64)a.q_hs;
 #pragma unroll
     for (int n = 0; n < 2 * C; ++n) {
-        const u32 at = (n >> 1) * 64 + g * 16 + (n & 1) * 8;
+        const u32 at = number_of<FMT, C>(n, g);
         raw.x[n] = make_uint4(0, 0, 0, 0);
         if (row < w.rows && at < a.c.dim) raw.x[n] = *(const uint4*)((const uint16_t*)a.q + from + at);
     }
@@ -121,17 +180,32 @@ struct Scales {
     static constexpr int N = LISTED ? 8 : 2;
     float ek[N], ev[N], down[N];
     int at[N];
+    float fine[2][2];          // 4-bit codes whose keys share ek and ev: 2^-e of the keys and of the values of either half, which their parts' exponents are above
 };
 
 // T tiles of rows against one of keys.  keep: bit j set if the row may read key j; looked at only if `masked`.  far: the
 // sum takes weights without their values' scale.  SLOPES: of lists, whether the call has slopes; otherwise that is looked up.  CAPPED: by a cap above
 // NEAR_CAP.  Both are kernels of their own: code that a call does not run lies between code that it does, and short calls wait for
 // its fetch (one request of 500 tokens 10.1 us with the large caps' code, 9.6 without).
-template <int FMT, int C, int T, bool LISTED, bool SLOPES, bool CAPPED>
-__device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, Rows<C> (&rows)[T], const Scales<LISTED>& x, bool masked, const u32 (&keep)[T], bool far) {
+// BLOCKS: listed blocks of tokens.
+template <int FMT, int C, int T, bool LISTED, bool SLOPES, bool CAPPED, bool BLOCKS = false>
+__device__ __forceinline__ void add_tile(const Attend& a, const Tile<FMT, C>& tile, Rows<C> (&rows)[T], const Scales<LISTED>& x, bool masked, const u32 (&keep)[T], bool far) {
     float4_t s[T][2];
 #pragma unroll
     for (int y = 0; y < T; ++y) s[y][0] = s[y][1] = float4_t{ 0.f, 0.f, 0.f, 0.f };
+    if constexpr (FMT == PAG_KV_FP4) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int n = 0; n < 2 * C; ++n) {
+                float scale = power(tile.ke[b][n / Tile<FMT, C>::WORDS]);
+                if constexpr (!LISTED) scale *= x.fine[b][0];
+                const half8_t k = widen8_fp4(tile.k[b][n], scale);
+#pragma unroll
+                for (int y = 0; y < T; ++y) s[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, rows[y].q[n], s[y][b], 0, 0, 0);
+            }
+        }
+    } else
 #pragma unroll
     for (int h = 0; h < C; ++h) {
 #pragma unroll
@@ -150,7 +224,7 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
         Rows<C>& r = rows[y];
         // t = score * log2 e + e of the values - offset.  Listed keys may all be far away, slope * distance 10^5 and more, of which the distances from each
         // other are a small part: with slopes of lists the difference from the offset comes out of one rounding, before the score is added.
-        constexpr bool APART = LISTED && SLOPES;
+        constexpr bool APART = (LISTED || BLOCKS) && SLOPES;
         float t[8];
         const auto exponents = [&](float base) {
             if constexpr (CAPPED) {
@@ -180,8 +254,8 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
             if constexpr (APART) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int distance = r.position - x.at[j];          // in two parts that a float holds
-                    t[j] += __builtin_fmaf(-r.slope, (float)(distance & 4095), __builtin_fmaf(-r.slope, (float)(distance & ~4095), -base)) + x.ev[j];
+                    const int distance = r.position - (LISTED ? x.at[LISTED ? j : 0] : x.at[j >> 2] + (j & 3));          // in two parts that a float holds
+                    t[j] += __builtin_fmaf(-r.slope, (float)(distance & 4095), __builtin_fmaf(-r.slope, (float)(distance & ~4095), -base)) + x.ev[LISTED ? j : j >> 2];
                 }
             } else if (!LISTED && a.slopes) {
 #pragma unroll
@@ -252,6 +326,30 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<C>& tile, R
             r.sum = __builtin_fmaf(part, x.down[n], r.sum);
         }
     }
+    if constexpr (FMT == PAG_KV_FP4) {
+        float scale[8];
+#pragma unroll
+        for (int w = 0; w < C; ++w) {
+            if (w < Tile<FMT, C>::PARTS) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    scale[j] = power_of_byte(tile.ve[j >> 2][w], j & 3);
+                    if constexpr (!LISTED) scale[j] *= x.fine[j >> 2][1];
+                }
+            }
+            u32 words[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) words[j] = tile.v[j][w / 2];
+            half8_t v[4];
+            if (w % 2) columns_fp4<1>(words, scale, v);
+            else columns_fp4<0>(words, scale, v);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                for (int y = 0; y < T; ++y) rows[y].acc[4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[c], p[y], rows[y].acc[4 * w + c], 0, 0, 0);
+            }
+        }
+    } else
 #pragma unroll
     for (int w = 0; w < C; ++w) {
         u32 words[8];
@@ -377,8 +475,12 @@ struct Piece {
     Where w;
     Span s;
     u32 b, units, u0, u1;
-    int p0, p1, start, stop;
+    int p0, p1, start, stop;   // positions of the first and last row; keys
     int last;                  // the workgroup that ends the tile
+    // listed blocks: keys are numbered through them, and through the window behind them, from its block of 16 on
+    const int32_t* ids;
+    u32 listed;                // keys of the list
+    int near;                  // the window's first block
 };
 
 // rows, first and last key of the piece with units u0 to u1 - 1, of `unit` keys each, of row tile `tile`
@@ -397,8 +499,8 @@ __device__ __forceinline__ void place_piece(const Attend& a, Piece& p, const Spa
 }
 
 // The pieces that next(p) gives, one after the other.  A wave has T tiles of rows: keys are widened once for all of them.  WHOLE: the pieces
-// are whole row tiles.
-template <int FMT, int C, int T, int NW, bool WHOLE, bool CAPPED, typename Next>
+// are whole row tiles.  BLOCKS: the keys of listed blocks and of a window, one token's; SLOPES is for them.
+template <int FMT, int C, int T, int NW, bool WHOLE, bool CAPPED, bool BLOCKS, bool SLOPES, typename Next>
 __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& sh, Next&& next) {
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     Piece p;
@@ -411,24 +513,61 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
     uint16_t exponents = 0;
     u64 there = 0;
     bool far = false;
+    int first = 0, first_next = 0;            // BLOCKS: position of the first token of lane's block
     const auto page_of = [&](int at_key) -> u32 {
+        if constexpr (BLOCKS) {
+            first_next = -1;
+            if (at_key < p.stop) {
+                if ((u32)at_key < p.listed) {
+                    const int id = p.ids[(u32)at_key / a.block];
+                    // a block of tokens that lie in the window or behind it is none
+                    if (id >= 0 && (int64_t)id * a.block <= (int64_t)p.p0 - a.window) first_next = id * (int)a.block + (int)((u32)at_key % a.block);
+                    if (first_next > p.p0 - (int)a.window) first_next = -1;
+                } else {
+                    first_next = p.near + (at_key - (int)p.listed);
+                }
+            }
+            return first_next >= 0 ? (u32)a.s.table[p.b * a.s.table_stride + (u32)first_next / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
+        }
         return at_key < p.stop ? (u32)a.s.table[p.b * a.s.table_stride + (u32)at_key / BLOCK / a.c.page_blocks] : 0xFFFFFFFFu;
     };
     const auto ask = [&]() {                  // what does not depend on each other is asked for together: pages and rows,
         from = p.start + (int)(wave * TILE);
         page = page_of(from + mine_at);
         far = false;
-        if (T == 1) fetch_rows<C>(a, p.w, raw);
+        if (T == 1) fetch_rows<FMT, C>(a, p.w, raw);
     };
     const auto look_up = [&]() {              // then exponents and the first tile
         const bool ok = page < a.c.num_pages;
-        block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)(from + mine_at) / BLOCK % a.c.page_blocks * BLOCK) : 0;
-        exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
+        if (BLOCKS) first = first_next;
+        const int at_key = BLOCKS ? first : from + mine_at;
+        block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)at_key / BLOCK % a.c.page_blocks * BLOCK) : 0;
+        if constexpr (FMT == PAG_KV_FP4) {
+            const int tokens = ok ? (BLOCKS ? p.p0 + 1 : p.stop) - at_key : 0;
+            const int k = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 0), tokens), v = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 1), tokens);
+            exponents = (uint16_t)((k & 255) | v << 8);
+        } else {
+            exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
+        }
         there = __ballot(ok);
         page = page_of(from + 32 * (int)(NW * TILE) + mine_at);
     };
     const u32 k_at = col * (128 * C) + g * 16, v_at = 4 * g * (128 * C) + 64 * C + col * (4 * C);
-    const auto load = [&](Tile<C>& tile, int i) {
+    const auto load = [&](Tile<FMT, C>& tile, int i) {
+        if constexpr (FMT == PAG_KV_FP4) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const u32 row = (u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s);
+                const uint8_t* rows_at = a.c.data + (u64)row * (64 * C);
+                load_codes<C>(tile, s, rows_at + col * (64 * C), [&](int j) { return rows_at + (4 * g + j) * (64 * C); }, col, g);
+                const int8_t *ke = parts_of<C>(a.c, row / BLOCK, 0), *ve = parts_of<C>(a.c, row / BLOCK, 1);
+#pragma unroll
+                for (int h = 0; h < Tile<FMT, C>::PIECES; ++h) tile.ke[s][h] = ke[key_part<C>(h, g) * BLOCK + col];
+#pragma unroll
+                for (int w = 0; w < Tile<FMT, C>::PARTS; ++w) tile.ve[s][w] = *(const u32*)(ve + value_part<C>(w, col) * BLOCK + 4 * g);
+            }
+            return;
+        } else
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const uint8_t* rows_at = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s) * (128 * C);
@@ -438,7 +577,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             for (int j = 0; j < 4; ++j) load_words<C>(rows_at + v_at + j * (128 * C), tile.v[4 * s + j]);
         }
     };
-    const auto add = [&](Tile<C>& tile, int i) {
+    const auto add = [&](Tile<FMT, C>& tile, int i) {
         const int pos = from + i * (int)(NW * TILE);
         Scales<false> x;
 #pragma unroll
@@ -448,10 +587,50 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             x.ev[s] = (float)ev;
             far = far || ev > FAR_EXPONENT;
             x.down[s] = power(-ev);
-            x.at[s] = pos + s * (int)BLOCK + 4 * (int)g;
+            if constexpr (FMT == PAG_KV_FP4) {
+                x.fine[s][0] = power(-(int)(int8_t)e);
+                x.fine[s][1] = x.down[s];
+            }
+            x.at[s] = (BLOCKS ? __builtin_amdgcn_readlane(first, 2 * i + s) : pos + s * (int)BLOCK) + 4 * (int)g;
         }
         if (far) x.down[0] = x.down[1] = 0.f;
         const u32 two = (u32)(there >> (2 * i)) & 3u;
+        // behind the last token there may be anything
+        const auto no_value = [&](int j) {
+            if constexpr (FMT == PAG_KV_FP4) {
+#pragma unroll
+                for (int w = 0; w < Tile<FMT, C>::PARTS; ++w)
+                    tile.ve[j >> 2][w] = (tile.ve[j >> 2][w] & ~(255u << (8 * (j & 3)))) | 0x81u << (8 * (j & 3));          // 2^-127 counts as 0
+            } else {
+#pragma unroll
+                for (int y = 0; y < C; ++y) tile.v[j][y] = 0;
+            }
+        };
+        if constexpr (BLOCKS) {
+            // listed tokens end where the window begins, the window's end with the token itself
+            int oldest[2], newest[2];
+            bool whole = two == 3u;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const bool listed = (u32)(pos + s * (int)BLOCK) < p.listed;
+                const int block = x.at[s] - 4 * (int)g;
+                oldest[s] = listed ? 0 : p.p0 - (int)a.window + 1;
+                newest[s] = listed ? p.p0 - (int)a.window : p.p0;
+                whole = whole && block >= oldest[s] && block + (int)BLOCK - 1 <= newest[s];
+            }
+            u32 keep[1] = { 0xFF };
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int k = x.at[j >> 2] + (j & 3);
+                    const bool exists = (two >> (j >> 2) & 1u) && k <= p.p0;
+                    if (!exists || k < oldest[j >> 2] || k > newest[j >> 2]) keep[0] &= ~(1u << j);
+                    if (!exists) no_value(j);
+                }
+            }
+            add_tile<FMT, C, 1, false, SLOPES, CAPPED, true>(a, tile, rows, x, !whole, keep, far);
+            return;
+        } else {
         const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos < oldest_of(a, p.p1);
         u32 keep[T];
 #pragma unroll
@@ -465,19 +644,17 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 for (int y = 0; y < T; ++y) {
                     if (!exists || k > rows[y].position || k < oldest_of(a, rows[y].position)) keep[y] &= ~(1u << j);
                 }
-                if (!exists) {
-#pragma unroll
-                    for (int y = 0; y < C; ++y) tile.v[j][y] = 0;      // the memory behind the last token may hold anything
-                }
+                if (!exists) no_value(j);
             }
         }
         add_tile<FMT, C, T, false, false, CAPPED>(a, tile, rows, x, masked, keep, far);
+        }
     };
     const auto start = [&]() {
 #pragma unroll
         for (int y = 0; y < T; ++y) {
-            if (T > 1) fetch_rows<C>(a, tile_of(p.w, y), raw);
-            start_rows<C>(a, tile_of(p.w, y), p.s.first, raw, rows[y]);
+            if (T > 1) fetch_rows<FMT, C>(a, tile_of(p.w, y), raw);
+            start_rows<C>(a, tile_of(p.w, y), BLOCKS ? p.p0 : p.s.first, raw, rows[y]);
         }
     };
     constexpr u32 SLOT = ROWS * (64 * C + 2);
@@ -492,7 +669,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 look_up();
                 const int count = min(32, (p.stop - from + (int)(NW * TILE) - 1) / (int)(NW * TILE));
                 for (int i = 0; i < count; ++i) {
-                    Tile<C> tile;
+                    Tile<FMT, C> tile;
                     load(tile, i);
                     add(tile, i);
                 }
@@ -512,7 +689,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
         }
         return;
     }
-    Tile<C> even, odd;
+    Tile<FMT, C> even, odd;
     bool more = next(p);
     if (more) {
         ask();
@@ -631,7 +808,7 @@ __global__ void __launch_bounds__(256, groups_per_cu(64 * C, T)) k_attend(Attend
         }
         return false;
     };
-    attend_pieces<FMT, C, T, SPLIT_WAVES, false, CAPPED>(a, sh, next_piece);
+    attend_pieces<FMT, C, T, SPLIT_WAVES, false, CAPPED, false, false>(a, sh, next_piece);
 }
 
 // A workgroup for each request and key/value head, which reads all of its keys: nothing to share out and nothing to join.
@@ -648,7 +825,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_whole(Attend
     }
     const u32 tiles = (s.tokens * a.group + T * ROWS - 1) / (T * ROWS);
     u32 tile = 0;
-    attend_pieces<FMT, C, T, NW, true, CAPPED>(a, sh, [&](Piece& p) -> bool {
+    attend_pieces<FMT, C, T, NW, true, CAPPED, false, false>(a, sh, [&](Piece& p) -> bool {
         if (tile == tiles) return false;
         p.b = b;
         p.units = p.u1 = 1;
@@ -662,10 +839,19 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_whole(Attend
 // ---- attention over listed tokens -----------------------------------------------------------------------------------
 
 // what a wave knows of 64 keys that it will add or is adding
+template <int FMT, int C>
 struct Entries {
     u32 row[64];
     float ek[64], ev[64], down[64];
     int at[64];
+};
+
+template <int C>
+struct Entries<PAG_KV_FP4, C> {
+    u32 row[64];
+    float ek[64], ev[64], down[64];
+    int at[64];
+    int8_t parts[2][2 * C][64];          // exponents of keys and values, less the largest of their row; -127: no such key
 };
 
 // a token's list, or a part of it
@@ -685,7 +871,7 @@ __device__ __forceinline__ void place_list(const Attend& a, ListPiece& p, u64 li
 
 // The pieces that next(p) gives; a list has `units` units of 32 NW entries.
 template <int FMT, int C, int NW, bool WHOLE, bool SLOPES, bool CAPPED, typename Next>
-__device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& sh, Entries (&sh_entries)[NW][2], u32 units, Next&& next) {
+__device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& sh, Entries<FMT, C> (&sh_entries)[NW][2], u32 units, Next&& next) {
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     const u32 entries = a.k + a.window;
     ListPiece w = {};
@@ -713,17 +899,34 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
         id = id_of(from + mine);
         request = a.s.request[w.t0];
         position = a.s.positions[w.t0];
-        fetch_rows<C>(a, w, raw);
+        fetch_rows<FMT, C>(a, w, raw);
     };
     const auto check = [&]() {
         if (request < 0 || (u32)request >= a.s.requests || (u64)(u32)max(position, 0) >= (u64)a.s.max_pages * a.c.page_tokens) position = -1;
     };
     // the 64 entries whose pages have been asked for, into LDS; the pages of the next and the ids after those are asked for
     const auto look_up = [&](u32 buffer) {
-        Entries& x = sh_entries[wave][buffer];
+        Entries<FMT, C>& x = sh_entries[wave][buffer];
         const bool ok = page < a.c.num_pages;
         const u32 row = ok ? row_of(a.c, page, w.kv_head, (u32)key / BLOCK % a.c.page_blocks * BLOCK + ((u32)key & (BLOCK - 1))) : 0;
-        const u32 e = ok ? *(const uint16_t*)(a.c.exponents + (u64)(row / BLOCK) * 2) : 0;
+        u32 e = 0;
+        if constexpr (FMT == PAG_KV_FP4) {
+#pragma unroll
+            for (int kind = 0; kind < 2; ++kind) {
+                const int8_t* parts = parts_of<C>(a.c, row / BLOCK, kind) + row % BLOCK;
+                int y[2 * C], most = LOWEST_EXPONENT;
+#pragma unroll
+                for (int b = 0; b < 2 * C; ++b) {
+                    y[b] = parts[b * BLOCK];
+                    most = max(most, y[b]);
+                }
+#pragma unroll
+                for (int b = 0; b < 2 * C; ++b) x.parts[kind][b][lane] = (int8_t)(ok ? max(y[b] - most, -127) : -127);
+                if (ok) e |= (u32)(most & 255) << (8 * kind);
+            }
+        } else {
+            e = ok ? *(const uint16_t*)(a.c.exponents + (u64)(row / BLOCK) * 2) : 0;
+        }
         there = __ballot(ok);
         far = far || __ballot((int)(int8_t)(e >> 8) > FAR_EXPONENT);
         x.row[lane] = row;
@@ -741,8 +944,21 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
-    const auto load = [&](Tile<C>& tile, u32 buffer, int i) {
-        const Entries& x = sh_entries[wave][buffer];
+    const auto load = [&](Tile<FMT, C>& tile, u32 buffer, int i) {
+        const Entries<FMT, C>& x = sh_entries[wave][buffer];
+        if constexpr (FMT == PAG_KV_FP4) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint4 r = *(const uint4*)&x.row[32 * i + 16 * s + 4 * g];
+                const u32 rows_at[4] = { r.x, r.y, r.z, r.w };
+                load_codes<C>(tile, s, a.c.data + (u64)x.row[32 * i + 16 * s + col] * (64 * C), [&](int j) { return a.c.data + (u64)rows_at[j] * (64 * C); }, col, g);
+#pragma unroll
+                for (int h = 0; h < Tile<FMT, C>::PIECES; ++h) tile.ke[s][h] = x.parts[0][key_part<C>(h, g)][32 * i + 16 * s + col];
+#pragma unroll
+                for (int w = 0; w < Tile<FMT, C>::PARTS; ++w) tile.ve[s][w] = *(const u32*)&x.parts[1][value_part<C>(w, col)][32 * i + 16 * s + 4 * g];
+            }
+            return;
+        } else
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const uint8_t* k = a.c.data + (u64)x.row[32 * i + 16 * s + col] * (128 * C) + g * 16;
@@ -754,8 +970,8 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
             for (int j = 0; j < 4; ++j) load_words<C>(a.c.data + (u64)v[j] * (128 * C) + 64 * C + col * (4 * C), tile.v[4 * s + j]);
         }
     };
-    const auto add = [&](Tile<C>& tile, u32 buffer, int i, u32 found, bool far_now) {
-        const Entries& x = sh_entries[wave][buffer];
+    const auto add = [&](Tile<FMT, C>& tile, u32 buffer, int i, u32 found, bool far_now) {
+        const Entries<FMT, C>& x = sh_entries[wave][buffer];
         Scales<true> scales;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -769,18 +985,20 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
         }
         const bool masked = found != 0xFFFFFFFFu;
         const u32 keep[1] = { (found >> (4 * g) & 15u) | (found >> (16 + 4 * g) & 15u) << 4 };
-        if (masked) {
+        if constexpr (FMT != PAG_KV_FP4) {           // which have an exponent for keys that are none
+            if (masked) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (!(keep[0] >> j & 1u)) {
+                for (int j = 0; j < 8; ++j) {
+                    if (!(keep[0] >> j & 1u)) {
 #pragma unroll
-                    for (int y = 0; y < C; ++y) tile.v[j][y] = 0;
+                        for (int y = 0; y < C; ++y) tile.v[j][y] = 0;
+                    }
                 }
             }
         }
         add_tile<FMT, C, 1, true, SLOPES, CAPPED>(a, tile, rows, scales, masked, keep, far_now);
     };
-    Tile<C> even, odd;
+    Tile<FMT, C> even, odd;
     u32 buffer = 0;
     const auto begin_piece = [&]() {
         check();
@@ -832,7 +1050,7 @@ constexpr u32 list_groups_per_cu(u32 width, bool slopes) { return slopes ? std::
 template <int FMT, int C, bool SLOPES, bool CAPPED>
 __global__ void __launch_bounds__(256, list_groups_per_cu(64 * C, SLOPES)) k_attend_selected(Attend a, u32 units, u32 tiles) {
     __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
-    __shared__ __align__(16) Entries sh_entries[SPLIT_WAVES][2];
+    __shared__ __align__(16) Entries<FMT, C> sh_entries[SPLIT_WAVES][2];
     const u32 cost = units + PIECE;
     const u64 total = (u64)a.s.tokens * a.id_heads * tiles * cost;
     const u32 parts = (u32)min((u64)gridDim.x, total);
@@ -858,7 +1076,7 @@ __global__ void __launch_bounds__(256, list_groups_per_cu(64 * C, SLOPES)) k_att
 template <int FMT, int C, int NW, bool SLOPES, bool CAPPED>
 __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_selected_whole(Attend a, u32 tiles) {
     __shared__ __align__(16) Exchange<C, NW> sh;
-    __shared__ __align__(16) Entries sh_entries[NW][2];
+    __shared__ __align__(16) Entries<FMT, C> sh_entries[NW][2];
     const u32 units = max((a.k + a.window + NW * TILE - 1) / (NW * TILE), 1u);
     bool first = true;
     attend_lists<FMT, C, NW, true, SLOPES, CAPPED>(a, sh, sh_entries, units, [&](ListPiece& p) -> bool {

@@ -1,0 +1,4 @@
+// Instantiations of the attention kernels for few query rows: 4-bit codes, rows of up to 192 numbers.
+#include "pag_kv_narrow.h"
+
+template void pagkv::launch_narrow<PAG_KV_FP4, 3>(hipStream_t, const pagkv::Attend&, int, bool);

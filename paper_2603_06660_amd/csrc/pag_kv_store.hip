@@ -153,12 +153,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_release(pag_kv_tables t, const
     if (threadIdx.x == 0) *t.free_count = (int32_t)sh_end;
 }
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-    return x;
-}
-
 // ---- rotation ---------------------------------------------------------------------------------------------------------
 
 // cos and sin of an angle below 2^31 or so, to 2^-50: the nearest multiple of pi / 2 is taken off in two parts, which leaves r with |r| <= pi / 4

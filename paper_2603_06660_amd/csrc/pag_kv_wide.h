@@ -10,6 +10,8 @@
 // 8192 x 8192 x 8192 reaches 1,160.  The matrix units are busy for 40 % of it and the vector units for 50 %: in a wave scores, weights and values' products
 // follow one another, and all waves meet every 64 keys, so that the two waves of a SIMD overlap in part only.  (No third wave: 250 of 256 registers are taken;
 // the four-wave kernel for 72 to 128 numbers spills 8 to 17.)
+#pragma once
+
 #include <algorithm>
 
 #include "pag_kv_attend.h"
@@ -17,7 +19,6 @@
 namespace pagkv {
 namespace {
 
-constexpr u32 WROWS = 32;                   // query rows of a wave
 constexpr u32 STEP = 64;                    // keys of a step, one block of 16 a wave to fetch
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
@@ -57,11 +58,6 @@ __device__ __forceinline__ Tiles tiles_of(const Attend& a, u32 b) {
     return t;
 }
 
-struct Head {                               // of a piece that another workgroup goes on with
-    u32 t0, rows, row0, head0;
-    int last;                               // workgroup that ends it; -1: none
-};
-
 // halves of a row of keys, in pieces of 8; of a row of values (64 tokens of a number), likewise.  Rows that a wave reads together lie in
 // different banks.
 template <int C>
@@ -75,12 +71,26 @@ __device__ __forceinline__ u32 value_at(u32 d, u32 piece) { return d * STEP + (p
 // What a thread fetches of the next 64 keys.  NW waves share them, NW / 4 of them a block of 16: 64 C / NW bytes of a key, and words of eight
 // tokens' values.  With four waves a word's four numbers are one lane's, with eight two lanes have the same word and two numbers each.
 template <int C, int NW>
-struct Fetch {
+struct Share {
     static constexpr int PIECES = 8 * C / NW;            // of 8 numbers of a key
     static constexpr int N = (32 * C + 63) / 64;         // words of values a lane has at most
     static constexpr int COLUMNS = 16 / NW;              // numbers of a word
-    uint2 k[PIECES];
-    u32 v[N][8];
+};
+
+template <int FMT, int C, int NW>
+struct Fetch : Share<C, NW> {
+    uint2 k[Share<C, NW>::PIECES];
+    u32 v[Share<C, NW>::N][8];
+};
+
+// 4-bit codes: half as wide, with the exponents of their parts; a part is four pieces, and two pieces that begin at an even number lie in one
+template <int C, int NW>
+struct Fetch<PAG_KV_FP4, C, NW> : Share<C, NW> {
+    static constexpr int PARTS = Share<C, NW>::PIECES % 4 ? (Share<C, NW>::PIECES + 1) / 2 : Share<C, NW>::PIECES / 4, EACH = (Share<C, NW>::PIECES + PARTS - 1) / PARTS;
+    u32 k[Share<C, NW>::PIECES];
+    int ke[PARTS];
+    u32 v[Share<C, NW>::N][8];
+    u32 ve[Share<C, NW>::N][2];                          // of the word's first four tokens and its last four
 };
 
 // bytes first and first + 1 of eight words: columns of eight tokens
@@ -107,6 +117,19 @@ __device__ __forceinline__ void two_columns(const u32* w, u32 first, half8_t* ou
 #pragma unroll
         for (int c = 0; c < 2; ++c) out[c] = widen8<FMT>(t[0][c], t[1][c]);
     }
+}
+
+// two 4-bit codes, byte 0 of eight words, each word with a scale of its own: columns of eight tokens
+__device__ __forceinline__ void two_columns_fp4(const u32 (&w)[8], const float (&scale)[8], half8_t* out) {
+    u32 lo[4], hi[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const u32 x = __builtin_bit_cast(u32, widen2_fp4<0>(w[2 * p], scale[2 * p])), y = __builtin_bit_cast(u32, widen2_fp4<0>(w[2 * p + 1], scale[2 * p + 1]));
+        lo[p] = perm(y, x, 0x05040100);
+        hi[p] = perm(y, x, 0x07060302);
+    }
+    out[0] = __builtin_bit_cast(half8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+    out[1] = __builtin_bit_cast(half8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
 }
 
 // What far_sum looks at: a piece's keys and this lane's row.
@@ -150,24 +173,38 @@ __device__ __attribute__((noinline)) float far_sum(FarRows r) {
         const u32 page = first < r.stop ? (u32)r.table[(u32)first / BLOCK / r.page_blocks] : 0xFFFFFFFFu;
         const bool ok = page < r.num_pages;
         const u32 row = ok ? (page * r.kv_heads + r.kv_head) * r.page_tokens + (u32)first / BLOCK % r.page_blocks * BLOCK : 0;
-        const int e = ok ? r.exponents[(u64)(row / BLOCK) * 2] : 0;
+        // of 4-bit codes e is the key's own: the largest of its parts'
+        int e = 0;
+        const int8_t* parts = r.exponents + (u64)(row / BLOCK) * (4 * C * BLOCK) + (col & (BLOCK - 1));
+        if constexpr (FMT == PAG_KV_FP4) {
+            e = LOWEST_EXPONENT;
+            for (int b = 0; b < 2 * C; ++b) e = max(e, (int)parts[b * BLOCK]);
+        } else {
+            e = ok ? r.exponents[(u64)(row / BLOCK) * 2] : 0;
+        }
         const u64 there = __ballot(ok);
-        const uint8_t* k = r.data + (u64)(row + (col & (BLOCK - 1))) * (2 * W) + hi * 8;
+        const uint8_t* k = r.data + (u64)(row + (col & (BLOCK - 1))) * (2 * row_bytes<FMT, C>()) + hi * (FMT == PAG_KV_FP4 ? 4 : 8);
         float16_t S;
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[i] = 0.f;
         for (int n = 0; n < 4 * C; ++n) {
-            const uint2 codes = *(const uint2*)(k + 16 * n);
-            half8_t q;
+            half8_t q, key;
+            if constexpr (FMT == PAG_KV_FP4) {
+                key = widen8_fp4(*(const u32*)(k + 8 * n), power((int)parts[n / 2 * BLOCK]) * power(-e));
+            } else {
+                const uint2 codes = *(const uint2*)(k + 16 * n);
+                key = widen8<FMT>(codes.x, codes.y);
+            }
             numbers(n, x);
 #pragma unroll
             for (int j = 0; j < 8; ++j) q[j] = (_Float16)(x[j] * down);
-            S = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8<FMT>(codes.x, codes.y), q, S, 0, 0, 0);
+            S = __builtin_amdgcn_mfma_f32_32x32x16_f16(key, q, S, 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int key = from + 8 * (i >> 2) + 4 * (int)hi + (i & 3);
-            float t = S[i] * (factor * power(__builtin_amdgcn_readlane(e, (i >> 3) * (int)BLOCK)));
+            const int e_of = FMT == PAG_KV_FP4 ? __shfl(e, 8 * (i >> 2) + 4 * (int)hi + (i & 3)) : __builtin_amdgcn_readlane(e, (i >> 3) * (int)BLOCK);
+            float t = S[i] * (factor * power(e_of));
             if (r.cap > 0.f) t = capped(t, cap, 1.f / cap);
             t -= r.slope * (float)(r.position - key);
             if ((there >> ((i >> 3) * BLOCK) & 1u) && key <= r.position && key >= r.oldest) sum += __builtin_amdgcn_exp2f(t - r.M);
@@ -337,15 +374,20 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                 if (page < a.c.num_pages) {
                     ok = true;
                     block_row = row_of(a.c, page, kv_head, blk % a.c.page_blocks * BLOCK);
-                    const int8_t* e = a.c.exponents + (u64)(block_row / BLOCK) * 2;
-                    ek_mine = e[0];
-                    ev_mine = e[1];
+                    if constexpr (FMT == PAG_KV_FP4) {
+                        ek_mine = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 0), stop - at_key);
+                        ev_mine = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 1), stop - at_key);
+                    } else {
+                        const int8_t* e = a.c.exponents + (u64)(block_row / BLOCK) * 2;
+                        ek_mine = e[0];
+                        ev_mine = e[1];
+                    }
                 }
             }
             there = __ballot(ok);
         };
-        Fetch<C, NW> f;
-        const u32 key = part * (64 / NW) + lane / NW, key_piece0 = lane % NW * Fetch<C, NW>::PIECES;
+        Fetch<FMT, C, NW> f;
+        const u32 key = part * (64 / NW) + lane / NW, key_piece0 = lane % NW * Share<C, NW>::PIECES;
         const auto word_of = [&](int i, u32& word, u32& half, u32& first) -> bool {
             const u32 item = lane + 64 * i;
             if (NW == 4) {
@@ -356,41 +398,98 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
             return word < 16 * C;
         };
         const auto fetch = [&](u32 n) {
+            if constexpr (FMT == PAG_KV_FP4) {
+                typedef Fetch<FMT, C, NW> F;
+                const u32 row = (u32)__builtin_amdgcn_readlane((int)block_row, (int)(n & 63));
+                const uint8_t *rows = a.c.data + (u64)row * W, *k = rows + key * W + key_piece0 * 4;
+                const int8_t *ke = parts_of<C>(a.c, row / BLOCK, 0) + key, *ve = parts_of<C>(a.c, row / BLOCK, 1);
+                if constexpr (F::PIECES % 4 == 0) {
+#pragma unroll
+                    for (int i = 0; i < F::PIECES; i += 4) {
+                        const uint4 x = *(const uint4*)(k + 4 * i);
+                        f.k[i] = x.x; f.k[i + 1] = x.y; f.k[i + 2] = x.z; f.k[i + 3] = x.w;
+                    }
+                } else if constexpr (F::PIECES % 2 == 0) {
+#pragma unroll
+                    for (int i = 0; i < F::PIECES; i += 2) {
+                        const uint2 x = *(const uint2*)(k + 4 * i);
+                        f.k[i] = x.x; f.k[i + 1] = x.y;
+                    }
+                } else {
+                    f.k[0] = *(const u32*)k;
+                }
+#pragma unroll
+                for (int i = 0; i < F::PARTS; ++i) f.ke[i] = ke[(key_piece0 + F::EACH * i) / 4 * BLOCK];
+#pragma unroll
+                for (int i = 0; i < F::N; ++i) {
+                    u32 word, half, first;
+                    if (word_of(i, word, half, first)) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint8_t* p = rows + (8 * (j >> 2) + 4 * half + (j & 3)) * W + W / 2 + word * 2;
+                            f.v[i][j] = NW == 4 ? *(const uint16_t*)p : p[first / 2];
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) f.ve[i][j] = *(const u32*)(ve + word / 8 * BLOCK + 8 * j + 4 * half);
+                    }
+                }
+                return;
+            } else {
             const uint8_t* rows = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, (int)(n & 63)) * (2 * W);
             const uint8_t* k = rows + key * (2 * W) + key_piece0 * 8;
 #pragma unroll
-            for (int i = 0; i < Fetch<C, NW>::PIECES; ++i) f.k[i] = *(const uint2*)(k + 8 * i);
+            for (int i = 0; i < Share<C, NW>::PIECES; ++i) f.k[i] = *(const uint2*)(k + 8 * i);
 #pragma unroll
-            for (int i = 0; i < Fetch<C, NW>::N; ++i) {
+            for (int i = 0; i < Share<C, NW>::N; ++i) {
                 u32 word, half, first;
                 if (word_of(i, word, half, first)) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) f.v[i][j] = *(const u32*)(rows + (8 * (j >> 2) + 4 * half + (j & 3)) * (2 * W) + W + word * 4);
                 }
             }
+            }
         };
         const auto stage = [&](u32 n, int from, u32 buffer) {
             _Float16* keys = lds + buffer * (KEYS + VALUES);
             _Float16* values = keys + KEYS;
+            const float fine_k = FMT == PAG_KV_FP4 ? power(-__builtin_amdgcn_readlane(ek_mine, (int)(n & 63))) : 0.f;
+            const float fine_v = FMT == PAG_KV_FP4 ? power(-__builtin_amdgcn_readlane(ev_mine, (int)(n & 63))) : 0.f;
 #pragma unroll
-            for (int i = 0; i < Fetch<C, NW>::PIECES; ++i)
-                *(half8_t*)(keys + key_at<C>(block * BLOCK + key, key_piece0 + i)) = widen8<FMT>(f.k[i].x, f.k[i].y);
+            for (int i = 0; i < Share<C, NW>::PIECES; ++i) {
+                half8_t wide;
+                if constexpr (FMT == PAG_KV_FP4) wide = widen8_fp4(f.k[i], power(f.ke[i / Fetch<FMT, C, NW>::EACH]) * fine_k);
+                else wide = widen8<FMT>(f.k[i].x, f.k[i].y);
+                *(half8_t*)(keys + key_at<C>(block * BLOCK + key, key_piece0 + i)) = wide;
+            }
             const bool ok = there >> (n & 63) & 1;
             const int base = from + (int)(block * BLOCK);
 #pragma unroll
-            for (int i = 0; i < Fetch<C, NW>::N; ++i) {
+            for (int i = 0; i < Share<C, NW>::N; ++i) {
                 u32 word, half, first;
                 if (word_of(i, word, half, first)) {
-                    if (!ok || base + (int)BLOCK > stop) {      // the memory behind the last token may hold anything
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (!ok || base + (int)(8 * (j >> 2) + 4 * half + (j & 3)) >= stop) f.v[i][j] = 0;
-                    }
                     half8_t v[4];
-                    if constexpr (NW == 4) columns<FMT>(f.v[i], v);
-                    else two_columns<FMT>(f.v[i], first, v);
+                    if constexpr (FMT == PAG_KV_FP4) {
+                        float scale[8];
 #pragma unroll
-                    for (int c = 0; c < Fetch<C, NW>::COLUMNS; ++c) *(half8_t*)(values + value_at(word * 4 + first + c, block * 2 + half)) = v[c];
+                        for (int j = 0; j < 8; ++j) scale[j] = power_of_byte(f.ve[i][j >> 2], j & 3) * fine_v;
+                        if (!ok || base + (int)BLOCK > stop) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (!ok || base + (int)(8 * (j >> 2) + 4 * half + (j & 3)) >= stop) scale[j] = 0.f;
+                        }
+                        if constexpr (NW == 4) columns_fp4<0>(f.v[i], scale, v);
+                        else two_columns_fp4(f.v[i], scale, v);
+                    } else {
+                        if (!ok || base + (int)BLOCK > stop) {      // the memory behind the last token may hold anything
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (!ok || base + (int)(8 * (j >> 2) + 4 * half + (j & 3)) >= stop) f.v[i][j] = 0;
+                        }
+                        if constexpr (NW == 4) columns<FMT>(f.v[i], v);
+                        else two_columns<FMT>(f.v[i], first, v);
+                    }
+#pragma unroll
+                    for (int c = 0; c < Share<C, NW>::COLUMNS; ++c) *(half8_t*)(values + value_at(word * 4 + first + c, block * 2 + half)) = v[c];
                 }
             }
             if (lane == 0 && part == 0) {
@@ -671,14 +770,12 @@ __global__ void __launch_bounds__(256) k_join_wide(Attend a, const Head* heads) 
     if (a.lse && lane == 0) a.lse[(u64)t * a.heads + head] = all != 0.f ? LN2 * (top + __builtin_amdgcn_logf(all)) : -INFINITY;
 }
 
-// workgroups of a CU: as many as its registers last for
-constexpr u32 wide_groups_per_cu(u32 width, int waves) { return waves == 4 && width <= 128 ? 2 : 1; }
 constexpr u32 lds_bytes(u32 width) { return 2 * 2 * STEP * width * 2; }
 
 // Eight waves share a step's keys where there are rows for them, and registers: they are widened half as often.  Four and eight waves, in us: 4 chunks of
 // 700 to 2,000 tokens 605, 587; 256 rows over 30,000 keys 70, 65; 32 requests of 256 rows over 3,000 keys 155, 140;
 // where a request has up to 128 rows half of the waves have none (32 requests of 64 rows, 300 to 12,000 keys: 118, 165).
-constexpr int MANY = 8;
+constexpr int MANY = (int)MANY_WAVES;
 
 template <int FMT, int C, int CAP, int NW>
 int run_wide(hipStream_t st, const Attend& a, int num_cu) {
@@ -710,25 +807,11 @@ int run_format(hipStream_t st, const Attend& a, int num_cu) {
     return run<FMT, 4, CAP>(st, a, num_cu);
 }
 
-template <int CAP>
-int run_cap(hipStream_t st, const Attend& a, int num_cu) {
-    return a.c.fmt == PAG_KV_INT8 ? run_format<PAG_KV_INT8, CAP>(st, a, num_cu) : run_format<PAG_KV_FP8, CAP>(st, a, num_cu);
-}
-
 }  // namespace
 
-u64 wide_workspace(u32 width, int num_cu) {
-    // twice the workgroups have half the rows, or the other way round
-    const u64 grid = (u64)num_cu * wide_groups_per_cu(width, 4), rows = std::max(grid * 4 * WROWS, width <= 128 ? (u64)num_cu * MANY * WROWS : 0);
-    return 4 * 2 * rows * (width + 2) + (grid * sizeof(Head) + 15) / 16 * 16;
-}
-
-int launch_attend_wide(hipStream_t st, const Attend& a, int num_cu) {
-    const int rc = a.softcap > NEAR_CAP ? run_cap<2>(st, a, num_cu) : a.softcap > 0.f ? run_cap<1>(st, a, num_cu) : run_cap<0>(st, a, num_cu);
-    if (rc) return rc;
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) { pag_set_error(std::string("pag_kv_attend: ") + hipGetErrorString(e)); return PAG_EHIP; }
-    return PAG_OK;
+template <int FMT>
+int launch_wide(hipStream_t st, const Attend& a, int num_cu) {
+    return a.softcap > NEAR_CAP ? run_format<FMT, 2>(st, a, num_cu) : a.softcap > 0.f ? run_format<FMT, 1>(st, a, num_cu) : run_format<FMT, 0>(st, a, num_cu);
 }
 
 }  // namespace pagkv

@@ -59,6 +59,10 @@ class _Rotation(C.Structure):
                 ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64)]
 
 
+class _Blocks(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("block_tokens", C.c_uint32), ("codes", C.c_void_p), ("exponents", C.c_void_p)]
+
+
 def _gpu(device):
     device = torch.device("cuda" if device is None else device)
     if device.type != "cuda":
@@ -98,6 +102,9 @@ _ARGTYPES = {"pag_kv_extend": [_P, _P, _P, _P], "pag_kv_release": [_P, _P, _P],
              "pag_kv_append": [_P, C.c_uint32, _P, _I, _I, _P, _I, _I, _P, C.c_uint64, _P],
              "pag_kv_append_rotated": [_P, C.c_uint32, _P, _I, _I, _P, _I, _I, _P, C.c_uint64, _P, _P],
              "pag_kv_read": [_P, _P, C.c_uint64, C.c_uint32, _P, _I, _I, _P, _I, _I, _P],
+             "pag_kv_blocks_update": [_P, _P, _P, C.c_uint64, _P],
+             "pag_kv_blocks_select": [_P, _P, _P, _P, C.c_uint32, C.c_uint32, _P, _I, _I, _P],
+             "pag_kv_attend_blocks": [_P, _P, _P, _P, _I, _I, C.c_uint32, C.c_uint32, C.c_uint32, _P],
              "pag_kv_workspace_bytes": [_P, _P, _P, C.c_int, C.c_uint32, C.c_uint32, _P],
              "pag_kv_attend": [_P, _P, _P, _P], "pag_kv_attend_selected": [_P, _P, _P, _P, _I, _I, C.c_uint32, C.c_uint32, _P]}
 _calls = {}
@@ -377,19 +384,23 @@ class KvCache:
         _call("pag_kv_read", self.device, C.addressof(self._c), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens, _DTYPES[dtype], *args)
         return k, v
 
-    def _attention(self, q, step, scale, window, softcap, slopes, out, id_heads=0, k=-1):
-        """Checks a call's tensors -> out, its arguments, and its workspace, which has to live until the call is made."""
+    def _queries(self, q, step, window):
+        """Checks what every call over a step looks at."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise PagError("q must be a tensor [tokens, heads, head_dim]")
-        tokens, heads, dim = shape = q.shape
-        device = self.device
-        if dim != self.head_dim:
-            raise PagError("q has rows of %d numbers, the cache of %d" % (dim, self.head_dim))
-        _rows(q, shape, device, "q", _ROW_DTYPES)
-        if step.table is not None and step.device != device:
-            raise PagError("the step is on %s, the cache on %s" % (step.device, device))
+        if q.shape[2] != self.head_dim:
+            raise PagError("q has rows of %d numbers, the cache of %d" % (q.shape[2], self.head_dim))
+        _rows(q, q.shape, self.device, "q", _ROW_DTYPES)
+        if step.table is not None and step.device != self.device:
+            raise PagError("the step is on %s, the cache on %s" % (step.device, self.device))
         if not 0 <= window < 1 << 31:
             raise PagError("window must be between 0 and 2^31 - 1")
+
+    def _attention(self, q, step, scale, window, softcap, slopes, out, id_heads=0, k=-1, block=0):
+        """Checks a call's tensors -> out, its arguments, and its workspace, which has to live until the call is made."""
+        self._queries(q, step, window)
+        tokens, heads, dim = shape = q.shape
+        device = self.device
         if out is None:
             o, lse = out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty((tokens, heads), dtype=torch.float32, device=device)
         else:
@@ -401,21 +412,29 @@ class KvCache:
         a = _Attention(C.sizeof(_Attention), _DTYPES[q.dtype], heads, window, dim ** -0.5 if scale is None else scale, softcap,
                        None if slopes is None else _array(slopes, torch.float32, (heads,), device, "slopes"),
                        q.data_ptr(), q.stride(0), q.stride(1), o.data_ptr(), o.stride(0), o.stride(1), None if lse is None else lse.data_ptr())
-        key = (tokens, heads, window, s.requests, s.max_new, s.max_pages, id_heads, k)
+        return out, a, self._room(a, s, (tokens, heads, window, s.requests, s.max_new, s.max_pages, id_heads, k, block), id_heads, k, block)
+
+    def _room(self, a, s, key, id_heads, k, block=0, select=False):
+        """The workspace of a call, None if it needs none."""
         size = self._rooms.get(key)
         if size is None:
             n = C.c_uint64()
-            with torch.cuda.device(device):
-                _check(load_library().pag_kv_workspace_bytes(C.byref(self._c), C.byref(s), C.byref(a), C.c_int(k >= 0), C.c_uint32(id_heads),
-                                                             C.c_uint32(max(k, 0)), C.byref(n)), "pag_kv_workspace_bytes")
+            with torch.cuda.device(self.device):
+                if block:
+                    _check(load_library().pag_kv_blocks_workspace_bytes(C.byref(self._c), C.byref(s), C.byref(a), C.c_uint32(id_heads), C.c_uint32(k), C.c_uint32(block),
+                                                                        C.byref(n) if select else None, None if select else C.byref(n)),
+                           "pag_kv_blocks_workspace_bytes")
+                else:
+                    _check(load_library().pag_kv_workspace_bytes(C.byref(self._c), C.byref(s), C.byref(a), C.c_int(k >= 0), C.c_uint32(id_heads),
+                                                                 C.c_uint32(max(k, 0)), C.byref(n)), "pag_kv_workspace_bytes")
             if len(self._rooms) > 4096:
                 self._rooms.clear()
             size = self._rooms[key] = n.value
-        room = None
-        if size:
-            room = torch.empty(size, dtype=torch.uint8, device=device)
-            a.workspace, a.workspace_bytes = room.data_ptr(), size
-        return out, a, room
+        if not size:
+            return None
+        room = torch.empty(size, dtype=torch.uint8, device=self.device)
+        a.workspace, a.workspace_bytes = room.data_ptr(), size
+        return room
 
     def attend(self, q, step, scale=None, window=0, softcap=0.0, slopes=None, out=None):
         """-> (out like q, lse float32 [tokens, heads]): every token of q [tokens, heads, head_dim] (float16 or bfloat16) attends to its request's
@@ -439,4 +458,84 @@ class KvCache:
         out, a, room = self._attention(q, step, scale, window, softcap, slopes, out, ids.shape[1], ids.shape[2])
         _call("pag_kv_attend_selected", self.device, C.addressof(self._c), C.addressof(step._s), C.addressof(a), ids.data_ptr(), ids.stride(0), ids.stride(1),
               ids.shape[1], ids.shape[2])
+        return out
+
+
+class KvBlocks:
+    """Summaries of a cache's blocks of `block_tokens` tokens, and attention over those that are chosen by them (pag_kv_blocks).  After each append:
+
+        blocks.update(step.slots)
+        ids = blocks.select(q, step, k, window)             # int32 [tokens, id_heads, k], ascending, -1 behind them
+        out, lse = blocks.attend(q, ids, step, window=window)
+    """
+
+    def __init__(self, cache, block_tokens=64):
+        if not isinstance(cache, KvCache) or block_tokens <= 0 or block_tokens % 16 or cache.page_tokens % block_tokens:
+            raise PagError("block_tokens must be a multiple of 16 that divides the cache's page_tokens")
+        per = cache.page_tokens // block_tokens
+        self._set(cache, torch.zeros((cache.num_pages, cache.kv_heads, per, 2, -(-cache.head_dim // 64) * 64), dtype=torch.int8, device=cache.device),
+                  torch.zeros((cache.num_pages, cache.kv_heads, per), dtype=torch.int8, device=cache.device))
+
+    @classmethod
+    def from_tensors(cls, cache, codes, exponents):
+        """Over the caller's tensors: int8 [num_pages, kv_heads, page_tokens / block_tokens, 2, width] (largest and smallest), int8 [num_pages, kv_heads,
+        page_tokens / block_tokens]."""
+        self = cls.__new__(cls)
+        self._set(cache, codes, exponents)
+        return self
+
+    def _set(self, cache, codes, exponents):
+        if not isinstance(cache, KvCache) or not isinstance(codes, torch.Tensor) or codes.dim() != 5 or codes.shape[2] == 0 or cache.page_tokens % codes.shape[2] or \
+                cache.page_tokens // codes.shape[2] % 16:
+            raise PagError("codes must be an int8 tensor [num_pages, kv_heads, page_tokens / block_tokens, 2, width] for a KvCache")
+        per = codes.shape[2]
+        self.cache, self.block_tokens = cache, cache.page_tokens // per
+        self._b = _Blocks(C.sizeof(_Blocks), self.block_tokens,
+                          _array(codes, torch.int8, (cache.num_pages, cache.kv_heads, per, 2, -(-cache.head_dim // 64) * 64), cache.device, "codes"),
+                          _array(exponents, torch.int8, (cache.num_pages, cache.kv_heads, per), cache.device, "exponents"))
+        self.codes, self.exponents = codes, exponents
+
+    def update(self, slots):
+        """Summarises the blocks that slots (int64 [tokens], of the append before) lie in; the last of a block's tokens is the last that it holds."""
+        c = self.cache
+        _call("pag_kv_blocks_update", c.device, C.addressof(c._c), C.addressof(self._b), _array(slots, torch.int64, (slots.shape[0],), c.device, "slots"), slots.shape[0])
+
+    def select(self, q, step, k, window=0, id_heads=None, out=None):
+        """-> int32 [tokens, id_heads, k]: for each token the k blocks of the best scores among those that begin before its last `window` tokens.
+        id_heads: lists of a token, kv_heads if not given, else as attend_selected takes them; a list's heads share it by the largest of their scores."""
+        c = self.cache
+        c._queries(q, step, window)
+        if step.requests is None or step.positions is None:
+            raise PagError("select needs the step's requests and positions")
+        tokens, heads = q.shape[:2]
+        if id_heads is None:
+            id_heads = c.kv_heads
+        if k < 0 or id_heads <= 0:
+            raise PagError("k must not be negative, id_heads positive")
+        if out is None:
+            out = torch.empty((tokens, id_heads, k), dtype=torch.int32, device=c.device)
+        elif not isinstance(out, torch.Tensor) or out.dtype != torch.int32 or out.shape != (tokens, id_heads, k) or out.device != c.device or \
+                (k > 1 and out.stride(2) != 1):
+            raise PagError("out must be an int32 tensor [tokens, id_heads, k] on %s whose last dimension is dense" % c.device)
+        s = step._with(tokens)
+        a = _Attention(struct_size=C.sizeof(_Attention), dtype=_DTYPES[q.dtype], heads=heads, window=window, q=q.data_ptr(), q_token_stride=q.stride(0),
+                       q_head_stride=q.stride(1))
+        room = c._room(a, s, ("select", tokens, heads, window, s.requests, s.max_pages, id_heads, k, self.block_tokens), id_heads, k, self.block_tokens, True)
+        _call("pag_kv_blocks_select", c.device, C.addressof(c._c), C.addressof(self._b), C.addressof(s), C.addressof(a), id_heads, k, out.data_ptr(),
+              out.stride(0), out.stride(1))
+        del room
+        return out
+
+    def attend(self, q, ids, step, scale=None, window=0, softcap=0.0, slopes=None, out=None):
+        """KvCache.attend_selected over the tokens of listed blocks: ids int32 [tokens, id_heads, k] (-1: none), as select() returns them."""
+        c = self.cache
+        if step.requests is None or step.positions is None:
+            raise PagError("attend needs the step's requests and positions")
+        if not isinstance(ids, torch.Tensor) or ids.dtype != torch.int32 or ids.dim() != 3 or ids.device != c.device or ids.shape[0] != q.shape[0] or \
+                (ids.shape[2] > 1 and ids.stride(2) != 1):
+            raise PagError("ids must be an int32 tensor [tokens, id_heads, k] on %s whose last dimension is dense" % c.device)
+        out, a, room = c._attention(q, step, scale, window, softcap, slopes, out, ids.shape[1], ids.shape[2], self.block_tokens)
+        _call("pag_kv_attend_blocks", c.device, C.addressof(c._c), C.addressof(step._s), C.addressof(a), ids.data_ptr(), ids.stride(0), ids.stride(1), ids.shape[1],
+              ids.shape[2], self.block_tokens)
+        del room
         return out

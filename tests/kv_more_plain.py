@@ -86,3 +86,23 @@ def rounded(x, dtype):
     _, e = np.frexp(x)
     step = 2.0 ** (np.maximum(e - 1, least) - (bits - 1)).astype(np.float64)
     return np.rint(x / step) * step
+
+
+def summary(keys):
+    """keys [tokens, dim] -> (largest, smallest) as integers [2, dim], and their exponent."""
+    hi, lo = keys.max(0), keys.min(0)
+    e = plain.least_exponent(max(np.abs(hi).max(), np.abs(lo).max()), "int8")
+    return np.stack([np.ceil(hi * 2.0 ** -e), np.floor(lo * 2.0 ** -e)]), e
+
+
+def query_codes(q):
+    """A row of q -> integers and their exponent."""
+    finite = np.abs(q[np.isfinite(q)])
+    e = plain.least_exponent(finite.max() if finite.size else 0.0, "int8")
+    return plain.encode(q * 2.0 ** -e, "int8").view(np.int8).astype(np.float64), e
+
+
+def select(scores, k):
+    """scores: (block, score) of those that may be chosen -> the k best, ascending, -1 behind them."""
+    best = sorted(sorted(scores, key=lambda x: (-x[1], x[0]))[:k])
+    return [b for b, _ in best] + [-1] * (k - len(best))
