@@ -13,7 +13,8 @@ __device__ __forceinline__ void place_blocks(const Attend& a, Piece& p, u64 list
     ListPiece w;
     place_list(a, w, list, tile);
     p.w = w;
-    int request = a.s.request[w.t0], position = a.s.positions[w.t0];
+    const int request = __builtin_amdgcn_readfirstlane(a.s.request[w.t0]);
+    int position = __builtin_amdgcn_readfirstlane(a.s.positions[w.t0]);
     if (request < 0 || (u32)request >= a.s.requests || (u64)(u32)max(position, 0) >= (u64)a.s.max_pages * a.c.page_tokens) position = -1;
     p.b = position >= 0 ? (u32)request : 0;
     p.s = Span{ w.t0, 1, position + 1, position };
