@@ -427,8 +427,9 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
 /*
  * pag_kv_append_rotated: pag_kv_append of keys that are turned by their positions, and of values as they are; and the same turn for queries.
  * Of the first `turned` numbers of a row at position p each pair (x, y), numbers i and i + turned / 2 or 2 i and 2 i + 1, becomes
- * (x cos a - y sin a, y cos a + x sin a) with the angle a = p * frequencies[i], a product in 64 bits.  Angles below 2^31 in magnitude are turned by as
- * computed in 64 bits, so what is held and what comes out is rounded once.  A pair with an infinity or NaN becomes whatever these formulas give.
+ * (x cos a - y sin a, y cos a + x sin a) with the angle a = p * frequencies[i], a product in 64 bits.  Keys are turned in 64 bits where angles are below 2^31 in
+ * magnitude, so that what is held is rounded once; queries in 32 bits, by cosines and sines of 64 bits that are rounded to 32, and rounded to their type.
+ * A pair with an infinity or NaN becomes whatever these formulas give.
  */
 typedef enum { PAG_KV_HALVES = 0, PAG_KV_NEIGHBOURS = 1 } pag_kv_pairs;
 

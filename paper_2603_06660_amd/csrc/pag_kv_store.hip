@@ -193,10 +193,18 @@ __device__ __forceinline__ float odd(double x) {
     return __uint_as_float((bits - (fabs(y) > fabs(x) ? 1u : 0u)) | 1u);
 }
 
-// the angles of tokens t0 to t0 + n - 1, into LDS, by the workgroup
+// the angles of tokens t0 to t0 + n - 1, into LDS, by the workgroup; for keys in 64 bits, for queries in 32
 __device__ __forceinline__ void spin_tokens(const Store& a, u64 t0, u32 n, double2* spin) {
     const u32 half = a.turned / 2;
     for (u32 i = threadIdx.x; i < n * half; i += blockDim.x) spin[i] = spin_of((double)a.positions[t0 + i / half] * (double)a.frequencies[i % half]);
+}
+
+__device__ __forceinline__ void spin_queries(const Store& a, u64 t0, u32 n, float2* spin) {
+    const u32 half = a.turned / 2;
+    for (u32 i = threadIdx.x; i < n * half; i += blockDim.x) {
+        const double2 x = spin_of((double)a.positions[t0 + i / half] * (double)a.frequencies[i % half]);
+        spin[i] = make_float2((float)x.x, (float)x.y);
+    }
 }
 
 // Numbers at to at + 7 of a row, which x holds as they came, turned.  row: the element that the row begins with.
@@ -228,78 +236,121 @@ __device__ __forceinline__ void turn8(const Store& a, const void* p, u64 row, u3
     }
 }
 
-template <int N>
-__device__ __forceinline__ void load_numbers(const void* p, u64 at, u32 dtype, float* x) {
-    if constexpr (N == 8) load8(p, at, dtype, x);
-    else load4(p, at, dtype, x);
+constexpr u32 QUERY_TOKENS = 4;       // of a workgroup that turns queries, where there are many
+constexpr u32 QUERY_TURNS = 4;
+
+__device__ __forceinline__ void store_past(uint8_t* to, const uint4& x) {
+    typedef u32 word4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(word4{ x.x, x.y, x.z, x.w }, (word4*)to);
 }
 
-// N numbers in the call's type, each rounded once
-template <int N>
-__device__ __forceinline__ void store_numbers(void* p, u64 at, u32 dtype, const double* x) {
-    if (dtype == PAG_F32) {
+// 16 bytes of a row as they come, and as they go
+template <bool WIDE>
+__device__ __forceinline__ void numbers_of(const uint4& r, u32 dtype, float* x) {
+    if constexpr (WIDE) {
+        x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+    } else {
+        widen_row8(r, dtype, x);
+    }
+}
+
+template <bool WIDE>
+__device__ __forceinline__ uint4 bytes_of(const float* x, u32 dtype) {
+    if constexpr (WIDE) return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    else return make_uint4(pack2(x[0], x[1], dtype), pack2(x[2], x[3], dtype), pack2(x[4], x[5], dtype), pack2(x[6], x[7], dtype));
+}
+
+// q's rows of tokens t0 to t0 + n - 1, n <= QUERY_TOKENS, by the workgroup, in 32 bits.  A pair is one thread's, so that rows may be turned in place.  N numbers, 16 bytes, are
+// a thread's piece; of halves it has the N numbers half a turn on as well, and QUERY_TURNS rows' pieces are asked for before the first is turned.  Rows whose
+// halves do not begin at a multiple of N go in pieces of 4 numbers of 16 bits, 8 bytes.
+template <bool WIDE>
+__device__ __forceinline__ void turn_queries(const Store& a, u64 t0, u32 n, const float2* spin) {
+    constexpr u32 N = WIDE ? 4 : 8, SIZE = WIDE ? 4 : 2;
+    const u32 half = a.turned / 2;
+    const bool neighbours = a.pairs == PAG_KV_NEIGHBOURS;
+    if (!neighbours && half % N) {
+        const u32 pairs = half / 4, pieces = pairs + (a.c.dim - a.turned) / 8;
+        for (u32 i = threadIdx.x; i < n * a.heads * pieces; i += blockDim.x) {
+            const u32 piece = i % pieces, head = i / pieces % a.heads, token = i / pieces / a.heads;
+            const u64 from = (t0 + token) * (u64)a.q_ts + head * (u64)a.q_hs, to = (t0 + token) * (u64)a.o_ts + head * (u64)a.o_hs;
+            if (piece >= pairs) {
+                const u32 at = a.turned + (piece - pairs) * 8;
+                *(uint4*)((uint16_t*)a.out + to + at) = *(const uint4*)((const uint16_t*)a.q + from + at);
+            } else {
+                float x[4], y[4], u[4], v[4];
+                load4(a.q, from + piece * 4, a.dtype, x);
+                load4(a.q, from + half + piece * 4, a.dtype, y);
 #pragma unroll
-        for (int j = 0; j < N; j += 4) *(float4*)((float*)p + at + j) = make_float4((float)x[j], (float)x[j + 1], (float)x[j + 2], (float)x[j + 3]);
+                for (int j = 0; j < 4; ++j) {
+                    const float2 by = spin[token * half + piece * 4 + j];
+                    u[j] = __builtin_fmaf(x[j], by.x, -(y[j] * by.y));
+                    v[j] = __builtin_fmaf(y[j], by.x, x[j] * by.y);
+                }
+                *(uint2*)((uint16_t*)a.out + to + piece * 4) = make_uint2(pack2(u[0], u[1], a.dtype), pack2(u[2], u[3], a.dtype));
+                *(uint2*)((uint16_t*)a.out + to + half + piece * 4) = make_uint2(pack2(v[0], v[1], a.dtype), pack2(v[2], v[3], a.dtype));
+            }
+        }
         return;
     }
+    // A wave has 64 / pieces rows at a time; a lane keeps its piece, so that nothing is divided on the way.
+    const u32 pairs = neighbours ? a.turned / N : half / N, pieces = pairs + (a.c.dim - a.turned) / N, per_wave = 64 / pieces;
+    const u32 lane = threadIdx.x & 63, piece = lane % pieces, sub = lane / pieces, rows = n * a.heads, step = per_wave * (blockDim.x / 64);
+    if (sub >= per_wave) return;
+    const bool turns = piece < pairs, two = turns && !neighbours;
+    const u32 at = turns ? piece * N : a.turned + (piece - pairs) * N, other = two ? half : 0;
+    const float2* by = spin + (turns ? (neighbours ? piece * (N / 2) : at) : 0);
+    for (u32 row0 = wave_of() * per_wave + sub; row0 < rows; row0 += QUERY_TURNS * step) {
+        uint4 r[QUERY_TURNS][2];
+        u32 token[QUERY_TURNS];
+        u64 to[QUERY_TURNS];
 #pragma unroll
-    for (int j = 0; j < N; j += 4)
-        *(uint2*)((uint16_t*)p + at + j) = make_uint2(pack2(odd(x[j]), odd(x[j + 1]), dtype), pack2(odd(x[j + 2]), odd(x[j + 3]), dtype));
-}
-
-// N pairs whose first numbers lie at x_at and second ones at y_at of a row
-template <int N>
-__device__ __forceinline__ void turn_halves(const Store& a, u64 from, u64 to, u32 x_at, u32 y_at, const double2* spin) {
-    float x[N], y[N];
-    load_numbers<N>(a.q, from + x_at, a.dtype, x);
-    load_numbers<N>(a.q, from + y_at, a.dtype, y);
-    double u[N], v[N];
+        for (u32 i = 0; i < QUERY_TURNS; ++i) {
+            const u32 row = min(row0 + i * step, rows - 1);
+            token[i] = (row >= a.heads) + (row >= 2 * a.heads) + (row >= 3 * a.heads);
+            const u32 head = row - token[i] * a.heads;
+            const uint8_t* from = (const uint8_t*)a.q + ((t0 + token[i]) * (u64)a.q_ts + head * (u64)a.q_hs + at) * SIZE;
+            to[i] = (t0 + token[i]) * (u64)a.o_ts + head * (u64)a.o_hs + at;
+            r[i][0] = *(const uint4*)from;
+            if (two) r[i][1] = *(const uint4*)(from + other * SIZE);
+        }
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const double2 by = spin[x_at + j];
-        u[j] = __builtin_fma((double)x[j], by.x, -(double)y[j] * by.y);
-        v[j] = __builtin_fma((double)y[j], by.x, (double)x[j] * by.y);
-    }
-    store_numbers<N>(a.out, to + x_at, a.dtype, u);
-    store_numbers<N>(a.out, to + y_at, a.dtype, v);
-}
-
-// q's rows of tokens t0 to t0 + n - 1, by the workgroup.  A pair is one thread's, so that rows may be turned in place.
-__device__ __forceinline__ void turn_queries(const Store& a, u64 t0, u32 n, const double2* spin) {
-    const u32 half = a.turned / 2, each = half % 8 == 0 ? 8 : 4;
-    const u32 pairs = a.pairs == PAG_KV_NEIGHBOURS ? a.turned / 8 : half / each, pieces = pairs + (a.c.dim - a.turned) / 8, all = n * a.heads * pieces;
-    for (u32 i = threadIdx.x; i < all; i += blockDim.x) {
-        const u32 piece = i % pieces, head = i / pieces % a.heads, token = i / pieces / a.heads;
-        const u64 from = (t0 + token) * (u64)a.q_ts + head * (u64)a.q_hs, to = (t0 + token) * (u64)a.o_ts + head * (u64)a.o_hs;
-        const double2* by = spin + token * half;
-        if (piece >= pairs) {
-            const u32 at = a.turned + (piece - pairs) * 8;
-            float x[8];
-            double y[8];
-            load8(a.q, from + at, a.dtype, x);
+        for (u32 i = 0; i < QUERY_TURNS; ++i) {
+            if (row0 + i * step >= rows) break;
+            uint8_t* out = (uint8_t*)a.out + to[i] * SIZE;
+            const float2* spins = by + token[i] * half;
+            if (two) {
+                float x[N], y[N], u[N], v[N];
+                numbers_of<WIDE>(r[i][0], a.dtype, x);
+                numbers_of<WIDE>(r[i][1], a.dtype, y);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = x[j];
-            store_numbers<8>(a.out, to + at, a.dtype, y);
-        } else if (a.pairs == PAG_KV_NEIGHBOURS) {
-            float x[8];
-            double y[8];
-            load8(a.q, from + piece * 8, a.dtype, x);
+                for (u32 j = 0; j < N; ++j) {
+                    const float2 s = spins[j];
+                    u[j] = __builtin_fmaf(x[j], s.x, -(y[j] * s.y));
+                    v[j] = __builtin_fmaf(y[j], s.x, x[j] * s.y);
+                }
+                store_past(out, bytes_of<WIDE>(u, a.dtype));
+                store_past(out + other * SIZE, bytes_of<WIDE>(v, a.dtype));
+            } else if (turns) {
+                float x[N], u[N];
+                numbers_of<WIDE>(r[i][0], a.dtype, x);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const double2 s = by[piece * 4 + j];
-                y[2 * j] = __builtin_fma((double)x[2 * j], s.x, -(double)x[2 * j + 1] * s.y);
-                y[2 * j + 1] = __builtin_fma((double)x[2 * j + 1], s.x, (double)x[2 * j] * s.y);
+                for (u32 j = 0; j < N / 2; ++j) {
+                    const float2 s = spins[j];
+                    u[2 * j] = __builtin_fmaf(x[2 * j], s.x, -(x[2 * j + 1] * s.y));
+                    u[2 * j + 1] = __builtin_fmaf(x[2 * j + 1], s.x, x[2 * j] * s.y);
+                }
+                store_past(out, bytes_of<WIDE>(u, a.dtype));
+            } else {
+                store_past(out, r[i][0]);
             }
-            store_numbers<8>(a.out, to + piece * 8, a.dtype, y);
-        } else if (each == 8) {
-            turn_halves<8>(a, from, to, piece * 8, half + piece * 8, by);
-        } else {
-            turn_halves<4>(a, from, to, piece * 4, half + piece * 4, by);
         }
     }
 }
 
-constexpr u32 QUERY_TOKENS = 4;       // of a workgroup that turns queries, where there are many
+__device__ __forceinline__ void turn_queries(const Store& a, u64 t0, u32 n, const float2* spin) {
+    if (a.dtype == PAG_F32) turn_queries<true>(a, t0, n, spin);
+    else turn_queries<false>(a, t0, n, spin);
+}
 
 // A wave has a window of new tokens, one head and one kind.  It writes the blocks whose first new token lies in its window, with all
 // their new tokens, one block after the other.  8 numbers of a row are a lane's; a block of 16 rows is 2 C of these pieces a lane.
@@ -320,9 +371,9 @@ __global__ void __launch_bounds__(256) k_append(Store a, u32 window, u32 writers
         if (blockIdx.x >= writers) {
             const u64 first = (u64)(blockIdx.x - writers) * each;
             const u32 n = (u32)min((u64)each, a.tokens - first);
-            spin_tokens(a, first, n, spin);
+            spin_queries(a, first, n, (float2*)spin);
             __syncthreads();
-            turn_queries(a, first, n, spin);
+            turn_queries(a, first, n, (const float2*)spin);
             return;
         }
         const u32 fours = (a.c.kv_heads + 3) / 4, part = blockIdx.x % (2 * fours);
@@ -424,46 +475,70 @@ __global__ void __launch_bounds__(256) k_append(Store a, u32 window, u32 writers
 }
 
 // 4-bit codes: a row's parts have their exponents to themselves, so that 8 numbers of a row are a thread's, whatever else the call writes, and four
-// threads share a part.  A workgroup has `each` tokens, all their heads, keys and values, and their queries.
+// threads share a part.  A workgroup has `each` tokens, all their heads, keys and values; the workgroups from number `writers` on turn queries.  A lane keeps its
+// piece of a row, and FP4_TURNS rows' pieces are asked for before the first is encoded.
+constexpr u32 FP4_TURNS = 4;
+
 template <int C, bool TURN>
-__global__ void __launch_bounds__(256) k_append_fp4(Store a, u32 each) {
+__global__ void __launch_bounds__(256) k_append_fp4(Store a, u32 writers, u32 each) {
     extern __shared__ double2 spin[];
-    const u64 first = (u64)blockIdx.x * each;
+    const bool writes = !TURN || blockIdx.x < writers;
+    const u64 first = (u64)(writes ? blockIdx.x : blockIdx.x - writers) * each;
     const u32 n = (u32)min((u64)each, a.tokens - first);
     if constexpr (TURN) {
+        if (!writes) {
+            spin_queries(a, first, n, (float2*)spin);
+            __syncthreads();
+            turn_queries(a, first, n, (const float2*)spin);
+            return;
+        }
         spin_tokens(a, first, n, spin);
         __syncthreads();
     }
-    const u32 pieces = 8 * C, all = n * a.c.kv_heads * 2 * pieces;
-    for (u32 i = threadIdx.x; i < all; i += 256) {
-        const u32 at = i % pieces * 8, kind = i / pieces & 1, head = i / (2 * pieces) % a.c.kv_heads, token = i / (2 * pieces) / a.c.kv_heads;
-        const int64_t slot = a.slots[first + token];
-        if (slot < 0 || slot >= (int64_t)a.c.num_pages * a.c.page_tokens) continue;
-        float x[8] = { 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f };
-        if (at < a.c.dim) {
-            const u64 from = (first + token) * (u64)a.ts[kind] + head * (u64)a.hs[kind];
-            load8(a.x[kind], from + at, a.dtype, x);
+    // rows: token and head, all keys before all values, so that a wave has one kind and what turns keys stays out of the values' way
+    constexpr u32 PIECES = 8 * C, PER_WAVE = 64 / PIECES;
+    const u32 lane = threadIdx.x & 63, at = lane % PIECES * 8, sub = lane / PIECES, kv = a.c.kv_heads, rows = 2 * n * kv, step = PER_WAVE * 4;
+    if (sub >= PER_WAVE) return;
+    for (u32 row0 = wave_of() * PER_WAVE + sub; row0 < rows; row0 += FP4_TURNS * step) {
+        float x[FP4_TURNS][8];
+        int64_t slot[FP4_TURNS];
+        u32 token[FP4_TURNS], head[FP4_TURNS];
+        u64 from[FP4_TURNS];
+#pragma unroll
+        for (u32 i = 0; i < FP4_TURNS; ++i) {
+            const u32 both = min(row0 + i * step, rows - 1), kind = both >= n * kv, row = both - kind * n * kv;
+            token[i] = (row >= kv) + (row >= 2 * kv) + (row >= 3 * kv);
+            head[i] = row - token[i] * kv;
+            slot[i] = a.slots[first + token[i]];
+            from[i] = (first + token[i]) * (u64)(kind ? a.ts[1] : a.ts[0]) + head[i] * (u64)(kind ? a.hs[1] : a.hs[0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
+            if (at < a.c.dim) load8(kind ? a.x[1] : a.x[0], from[i] + at, a.dtype, x[i]);
+        }
+#pragma unroll
+        for (u32 i = 0; i < FP4_TURNS; ++i) {
+            const u32 row = row0 + i * step, kind = row >= n * kv;
+            if (row >= rows || slot[i] < 0 || slot[i] >= (int64_t)a.c.num_pages * a.c.page_tokens) continue;          // the same for a part's four lanes
             if constexpr (TURN) {
-                if (kind == 0) turn8(a, a.x[0], from, at, spin + token * (a.turned / 2), x);
+                if (kind == 0 && at < a.c.dim) turn8(a, a.x[0], from[i], at, spin + token[i] * (a.turned / 2), x[i]);
             }
-        }
-        float most = 0.f;
+            float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float y = fabsf(x[j]);
-            if (y <= 3.402823466e38f) most = fmaxf(most, y);
-        }
-        most = fmaxf(most, __shfl_xor(most, 1));
-        most = fmaxf(most, __shfl_xor(most, 2));
-        const int e = least_exponent<PAG_KV_FP4>(most);
-        const float down = power(-e);
+            for (int j = 0; j < 8; ++j) {
+                const float y = fabsf(x[i][j]);
+                if (y <= 3.402823466e38f) most = fmaxf(most, y);
+            }
+            most = fmaxf(most, __shfl_xor(most, 1));
+            most = fmaxf(most, __shfl_xor(most, 2));
+            const int e = least_exponent<PAG_KV_FP4>(most);
+            const float down = power(-e);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= down;
-        const u32 page = (u32)((u64)slot / a.c.page_tokens), row = row_of(a.c, page, head, (u32)((u64)slot % a.c.page_tokens));
-        *(u32*)(a.c.data + (u64)row * (64 * C) + kind * (32 * C) + at / 2) = encode8_fp4(x);
-        if (at % PART == 0) a.c.exponents[((u64)(row / BLOCK) * 2 + kind) * (2 * C * BLOCK) + at / PART * BLOCK + row % BLOCK] = (int8_t)e;
+            for (int j = 0; j < 8; ++j) x[i][j] *= down;
+            const u32 page = (u32)((u64)slot[i] / a.c.page_tokens), place = row_of(a.c, page, head[i], (u32)((u64)slot[i] % a.c.page_tokens));
+            *(u32*)(a.c.data + (u64)place * (64 * C) + kind * (32 * C) + at / 2) = encode8_fp4(x[i]);
+            if (at % PART == 0) a.c.exponents[((u64)(place / BLOCK) * 2 + kind) * (2 * C * BLOCK) + at / PART * BLOCK + place % BLOCK] = (int8_t)e;
+        }
     }
-    if constexpr (TURN) turn_queries(a, first, n, spin);
 }
 
 struct Load {
@@ -599,8 +674,8 @@ struct RunAppend {
         const u32 each = a.tokens <= 1024 ? 1 : QUERY_TOKENS;
         if constexpr (FMT == PAG_KV_FP4) {
             const u32 grid = (u32)((a.tokens + each - 1) / each);
-            if (a.turned) k_append_fp4<C, true><<<grid, 256, each * spins, st>>>(a, each);
-            else k_append_fp4<C, false><<<grid, 256, 0, st>>>(a, each);
+            if (a.turned) k_append_fp4<C, true><<<a.heads ? 2 * grid : grid, 256, each * spins, st>>>(a, grid, each);
+            else k_append_fp4<C, false><<<grid, 256, 0, st>>>(a, grid, each);
         } else {
             const u32 window = waves <= 4096 ? 1 : waves <= 32768 ? 4 : 16;
             const u64 windows = (a.tokens + window - 1) / window;

@@ -1,5 +1,5 @@
-"""Keys and queries turned by their positions on the way into the cache, and the 4-bit cache's codes, against 64 bits: bit for bit, since what is
-held and what comes out is rounded once."""
+"""Keys and queries turned by their positions on the way into the cache, and the 4-bit cache's codes, against 64 bits: what is held bit for bit, since
+it is rounded once, queries to the roundings of 32 bits."""
 import math
 
 import numpy as np
@@ -47,6 +47,20 @@ def same_cache(cache, data, exponents):
         fold = lambda x: np.where(x & 0x70 == 0, x & 0x7F, x) & np.where(x & 7 == 0, 0xF7, 0xFF)
         got, data = fold(got), fold(data)
     assert (got == data).all()
+
+
+def same_queries(got, q, positions, f, pairs, dtype):
+    """x cos a - y sin a in 32 bits: the cosine and sine, one product and the sum are rounded, each by 2^-24 of |x cos a| + |y sin a| at most, which is below sqrt(2) of the
+    pair's length: 3 * sqrt(2) * 2^-24.  Then the rounding to the type: half a step of the result, 2^-9, 2^-12 or 2^-24 of it, and half the least step of all, 2^-25 for fp16."""
+    want = more.turn(q, positions, f, pairs)
+    n = 2 * len(f)
+    size = np.zeros_like(q)
+    first, second = (slice(0, n // 2), slice(n // 2, n)) if pairs == "halves" else (slice(0, n, 2), slice(1, n, 2))
+    size[..., first] = size[..., second] = np.hypot(q[..., first], q[..., second])
+    wrong = 3 * math.sqrt(2) * 2.0 ** -24 * size
+    half = {"bf16": 2.0 ** -9, "fp16": 2.0 ** -12, "fp32": 2.0 ** -24}[dtype] * 2        # a step is 2^-8 of a number at the low end of its binade
+    assert (np.abs(wide(got) - want) <= wrong + half * (np.abs(want) + wrong) + (2.0 ** -25 if dtype == "fp16" else 0)).all()
+    assert (wide(got)[..., n:] == q[..., n:]).all()
 
 
 @pytest.mark.parametrize("dim, heads, page, dtype", [(64, 1, 16, "bf16"), (128, 2, 32, "fp16"), (80, 3, 48, "fp32"), (192, 2, 16, "fp32"),
@@ -126,7 +140,7 @@ def test_rotated_write_bit_for_bit(kv, fmt, dim, turned, kv_heads, heads, page, 
         if q is None:
             assert got is None
         else:
-            assert (wide(got) == more.rounded(more.turn(wide(q), positions, f, pairs), dtype)).all()
+            same_queries(got, wide(q), positions, f, pairs, dtype)
         length += n
 
 
@@ -156,7 +170,7 @@ def test_rotated_write_of_prompts(kv, fmt, tokens, heads):
     assert got is q
     more.append(data, exponents, dim, fmt, more.turn(wide(x[0]), positions, f, "halves"), wide(x[1]), slots)
     same_cache(cache, data, exponents)
-    assert (wide(q) == more.rounded(more.turn(wide(before), positions, f, "halves"), "bf16")).all()
+    same_queries(q, wide(before), positions, f, "halves", "bf16")
 
 
 @pytest.mark.parametrize("fmt", ["int8", "fp4"])
