@@ -98,11 +98,18 @@ __device__ __forceinline__ void columns_fp4(const u32 (&w)[8], const float (&sca
 // The largest of the exponents of 16 tokens' parts of one kind (parts_of), of the first n tokens: what the block's numbers are held as multiples of in
 // 16-bit floats.  What those behind the last token hold may be anything.  Bytes are compared as the upper halves of 16-bit words; LOWEST_EXPONENT if n is 0.
 template <int C>
-__device__ __forceinline__ int most_of_parts(const int8_t* parts, int n) {
-    typedef uint16_t half2u __attribute__((ext_vector_type(2)));
-    uint4 e[2 * C];
+struct Parts { uint4 e[2 * C]; };
+
+template <int C>
+__device__ __forceinline__ void load_parts(const int8_t* parts, Parts<C>& p) {
 #pragma unroll
-    for (int b = 0; b < 2 * C; ++b) e[b] = *(const uint4*)(parts + b * BLOCK);
+    for (int b = 0; b < 2 * C; ++b) p.e[b] = *(const uint4*)(parts + b * BLOCK);
+}
+
+template <int C>
+__device__ __forceinline__ int most_of_parts(const Parts<C>& p, int n) {
+    typedef uint16_t half2u __attribute__((ext_vector_type(2)));
+    const uint4* e = p.e;
     half2u even = { 0, 0 }, odd = { 0, 0 };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -119,8 +126,30 @@ __device__ __forceinline__ int most_of_parts(const int8_t* parts, int n) {
     return max((int)(max(both.x, both.y) >> 8) - 128, LOWEST_EXPONENT);
 }
 
-// byte i of a word of exponents as a power of two, 0 for -127
-__device__ __forceinline__ float power_of_byte(u32 w, int i) { return power((int)(int8_t)(w >> (8 * i))); }
+// 2^(e - R) as the bits of e << 23 and of `less` = (127 - R) << 23, for e >= R - 127, which gives 0: one instruction, and one more for a byte i of a word of exponents.
+// Where R is above LOWEST_EXPONENT + 127 exponents may be smaller, and are raised to R - 127 first.
+constexpr int MOST_PLAIN = LOWEST_EXPONENT + 127;
+__device__ __forceinline__ int less_of(int R) { return (127 - R) * (1 << 23); }
+__device__ __forceinline__ float power_less(int e, int less) { return __int_as_float((int)((u32)e << 23) + less); }
+template <int I>
+__device__ __forceinline__ int byte_of(u32 w) {             // by one instruction: the compiler would shift, mask and add
+    int x;
+    if constexpr (I == 3) x = (int)w >> 24;
+    else asm("v_bfe_i32 %0, %1, %2, 8" : "=v"(x) : "v"(w), "n"(8 * I));
+    return x;
+}
+__device__ __forceinline__ void powers_of_bytes(u32 w, int less, float* x) {
+    x[0] = power_less(byte_of<0>(w), less);
+    x[1] = power_less(byte_of<1>(w), less);
+    x[2] = power_less(byte_of<2>(w), less);
+    x[3] = power_less(byte_of<3>(w), less);
+}
+__device__ __forceinline__ u32 raised_bytes(u32 w, int least) {
+    u32 x = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x |= (u32)(max((int)__builtin_amdgcn_sbfe((int)w, 8 * i, 8), least) & 255) << (8 * i);
+    return x;
+}
 
 // byte c of eight words, c = 0 .. 3: a column of eight tokens for each of four numbers of a row
 template <int FMT>

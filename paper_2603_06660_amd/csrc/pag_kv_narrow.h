@@ -83,22 +83,22 @@ __device__ __forceinline__ void load_halves(const uint8_t* p, u32* w) {
     }
 }
 
-// A lane's part of a tile of 4-bit codes.  k: its row of keys; v(j): the rows of values of its 8 tokens
+// A lane's part of half a tile of 4-bit codes.  k: its first piece of its row of keys; v(j): its numbers of the values of token j of its 4
 template <int C, typename V>
-__device__ __forceinline__ void load_codes(Tile<PAG_KV_FP4, C>& tile, int s, const uint8_t* k, V&& v, u32 col, u32 g) {
+__device__ __forceinline__ void load_codes(Tile<PAG_KV_FP4, C>& tile, int s, const uint8_t* k, V&& v) {
     typedef Tile<PAG_KV_FP4, C> Tile4;
 #pragma unroll
     for (int h = 0; h < Tile4::PIECES; ++h) {
         if constexpr (Tile4::WORDS == 4) {
-            const uint4 x = *(const uint4*)(k + g * 16 + h * 64);
+            const uint4 x = *(const uint4*)(k + h * 64);
             tile.k[s][4 * h] = x.x; tile.k[s][4 * h + 1] = x.y; tile.k[s][4 * h + 2] = x.z; tile.k[s][4 * h + 3] = x.w;
         } else {
-            const uint2 x = *(const uint2*)(k + g * 8 + h * 32);
+            const uint2 x = *(const uint2*)(k + h * 32);
             tile.k[s][2 * h] = x.x; tile.k[s][2 * h + 1] = x.y;
         }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) load_halves<C>(v(j) + 32 * C + col * (2 * C), tile.v[4 * s + j]);
+    for (int j = 0; j < 4; ++j) load_halves<C>(v(j), tile.v[4 * s + j]);
 }
 
 // parts of a lane's pieces of keys and numbers of values
@@ -180,7 +180,7 @@ struct Scales {
     static constexpr int N = LISTED ? 8 : 2;
     float ek[N], ev[N], down[N];
     int at[N];
-    float fine[2][2];          // 4-bit codes whose keys share ek and ev: 2^-e of the keys and of the values of either half, which their parts' exponents are above
+    int less[2][2];            // 4-bit codes: what power_less takes, of the keys and of the values of either half (of listed ones, whose exponents are relative, of 0)
 };
 
 // T tiles of rows against one of keys.  keep: bit j set if the row may read key j; looked at only if `masked`.  far: the
@@ -198,9 +198,7 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<FMT, C>& ti
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
             for (int n = 0; n < 2 * C; ++n) {
-                float scale = power(tile.ke[b][n / Tile<FMT, C>::WORDS]);
-                if constexpr (!LISTED) scale *= x.fine[b][0];
-                const half8_t k = widen8_fp4(tile.k[b][n], scale);
+                const half8_t k = widen8_fp4(tile.k[b][n], power_less(tile.ke[b][n / Tile<FMT, C>::WORDS], x.less[b][0]));
 #pragma unroll
                 for (int y = 0; y < T; ++y) s[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, rows[y].q[n], s[y][b], 0, 0, 0);
             }
@@ -331,11 +329,8 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<FMT, C>& ti
 #pragma unroll
         for (int w = 0; w < C; ++w) {
             if (w < Tile<FMT, C>::PARTS) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    scale[j] = power_of_byte(tile.ve[j >> 2][w], j & 3);
-                    if constexpr (!LISTED) scale[j] *= x.fine[j >> 2][1];
-                }
+                powers_of_bytes(tile.ve[0][w], x.less[0][1], scale);
+                powers_of_bytes(tile.ve[1][w], x.less[1][1], scale + 4);
             }
             u32 words[8];
 #pragma unroll
@@ -537,34 +532,44 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
         far = false;
         if (T == 1) fetch_rows<FMT, C>(a, p.w, raw);
     };
-    const auto look_up = [&]() {              // then exponents and the first tile
+    // then exponents and, by then(), the first tile; the next 64 blocks' pages
+    const auto look_up = [&](auto&& then) {
         const bool ok = page < a.c.num_pages;
         if (BLOCKS) first = first_next;
         const int at_key = BLOCKS ? first : from + mine_at;
         block_row = ok ? row_of(a.c, page, p.w.kv_head, (u32)at_key / BLOCK % a.c.page_blocks * BLOCK) : 0;
+        there = __ballot(ok);
         if constexpr (FMT == PAG_KV_FP4) {
+            // the parts' exponents are asked for, then the tile, before the largest are looked for
+            Parts<C> k, v;
+            load_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 0), k);
+            load_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 1), v);
+            then();
             const int tokens = ok ? (BLOCKS ? p.p0 + 1 : p.stop) - at_key : 0;
-            const int k = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 0), tokens), v = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 1), tokens);
-            exponents = (uint16_t)((k & 255) | v << 8);
+            exponents = (uint16_t)((most_of_parts<C>(k, tokens) & 255) | most_of_parts<C>(v, tokens) << 8);
+            page = page_of(from + 32 * (int)(NW * TILE) + mine_at);
         } else {
             exponents = ok ? *(const uint16_t*)(a.c.exponents + (u64)(block_row / BLOCK) * 2) : 0;
+            page = page_of(from + 32 * (int)(NW * TILE) + mine_at);
+            then();
         }
-        there = __ballot(ok);
-        page = page_of(from + 32 * (int)(NW * TILE) + mine_at);
     };
-    const u32 k_at = col * (128 * C) + g * 16, v_at = 4 * g * (128 * C) + 64 * C + col * (4 * C);
+    // a lane's offset from where a block begins; what is added to it is the same for all lanes
+    constexpr u32 HALF = FMT == PAG_KV_FP4 ? 1 : 2;          // bytes of two numbers
+    const u32 k_at = col * (64 * C * HALF) + g * (FMT == PAG_KV_FP4 && C % 2 ? 8 : 16), v_at = 4 * g * (64 * C * HALF) + 32 * C * HALF + col * (2 * C * HALF);
     const auto load = [&](Tile<FMT, C>& tile, int i) {
         if constexpr (FMT == PAG_KV_FP4) {
+            typedef Tile<FMT, C> T4;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const u32 row = (u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s);
                 const uint8_t* rows_at = a.c.data + (u64)row * (64 * C);
-                load_codes<C>(tile, s, rows_at + col * (64 * C), [&](int j) { return rows_at + (4 * g + j) * (64 * C); }, col, g);
-                const int8_t *ke = parts_of<C>(a.c, row / BLOCK, 0), *ve = parts_of<C>(a.c, row / BLOCK, 1);
+                load_codes<C>(tile, s, rows_at + k_at, [&](int j) { return rows_at + v_at + j * (64 * C); });
+                const int8_t* parts = parts_of<C>(a.c, row / BLOCK, 0);
 #pragma unroll
-                for (int h = 0; h < Tile<FMT, C>::PIECES; ++h) tile.ke[s][h] = ke[key_part<C>(h, g) * BLOCK + col];
+                for (int h = 0; h < T4::PIECES; ++h) tile.ke[s][h] = parts[key_part<C>(h, g) * BLOCK + col];
 #pragma unroll
-                for (int w = 0; w < Tile<FMT, C>::PARTS; ++w) tile.ve[s][w] = *(const u32*)(ve + value_part<C>(w, col) * BLOCK + 4 * g);
+                for (int w = 0; w < T4::PARTS; ++w) tile.ve[s][w] = *(const u32*)(parts + ((2 * C + value_part<C>(w, col)) * BLOCK + 4 * g));
             }
             return;
         } else
@@ -588,8 +593,14 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             far = far || ev > FAR_EXPONENT;
             x.down[s] = power(-ev);
             if constexpr (FMT == PAG_KV_FP4) {
-                x.fine[s][0] = power(-(int)(int8_t)e);
-                x.fine[s][1] = x.down[s];
+                x.less[s][0] = less_of((int)(int8_t)e);
+                x.less[s][1] = less_of(ev);
+                if ((int)(int8_t)e > MOST_PLAIN || ev > MOST_PLAIN) {
+#pragma unroll
+                    for (int h = 0; h < Tile<FMT, C>::PIECES; ++h) tile.ke[s][h] = max(tile.ke[s][h], (int)(int8_t)e - 127);
+#pragma unroll
+                    for (int w = 0; w < Tile<FMT, C>::PARTS; ++w) tile.ve[s][w] = raised_bytes(tile.ve[s][w], ev - 127);
+                }
             }
             x.at[s] = (BLOCKS ? __builtin_amdgcn_readlane(first, 2 * i + s) : pos + s * (int)BLOCK) + 4 * (int)g;
         }
@@ -597,14 +608,12 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
         const u32 two = (u32)(there >> (2 * i)) & 3u;
         // behind the last token there may be anything
         const auto no_value = [&](int j) {
-            if constexpr (FMT == PAG_KV_FP4) {
+            if constexpr (FMT == PAG_KV_FP4) {                // nor may its exponent be anything
 #pragma unroll
-                for (int w = 0; w < Tile<FMT, C>::PARTS; ++w)
-                    tile.ve[j >> 2][w] = (tile.ve[j >> 2][w] & ~(255u << (8 * (j & 3)))) | 0x81u << (8 * (j & 3));          // 2^-127 counts as 0
-            } else {
-#pragma unroll
-                for (int y = 0; y < C; ++y) tile.v[j][y] = 0;
+                for (int w = 0; w < Tile<FMT, C>::PARTS; ++w) tile.ve[j >> 2][w] &= ~(255u << (8 * (j & 3)));
             }
+#pragma unroll
+            for (int y = 0; y < (FMT == PAG_KV_FP4 ? (C + 1) / 2 : C); ++y) tile.v[j][y] = 0;
         };
         if constexpr (BLOCKS) {
             // listed tokens end where the window begins, the window's end with the token itself
@@ -666,12 +675,21 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             ask();
             start();
             while (from < p.stop) {
-                look_up();
                 const int count = min(32, (p.stop - from + (int)(NW * TILE) - 1) / (int)(NW * TILE));
-                for (int i = 0; i < count; ++i) {
+                if constexpr (FMT == PAG_KV_FP4) {
                     Tile<FMT, C> tile;
-                    load(tile, i);
-                    add(tile, i);
+                    look_up([&]() { load(tile, 0); });
+                    for (int i = 0; i < count; ++i) {
+                        if (i) load(tile, i);
+                        add(tile, i);
+                    }
+                } else {
+                    look_up([]() {});
+                    for (int i = 0; i < count; ++i) {
+                        Tile<FMT, C> tile;
+                        load(tile, i);
+                        add(tile, i);
+                    }
                 }
                 from += 32 * (int)(NW * TILE);
             }
@@ -694,8 +712,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
     if (more) {
         ask();
         if (from < p.stop) {
-            look_up();
-            load(even, 0);
+            look_up([&]() { load(even, 0); });
         }
     }
     while (more) {
@@ -713,8 +730,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             }
             from += 32 * (int)(NW * TILE);
             if (from < p.stop) {
-                look_up();
-                load(even, 0);
+                look_up([&]() { load(even, 0); });
             }
         }
         // the next piece's first tile is on its way while this one's waves are added up
@@ -726,8 +742,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
         if (more) ask();
         exchange(rows[0], w, sh);
         if (more && from < p.stop) {
-            look_up();
-            load(even, 0);
+            look_up([&]() { load(even, 0); });
         }
         finish(a, w, sh, partial);
     }
@@ -951,7 +966,8 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
             for (int s = 0; s < 2; ++s) {
                 const uint4 r = *(const uint4*)&x.row[32 * i + 16 * s + 4 * g];
                 const u32 rows_at[4] = { r.x, r.y, r.z, r.w };
-                load_codes<C>(tile, s, a.c.data + (u64)x.row[32 * i + 16 * s + col] * (64 * C), [&](int j) { return a.c.data + (u64)rows_at[j] * (64 * C); }, col, g);
+                load_codes<C>(tile, s, a.c.data + (u64)x.row[32 * i + 16 * s + col] * (64 * C) + g * (C % 2 ? 8 : 16),
+                              [&](int j) { return a.c.data + (u64)rows_at[j] * (64 * C) + 32 * C + col * (2 * C); });
 #pragma unroll
                 for (int h = 0; h < Tile<FMT, C>::PIECES; ++h) tile.ke[s][h] = x.parts[0][key_part<C>(h, g)][32 * i + 16 * s + col];
 #pragma unroll
@@ -983,6 +999,7 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
             scales.down[4 * s] = down.x; scales.down[4 * s + 1] = down.y; scales.down[4 * s + 2] = down.z; scales.down[4 * s + 3] = down.w;
             scales.at[4 * s] = pos.x; scales.at[4 * s + 1] = pos.y; scales.at[4 * s + 2] = pos.z; scales.at[4 * s + 3] = pos.w;
         }
+        scales.less[0][0] = scales.less[0][1] = scales.less[1][0] = scales.less[1][1] = less_of(0);
         const bool masked = found != 0xFFFFFFFFu;
         const u32 keep[1] = { (found >> (4 * g) & 15u) | (found >> (16 + 4 * g) & 15u) << 4 };
         if constexpr (FMT != PAG_KV_FP4) {           // which have an exponent for keys that are none

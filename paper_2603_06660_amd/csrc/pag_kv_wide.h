@@ -375,8 +375,11 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                     ok = true;
                     block_row = row_of(a.c, page, kv_head, blk % a.c.page_blocks * BLOCK);
                     if constexpr (FMT == PAG_KV_FP4) {
-                        ek_mine = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 0), stop - at_key);
-                        ev_mine = most_of_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 1), stop - at_key);
+                        Parts<C> parts;
+                        load_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 0), parts);
+                        ek_mine = most_of_parts<C>(parts, stop - at_key);
+                        load_parts<C>(parts_of<C>(a.c, block_row / BLOCK, 1), parts);
+                        ev_mine = most_of_parts<C>(parts, stop - at_key);
                     } else {
                         const int8_t* e = a.c.exponents + (u64)(block_row / BLOCK) * 2;
                         ek_mine = e[0];
@@ -452,12 +455,22 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
         const auto stage = [&](u32 n, int from, u32 buffer) {
             _Float16* keys = lds + buffer * (KEYS + VALUES);
             _Float16* values = keys + KEYS;
-            const float fine_k = FMT == PAG_KV_FP4 ? power(-__builtin_amdgcn_readlane(ek_mine, (int)(n & 63))) : 0.f;
-            const float fine_v = FMT == PAG_KV_FP4 ? power(-__builtin_amdgcn_readlane(ev_mine, (int)(n & 63))) : 0.f;
+            const int ek_most = __builtin_amdgcn_readlane(ek_mine, (int)(n & 63)), ev_most = __builtin_amdgcn_readlane(ev_mine, (int)(n & 63));
+            if constexpr (FMT == PAG_KV_FP4) {
+                if (ek_most > MOST_PLAIN || ev_most > MOST_PLAIN) {
+#pragma unroll
+                    for (int i = 0; i < Fetch<FMT, C, NW>::PARTS; ++i) f.ke[i] = max(f.ke[i], ek_most - 127);
+#pragma unroll
+                    for (int i = 0; i < Share<C, NW>::N; ++i) {
+                        f.ve[i][0] = raised_bytes(f.ve[i][0], ev_most - 127);
+                        f.ve[i][1] = raised_bytes(f.ve[i][1], ev_most - 127);
+                    }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < Share<C, NW>::PIECES; ++i) {
                 half8_t wide;
-                if constexpr (FMT == PAG_KV_FP4) wide = widen8_fp4(f.k[i], power(f.ke[i / Fetch<FMT, C, NW>::EACH]) * fine_k);
+                if constexpr (FMT == PAG_KV_FP4) wide = widen8_fp4(f.k[i], power_less(f.ke[i / Fetch<FMT, C, NW>::EACH], less_of(ek_most)));
                 else wide = widen8<FMT>(f.k[i].x, f.k[i].y);
                 *(half8_t*)(keys + key_at<C>(block * BLOCK + key, key_piece0 + i)) = wide;
             }
@@ -470,8 +483,8 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                     half8_t v[4];
                     if constexpr (FMT == PAG_KV_FP4) {
                         float scale[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) scale[j] = power_of_byte(f.ve[i][j >> 2], j & 3) * fine_v;
+                        powers_of_bytes(f.ve[i][0], less_of(ev_most), scale);
+                        powers_of_bytes(f.ve[i][1], less_of(ev_most), scale + 4);
                         if (!ok || base + (int)BLOCK > stop) {
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
@@ -493,8 +506,8 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 ? 2 : 1) k_attend_wide(Attend 
                 }
             }
             if (lane == 0 && part == 0) {
-                sh_scale[buffer][block][0] = power(__builtin_amdgcn_readlane(ek_mine, (int)(n & 63)));
-                sh_scale[buffer][block][1] = (float)__builtin_amdgcn_readlane(ev_mine, (int)(n & 63));
+                sh_scale[buffer][block][0] = power(ek_most);
+                sh_scale[buffer][block][1] = (float)ev_most;
                 sh_there[buffer][block] = ok && base < stop ? 1u : 0u;
             }
         };
