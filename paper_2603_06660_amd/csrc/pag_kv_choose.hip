@@ -18,12 +18,103 @@ constexpr u32 MOST_SHORT = 1024;            // keys of a list that a wave holds 
 
 // ---- summaries ------------------------------------------------------------------------------------------------------
 
+// The largest and smallest of 16 numbers of a lane over rows r0 to r1 - 1 of a block, and then over the lanes that have the same numbers: lanes 0 .. 4 C - 1 end up with
+// all of them.  16 / C rows a turn, TURNS turns asked for together.
+template <int FMT, int C, int TURNS>
+__device__ __forceinline__ void extremes_of(const Cache& c, u32 row0, u32 r0, u32 r1, float* hi, float* lo) {
+    constexpr u32 LANES = 4 * C, ROWS_A_TURN = 64 / LANES;          // of a row; 12 lanes a row leave four without one
+    const u32 lane = threadIdx.x & 63, row = lane / LANES, at = lane % LANES * 16;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) { hi[j] = -INFINITY; lo[j] = INFINITY; }
+    for (; r0 < r1; r0 += TURNS * ROWS_A_TURN) {
+        uint4 w[TURNS];
+        int e[TURNS];
+#pragma unroll
+        for (u32 n = 0; n < TURNS; ++n) {                  // behind the last row the last one again
+            const u32 r = row0 + min(r0 + n * ROWS_A_TURN + (row < ROWS_A_TURN ? row : 0), r1 - 1);
+            if constexpr (FMT == PAG_KV_FP4) {
+                const uint2 x = *(const uint2*)(c.data + (u64)r * (64 * C) + at / 2);
+                w[n] = make_uint4(x.x, x.y, 0, 0);
+                e[n] = parts_of<C>(c, r / BLOCK, 0)[at / PART * BLOCK + r % BLOCK];
+            } else {
+                w[n] = *(const uint4*)(c.data + (u64)r * (128 * C) + at);
+                e[n] = c.exponents[(u64)(r / BLOCK) * 2];
+            }
+        }
+#pragma unroll
+        for (u32 n = 0; n < TURNS; ++n) {
+            const float up = power(e[n]);
+            float x[16];
+            if constexpr (FMT == PAG_KV_FP4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) decode4_fp4((j < 2 ? w[n].x : w[n].y) >> (16 * (j & 1)), 1.f, x + 4 * j);
+            } else {
+                decode4<FMT>(w[n].x, x);
+                decode4<FMT>(w[n].y, x + 4);
+                decode4<FMT>(w[n].z, x + 8);
+                decode4<FMT>(w[n].w, x + 12);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float y = x[j] * up;
+                hi[j] = fmaxf(hi[j], y);
+                lo[j] = fminf(lo[j], y);
+            }
+        }
+    }
+    // rows LANES apart, whatever their number
+#pragma unroll
+    for (u32 o = 1; o < ROWS_A_TURN; o *= 2) {
+        const u32 from = lane + o * LANES < ROWS_A_TURN * LANES ? lane + o * LANES : lane;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            hi[j] = fmaxf(hi[j], __shfl(hi[j], (int)from));
+            lo[j] = fminf(lo[j], __shfl(lo[j], (int)from));
+        }
+    }
+}
+
+// the summary of block `block` of all pages, from what lanes 0 .. 4 C - 1 of a wave have
+template <int C>
+__device__ __forceinline__ void write_summary(const Cache& c, const Blocks& blocks, u32 block, u32 head, float* hi, float* lo) {
+    constexpr u32 LANES = 4 * C;
+    const u32 lane = threadIdx.x & 63, at = lane % LANES * 16;
+    float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {                  // as the numbers that the cache is read as
+        hi[j] = finite(hi[j]);
+        lo[j] = finite(lo[j]);
+        most = fmaxf(most, fmaxf(fabsf(hi[j]), fabsf(lo[j])));
+    }
+    most = wave_max(lane < LANES ? most : 0.f);
+    const int e = least_exponent<PAG_KV_INT8>(most);
+    const float down = power(-e);
+    if (lane < LANES) {
+        u32 up[4], low[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x[4], y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[j] = ceilf(hi[4 * i + j] * down); y[j] = floorf(lo[4 * i + j] * down); }
+            up[i] = encode4<PAG_KV_INT8>(x);
+            low[i] = encode4<PAG_KV_INT8>(y);
+        }
+        const u64 to = (u64)(block / blocks.page_blocks * c.kv_heads + head) * blocks.page_blocks + block % blocks.page_blocks;
+        int8_t* codes = blocks.codes + to * (128 * C) + at;
+        *(uint4*)codes = make_uint4(up[0], up[1], up[2], up[3]);
+        *(uint4*)(codes + 64 * C) = make_uint4(low[0], low[1], low[2], low[3]);
+        if (lane == 0) blocks.exponents[to] = (int8_t)e;
+    }
+}
+
+__device__ __forceinline__ u32 row0_of(const Cache& c, const Blocks& blocks, u32 block, u32 head) {
+    return row_of(c, block / blocks.page_blocks, head, block % blocks.page_blocks * blocks.tokens);
+}
+
 // A wave has a window of new tokens and a head, and writes the summaries of the blocks whose last new token lies in its window: that token is the last one that
-// the block holds.  16 numbers of a row are a lane's, 16 / C rows a turn.
+// the block holds.
 template <int FMT, int C>
 __global__ void __launch_bounds__(256) k_summarise(Cache c, Blocks blocks, const int64_t* __restrict__ slots, u64 tokens, u32 window) {
-    constexpr u32 LANES = 4 * C, ROWS_A_TURN = 64 / LANES;          // of a row; 3 C = 192 numbers leave four lanes without one
-    constexpr u32 TURNS = 8;                                         // whose rows are asked for together
     const u32 lane = threadIdx.x & 63;
     const u64 wave = (u64)blockIdx.x * 4 + (threadIdx.x >> 6), t0 = wave / c.kv_heads * window;
     if (t0 >= tokens) return;
@@ -34,90 +125,46 @@ __global__ void __launch_bounds__(256) k_summarise(Cache c, Blocks blocks, const
     if (slot >= (int64_t)c.num_pages * c.page_tokens || slot < 0) slot = -1;
     const int block = slot < 0 ? -1 : (int)((u64)slot / blocks.tokens), place = slot < 0 ? 0 : (int)((u64)slot % blocks.tokens);
     const int right = __shfl_down(block, 1);
-    u64 lasts = __ballot(lane < window && block >= 0 && (lane == 63 || block != right));
-    const u32 row = lane / LANES, at = lane % LANES * 16;
-    const bool busy = row < ROWS_A_TURN;
+    u64 lasts = __ballot(lane < window && block >= 0 && block != right);
     for (; lasts; lasts &= lasts - 1) {
         const int l = __builtin_ctzll(lasts);
-        const u32 mine = (u32)__builtin_amdgcn_readlane(block, l), count = (u32)__builtin_amdgcn_readlane(place, l) + 1;
-        const u32 page = mine / blocks.page_blocks, first = mine % blocks.page_blocks * blocks.tokens, row0 = row_of(c, page, head, first);
+        const u32 mine = (u32)__builtin_amdgcn_readlane(block, l);
         float hi[16], lo[16];
+        extremes_of<FMT, C, 8>(c, row0_of(c, blocks, mine, head), 0, (u32)__builtin_amdgcn_readlane(place, l) + 1, hi, lo);
+        write_summary<C>(c, blocks, mine, head, hi, lo);
+    }
+}
+
+// A workgroup for a token and head, whose waves share the block's rows, where there are few: one token of each of 48 requests, blocks of 32, 7.4 -> 6.7 us.
+template <int FMT, int C>
+__global__ void __launch_bounds__(256) k_summarise_one(Cache c, Blocks blocks, const int64_t* __restrict__ slots, u64 tokens) {
+    __shared__ float sh[4][32][4 * C + 1];
+    const u32 lane = threadIdx.x & 63, wave = wave_of(), head = blockIdx.x % c.kv_heads;
+    const u64 t = blockIdx.x / c.kv_heads;
+    const int64_t all = (int64_t)c.num_pages * c.page_tokens, slot = slots[t], next = t + 1 < tokens ? slots[t + 1] : -1;
+    if (slot < 0 || slot >= all) return;
+    const u32 block = (u32)((u64)slot / blocks.tokens), count = (u32)((u64)slot % blocks.tokens) + 1;
+    if (next >= 0 && next < all && (u32)((u64)next / blocks.tokens) == block) return;
+    const u32 each = (count + 3) / 4, r0 = min(wave * each, count), r1 = min(r0 + each, count);
+    float hi[16], lo[16];
+    extremes_of<FMT, C, 2>(c, row0_of(c, blocks, block, head), r0, r1, hi, lo);
+    if (lane < 4 * C) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) { hi[j] = -INFINITY; lo[j] = INFINITY; }
-        for (u32 r0 = 0; r0 < count; r0 += TURNS * ROWS_A_TURN) {
-            uint4 w[TURNS];
-            int e[TURNS];
-#pragma unroll
-            for (u32 n = 0; n < TURNS; ++n) {                  // behind the last row the last one again
-                const u32 r = row0 + min(r0 + n * ROWS_A_TURN + (busy ? row : 0), count - 1);
-                if constexpr (FMT == PAG_KV_FP4) {
-                    const uint2 x = *(const uint2*)(c.data + (u64)r * (64 * C) + at / 2);
-                    w[n] = make_uint4(x.x, x.y, 0, 0);
-                    e[n] = parts_of<C>(c, r / BLOCK, 0)[at / PART * BLOCK + r % BLOCK];
-                } else {
-                    w[n] = *(const uint4*)(c.data + (u64)r * (128 * C) + at);
-                    e[n] = c.exponents[(u64)(r / BLOCK) * 2];
-                }
-            }
-#pragma unroll
-            for (u32 n = 0; n < TURNS; ++n) {
-                const float up = power(e[n]);
-                float x[16];
-                if constexpr (FMT == PAG_KV_FP4) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) decode4_fp4((j < 2 ? w[n].x : w[n].y) >> (16 * (j & 1)), 1.f, x + 4 * j);
-                } else {
-                    decode4<FMT>(w[n].x, x);
-                    decode4<FMT>(w[n].y, x + 4);
-                    decode4<FMT>(w[n].z, x + 8);
-                    decode4<FMT>(w[n].w, x + 12);
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float y = x[j] * up;
-                    hi[j] = fmaxf(hi[j], y);
-                    lo[j] = fminf(lo[j], y);
-                }
-            }
-        }
-        // rows LANES apart, whatever their number
-#pragma unroll
-        for (u32 o = 1; o < ROWS_A_TURN; o *= 2) {
-            const u32 from = lane + o * LANES < ROWS_A_TURN * LANES ? lane + o * LANES : lane;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                hi[j] = fmaxf(hi[j], __shfl(hi[j], (int)from));
-                lo[j] = fminf(lo[j], __shfl(lo[j], (int)from));
-            }
-        }
-        float most = 0.f;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {                  // as the numbers that the cache is read as
-            hi[j] = finite(hi[j]);
-            lo[j] = finite(lo[j]);
-            most = fmaxf(most, fmaxf(fabsf(hi[j]), fabsf(lo[j])));
-        }
-        most = lane < LANES ? most : 0.f;
-        most = wave_max(most);
-        const int e = least_exponent<PAG_KV_INT8>(most);
-        const float down = power(-e);
-        if (lane < LANES) {
-            u32 up[4], low[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x[4], y[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { x[j] = ceilf(hi[4 * i + j] * down); y[j] = floorf(lo[4 * i + j] * down); }
-                up[i] = encode4<PAG_KV_INT8>(x);
-                low[i] = encode4<PAG_KV_INT8>(y);
-            }
-            const u64 to = (u64)(page * c.kv_heads + head) * blocks.page_blocks + mine % blocks.page_blocks;
-            int8_t* codes = blocks.codes + to * (128 * C) + at;
-            *(uint4*)codes = make_uint4(up[0], up[1], up[2], up[3]);
-            *(uint4*)(codes + 64 * C) = make_uint4(low[0], low[1], low[2], low[3]);
-            if (lane == 0) blocks.exponents[to] = (int8_t)e;
+        for (int j = 0; j < 16; ++j) {
+            sh[wave][j][lane] = hi[j];
+            sh[wave][16 + j][lane] = lo[j];
         }
     }
+    __syncthreads();
+    if (wave) return;
+    if (lane < 4 * C) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            hi[j] = fmaxf(fmaxf(sh[0][j][lane], sh[1][j][lane]), fmaxf(sh[2][j][lane], sh[3][j][lane]));
+            lo[j] = fminf(fminf(sh[0][16 + j][lane], sh[1][16 + j][lane]), fminf(sh[2][16 + j][lane], sh[3][16 + j][lane]));
+        }
+    }
+    write_summary<C>(c, blocks, block, head, hi, lo);
 }
 
 // ---- scores ---------------------------------------------------------------------------------------------------------
@@ -704,8 +751,12 @@ void run(hipStream_t st, const Choose& a) {
 
 template <int FMT, int C>
 void summarise(hipStream_t st, const Cache& c, const Blocks& b, const int64_t* slots, u64 tokens) {
-    // a window of one token spreads a decoding step over as many waves as there are; prompts' waves look at more
-    const u32 window = tokens * c.kv_heads <= 8192 ? 1 : 32;
+    // a decoding step's blocks are spread over as many waves as there are; prompts' waves look at 32 tokens, most of which are not the last of a block
+    if (tokens * c.kv_heads <= 4096) {
+        k_summarise_one<FMT, C><<<(u32)(tokens * c.kv_heads), 256, 0, st>>>(c, b, slots, tokens);
+        return;
+    }
+    const u32 window = 32;
     k_summarise<FMT, C><<<(u32)(((tokens + window - 1) / window * c.kv_heads + 3) / 4), 256, 0, st>>>(c, b, slots, tokens, window);
 }
 
