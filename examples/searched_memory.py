@@ -1,4 +1,4 @@
-"""A memory that is searched: one attention layer whose long context lies in an 8-bit cache and is read through PAG searches.
+"""A memory that is searched: one attention layer whose long context lies in a cache of 8 or 4 bits and is read through PAG searches.
 
 The context's keys are written into the cache, read back as the numbers that the cache holds, and indexed, one index for each
 key/value head.  A decoding step then gives every request a new token: its key and value are appended, its queries are searched, and attention
@@ -109,7 +109,7 @@ if __name__ == "__main__":
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     p.add_argument("--tokens", type=int, default=20_000)
     p.add_argument("--steps", type=int, default=64)
-    p.add_argument("--format", default="int8", choices=("int8", "fp8"))
+    p.add_argument("--format", default="int8", choices=("int8", "fp8", "fp4"))
     a = p.parse_args()
     share, error = run(a.tokens, a.steps, a.format)
     print("read %.4f of the softmax weight, outputs differ from attention over all %d tokens by %.4f (root mean square)" % (share, a.tokens, error))

@@ -321,7 +321,7 @@ int pag_searcher_free(pag_searcher* s);
  * A cache of 4 bits a number (PAG_KV_FP4: a sign, 2 exponent and 1 mantissa bits: 0, 1/2, 1, 3/2, 2, 3, 4, 6) has rows of W / 2 bytes, number 2 i in the
  * low bits of byte i and number 2 i + 1 above it, and an exponent per 32 numbers of a row, those of 16 tokens side by side:
  *     data      uint8 [num_pages][kv_heads][page_tokens][2][W / 2]
- *     exponents int8  [num_pages][kv_heads][page_tokens / 16][2][W / 32][16]
+ *     exponents int8  [num_pages][kv_heads][page_tokens / 16][2][W / 32][16]            exponents of -64 to 126
  */
 typedef enum { PAG_KV_INT8 = 0, PAG_KV_FP8 = 1, PAG_KV_FP4 = 4 } pag_kv_format;
 typedef enum { PAG_F32 = 0, PAG_F16 = 1, PAG_BF16 = 2 } pag_dtype;
@@ -462,7 +462,8 @@ int pag_kv_append_rotated(const pag_kv_cache* cache, uint32_t dtype, const void*
  * A token that finds nothing to attend to gets zeros and an lse of -inf; so does padding.
  * Sums, maxima and scores are held in 32 bits.  Rounded to 16-bit floats (11 bits) are the softmax weights for their product with the values,
  * together with the values' scale: what lies below 2^-31 of a row's largest weight * 2^exponent is lost from out, not from lse or from the sum
- * that out is divided by; and q, as multiples of 2^-32 of its row's largest magnitude at least.
+ * that out is divided by; and q, as multiples of 2^-32 of its row's largest magnitude at least.  Of PAG_KV_FP4 keys and values are multiples of 2^-24 of the largest
+ * power of two among the parts of 16 tokens (of listed keys among their own): numbers whose part's power of two is within 2^-22 of that are held exactly.
  */
 int pag_kv_workspace_bytes(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_attention* args, int selected, uint32_t id_heads,
                            uint32_t k, uint64_t* bytes);

@@ -724,8 +724,12 @@ __global__ void __launch_bounds__(64 * WAVES) k_pick(Choose a) {
     pick_long<WAVES, HELD>(a.keys + (u64)blockIdx.x * a.most_blocks, x.blocks, a.k, a.ids + (int64_t)t * a.ids_ts + (int64_t)list * a.ids_hs);
 }
 
-// One workgroup for all of a list, or parts of it and a second kernel.
-bool choose_whole(const Choose& a) { return a.most_blocks <= MOST_SHORT && (u64)(a.id_heads / a.c.kv_heads) * a.most_blocks * 4 <= 61440; }
+// One workgroup for all lists of a head, or parts of them and a second kernel, where a wave's registers do not last for a list's keys, or LDS for all lists'
+// (64 KB, of which the queries take up to 8.5).
+bool choose_whole(const Choose& a) {
+    static_assert(sizeof(SharedQueries<4>) <= 9 * 1024, "queries and keys share 64 KB");
+    return a.most_blocks <= MOST_SHORT && (u64)(a.id_heads / a.c.kv_heads) * a.most_blocks * 4 <= 55 * 1024;
+}
 
 template <int C, bool MANY>
 void launch(hipStream_t st, const Choose& a, const Columns& columns) {

@@ -493,6 +493,7 @@ class KvBlocks:
         self._b = _Blocks(C.sizeof(_Blocks), self.block_tokens,
                           _array(codes, torch.int8, (cache.num_pages, cache.kv_heads, per, 2, -(-cache.head_dim // 64) * 64), cache.device, "codes"),
                           _array(exponents, torch.int8, (cache.num_pages, cache.kv_heads, per), cache.device, "exponents"))
+        _check(load_library().pag_kv_blocks_update(C.byref(cache._c), C.byref(self._b), None, C.c_uint64(0), None), "KvBlocks")      # of nothing: looks them over
         self.codes, self.exponents = codes, exponents
 
     def update(self, slots):

@@ -173,6 +173,26 @@ def test_select_by_every_path(kv, wide_table, k):
     select_case(kv, [9000, 3000, 33, 1600], 4, 2, 4, 64, 32, 16, k, 100, "int8", "bf16", wide_table=wide_table, edges=True)
 
 
+@pytest.mark.parametrize("dim, heads, wide_table", [(256, 15, 900), (256, 14, 900), (64, 16, 800), (192, 14, 990)])
+def test_select_of_as_many_lists_as_fit(kv, dim, heads, wide_table):
+    """Keys of all lists of a head that just fit LDS, or just do not."""
+    select_case(kv, [1500, 333], heads, 1, heads, dim, 16, 16, 7, 5, "fp4", "fp16", wide_table=wide_table)
+
+
+def test_pages_that_do_not_exist(kv):
+    """Page numbers out of range count as absent, in lists and in the window; requests and positions out of range read nothing."""
+    m = Memory(kv, [128, 40, 40], 1, 64, 32, "int8", 4)
+    table = m.table.copy()
+    table[0, 1], table[0, 3] = m.pages, -5
+    step = kv.KvStep(ints(table), requests=ints([0, 7, 2, -3]), positions=ints([127, 39, 2_000_000_000, 5]))
+    q = torch.randn(4, 2, 64).to(torch.bfloat16)
+    blocks = kv.KvBlocks(m.cache, 32)
+    out, lse = blocks.attend(q.cuda(), ints(np.tile(np.arange(-1, 5), (4, 1, 1))), step, window=10)
+    keys = lambda t, h: np.concatenate([np.arange(32), np.arange(64, 96)])
+    check_attention(m, q, out, lse, "bf16", [0, 0, 0, 0], [127, -1, -1, -1], keys, 64 ** -0.5)
+    assert (blocks.select(q.cuda(), step, 4)[1:] == -1).all() and blocks.select(q.cuda(), step, 4)[0, 0].tolist() == [0, 2, -1, -1]
+
+
 def test_select_of_many_equal_scores(kv):
     """Keys that repeat from block to block: the first blocks of those that are equal."""
     dim, page = 64, 64

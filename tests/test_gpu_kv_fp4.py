@@ -216,3 +216,47 @@ def test_rows_beyond_32_bits_of_offset(kv):
     a, b = kv.KvStep(ints([order]), ints([0, 1]), ints([250]), ints([0]), ints([249])), kv.KvStep(ints([[0, 1, 2, 3]]), ints([0, 1]), ints([250]), ints([0]), ints([249]))
     assert all(torch.equal(x, y) for x, y in zip(cache.attend(q, a), small.attend(q, b)))
     assert all(torch.equal(x, y) for x, y in zip(cache.attend_selected(q, ids, a), small.attend_selected(q, ids, b)))
+
+
+@pytest.mark.parametrize("max_new, n", [(1, 1), (20, 4), (300, 40)])
+def test_the_largest_numbers_stay_finite(kv, max_new, n):
+    """Values of 3e38 are held as 4 * 2^126, which is read, and averaged, as the largest finite bf16; averages of them and their negatives are finite."""
+    dim, page, context = 64, 16, 100
+    cache = kv.KvCache(7, 1, dim, page, "fp4")
+    k, v = torch.randn(context, 1, dim, device="cuda"), torch.full((context, 1, dim), 3.0e38, device="cuda")
+    v[:, :, 1::2] *= -1
+    v[::2, :, 32:] *= -1
+    slots = torch.arange(context, device="cuda")
+    cache.append(k, v, slots)
+    step = kv.KvStep(ints([[0, 1, 2, 3, 4, 5, 6]]), ints([0, n]), ints([context]), ints([0] * n), ints(range(context - n, context)), max_new=max_new)
+    q = torch.randn(n, 2, dim, device="cuda").to(torch.bfloat16)
+    ids = slots.expand(n, 1, context).contiguous()
+    for out, lse in (cache.attend(q, step), cache.attend_selected(q, ids, step)):
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+        assert (out[..., 0:32:2] == 255.0 * 2.0 ** 120).all() and (out[..., 1:32:2] == -255.0 * 2.0 ** 120).all()
+
+
+def test_rows_with_infinities_and_nan_spoil_only_themselves(kv):
+    m = Memory(kv, [50, 90], 2, 64, 32, "fp4", 4)
+    q = torch.randn(4, 4, 64).half()
+    step = kv.KvStep(ints(m.table), offsets=ints([0, 2, 4]), context=ints([50, 90]), requests=ints([0, 0, 1, 1]), positions=ints([48, 49, 88, 89]))
+    ids = ints(np.tile(np.arange(3), (4, 2, 1)))
+    blocks = kv.KvBlocks(m.cache, 16)
+    clean = m.cache.attend(q.cuda(), step), blocks.attend(q.cuda(), ids, step, window=9)
+    q[0, 1, 5], q[3, 2, 0], q[2, 0, 7] = math.nan, math.inf, -math.inf
+    spoilt = torch.zeros(4, 4, dtype=torch.bool)
+    spoilt[0, 1] = spoilt[3, 2] = spoilt[2, 0] = True
+    for (out, lse), before in zip((m.cache.attend(q.cuda(), step), blocks.attend(q.cuda(), ids, step, window=9)), clean):
+        assert torch.isnan(out.cpu()[spoilt]).all()
+        assert torch.equal(out.cpu()[~spoilt], before[0].cpu()[~spoilt]) and torch.equal(lse.cpu()[~spoilt], before[1].cpu()[~spoilt])
+
+
+def test_the_example_in_4_bits():
+    """It runs, reads what was found and the window, and its share of the weight is a share."""
+    import importlib.util
+    import os
+    spec = importlib.util.spec_from_file_location("searched_memory", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "searched_memory.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    share, error = example.run(3000, 5, "fp4")
+    assert 0.0 < share <= 1.0 + 2.0 ** -10 and math.isfinite(error)
