@@ -654,7 +654,7 @@ __device__ __forceinline__ void pick_long(const u32* keys, u32 n, u32 k, int32_t
 
 // A workgroup for a token and key/value head: scores into LDS, then a wave a list.  MANY: several tiles of columns.
 template <int C, int NW, bool MANY>
-__global__ void __launch_bounds__(64 * NW, C <= 2 ? 4 : 2) k_choose(Choose a, Columns columns, u32 room) {
+__global__ void __launch_bounds__(64 * NW, C <= 2 && !MANY ? 4 : 2) k_choose(Choose a, Columns columns, u32 room) {
     extern __shared__ u32 sh_keys[];
     const u32 t = blockIdx.x / a.c.kv_heads, kv_head = blockIdx.x % a.c.kv_heads, wave = wave_of(), lists = a.group / columns.heads;
     u32 blocks;

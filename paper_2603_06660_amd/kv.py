@@ -71,8 +71,8 @@ def _gpu(device):
 
 
 def _no_graph(t, what):
-    """The cache is 8 bits, written once, and its calls have no backward: a graph that ends here would be a silent zero."""
-    if t.requires_grad and torch.is_grad_enabled():
+    """The cache is 8 or 4 bits, written once, and its calls have no backward: a graph that ends here would be a silent zero."""
+    if torch.is_grad_enabled():
         raise PagError("%s requires a gradient, and the cache has no backward: detach it, or call under torch.no_grad()" % what)
 
 
@@ -80,18 +80,27 @@ def _array(t, dtype, shape, device, what):
     """The address of a dense tensor of this type, shape and device."""
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise PagError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
-    _no_graph(t, what)
+    if t.requires_grad:
+        _no_graph(t, what)
     return t.data_ptr()
 
 
 def _rows(t, shape, device, what, dtypes=_DTYPES):
-    """Checks a [tokens, heads, dim] tensor whose last dimension is dense; the other strides are free."""
+    """Checks a [tokens, heads, dim] tensor whose last dimension is dense; the other strides are free. -> its address, those two strides."""
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.shape != shape or t.device != device:
         raise PagError("%s must be a tensor of shape %s on %s, of type %s" %
                        (what, tuple(shape), device, ", ".join(str(x) for x in dtypes)))
-    if t.stride(2) != 1 and t.shape[2] > 1:
+    token, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
         raise PagError("%s: the last dimension must be dense" % what)
-    _no_graph(t, what)
+    if t.requires_grad:
+        _no_graph(t, what)
+    return t.data_ptr(), token, head
+
+
+def _empty_rows(like):
+    """A dense tensor of the same shape and type."""
+    return torch.empty_like(like) if like.is_contiguous() else torch.empty_like(like, memory_format=torch.contiguous_format)
 
 
 # the number of a GPU's current stream, without an object around it where torch offers that
@@ -325,18 +334,18 @@ class KvCache:
         """Writes k and v [tokens, kv_heads, head_dim] (float32, float16 or bfloat16) into slots (int64 [tokens], -1: left out)."""
         tokens = slots.shape[0]
         shape = (tokens, self.kv_heads, self.head_dim)
-        _rows(k, shape, self.device, "k")
-        _rows(v, shape, self.device, "v", (k.dtype,))
-        _call("pag_kv_append", self.device, C.addressof(self._c), _DTYPES[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
-              v.stride(0), v.stride(1), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens)
+        keys = _rows(k, shape, self.device, "k")
+        values = _rows(v, shape, self.device, "v", (k.dtype,))
+        _call("pag_kv_append", self.device, C.addressof(self._c), _DTYPES[k.dtype], *keys, *values,
+              _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens)
 
     def append_rotated(self, k, v, slots, positions, rotation, q=None, out=None):
         """append() of k turned by `rotation` (a KvRotation) at positions (int32 [tokens]; a step's, or others) and of v as it is.
         -> q [tokens, heads, head_dim], of k's type, turned likewise: a new tensor, or `out` (q itself: in place); None if there is no q."""
         tokens = slots.shape[0]
         shape = (tokens, self.kv_heads, self.head_dim)
-        _rows(k, shape, self.device, "k")
-        _rows(v, shape, self.device, "v", (k.dtype,))
+        keys = _rows(k, shape, self.device, "k")
+        values = _rows(v, shape, self.device, "v", (k.dtype,))
         if not isinstance(rotation, KvRotation) or rotation.device != self.device:
             raise PagError("rotation must be a KvRotation on %s" % self.device)
         r = _Rotation(C.sizeof(_Rotation), _PAIRS[rotation.pairs], rotation.turned, 0, rotation._where,
@@ -348,16 +357,13 @@ class KvCache:
             if not isinstance(q, torch.Tensor) or q.dim() != 3:
                 raise PagError("q must be a tensor [tokens, heads, head_dim]")
             rows = (tokens, q.shape[1], self.head_dim)
-            _rows(q, rows, self.device, "q", (k.dtype,))
+            r.q, r.q_token_stride, r.q_head_stride = _rows(q, rows, self.device, "q", (k.dtype,))
             if out is None:
-                out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            else:
-                _rows(out, rows, self.device, "out", (k.dtype,))
-            r.heads = q.shape[1]
-            r.q, r.q_token_stride, r.q_head_stride = q.data_ptr(), q.stride(0), q.stride(1)
-            r.out, r.out_token_stride, r.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
-        _call("pag_kv_append_rotated", self.device, C.addressof(self._c), _DTYPES[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
-              v.stride(0), v.stride(1), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens, C.addressof(r))
+                out = _empty_rows(q)
+            r.out, r.out_token_stride, r.out_head_stride = _rows(out, rows, self.device, "out", (k.dtype,))
+            r.heads = rows[1]
+        _call("pag_kv_append_rotated", self.device, C.addressof(self._c), _DTYPES[k.dtype], *keys, *values,
+              _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens, C.addressof(r))
         return out
 
     def read(self, slots, dtype=torch.float32, out=None):
@@ -366,7 +372,8 @@ class KvCache:
         tokens = slots.shape[0]
         shape = (tokens, self.kv_heads, self.head_dim)
         if out is None:
-            out = (torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device))
+            k = torch.empty(shape, dtype=dtype, device=self.device)
+            out = (k, torch.empty_like(k))
         k, v = out
         some = k if k is not None else v
         if some is None:
@@ -379,39 +386,38 @@ class KvCache:
             if t is None:
                 args += [None, 0, 0]
             else:
-                _rows(t, shape, self.device, what, (dtype,))
-                args += [t.data_ptr(), t.stride(0), t.stride(1)]
+                args += _rows(t, shape, self.device, what, (dtype,))
         _call("pag_kv_read", self.device, C.addressof(self._c), _array(slots, torch.int64, (tokens,), self.device, "slots"), tokens, _DTYPES[dtype], *args)
         return k, v
 
     def _queries(self, q, step, window):
-        """Checks what every call over a step looks at."""
+        """Checks what every call over a step looks at. -> q's address and strides."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise PagError("q must be a tensor [tokens, heads, head_dim]")
         if q.shape[2] != self.head_dim:
             raise PagError("q has rows of %d numbers, the cache of %d" % (q.shape[2], self.head_dim))
-        _rows(q, q.shape, self.device, "q", _ROW_DTYPES)
+        rows = _rows(q, q.shape, self.device, "q", _ROW_DTYPES)
         if step.table is not None and step.device != self.device:
             raise PagError("the step is on %s, the cache on %s" % (step.device, self.device))
         if not 0 <= window < 1 << 31:
             raise PagError("window must be between 0 and 2^31 - 1")
+        return rows
 
     def _attention(self, q, step, scale, window, softcap, slopes, out, id_heads=0, k=-1, block=0):
         """Checks a call's tensors -> out, its arguments, and its workspace, which has to live until the call is made."""
-        self._queries(q, step, window)
+        queries = self._queries(q, step, window)
         tokens, heads, dim = shape = q.shape
         device = self.device
         if out is None:
-            o, lse = out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty((tokens, heads), dtype=torch.float32, device=device)
+            o, lse = out = _empty_rows(q), torch.empty((tokens, heads), dtype=torch.float32, device=device)
         else:
             o, lse = out
-            _rows(o, shape, device, "out", (q.dtype,))
             if lse is not None:
                 _array(lse, torch.float32, (tokens, heads), device, "lse")
         s = step._with(tokens)
         a = _Attention(C.sizeof(_Attention), _DTYPES[q.dtype], heads, window, dim ** -0.5 if scale is None else scale, softcap,
                        None if slopes is None else _array(slopes, torch.float32, (heads,), device, "slopes"),
-                       q.data_ptr(), q.stride(0), q.stride(1), o.data_ptr(), o.stride(0), o.stride(1), None if lse is None else lse.data_ptr())
+                       *queries, *_rows(o, shape, device, "out", (q.dtype,)), None if lse is None else lse.data_ptr())
         return out, a, self._room(a, s, (tokens, heads, window, s.requests, s.max_new, s.max_pages, id_heads, k, block), id_heads, k, block)
 
     def _room(self, a, s, key, id_heads, k, block=0, select=False):
@@ -505,7 +511,7 @@ class KvBlocks:
         """-> int32 [tokens, id_heads, k]: for each token the k blocks of the best scores among those that begin before its last `window` tokens.
         id_heads: lists of a token, kv_heads if not given, else as attend_selected takes them; a list's heads share it by the largest of their scores."""
         c = self.cache
-        c._queries(q, step, window)
+        queries = c._queries(q, step, window)
         if step.requests is None or step.positions is None:
             raise PagError("select needs the step's requests and positions")
         tokens, heads = q.shape[:2]
@@ -519,8 +525,7 @@ class KvBlocks:
                 (k > 1 and out.stride(2) != 1):
             raise PagError("out must be an int32 tensor [tokens, id_heads, k] on %s whose last dimension is dense" % c.device)
         s = step._with(tokens)
-        a = _Attention(struct_size=C.sizeof(_Attention), dtype=_DTYPES[q.dtype], heads=heads, window=window, q=q.data_ptr(), q_token_stride=q.stride(0),
-                       q_head_stride=q.stride(1))
+        a = _Attention(C.sizeof(_Attention), _DTYPES[q.dtype], heads, window, 0.0, 0.0, None, *queries)
         room = c._room(a, s, ("select", tokens, heads, window, s.requests, s.max_pages, id_heads, k, self.block_tokens), id_heads, k, self.block_tokens, True)
         _call("pag_kv_blocks_select", c.device, C.addressof(c._c), C.addressof(self._b), C.addressof(s), C.addressof(a), id_heads, k, out.data_ptr(),
               out.stride(0), out.stride(1))
