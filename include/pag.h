@@ -429,7 +429,7 @@ int pag_kv_read(const pag_kv_cache* cache, const int64_t* slots, uint64_t tokens
  * Of the first `turned` numbers of a row at position p each pair (x, y), numbers i and i + turned / 2 or 2 i and 2 i + 1, becomes
  * (x cos a - y sin a, y cos a + x sin a) with the angle a = p * frequencies[i], a product in 64 bits.  Keys are turned in 64 bits where angles are below 2^31 in
  * magnitude, so that what is held is rounded once; queries in 32 bits, by cosines and sines of 64 bits that are rounded to 32, and rounded to their type.
- * A pair with an infinity or NaN becomes whatever these formulas give.
+ * A pair with an infinity or NaN becomes whatever these formulas give.  At most 2^24 tokens and 65536 heads a call, tokens * heads below 2^31.
  */
 typedef enum { PAG_KV_HALVES = 0, PAG_KV_NEIGHBOURS = 1 } pag_kv_pairs;
 
@@ -488,8 +488,10 @@ typedef struct {
 } pag_kv_blocks;
 
 /*
- * pag_kv_blocks_update: after pag_kv_append of these slots (dev int64 [tokens]; the same rules): writes the summaries of the blocks that they lie in, of all tokens
- * from the block's first one to the last one in the call, which has to be the last one that the block holds.
+ * pag_kv_blocks_update: after pag_kv_append of these slots (dev int64 [tokens]; -1 or out of range: left out): writes the summaries of the blocks that they lie in,
+ * of all tokens from the block's first one to the last one in the call, which has to be the last one that the block holds.  The tokens of one of these blocks
+ * have to follow each other in the call, in ascending order, with no other ones and none that are left out between them, as pag_kv_extend numbers them, also of a PAG_KV_FP4 cache:
+ * otherwise several waves write its summary, and what it holds then is not defined.  tokens * kv_heads below 2^27.
  * pag_kv_blocks_select: for each token and list the k best of the blocks that begin before the token's window (args->window; 0: up to the token itself), of a list's heads by the
  * largest of their scores, of equal ones the first; their numbers in ascending order, -1 behind them (dev int32 [tokens][id_heads][k], strides in elements, last dimension dense).
  * Blocks in pages that are none are left out.  id_heads as in pag_kv_attend_selected.  Of args it reads dtype, heads, window, q and its strides,

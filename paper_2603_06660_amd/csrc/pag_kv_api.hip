@@ -248,8 +248,9 @@ extern "C" int pag_kv_append_rotated(const pag_kv_cache* cache, uint32_t dtype, 
         PAG_CHECK(r->struct_size == sizeof(pag_kv_rotation), PAG_EINVAL, "pag_kv_rotation.struct_size does not match this library");
         PAG_CHECK(r->pairs <= PAG_KV_NEIGHBOURS, PAG_EINVAL, "unknown pairs");
         PAG_CHECK(r->turned > 0 && r->turned % 8 == 0 && r->turned <= a.c.dim, PAG_EUNSUPPORTED, "this build needs turned % 8 == 0 and 0 < turned <= head_dim");
-        PAG_CHECK(tokens < (1ull << 25) && r->heads <= 65536 && tokens * r->heads < (1ull << 31), PAG_EUNSUPPORTED,
-                  "tokens must be below 2^25, heads at most 65536, tokens * heads below 2^31");
+        // of 4-bit codes as many workgroups turn queries as write rows, and a launch has fewer than 2^32 threads
+        PAG_CHECK(tokens <= (1ull << 24) && r->heads <= 65536 && tokens * r->heads < (1ull << 31), PAG_EUNSUPPORTED,
+                  "tokens must be at most 2^24, heads at most 65536, tokens * heads below 2^31");
         if (tokens == 0) return PAG_OK;
         PAG_CHECK(r->frequencies && r->positions && aligned(r->frequencies, 4) && aligned(r->positions, 4), PAG_EINVAL,
                   "frequencies or positions is null or not 4-byte aligned");

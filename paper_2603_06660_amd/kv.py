@@ -503,7 +503,8 @@ class KvBlocks:
         self.codes, self.exponents = codes, exponents
 
     def update(self, slots):
-        """Summarises the blocks that slots (int64 [tokens], of the append before) lie in; the last of a block's tokens is the last that it holds."""
+        """Summarises the blocks that slots (int64 [tokens], of the append before) lie in.  A block's tokens stand side by side in ascending order; the last of them is
+        the last that the block holds."""
         c = self.cache
         _call("pag_kv_blocks_update", c.device, C.addressof(c._c), C.addressof(self._b), _array(slots, torch.int64, (slots.shape[0],), c.device, "slots"), slots.shape[0])
 

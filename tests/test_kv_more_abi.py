@@ -64,7 +64,7 @@ def test_wrong_rotated_calls_are_refused(kv):
     assert _append(kv, _cache(kv), None) == -1 and b"rotation is null" in lib.pag_last_error()
     assert _append(kv, _cache(kv, head_dim=12), _rotation(kv)) == -5 and _append(kv, _cache(kv), _rotation(kv), dtype=3) == -1
     assert _append(kv, _cache(kv), _rotation(kv), rows=none) == -1 and _append(kv, _cache(kv), _rotation(kv), slots=None) == -1
-    for tokens in (1 << 25, 1 << 26, 1 << 63):
+    for tokens in ((1 << 24) + 1, 1 << 25, 1 << 26, 1 << 63):
         assert _append(kv, _cache(kv, kv_heads=1), _rotation(kv), tokens=tokens) == -5
     # nothing to do: no GPU is needed
     assert _append(kv, _cache(kv), _rotation(kv, q=None, out=None, positions=None), rows=none, slots=None, tokens=0) == 0
