@@ -471,9 +471,10 @@ __device__ __forceinline__ void write_none(int32_t* ids, u32 from, u32 k, u32 th
 
 // The k largest of up to 64 R keys, the first ones of those that are equal, in their order, by a wave: the k-th largest key is found bit by bit, by counting,
 // from the first bit in which keys differ on; once exactly k keys reach what is found, the rest of the bits does not matter.  Registers without a key hold 0 and
-// are counted like the others: a branch around each costs more than its comparison.
+// are counted like the others: a branch around each costs more than its comparison.  Once the k-th is among 64 keys or fewer these go into one register,
+// by way of the keys' own place in LDS.
 template <int R>
-__device__ __forceinline__ void pick_short(const u32* keys, u32 n, u32 k, int32_t* ids) {
+__device__ __forceinline__ void pick_short(u32* keys, u32 n, u32 k, int32_t* ids) {
     const u32 lane = threadIdx.x & 63;
     u32 x[R], most = 0, least = 0xFFFFFFFFu, valid = 0;
 #pragma unroll
@@ -494,16 +495,39 @@ __device__ __forceinline__ void pick_short(const u32* keys, u32 n, u32 k, int32_
         int bit = differ ? 31 - __builtin_clz(differ) : -1;
         u32 at = bit < 0 ? most : most & ~((2u << bit) - 1);
         at = (u32)__builtin_amdgcn_readfirstlane((int)at);
-        u32 above = 0;
+        u32 above = 0, upto = valid;             // keys of at + 2^(bit + 1) and more, and of `at` and more
+        const auto step = [&](u32 count) {
+            if (count >= k) {
+                at |= 1u << bit;
+                upto = count;
+            } else {
+                above = count;
+            }
+            --bit;
+            return count == k;
+        };
         bool done = false;
-        for (; bit >= 0; --bit) {
-            const u32 to = at | 1u << bit;
+        while (!done && bit >= 0 && upto - above > 64) {
             u32 count = 0;
 #pragma unroll
-            for (int r = 0; r < R; ++r) count += (u32)__popcll(__ballot(x[r] >= to));
-            if (count >= k) at = to;
-            else above = count;
-            if (count == k) { done = true; break; }
+            for (int r = 0; r < R; ++r) count += (u32)__popcll(__ballot(x[r] >= (at | 1u << bit)));
+            done = step(count);
+        }
+        if (!done && bit >= 0) {
+            u32 found = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bool in = x[r] != 0 && x[r] >= at && (x[r] - at) >> bit < 2;
+                const u64 mask = __ballot(in);
+                if (in) keys[found + below(mask)] = x[r];
+                found += (u32)__popcll(mask);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            const u32 y = lane < found ? keys[lane] : 0u;
+            const u32 more = above;
+            while (!done && bit >= 0) done = step(more + (u32)__popcll(__ballot(y >= (at | 1u << bit))));
         }
         cut = done ? at - 1 : at;
         ties = done ? 0 : k - above;
@@ -685,7 +709,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 && !MANY ? 4 : 2) k_choose(Cho
     }
     __syncthreads();
     for (u32 list = wave; list < lists; list += NW) {
-        const u32* keys = sh_keys + list * room;
+        u32* keys = sh_keys + list * room;
         int32_t* ids = a.ids + (int64_t)t * a.ids_ts + (int64_t)(kv_head * lists + list) * a.ids_hs;
         if (blocks <= 64 * 4) pick_short<4>(keys, blocks, a.k, ids);
         else if (blocks <= 64 * 8) pick_short<8>(keys, blocks, a.k, ids);
