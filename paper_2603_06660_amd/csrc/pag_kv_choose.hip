@@ -759,7 +759,11 @@ template <int C, bool MANY>
 void launch(hipStream_t st, const Choose& a, const Columns& columns) {
     const u32 lists = a.id_heads / a.c.kv_heads;
     if (choose_whole(a)) {
-        k_choose<C, 8, MANY><<<a.s.tokens * a.c.kv_heads, 512, lists * a.most_blocks * 4, st>>>(a, columns, a.most_blocks);
+        // as many waves as have 64 blocks to score or a list to choose from
+        const u32 waves = std::max((a.most_blocks + 63) / 64, lists), grid = a.s.tokens * a.c.kv_heads, room = lists * a.most_blocks * 4;
+        if (!MANY && waves <= 2) k_choose<C, 2, false><<<grid, 128, room, st>>>(a, columns, a.most_blocks);
+        else if (!MANY && waves <= 4) k_choose<C, 4, false><<<grid, 256, room, st>>>(a, columns, a.most_blocks);
+        else k_choose<C, 8, MANY><<<grid, 512, room, st>>>(a, columns, a.most_blocks);
         return;
     }
     const u32 chunks = (a.most_blocks + CHUNK - 1) / CHUNK, grid = a.s.tokens * a.id_heads;
