@@ -251,8 +251,11 @@ constexpr u32 UNIT = SPLIT_WAVES * TILE;  // and keys of the smallest share
 // 12,000 tokens with 1, 2, 4, 8: 122, 117, 112, 117 us; heads of 64: 64, 57, 51, 54)
 constexpr u32 PIECE = 4;
 
+// whether a wave of such a call has one tile of keys at a time
+constexpr bool one_tile(u32 fmt, u32 width, int t) { return fmt == PAG_KV_FP4 && width == 192 && t == 1; }
+
 // workgroups of a CU: as many as its registers and LDS last for
-constexpr u32 groups_per_cu(u32 width, int t) { return width > 128 ? 1 : width == 64 && t == 1 ? 3 : 2; }
+constexpr u32 groups_per_cu(u32 fmt, u32 width, int t) { return width > 128 ? (one_tile(fmt, width, t) ? 2 : 1) : width == 64 && t == 1 ? 3 : 2; }
 
 // shapes of the kernel for many query rows
 constexpr u32 WROWS = 32;                 // query rows of a wave

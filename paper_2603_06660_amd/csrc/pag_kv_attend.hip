@@ -98,7 +98,7 @@ bool narrow_whole(const Attend& a, int num_cu) {
 }
 
 u64 partial_floats(const Attend& a, int num_cu) {
-    return 2ull * (u32)num_cu * groups_per_cu(a.c.width, (int)a.row_tiles) * a.row_tiles * ROWS * (a.c.width + 2);
+    return 2ull * (u32)num_cu * groups_per_cu(a.c.fmt, a.c.width, (int)a.row_tiles) * a.row_tiles * ROWS * (a.c.width + 2);
 }
 
 template <int C>
@@ -115,7 +115,7 @@ void run(hipStream_t st, const Attend& a, int num_cu) {
     } else {
         launch_narrow<PAG_KV_FP4, C>(st, a, num_cu, whole);
     }
-    if (!whole) k_join<C><<<a.s.tokens * a.heads, 256, 0, st>>>(a, num_cu * (int)groups_per_cu(64 * C, (int)a.row_tiles));
+    if (!whole) k_join<C><<<a.s.tokens * a.heads, 256, 0, st>>>(a, num_cu * (int)groups_per_cu(a.c.fmt, 64 * C, (int)a.row_tiles));
 }
 
 u64 wide_workspace(u32 width, int num_cu) {

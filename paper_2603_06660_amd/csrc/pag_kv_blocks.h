@@ -29,7 +29,7 @@ __device__ __forceinline__ void place_blocks(const Attend& a, Piece& p, u64 list
 }
 
 template <int FMT, int C, bool SLOPES, bool CAPPED>
-__global__ void __launch_bounds__(256, groups_per_cu(64 * C, 1)) k_attend_blocks(Attend a, u32 units, u32 tiles) {
+__global__ void __launch_bounds__(256, groups_per_cu(FMT, 64 * C, 1)) k_attend_blocks(Attend a, u32 units, u32 tiles) {
     __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
     const u32 cost = units + PIECE;
     const u64 total = (u64)a.s.tokens * a.id_heads * tiles * cost;
@@ -87,7 +87,7 @@ void run_blocks(hipStream_t st, const Attend& a, int num_cu, bool whole) {
     }
     // the window may begin anywhere in a block of 16
     const u32 keys = a.k * a.block + (a.window ? a.window + BLOCK - 1 : 0), units = std::max<u32>((keys + UNIT - 1) / UNIT, 1);
-    const u32 grid = (u32)num_cu * groups_per_cu(64 * C, 1);
+    const u32 grid = (u32)num_cu * groups_per_cu(FMT, 64 * C, 1);
     if (a.slopes) k_attend_blocks<FMT, C, true, CAPPED><<<grid, 256, 0, st>>>(a, units, tiles);
     else k_attend_blocks<FMT, C, false, CAPPED><<<grid, 256, 0, st>>>(a, units, tiles);
 }

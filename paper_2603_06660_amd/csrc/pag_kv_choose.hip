@@ -15,6 +15,7 @@ typedef int int4_t __attribute__((ext_vector_type(4)));
 
 constexpr u32 CHUNK = 256;                  // blocks that a workgroup scores where a list goes to several
 constexpr u32 MOST_SHORT = 1024;            // keys of a list that a wave holds in registers
+constexpr u32 QUEUE = 1024;                 // workgroups that are too many to run at once
 
 // ---- summaries ------------------------------------------------------------------------------------------------------
 
@@ -759,8 +760,9 @@ template <int C, bool MANY>
 void launch(hipStream_t st, const Choose& a, const Columns& columns) {
     const u32 lists = a.id_heads / a.c.kv_heads;
     if (choose_whole(a)) {
-        // as many waves as have 64 blocks to score or a list to choose from
-        const u32 waves = std::max((a.most_blocks + 63) / 64, lists), grid = a.s.tokens * a.c.kv_heads, room = lists * a.most_blocks * 4;
+        // As many waves as have 64 blocks to score or a list to choose from; where workgroups queue, a wave for 256 blocks, in us: 1,024 tokens of 4 requests and
+        // 8 heads, 129 blocks 52, 41, 257 blocks 115, 68, 938 blocks 258, 224; 512 requests and 4 heads of up to 313 blocks 40, 32
+        const u32 grid = a.s.tokens * a.c.kv_heads, each = grid >= QUEUE ? 256 : 64, waves = std::max((a.most_blocks + each - 1) / each, lists), room = lists * a.most_blocks * 4;
         if (!MANY && waves <= 2) k_choose<C, 2, false><<<grid, 128, room, st>>>(a, columns, a.most_blocks);
         else if (!MANY && waves <= 4) k_choose<C, 4, false><<<grid, 256, room, st>>>(a, columns, a.most_blocks);
         else k_choose<C, 8, MANY><<<grid, 512, room, st>>>(a, columns, a.most_blocks);

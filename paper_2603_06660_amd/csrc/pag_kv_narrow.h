@@ -75,7 +75,7 @@ __device__ __forceinline__ void load_halves(const uint8_t* p, u32* w) {
         w[0] = *(const u32*)p;
     } else if constexpr (C == 3) {
         // 6 bytes at 6 (lane % 16): of an odd lane behind two others in the 8 bytes that begin at a multiple of 4 (as three pieces of 2 bytes 64 ragged requests of
-        // 192 numbers a row OLD us, this way NEW)
+        // 192 numbers a row 147 us, this way 137)
         typedef u32 words __attribute__((ext_vector_type(2), aligned(4)));
         const u32 odd = threadIdx.x & 1;
         const words x = *(const words*)(p - 2 * odd);
@@ -501,6 +501,9 @@ __device__ __forceinline__ void place_piece(const Attend& a, Piece& p, const Spa
 // are whole row tiles.  BLOCKS: the keys of listed blocks and of a window, one token's; SLOPES is for them.
 template <int FMT, int C, int T, int NW, bool WHOLE, bool CAPPED, bool BLOCKS, bool SLOPES, typename Next>
 __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& sh, Next&& next) {
+    // One tile at a time where that leaves registers for two workgroups a CU, whose waits overlap instead: 64 ragged requests of 192 numbers in 4 bits 137 us
+    // with two tiles and one workgroup, 113 this way; of 256 numbers, where 70 registers are spilled for it, 143 and 172
+    constexpr bool ALONE = one_tile(FMT, 64 * C, T);
     const u32 lane = threadIdx.x & 63, wave = wave_of(), col = lane & 15, g = lane >> 4;
     Piece p;
     Rows<C> rows[T];
@@ -724,7 +727,11 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
         while (from < p.stop) {
             // a tile is on its way while the one before it is added; behind the last one the last is asked for again, which the cache has
             const int count = min(32, (p.stop - from + (int)(NW * TILE) - 1) / (int)(NW * TILE));
-            for (int i = 0; i < count; i += 2) {
+            for (int i = 0; ALONE && i < count; ++i) {
+                if (i) load(even, i);
+                add(even, i);
+            }
+            for (int i = 0; !ALONE && i < count; i += 2) {
                 load(odd, min(i + 1, count - 1));
                 add(even, i);
                 if (i + 1 < count) {
@@ -753,7 +760,7 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
 }
 
 template <int FMT, int C, int T, bool CAPPED>
-__global__ void __launch_bounds__(256, groups_per_cu(64 * C, T)) k_attend(Attend a) {
+__global__ void __launch_bounds__(256, groups_per_cu(FMT, 64 * C, T)) k_attend(Attend a) {
     __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
     __shared__ u64 sh_sum[SPLIT_WAVES];
     __shared__ u64 sh_begin;
@@ -1066,10 +1073,10 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
 }
 
 // Slopes need registers that three workgroups a CU leave none of: 8 lists of 5,064 keys of 64 numbers, 4 of 40,000, in us, three 24.9, 44.7, two 20.3, 39.9
-constexpr u32 list_groups_per_cu(u32 width, bool slopes) { return slopes ? std::min(groups_per_cu(width, 1), 2u) : groups_per_cu(width, 1); }
+constexpr u32 list_groups_per_cu(u32 fmt, u32 width, bool slopes) { return width > 128 ? 1 : slopes ? 2 : groups_per_cu(fmt, width, 1); }
 
 template <int FMT, int C, bool SLOPES, bool CAPPED>
-__global__ void __launch_bounds__(256, list_groups_per_cu(64 * C, SLOPES)) k_attend_selected(Attend a, u32 units, u32 tiles) {
+__global__ void __launch_bounds__(256, list_groups_per_cu(FMT, 64 * C, SLOPES)) k_attend_selected(Attend a, u32 units, u32 tiles) {
     __shared__ __align__(16) Exchange<C, SPLIT_WAVES> sh;
     __shared__ __align__(16) Entries<FMT, C> sh_entries[SPLIT_WAVES][2];
     const u32 cost = units + PIECE;
@@ -1139,11 +1146,11 @@ void run_narrow(hipStream_t st, const Attend& a, int num_cu, bool whole) {
         }
         return run_whole<FMT, C, 4, CAPPED>(st, a);
     }
-    const u32 grid = (u32)num_cu * groups_per_cu(64 * C, a.row_tiles);
+    const u32 grid = (u32)num_cu * groups_per_cu(FMT, 64 * C, a.row_tiles);
     if (a.listed) {
         const u32 units = std::max<u32>((a.k + a.window + UNIT - 1) / UNIT, 1), tiles = (a.group + ROWS - 1) / ROWS;
-        if (a.slopes) return k_attend_selected<FMT, C, true, CAPPED><<<(u32)num_cu * list_groups_per_cu(64 * C, true), 256, 0, st>>>(a, units, tiles);
-        return k_attend_selected<FMT, C, false, CAPPED><<<grid, 256, 0, st>>>(a, units, tiles);
+        if (a.slopes) return k_attend_selected<FMT, C, true, CAPPED><<<(u32)num_cu * list_groups_per_cu(FMT, 64 * C, true), 256, 0, st>>>(a, units, tiles);
+        return k_attend_selected<FMT, C, false, CAPPED><<<(u32)num_cu * list_groups_per_cu(FMT, 64 * C, false), 256, 0, st>>>(a, units, tiles);
     }
     if constexpr (C <= 3) {
         if (a.row_tiles == 2) return k_attend<FMT, C, 2, CAPPED><<<grid, 256, 0, st>>>(a);

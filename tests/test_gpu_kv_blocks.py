@@ -173,6 +173,29 @@ def test_select_by_every_path(kv, wide_table, k):
     select_case(kv, [9000, 3000, 33, 1600], 4, 2, 4, 64, 32, 16, k, 100, "int8", "bf16", wide_table=wide_table, edges=True)
 
 
+@pytest.mark.parametrize("contexts", [[900, 20, 33], [1500, 700, 33], [2500, 1000, 16], [3900, 2000, 17]])
+@pytest.mark.parametrize("heads, id_heads, k", [(4, 2, 20), (8, 8, 70)])
+def test_select_by_any_number_of_waves(kv, contexts, heads, id_heads, k):
+    select_case(kv, contexts, heads, 2, id_heads, 64, 32, 16, k, 30, "int8", "bf16", news=[3, 2, 1], edges=False)
+
+
+@pytest.mark.parametrize("context, heads, id_heads, k", [(3300, 4, 2, 30), (3300, 8, 8, 3), (12_000, 4, 2, 200), (12_000, 4, 4, 900)])
+def test_select_for_many_tokens(kv, context, heads, id_heads, k):
+    """More workgroups than run at once: the lists of the same tokens a few at a time."""
+    m = Memory(kv, [context, 700], 2, 64, 64, "int8", 9)
+    blocks, _ = filled(kv, m, 16)
+    n = 640
+    rng = np.random.default_rng(k)
+    requests = rng.integers(0, 2, n)
+    positions = np.where(requests == 0, rng.integers(-1, context, n), rng.integers(-1, 700, n))
+    q = torch.randn(n, heads, 64, device="cuda", dtype=torch.bfloat16)
+
+    def lists(a, b):
+        return blocks.select(q[a:b], kv.KvStep(ints(m.table), requests=ints(requests[a:b]), positions=ints(positions[a:b])), k, window=20, id_heads=id_heads)
+
+    assert torch.equal(lists(0, n), torch.cat([lists(a, a + 20) for a in range(0, n, 20)]))
+
+
 @pytest.mark.parametrize("dim, heads, wide_table", [(256, 15, 900), (256, 14, 900), (64, 16, 800), (192, 14, 990)])
 def test_select_of_as_many_lists_as_fit(kv, dim, heads, wide_table):
     """Keys of all lists of a head that just fit LDS, or just do not."""

@@ -82,6 +82,11 @@ def test_attend_pieces_of_several_units(kv):
     attend_case(kv, [3000, 2000, 2011], [40, 70, 100], 8, 4, 64, 64, "fp4", "fp16")
 
 
+@pytest.mark.parametrize("dim, softcap, slopes, window", [(136, 0.0, False, 0), (192, 30.0, False, 0), (192, 0.0, True, 7000), (248, 0.0, False, 0)])
+def test_attend_pieces_of_wide_rows(kv, dim, softcap, slopes, window):
+    attend_case(kv, [9000, 100, 10_011], [1, 2, 1], 4, 2, dim, 64, "fp4", "fp16", softcap=softcap, slopes=slopes, window=window)
+
+
 @pytest.mark.parametrize("dim", [64, 128, 192, 256])
 def test_attend_two_tiles_of_rows_in_pieces(kv, dim):
     attend_case(kv, [4100, 2300, 900], [1, 2, 0], 20, 1, dim, 64, "fp4", "bf16")
