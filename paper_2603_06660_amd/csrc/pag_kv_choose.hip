@@ -113,7 +113,8 @@ __device__ __forceinline__ u32 row0_of(const Cache& c, const Blocks& blocks, u32
 }
 
 // A wave has a window of new tokens and a head, and writes the summaries of the blocks whose last new token lies in its window: that token is the last one that
-// the block holds.
+// the block holds.  4 requests' 16,384 tokens each, 8 heads, blocks of 64 in int8: 38 us, where reading their keys is 11; widening, comparing and the shuffles at the end do not overlap
+// with it enough.
 template <int FMT, int C>
 __global__ void __launch_bounds__(256) k_summarise(Cache c, Blocks blocks, const int64_t* __restrict__ slots, u64 tokens, u32 window) {
     const u32 lane = threadIdx.x & 63;
@@ -677,7 +678,9 @@ __device__ __forceinline__ void pick_long(const u32* keys, u32 n, u32 k, int32_t
     write_none(ids, all + min(all_same, ties), k, threadIdx.x, 64 * WAVES);
 }
 
-// A workgroup for a token and key/value head: scores into LDS, then a wave a list.  MANY: several tiles of columns.
+// A workgroup for a token and key/value head: scores into LDS, then a wave a list.  MANY: several tiles of columns, whose rows of q need registers for two waves a SIMD only (64 heads
+// over 2 for 48 requests of up to 625 blocks 43 us with four waves and 43 spilled registers, 36 this way).  48 requests, 32 lists each of up to 625 blocks: 19 us, of which 6 for
+// choosing, by four waves of eight; the 33 MB of summaries are 6 at the memory's rate.
 template <int C, int NW, bool MANY>
 __global__ void __launch_bounds__(64 * NW, C <= 2 && !MANY ? 4 : 2) k_choose(Choose a, Columns columns, u32 room) {
     extern __shared__ u32 sh_keys[];
@@ -718,7 +721,7 @@ __global__ void __launch_bounds__(64 * NW, C <= 2 && !MANY ? 4 : 2) k_choose(Cho
     }
 }
 
-// Scores of a long list's part, 64 blocks a wave
+// Scores of a long list's part, 64 blocks a wave.  Bound by waits for table, exponents and summaries, one after the other: 8 lists of 6,250 blocks 7.7 us, and 7.9 for k_pick.
 template <int C, bool MANY>
 __global__ void __launch_bounds__(256) k_score(Choose a, Columns columns, u32 chunks) {
     const u32 part = blockIdx.x % chunks, list0 = blockIdx.x / chunks, t = list0 / a.c.kv_heads, kv_head = list0 % a.c.kv_heads, lists = a.group / columns.heads;

@@ -360,7 +360,8 @@ __device__ __forceinline__ void turn_queries(const Store& a, u64 t0, u32 n, cons
 // prompts: 256 tokens 8.5, 5.9, 5.9; 512 tokens 9.8, 6.5, 5.9; 2,048 tokens 18, 12.5, 11; 4,096 tokens 35, 20, 14; 15,000 tokens 139, 53, 36.
 // Bound by memory where there are many tokens (60,000: 370 MB in 124 us), by the waits for a slot, an exponent and a row where there are few.
 // TURN: keys are turned.  The four waves of a workgroup then have one window and kind, and four heads, and share their tokens' angles; the workgroups from
-// number `writers` on turn queries.
+// number `writers` on turn queries.  18,596 tokens, 8 heads of 128: 44 us as they are, 86 with keys turned, 128 with 32 heads of queries (419 MB, 81 as a copy); one token of each of
+// 192 requests 9 on the GPU.  144 registers, three waves a SIMD, whose waits for rows, angles and partners do not overlap enough.
 template <int FMT, int C, bool TURN>
 __global__ void __launch_bounds__(256) k_append(Store a, u32 window, u32 writers, u32 each) {
     extern __shared__ double2 spin[];
@@ -476,7 +477,8 @@ __global__ void __launch_bounds__(256) k_append(Store a, u32 window, u32 writers
 
 // 4-bit codes: a row's parts have their exponents to themselves, so that 8 numbers of a row are a thread's, whatever else the call writes, and four
 // threads share a part.  A workgroup has `each` tokens, all their heads, keys and values; the workgroups from number `writers` on turn queries.  A lane keeps its
-// piece of a row, and FP4_TURNS rows' pieces are asked for before the first is encoded.
+// piece of a row, and FP4_TURNS rows' pieces are asked for before the first is encoded.  18,596 tokens, 8 heads of 128: 30 us as they are, 50 with keys turned, 99 with 32 heads of
+// queries (400 MB, 77 as a copy).
 constexpr u32 FP4_TURNS = 4;
 
 template <int C, bool TURN>
