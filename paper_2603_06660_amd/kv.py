@@ -10,13 +10,15 @@ A decoding step, in order (every call goes onto the current stream and returns w
     out, lse = cache.attend_selected(q, ids, step, window=64)           # reads what a search found, and the last 64 tokens
     tables.commit(step)
 
-None of it has a backward: tensors that require a gradient are refused unless gradients are switched off (torch.no_grad).
+None of it has a backward: tensors that require a gradient are refused unless gradients are switched off (torch.no_grad), and so are tensors that carry a
+tangent (torch.autograd.forward_ad) unless forward derivatives are (torch.inference_mode; torch.no_grad leaves them on).
 """
 from __future__ import annotations
 
 import ctypes as C
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import PagError, _check, load_library
 
@@ -76,12 +78,20 @@ def _no_graph(t, what):
         raise PagError("%s requires a gradient, and the cache has no backward: detach it, or call under torch.no_grad()" % what)
 
 
+def _no_tangent(t, what):
+    """Forward derivatives would end here as well: a dual tensor's address is that of its value alone, and says nothing of its tangent."""
+    if torch._C._is_fwd_grad_enabled() and forward_ad.unpack_dual(t).tangent is not None:
+        raise PagError("%s carries a tangent, and the cache has no forward derivative: pass torch.autograd.forward_ad.unpack_dual(t).primal" % what)
+
+
 def _array(t, dtype, shape, device, what):
     """The address of a dense tensor of this type, shape and device."""
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise PagError("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), device))
     if t.requires_grad:
         _no_graph(t, what)
+    if forward_ad._current_level >= 0:
+        _no_tangent(t, what)
     return t.data_ptr()
 
 
@@ -95,6 +105,8 @@ def _rows(t, shape, device, what, dtypes=_DTYPES):
         raise PagError("%s: the last dimension must be dense" % what)
     if t.requires_grad:
         _no_graph(t, what)
+    if forward_ad._current_level >= 0:
+        _no_tangent(t, what)
     return t.data_ptr(), token, head
 
 
