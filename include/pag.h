@@ -495,9 +495,11 @@ typedef struct {
  * pag_kv_blocks_select: for each token and list the k best of the blocks that begin before the token's window (args->window; 0: up to the token itself), of a list's heads by the
  * largest of their scores, of equal ones the first; their numbers in ascending order, -1 behind them (dev int32 [tokens][id_heads][k], strides in elements, last dimension dense).
  * Blocks in pages that are none are left out.  id_heads as in pag_kv_attend_selected.  Of args it reads dtype, heads, window, q and its strides,
- * and the workspace.  tokens * heads < 2^23.
+ * and the workspace.  With `blocks` those that a row of the table has room for, max_pages * page_tokens / block_tokens: tokens * id_heads * blocks has to be at most 2^40 and
+ * kv_heads * blocks / 256, rounded up for each head, below 2^24.  The workspace is 4 * id_heads * blocks bytes for each token of a launch, of as many tokens as 512 MB have room for (one
+ * at least), or none where blocks and lists are few.
  * pag_kv_attend_blocks: pag_kv_attend_selected over the tokens of the listed blocks: those in the window or behind the token are passed over, a block listed twice counts
- * twice; k * block_tokens + window below 2^30.
+ * twice.  Both: tokens * heads and requests * kv_heads below 2^23, k * block_tokens + window below 2^30.
  * pag_kv_blocks_workspace_bytes: the workspaces of these two; either pointer may be null.
  */
 int pag_kv_blocks_update(const pag_kv_cache* cache, const pag_kv_blocks* blocks, const int64_t* slots, uint64_t tokens, void* stream);

@@ -205,7 +205,7 @@ struct Choose {
     const void* q;
     int64_t q_ts, q_hs, ids_ts, ids_hs;
     int32_t* ids;
-    u32* keys;                            // the workspace: scores [tokens * id_heads][most_blocks]
+    u32* keys;                            // the workspace: scores [tokens of a launch * id_heads][most_blocks]
     u32 heads, group, dtype, window, id_heads, k, most_blocks;      // group: heads of a key/value head; most_blocks: of a request
 };
 
@@ -236,7 +236,7 @@ int launch_attend(hipStream_t st, const Attend& a, int num_cu);
 int launch_summarise(hipStream_t st, const Cache& c, const Blocks& b, const int64_t* slots, u64 tokens);
 int launch_choose(hipStream_t st, const Choose& a);
 u64 choose_workspace(const Choose& a);          // bytes
-u64 choose_groups(const Choose& a);             // workgroups of 256 threads of its largest launch
+u64 choose_groups(const Choose& a);             // workgroups of 256 threads that one token has at most
 
 u64 attend_workspace(const Attend& a, int num_cu);      // bytes
 int num_cu_of_current();                        // < 0: no GPU

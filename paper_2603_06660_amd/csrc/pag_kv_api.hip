@@ -143,8 +143,10 @@ int choice_of(const pag_kv_cache* cache, const pag_kv_step* step, const pag_kv_a
     a->most_blocks = step->max_pages * (x.c.page_tokens / block);
     a->b.tokens = block;
     a->b.page_blocks = x.c.page_tokens / block;
-    // a launch has fewer than 2^32 threads
-    PAG_CHECK(choose_groups(*a) < (1ull << 23), PAG_EUNSUPPORTED, "tokens * kv_heads * blocks of a request is too large for one launch");
+    // a launch has fewer than 2^32 threads, and one token's scores are made by one; tokens go in as many launches as a bounded workspace takes, of which
+    // there are at most 2^14 this way
+    PAG_CHECK(choose_groups(*a) < (1ull << 24), PAG_EUNSUPPORTED, "kv_heads * blocks of a row of the table / 256 must be below 2^24");
+    PAG_CHECK((u64)a->s.tokens * id_heads * a->most_blocks <= (1ull << 40), PAG_EUNSUPPORTED, "tokens * id_heads * blocks of a row of the table must be at most 2^40");
     return PAG_OK;
 }
 

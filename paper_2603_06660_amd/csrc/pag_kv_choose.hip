@@ -759,6 +759,19 @@ bool choose_whole(const Choose& a) {
     return a.most_blocks <= MOST_SHORT && (u64)(a.id_heads / a.c.kv_heads) * a.most_blocks * 4 <= 55 * 1024;
 }
 
+// Tokens of a launch, where scores go through the workspace: as many as have room in ROOM bytes, one at least, in launches of about as many tokens each.  A launch has
+// fewer than 2^32 threads, 256 for CHUNK blocks of a key/value head (one token's are fewer, the host has looked) and up to 1024 for a list.
+// What several launches cost (32 lists of 8,192 blocks for 4,096 tokens, 10,810 us in one launch and 4.3 GB): 10,950 to 11,010 in 8 launches, 11,120 in 16 of 256 MB, 12,190 in 64 of 64 MB, whose
+// last workgroups leave the chip idle more often.
+constexpr u64 ROOM = 512ull << 20;
+
+u32 tokens_of_launch(const Choose& a) {
+    const u64 each = 4 * (u64)a.id_heads * a.most_blocks, groups = (u64)a.c.kv_heads * ((a.most_blocks + CHUNK - 1) / CHUNK);
+    const u64 most = std::max<u64>(std::min({ ROOM / each, ((1ull << 24) - 1) / groups, ((1ull << 22) - 1) / a.id_heads }), 1);
+    const u64 launches = std::max<u64>((a.s.tokens + most - 1) / most, 1);
+    return (u32)((a.s.tokens + launches - 1) / launches);
+}
+
 template <int C, bool MANY>
 void launch(hipStream_t st, const Choose& a, const Columns& columns) {
     const u32 lists = a.id_heads / a.c.kv_heads;
@@ -771,12 +784,21 @@ void launch(hipStream_t st, const Choose& a, const Columns& columns) {
         else k_choose<C, 8, MANY><<<grid, 512, room, st>>>(a, columns, a.most_blocks);
         return;
     }
-    const u32 chunks = (a.most_blocks + CHUNK - 1) / CHUNK, grid = a.s.tokens * a.id_heads;
-    k_score<C, MANY><<<a.s.tokens * a.c.kv_heads * chunks, 256, 0, st>>>(a, columns, chunks);
-    if (a.most_blocks <= 8 * 64 * 8) k_pick<8, 8><<<grid, 512, 0, st>>>(a);
-    else if (a.most_blocks <= 8 * 64 * 16) k_pick<8, 16><<<grid, 512, 0, st>>>(a);
-    else if (a.most_blocks <= 8 * 64 * 32) k_pick<8, 32><<<grid, 512, 0, st>>>(a);
-    else k_pick<16, 0><<<grid, 1024, 0, st>>>(a);
+    const u32 chunks = (a.most_blocks + CHUNK - 1) / CHUNK, each = tokens_of_launch(a);
+    for (u32 t0 = 0; t0 < a.s.tokens; t0 += each) {
+        Choose x = a;
+        x.s.tokens = std::min(each, a.s.tokens - t0);
+        x.s.request += t0;
+        x.s.positions += t0;
+        x.q = (const uint16_t*)a.q + (int64_t)t0 * a.q_ts;
+        x.ids += (int64_t)t0 * a.ids_ts;
+        const u32 grid = x.s.tokens * a.id_heads;
+        k_score<C, MANY><<<x.s.tokens * a.c.kv_heads * chunks, 256, 0, st>>>(x, columns, chunks);
+        if (a.most_blocks <= 8 * 64 * 8) k_pick<8, 8><<<grid, 512, 0, st>>>(x);
+        else if (a.most_blocks <= 8 * 64 * 16) k_pick<8, 16><<<grid, 512, 0, st>>>(x);
+        else if (a.most_blocks <= 8 * 64 * 32) k_pick<8, 32><<<grid, 512, 0, st>>>(x);
+        else k_pick<16, 0><<<grid, 1024, 0, st>>>(x);
+    }
 }
 
 template <int C>
@@ -814,12 +836,9 @@ int launched(const char* what) {
 
 }  // namespace
 
-u64 choose_workspace(const Choose& a) { return choose_whole(a) ? 0 : 4 * (u64)a.s.tokens * a.id_heads * a.most_blocks; }
+u64 choose_workspace(const Choose& a) { return choose_whole(a) ? 0 : 4 * (u64)tokens_of_launch(a) * a.id_heads * a.most_blocks; }
 
-u64 choose_groups(const Choose& a) {
-    if (choose_whole(a)) return (u64)a.s.tokens * a.c.kv_heads * 2;
-    return std::max((u64)a.s.tokens * a.c.kv_heads * ((a.most_blocks + CHUNK - 1) / CHUNK), (u64)a.s.tokens * a.id_heads * 4);
-}
+u64 choose_groups(const Choose& a) { return (u64)a.c.kv_heads * ((a.most_blocks + CHUNK - 1) / CHUNK); }
 
 int launch_summarise(hipStream_t st, const Cache& c, const Blocks& b, const int64_t* slots, u64 tokens) {
     if (c.fmt == PAG_KV_INT8) summarise_width<PAG_KV_INT8>(st, c, b, slots, tokens);
