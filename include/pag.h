@@ -417,7 +417,7 @@ int pag_kv_release(const pag_kv_tables* tables, const int32_t* done, void* strea
  * null.  Slots -1 or out of range give zeros.  PAG_F32 and PAG_BF16 hold every number of the cache exactly, but for what a block near the end of
  * 32 bits rounds up to 2^128 and infinities held as the largest code there: that is read as the largest finite PAG_BF16, 255 * 2^120, where
  * attention's results end as well.
- * tokens * kv_heads of a call has to be below 2^27.
+ * tokens * kv_heads of a call has to be below 2^27, and the tokens that pag_kv_append writes into a PAG_KV_FP4 cache below 2^25.
  */
 int pag_kv_append(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k_token_stride, int64_t k_head_stride,
                   const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, uint64_t tokens, void* stream);
