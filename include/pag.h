@@ -442,7 +442,7 @@ typedef struct {
     const int32_t* positions;      /* dev [tokens], of any sign; also those of tokens that are left out of the cache count, for q */
     const void* q;                 /* dev [tokens][heads][head_dim] of the call's dtype, strides in elements, multiples of 16 bytes */
     int64_t q_token_stride, q_head_stride;
-    void* out;                     /* dev, like q: the turned rows; q itself, with q's strides, or apart from it */
+    void* out;                     /* dev, like q: the turned rows; q itself, with q's strides, or apart from it; apart from k, v and each other */
     int64_t out_token_stride, out_head_stride;
 } pag_kv_rotation;
 

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstdlib>
 
 #include "pag_kv.h"
 
@@ -226,6 +227,21 @@ int store_of(const pag_kv_cache* cache, uint32_t dtype, const void* k, int64_t k
     return PAG_OK;
 }
 
+// Whether a row of a token of x lies over one of y: rows of `row` bytes, strides in bytes.  Looked at for the first token, at the rows of x next to each of y's: other tokens' lie
+// the same way, or the tensors have different token strides and nothing is said of them.
+bool rows_meet(const void* x, int64_t x_stride, u32 x_heads, const void* y, int64_t y_stride, u32 y_heads, int64_t row) {
+    if (x_heads == 1) x_stride = 0;          // may be anything then
+    if (y_heads == 1) y_stride = 0;
+    const int64_t apart = (int64_t)((uintptr_t)y - (uintptr_t)x), x_last = x_stride * ((int64_t)x_heads - 1), y_last = y_stride * ((int64_t)y_heads - 1);
+    if (apart + std::min<int64_t>(y_last, 0) >= std::max<int64_t>(x_last, 0) + row || apart + std::max<int64_t>(y_last, 0) + row <= std::min<int64_t>(x_last, 0)) return false;
+    for (u32 j = 0; j < y_heads; ++j) {
+        const int64_t at = apart + y_stride * (int64_t)j, near = x_stride ? at / x_stride : 0;
+        for (int64_t i = near - 1; i <= near + 1; ++i)
+            if (i >= 0 && i < (int64_t)x_heads && std::abs(at - x_stride * i) < row) return true;
+    }
+    return false;
+}
+
 }  // namespace
 }  // namespace pagkv
 
@@ -267,6 +283,14 @@ extern "C" int pag_kv_append_rotated(const pag_kv_cache* cache, uint32_t dtype, 
             if ((rc = check_rows(r->out, r->out_token_stride, r->out_head_stride, bytes, 16, "out and its strides must be multiples of 16 bytes"))) return rc;
             PAG_CHECK(r->q != r->out || (r->q_token_stride == r->out_token_stride && r->q_head_stride == r->out_head_stride), PAG_EINVAL,
                       "q may be turned in place with its own strides only");
+            // queries are written by other workgroups than those that read keys, values and other queries
+            const int64_t row = (int64_t)a.c.dim * bytes, step = r->out_head_stride * (int64_t)bytes;
+            PAG_CHECK((r->heads == 1 || std::abs(step) >= row) && (tokens == 1 || std::abs(r->out_token_stride * (int64_t)bytes) >= row), PAG_EINVAL,
+                      "rows of out lie over each other");
+            PAG_CHECK(!rows_meet(r->out, step, r->heads, k, k_head_stride * (int64_t)bytes, a.c.kv_heads, row) &&
+                      !rows_meet(r->out, step, r->heads, v, v_head_stride * (int64_t)bytes, a.c.kv_heads, row), PAG_EINVAL, "out has to lie apart from keys and values");
+            PAG_CHECK(r->q == r->out || !rows_meet(r->out, step, r->heads, r->q, r->q_head_stride * (int64_t)bytes, r->heads, row), PAG_EINVAL,
+                      "out has to be q itself or apart from it");
             a.heads = r->heads;
             a.q = r->q; a.q_ts = r->q_token_stride; a.q_hs = r->q_head_stride;
             a.out = r->out; a.o_ts = r->out_token_stride; a.o_hs = r->out_head_stride;

@@ -353,7 +353,7 @@ class KvCache:
 
     def append_rotated(self, k, v, slots, positions, rotation, q=None, out=None):
         """append() of k turned by `rotation` (a KvRotation) at positions (int32 [tokens]; a step's, or others) and of v as it is.
-        -> q [tokens, heads, head_dim], of k's type, turned likewise: a new tensor, or `out` (q itself: in place); None if there is no q."""
+        -> q [tokens, heads, head_dim], of k's type, turned likewise: a new tensor, or `out` (q itself: in place; otherwise apart from q, k and v); None if there is no q."""
         tokens = slots.shape[0]
         shape = (tokens, self.kv_heads, self.head_dim)
         keys = _rows(k, shape, self.device, "k")
