@@ -632,32 +632,32 @@ __device__ __forceinline__ void pick_long(const u32* keys, u32 n, u32 k, int32_t
         }
         // that part's keys, bit by bit: by each wave for itself where a register of them is enough, by all waves otherwise
         if (valid > k) {
-        const u32 low = least + (bin << shift), need = k - above, inside = (u32)__builtin_amdgcn_readfirstlane((int)sh_bins[place_of(bin)]);
-        int bit = shift - 1;
-        u32 at = 0, over = 0;                    // counted from low
-        bool done = inside == need;
-        const auto step = [&](u32 count, u32 to) {
-            if (count >= need) at = to;
-            else over = count;
-            done = count == need;
-        };
-        if (!done && inside <= 64) {
-            each([&](u32 y, u32) { if (y >= low && (y - low) >> shift == 0) sh_found[atomicAdd(&sh_count[0], 1u)] = y - low; });
-            lds_barrier();
-            const u32 y = lane < inside ? sh_found[lane] : 0u;
-            for (; bit >= 0 && !done; --bit) step((u32)__popcll(__ballot(lane < inside && y >= (at | 1u << bit))), at | 1u << bit);
-        } else if (!done) {
-            for (; bit >= 0 && !done; --bit) {
-                const u32 to = at | 1u << bit;
-                u32 count = 0;
-                each([&](u32 y, u32) { count += (u32)__popcll(__ballot(y >= low && (y - low) >> shift == 0 && y - low >= to)); });
-                if (lane == 0 && count) atomicAdd(&sh_count[bit], count);
+            const u32 low = least + (bin << shift), need = k - above, inside = (u32)__builtin_amdgcn_readfirstlane((int)sh_bins[place_of(bin)]);
+            int bit = shift - 1;
+            u32 at = 0, over = 0;                    // counted from low
+            bool done = inside == need;
+            const auto step = [&](u32 count, u32 to) {
+                if (count >= need) at = to;
+                else over = count;
+                done = count == need;
+            };
+            if (!done && inside <= 64) {
+                each([&](u32 y, u32) { if (y >= low && (y - low) >> shift == 0) sh_found[atomicAdd(&sh_count[0], 1u)] = y - low; });
                 lds_barrier();
-                step((u32)__builtin_amdgcn_readfirstlane((int)sh_count[bit]), to);
+                const u32 y = lane < inside ? sh_found[lane] : 0u;
+                for (; bit >= 0 && !done; --bit) step((u32)__popcll(__ballot(lane < inside && y >= (at | 1u << bit))), at | 1u << bit);
+            } else if (!done) {
+                for (; bit >= 0 && !done; --bit) {
+                    const u32 to = at | 1u << bit;
+                    u32 count = 0;
+                    each([&](u32 y, u32) { count += (u32)__popcll(__ballot(y >= low && (y - low) >> shift == 0 && y - low >= to)); });
+                    if (lane == 0 && count) atomicAdd(&sh_count[bit], count);
+                    lds_barrier();
+                    step((u32)__builtin_amdgcn_readfirstlane((int)sh_count[bit]), to);
+                }
             }
-        }
-        cut = low + at - (done ? 1 : 0);
-        ties = done ? 0 : need - over;
+            cut = low + at - (done ? 1 : 0);
+            ties = done ? 0 : need - over;
         }
     }
     // where this wave's keys go

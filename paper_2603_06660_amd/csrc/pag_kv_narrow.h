@@ -207,16 +207,17 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<FMT, C>& ti
                 for (int y = 0; y < T; ++y) s[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, rows[y].q[n], s[y][b], 0, 0, 0);
             }
         }
-    } else
+    } else {
 #pragma unroll
-    for (int h = 0; h < C; ++h) {
+        for (int h = 0; h < C; ++h) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const half8_t k0 = widen8<FMT>(tile.k[b][h].x, tile.k[b][h].y), k1 = widen8<FMT>(tile.k[b][h].z, tile.k[b][h].w);
+            for (int b = 0; b < 2; ++b) {
+                const half8_t k0 = widen8<FMT>(tile.k[b][h].x, tile.k[b][h].y), k1 = widen8<FMT>(tile.k[b][h].z, tile.k[b][h].w);
 #pragma unroll
-            for (int y = 0; y < T; ++y) {
-                s[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, rows[y].q[2 * h], s[y][b], 0, 0, 0);
-                s[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, rows[y].q[2 * h + 1], s[y][b], 0, 0, 0);
+                for (int y = 0; y < T; ++y) {
+                    s[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, rows[y].q[2 * h], s[y][b], 0, 0, 0);
+                    s[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, rows[y].q[2 * h + 1], s[y][b], 0, 0, 0);
+                }
             }
         }
     }
@@ -348,18 +349,19 @@ __device__ __forceinline__ void add_tile(const Attend& a, const Tile<FMT, C>& ti
                 for (int y = 0; y < T; ++y) rows[y].acc[4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[c], p[y], rows[y].acc[4 * w + c], 0, 0, 0);
             }
         }
-    } else
+    } else {
 #pragma unroll
-    for (int w = 0; w < C; ++w) {
-        u32 words[8];
+        for (int w = 0; w < C; ++w) {
+            u32 words[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) words[j] = tile.v[j][w];
-        half8_t v[4];
-        columns<FMT>(words, v);
+            for (int j = 0; j < 8; ++j) words[j] = tile.v[j][w];
+            half8_t v[4];
+            columns<FMT>(words, v);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 4; ++c) {
 #pragma unroll
-            for (int y = 0; y < T; ++y) rows[y].acc[4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[c], p[y], rows[y].acc[4 * w + c], 0, 0, 0);
+                for (int y = 0; y < T; ++y) rows[y].acc[4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[c], p[y], rows[y].acc[4 * w + c], 0, 0, 0);
+            }
         }
     }
 }
@@ -579,14 +581,15 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
                 for (int w = 0; w < T4::PARTS; ++w) tile.ve[s][w] = *(const u32*)(parts + ((2 * C + value_part<C>(w, col)) * BLOCK + 4 * g));
             }
             return;
-        } else
+        } else {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint8_t* rows_at = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s) * (128 * C);
+            for (int s = 0; s < 2; ++s) {
+                const uint8_t* rows_at = a.c.data + (u64)(u32)__builtin_amdgcn_readlane((int)block_row, 2 * i + s) * (128 * C);
 #pragma unroll
-            for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(rows_at + k_at + h * 64);
+                for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(rows_at + k_at + h * 64);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) load_words<C>(rows_at + v_at + j * (128 * C), tile.v[4 * s + j]);
+                for (int j = 0; j < 4; ++j) load_words<C>(rows_at + v_at + j * (128 * C), tile.v[4 * s + j]);
+            }
         }
     };
     const auto add = [&](Tile<FMT, C>& tile, int i) {
@@ -647,23 +650,23 @@ __device__ __forceinline__ void attend_pieces(const Attend& a, Exchange<C, NW>& 
             add_tile<FMT, C, 1, false, SLOPES, CAPPED, true>(a, tile, rows, x, !whole, keep, far);
             return;
         } else {
-        const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos < oldest_of(a, p.p1);
-        u32 keep[T];
+            const bool masked = two != 3u || pos + (int)TILE > p.p0 + 1 || pos < oldest_of(a, p.p1);
+            u32 keep[T];
 #pragma unroll
-        for (int y = 0; y < T; ++y) keep[y] = 0xFF;
-        if (masked) {
+            for (int y = 0; y < T; ++y) keep[y] = 0xFF;
+            if (masked) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int k = x.at[j >> 2] + (j & 3);
-                const bool exists = (two >> (j >> 2) & 1u) && k < p.stop;
+                for (int j = 0; j < 8; ++j) {
+                    const int k = x.at[j >> 2] + (j & 3);
+                    const bool exists = (two >> (j >> 2) & 1u) && k < p.stop;
 #pragma unroll
-                for (int y = 0; y < T; ++y) {
-                    if (!exists || k > rows[y].position || k < oldest_of(a, rows[y].position)) keep[y] &= ~(1u << j);
+                    for (int y = 0; y < T; ++y) {
+                        if (!exists || k > rows[y].position || k < oldest_of(a, rows[y].position)) keep[y] &= ~(1u << j);
+                    }
+                    if (!exists) no_value(j);
                 }
-                if (!exists) no_value(j);
             }
-        }
-        add_tile<FMT, C, T, false, false, CAPPED>(a, tile, rows, x, masked, keep, far);
+            add_tile<FMT, C, T, false, false, CAPPED>(a, tile, rows, x, masked, keep, far);
         }
     };
     const auto start = [&]() {
@@ -985,16 +988,17 @@ __device__ __forceinline__ void attend_lists(const Attend& a, Exchange<C, NW>& s
                 for (int w = 0; w < Tile<FMT, C>::PARTS; ++w) tile.ve[s][w] = *(const u32*)&x.parts[1][value_part<C>(w, col)][32 * i + 16 * s + 4 * g];
             }
             return;
-        } else
+        } else {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint8_t* k = a.c.data + (u64)x.row[32 * i + 16 * s + col] * (128 * C) + g * 16;
-            const uint4 r = *(const uint4*)&x.row[32 * i + 16 * s + 4 * g];
-            const u32 v[4] = { r.x, r.y, r.z, r.w };
+            for (int s = 0; s < 2; ++s) {
+                const uint8_t* k = a.c.data + (u64)x.row[32 * i + 16 * s + col] * (128 * C) + g * 16;
+                const uint4 r = *(const uint4*)&x.row[32 * i + 16 * s + 4 * g];
+                const u32 v[4] = { r.x, r.y, r.z, r.w };
 #pragma unroll
-            for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(k + h * 64);
+                for (int h = 0; h < C; ++h) tile.k[s][h] = *(const uint4*)(k + h * 64);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) load_words<C>(a.c.data + (u64)v[j] * (128 * C) + 64 * C + col * (4 * C), tile.v[4 * s + j]);
+                for (int j = 0; j < 4; ++j) load_words<C>(a.c.data + (u64)v[j] * (128 * C) + 64 * C + col * (4 * C), tile.v[4 * s + j]);
+            }
         }
     };
     const auto add = [&](Tile<FMT, C>& tile, u32 buffer, int i, u32 found, bool far_now) {

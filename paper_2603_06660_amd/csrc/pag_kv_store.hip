@@ -155,8 +155,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_release(pag_kv_tables t, const
 
 // ---- rotation ---------------------------------------------------------------------------------------------------------
 
-// cos and sin of an angle below 2^31 or so, to 2^-50: the nearest multiple of pi / 2 is taken off in two parts, which leaves r with |r| <= pi / 4
-// exact to 2^-70, and of r Taylor's series, whose first terms left out, r^17 / 17! and r^18 / 18!, are below 2^-54.
+// cos and sin of an angle below 2^31 or so, to 2^-50: the nearest multiple of pi / 2 is taken off in two parts, which leave out less than 2^-77 of it; r, |r| <= pi / 4, is
+// rounded to 53 bits, 2^-54 at most, and of r Taylor's series, whose first terms left out, r^17 / 17! and r^18 / 18!, are below 2^-54.
 __device__ __forceinline__ double2 spin_of(double angle) {
     const double n = __builtin_rint(angle * 0.63661977236758134308);
     double r = __builtin_fma(n, -1.57079632679489655800, angle);
