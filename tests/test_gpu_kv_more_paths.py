@@ -200,3 +200,35 @@ def test_queries_turned_in_place(kv, fmt, dim, turned, dtype, pairs, tokens, hea
         assert cache.append_rotated(k, k, slots, at, rotation, q=own, out=own) is own and torch.equal(own, apart)
     rows.fill_(3.0)
     assert bool((among == 3.0).all())
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp4"])
+@pytest.mark.parametrize("dim, heads, kv_heads, contexts, news", [
+    (128, 8, 2, [700], [1]), (128, 32, 8, [3000, 40, 9000], [1, 1, 1]), (128, 8, 2, [40_000], [1]), (128, 8, 2, [1500, 700], [1500, 700]), (192, 4, 1, [5000, 300], [10, 4]),
+    (64, 40, 2, [5000, 900], [1, 1]), (256, 4, 1, [2500], [100]), (64, 4, 1, [900, 2000], [70, 900])])
+def test_the_same_bits_every_time(kv, fmt, dim, heads, kv_heads, contexts, news):
+    """Attention over everything, over listed tokens and over blocks, in shares and in one workgroup, by the kernels for few rows and for many: runs of one call are equal bit for bit, also
+    beside each other on several streams."""
+    m = Written(kv, contexts, kv_heads, dim, 64, fmt, 5)
+    positions = [p for c, a in zip(contexts, news) for p in range(c - a, c)]
+    requests = [b for b, a in enumerate(news) for _ in range(a)]
+    n = len(positions)
+    gen = torch.Generator(device="cuda").manual_seed(dim)
+    q = torch.randn(n, heads, dim, device="cuda", generator=gen).half()
+    step = kv.KvStep(ints(m.table), ints(np.concatenate([[0], np.cumsum(news)])), ints(contexts), ints(requests), ints(positions), max_new=max(news))
+    few = kv.KvStep(ints(m.table), requests=ints(requests[-4:]), positions=ints(positions[-4:]))
+    ids = torch.randint(0, min(contexts), (min(n, 4), kv_heads, 2200), device="cuda", generator=gen)
+    chosen = torch.randint(0, min(contexts) // 64 + 1, (min(n, 4), kv_heads, 50), device="cuda", generator=gen).int()
+    blocks = kv.KvBlocks(m.cache, 64)
+
+    def one():
+        return (*m.cache.attend(q, step, softcap=30.0), *m.cache.attend(q, step), *m.cache.attend_selected(q[-4:], ids, few, window=64), *blocks.attend(q[-4:], chosen, few, window=64))
+
+    first, results = one(), []
+    torch.cuda.synchronize()
+    for s in [torch.cuda.Stream() for _ in range(3)] * 3:
+        with torch.cuda.stream(s):
+            results.append(one())
+    torch.cuda.synchronize()
+    for r in results:
+        assert all(torch.equal(a, b) for a, b in zip(r, first))
