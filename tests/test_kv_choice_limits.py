@@ -79,3 +79,33 @@ def test_tokens_that_go_in_several_launches(kv, dim, heads, kv_heads, id_heads, 
 def test_a_call_that_no_single_launch_has_threads_for(kv):
     """65,536 tokens over a table with room for 65,536 blocks."""
     lists_in_parts(kv, 8, 64, 1, 2, 65_536, 65_536, 4, [0, 1, 255, 256, 8191, 30_000, 65_535])
+
+
+@pytest.mark.gpu
+def test_several_launches_in_a_graph(kv):
+    """Every replay against the same call without a graph."""
+    n, heads, page, held = 6000, 8, 64, 30
+    cache = kv.KvCache(held, 1, 64, page)
+    blocks = kv.KvBlocks(cache, 16)
+    x, at = torch.randn(held * page, 1, 64, device="cuda"), torch.arange(held * page, device="cuda")
+    cache.append(x, x, at)
+    blocks.update(at)
+    table = np.full((1, 4000), -1)
+    table[0, :held] = np.arange(held)
+    step = kv.KvStep(ints(table), requests=ints([0] * n), positions=torch.randint(0, held * page, (n,), dtype=torch.int32, device="cuda"))
+    q = torch.randn(n, heads, 64, device="cuda").half()
+    assert 4 * heads * 16_000 * n > 512 << 20
+    select = lambda: blocks.select(q, step, 9, window=5, id_heads=heads)
+    select()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = select()
+    for _ in range(4):
+        q.copy_(torch.randn(q.shape))
+        step.positions.copy_(torch.randint(0, held * page, (n,), dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = select()
+        torch.cuda.synchronize()
+        assert torch.equal(captured, want) and bool((captured[:, :, 0] >= -1).all())
